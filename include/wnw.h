@@ -406,6 +406,111 @@ wnw_status wnw_triage(int32_t layers, int32_t kv_heads, int32_t group, int32_t n
 /* Error reporting, no passage behind it.  Message of the last failed triage call of this thread. */
 const char *wnw_triage_last_error(void);
 
+/* ---- a KV cache in 8 bits.  A bf16 cache row costs a decode step 4 d bytes of HBM (K and V); these
+ * calls hold it in half of that: rows are quantised as they are written, with one scale for every
+ * `block` rows of a head, and attention reads the bytes.  The calls need no context; the caller owns
+ * every buffer, and all of them only enqueue work on hip_stream (NULL = null stream) and allocate
+ * nothing, so they can be captured into a graph; lengths and positions are read on the device when the
+ * work runs.  Like the decode step's caches the buffers hold all layers; a call handles n_layers of
+ * them from first_layer on, so that a model can go layer by layer.  Sequences of a batch may have any
+ * lengths.
+ *
+ * What a byte stands for, before the scale:
+ *   WNW_QUANT_INT8  byte - 128, an integer in -127 .. 127; scale = max(amax / 127, 2^-126) in fp32
+ *   WNW_QUANT_E4M3  an e4m3 number; scale = the smallest power of two with amax <= 448 * scale, at
+ *                   least 2^-126
+ * with amax the largest magnitude of the block's rows of that head (K and V apart).  A byte is the value
+ * nearest to x / scale, ties to even, decided exactly.
+ *
+ * Layout (cfg->head_dim = d):
+ *   k        [B][L][H_kv][capacity][d]
+ *   v        [B][L][H_kv][capacity / 64][d][64]: tiles of 64 rows, each transposed, so that the matrix
+ *            cores read them without a shuffle; row 16 b + 4 h + i of a tile (b, h, i = 0 .. 3) stands at
+ *            place 16 h + 4 b + i
+ *   k_scale, v_scale  fp32 [B][L][H_kv][capacity / block]
+ * k and v are aligned to 16 bytes.  Only rows below a sequence's length are meaningful; other bytes and
+ * scales may hold anything.  Errors: WNW_ERR_INVALID / _UNSUPPORTED / _HIP, message from
+ * wnw_quant_last_error(). */
+typedef enum { WNW_QUANT_INT8 = 0, WNW_QUANT_E4M3 = 1 } wnw_quant_format;
+
+typedef struct {
+    int32_t batch;        /* B >= 1                                                        */
+    int32_t layers;       /* L >= 1 layers of the buffers                                  */
+    int32_t kv_heads;     /* H_kv >= 1                                                     */
+    int32_t head_dim;     /* d: 64 or 128                                                  */
+    int32_t capacity;     /* rows per head, a multiple of 64, 64 .. 2^24                   */
+    int32_t block;        /* rows that share a scale: 16, 32 or 64                         */
+    int32_t format;       /* wnw_quant_format                                              */
+    uint32_t flags;       /* WNW_F_OUT_BF16: wnw_quant_read and wnw_quant_attend write bf16 (each
+                             fp32 result rounded to nearest, ties to even) instead of fp32 */
+} wnw_quant_config;
+
+typedef struct {          /* device pointers                                               */
+    uint8_t *k, *v;
+    float *k_scale, *v_scale;
+} wnw_quant_cache;
+
+/* Write rows into the cache, quantised: sequence b's rows 0 .. count[b] - 1 become cache rows pos[b] ..
+ * pos[b] + count[b] - 1 of every head.  A block's scale is that of the rows written so far: rows in front
+ * of pos[b] in the first block keep theirs, and when the new rows need a larger scale they are rounded
+ * again under it (code * old scale / new scale, to nearest, ties to even).  A block that begins at or after pos[b] gets
+ * a new scale.  So the rows of a block do not depend on what is written after the block is full, and a
+ * sequence can be cut back by writing at an earlier pos (the scale of the block that holds pos never
+ * shrinks).  Rows at or after pos[b] + count[b] are dead.  A block with a NaN or an infinity among its
+ * rows has the scale NaN: all of its rows of that head stand for NaN until the block is begun anew.
+ *   k_dev, v_dev  device bf16 [B][n_layers][H_kv][n][d]; 16-byte aligned
+ *   pos_dev       device int32 [B]: rows that the sequence has; values outside 0 .. capacity count as the
+ *                 nearer end, and rows past the capacity are not written
+ *   count_dev     device int32 [B], 0 .. n (as the nearer end outside); NULL = n for every sequence
+ * 0 <= n <= capacity.  Two calls whose work overlaps must not write the same block. */
+wnw_status wnw_quant_write(const wnw_quant_config *cfg, const wnw_quant_cache *cache, int32_t first_layer,
+                           int32_t n_layers, int32_t n, const void *k_dev, const void *v_dev,
+                           const int32_t *pos_dev, const int32_t *count_dev, void *hip_stream);
+
+/* Read rows back: value * scale of cache rows pos[b] .. pos[b] + count[b] - 1 of every head, as fp32
+ * (one rounding) or, with WNW_F_OUT_BF16, bf16.
+ *   k_out, v_out  device fp32 / bf16 [B][n_layers][H_kv][n][d], 16-byte aligned; rows at or after
+ *                 count[b], and those that would lie past the capacity, are left as they were.  Either may
+ *                 be NULL (keys or values alone)
+ *   pos_dev, count_dev, n   as in wnw_quant_write */
+wnw_status wnw_quant_read(const wnw_quant_config *cfg, const wnw_quant_cache *cache, int32_t first_layer,
+                          int32_t n_layers, int32_t n, void *k_out, void *v_out, const int32_t *pos_dev,
+                          const int32_t *count_dev, void *hip_stream);
+
+/* Attention of a sequence's last count[b] tokens over its cache, their own rows (already written)
+ * among it: token i of count[b] sees rows 0 .. len[b] - count[b] + i.  Logit scale 1 / sqrt(d); the bytes are
+ * multiplied as they are, products summed in fp32, softmax statistics in fp32.  A softmax weight times
+ * its block's V scale is held to 22 bits (bf16 output: 11) and counts down to 2^-39 of the largest V scale of
+ * the rows seen.  A token that sees no row gets zeros and the log-sum-exp -inf.
+ *   q_heads    a multiple of kv_heads (any group size); q-head hq belongs to KV-head hq / (H_q / H_kv)
+ *   q_dev      device bf16 [B][n_layers][H_q][n][d], 16-byte aligned
+ *   len_dev    device int32 [B], rows of the sequence (as the nearer end outside 0 .. capacity)
+ *   count_dev  device int32 [B], 0 .. n (as the nearer end outside); NULL = n for every sequence
+ *   out_dev    device fp32 / bf16 [B][n_layers][H_q][n][d], 16-byte aligned
+ *   lse_dev    device fp32 [B][n_layers][H_q][n], natural log of the sum of exp(logit); may be NULL
+ *   mass_dev   device fp32 [B][n_layers][H_q][capacity / block], only with n = 1: the softmax mass of every
+ *              block of rows, 0 for blocks without rows (Eq. 2 before its sum over heads: sum it over the
+ *              anchor q-heads and divide by the block's rows for the chunk scores); may be NULL
+ *   max_len    upper bound of the lengths, 0 = capacity.  It only shapes the launch: a longer sequence is
+ *              still attended to in full
+ *   workspace  device memory, 16-byte aligned, of at least the bytes that wnw_quant_attend_workspace gives
+ *              for the same cfg, n_layers, q_heads, n and max_len; may be NULL where that is 0.  It holds
+ *              nothing between calls; calls whose work overlaps (two streams, two graphs replayed at once)
+ *              need one each
+ * Outputs of tokens at or after count[b] are left as they were. */
+wnw_status wnw_quant_attend(const wnw_quant_config *cfg, const wnw_quant_cache *cache, int32_t first_layer,
+                            int32_t n_layers, int32_t q_heads, int32_t n, const void *q_dev,
+                            const int32_t *len_dev, const int32_t *count_dev, void *out_dev, float *lse_dev,
+                            float *mass_dev, int32_t max_len, void *workspace, size_t workspace_bytes,
+                            void *hip_stream);
+
+/* Workspace of wnw_quant_attend for these sizes, in bytes (with or without lse_dev and mass_dev). */
+wnw_status wnw_quant_attend_workspace(const wnw_quant_config *cfg, int32_t n_layers, int32_t q_heads,
+                                      int32_t n, int32_t max_len, size_t *bytes);
+
+/* Error reporting, no passage behind it.  Message of the last failed call of this thread on an 8-bit cache. */
+const char *wnw_quant_last_error(void);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,904 @@
+// The 8-bit KV cache: quantising rows as they are written, reading them back, and attention over the
+// bytes.  Layout and formats as in wnw.h.
+//
+//   quant_write_kernel   a tile of 64 rows of one head's K or V per work-group
+//   quant_read_kernel    the same tiles back to fp32 / bf16
+//   quant_token_kernel   attention of few query rows: K and V bytes go from HBM to registers once and
+//                        straight into the matrix cores
+//   quant_merge_kernel   joins the parts of a cache split over work-groups, and finishes the block masses
+//
+// Bytes become fp16 on the way to the matrix cores, exactly: integers up to 127 and e4m3 numbers both fit.
+// A query row is scaled by a power of two (its largest magnitude to 2^14 .. 2^15) and is then exact in fp16 as well, but
+// for elements 2^28 times smaller than the largest, so logits carry fp32 rounding alone.  A softmax weight times its
+// block's V scale is rounded to fp16 once where the output is bf16 (2^-12 next to the output's 2^-9), and
+// to the sum of two fp16 (2^-23) where it is fp32.
+#include "wnw.h"
+#include "wnw_internal.h"
+
+#include <math.h>
+
+#include <algorithm>
+#include <cstring>
+#include <type_traits>
+
+namespace wnw {
+
+namespace {
+
+constexpr int QT = 64;          // rows of a tile
+constexpr int Q_THREADS = 256;  // four wavefronts
+constexpr float Q_LOG2E = 1.4426950408889634f;
+constexpr float Q_LN2 = 0.6931471805599453f;
+constexpr int Q_MAX_CAP = 1 << 24;
+constexpr int64_t Q_MAX_GROUPS = 0xffffffffll / Q_THREADS;   // a launch has fewer than 2^32 threads
+
+typedef _Float16 h2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 h8_t __attribute__((ext_vector_type(8)));
+typedef float qf4_t __attribute__((ext_vector_type(4)));
+typedef unsigned qu2_t __attribute__((ext_vector_type(2)));
+typedef unsigned qu4_t __attribute__((ext_vector_type(4)));
+
+// The cache and the layers of it that a call handles.
+struct QuantGeo {
+    int B, L, H, cap, l0, nl;
+    int bsh;          // log2 of the rows per scale
+    const uint8_t *k, *v;
+    const float *ks, *vs;
+    __host__ __device__ size_t head(int b, int l, int h) const { return ((size_t)b * L + l0 + l) * H + h; }
+};
+
+__device__ inline int q_clamp(int x, int hi)
+{
+    return min(max(x, 0), hi);
+}
+
+// ---- numbers ---------------------------------------------------------------------------------
+
+// Scale of a block whose largest magnitude has the (fp32) bits `amax`; NaN if that is not finite.
+template <int FMT>
+__device__ inline float quant_scale(unsigned amax)
+{
+    if (amax >= 0x7f800000u) return __uint_as_float(0x7fc00000u);
+    if constexpr (FMT == WNW_QUANT_INT8) return fmaxf(__uint_as_float(amax) / 127.f, 0x1p-126f);
+    // amax = 1.m * 2^(e - 127) <= 448 s = 1.75 * 2^8 s
+    const int e = (int)(amax >> 23) - 8 + ((amax & 0x7fffffu) > 0x600000u ? 1 : 0);
+    return __uint_as_float((unsigned)max(e, 1) << 23);
+}
+
+// Four values under scale s (inv = 1 / s) to four bytes: nearest, ties to even.
+// int8: the rounded product with inv is off by one at most, next to a tie; x - n s is exact in fp32 (n s is a
+// multiple of s's last bit, and so is x unless n = 0), so comparing it with s / 2 decides.
+// e4m3: s is a power of two, so the product is exact.
+template <int FMT>
+__device__ inline unsigned quant4(float x0, float x1, float x2, float x3, float s, float inv)
+{
+    if constexpr (FMT == WNW_QUANT_INT8) {
+        float x[4] = {x0, x1, x2, x3}, n[4], e[4];
+        const float half = 0.5f * s;
+        float worst = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            n[i] = rintf(x[i] * inv);
+            e[i] = fmaf(-n[i], s, x[i]);
+            worst = fmaxf(worst, fabsf(e[i]));
+        }
+        if (worst >= half) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bool odd = (int)n[i] & 1;
+                if (e[i] > half || (e[i] == half && odd)) n[i] += 1.f;
+                if (e[i] < -half || (e[i] == -half && odd)) n[i] -= 1.f;
+            }
+        }
+        unsigned r = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r |= (unsigned)((int)n[i] + 128) << (8 * i);
+        return r;
+    } else {
+        const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(x0 * inv, x1 * inv, 0, false);
+        return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(x2 * inv, x3 * inv, lo, true);
+    }
+}
+
+// Byte i of u as a number, before the scale.
+template <int FMT>
+__device__ inline float byte_value(unsigned u, int i)
+{
+    if constexpr (FMT == WNW_QUANT_INT8) return (float)((int)((u >> (8 * i)) & 255) - 128);
+    return __builtin_amdgcn_cvt_f32_fp8((int)(u >> (8 * i)), 0);
+}
+
+// A byte held under scale `was`, rounded again under the larger scale `now`.  int8: quotients that are no tie differ from
+// one by 2^-25 or more, which a double shows.
+template <int FMT>
+__device__ inline unsigned requant(unsigned byte, float was, float now)
+{
+    const float x = byte_value<FMT>(byte, 0);
+    if constexpr (FMT == WNW_QUANT_INT8) return (unsigned)((int)rint((double)x * (double)was / (double)now) + 128);
+    return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(x * (was / now), 0.f, 0, false) & 255u;
+}
+
+// Four bytes to four fp16, exactly.  int8: 0x64 in front of a byte u is the fp16 number 1024 + u.
+template <int FMT>
+__device__ inline void bytes_to_half(unsigned u, h2_t &lo, h2_t &hi)
+{
+    if constexpr (FMT == WNW_QUANT_INT8) {
+        const h2_t bias = {(_Float16)1152, (_Float16)1152};
+        lo = __builtin_bit_cast(h2_t, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) - bias;
+        hi = __builtin_bit_cast(h2_t, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) - bias;
+    } else {
+        lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(u, 1.f, false);
+        hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(u, 1.f, true);
+    }
+}
+template <int FMT>
+__device__ inline h8_t bytes_to_h8(unsigned a, unsigned b)
+{
+    h2_t p0, p1, p2, p3;
+    bytes_to_half<FMT>(a, p0, p1);
+    bytes_to_half<FMT>(b, p2, p3);
+    return h8_t{p0.x, p0.y, p1.x, p1.y, p2.x, p2.y, p3.x, p3.y};
+}
+
+__device__ inline uint16_t to_bf16(float f)
+{
+    return __builtin_bit_cast(uint16_t, (__bf16)f);   // nearest, ties to even
+}
+
+// ---- writing ---------------------------------------------------------------------------------
+
+// Work-group: one tile of 64 rows of one head, K (even) or V (odd).  Wavefront w has rows 16 w .. + 16; its lane has rows
+// 4 rg .. + 4 (rg = 4 w + lane / 16) at dimensions E (lane % 16) .. + E.
+// Dwords of four rows at one dimension, transposed through shared memory for whole tiles of V.
+template <int DH>
+struct QuantTileSmem {
+    static constexpr int E = DH / 16;
+    static constexpr int ROW = E * 16 + 4;   // dwords of a lane's E dimensions, padded: 4-way conflicts, not 16
+    alignas(16) unsigned t[16 * ROW];
+    // dword of rows 4 rg .. + 4 at dimension dg * E + j
+    static __device__ int at(int dg, int j, int rg) { return dg * ROW + j * 16 + (rg & 3) * 4 + (rg >> 2); }
+    // the 16 places from 16 h on of dimension d
+    static __device__ int unit(int d, int h) { return d / E * ROW + d % E * 16 + h * 4; }
+};
+
+template <int DH, int FMT>
+__global__ __launch_bounds__(Q_THREADS) void quant_write_kernel(QuantGeo g, int n, int tiles, const uint16_t *__restrict__ kn,
+                                                               const uint16_t *__restrict__ vn,
+                                                               const int32_t *__restrict__ pos_dev,
+                                                               const int32_t *__restrict__ count_dev)
+{
+    constexpr int E = DH / 16;
+    __shared__ QuantTileSmem<DH> sm;
+    __shared__ unsigned wmax[4];
+    const bool is_v = blockIdx.x & 1;
+    const int item = blockIdx.x >> 1, hd = item / tiles, h = hd % g.H, bl = hd / g.H, l = bl % g.nl, b = bl / g.nl;
+    const int pos = q_clamp(pos_dev[b], g.cap), cnt = count_dev ? q_clamp(count_dev[b], n) : n, end = min(pos + cnt, g.cap);
+    const int tile = pos / QT + (item - hd * tiles), row0 = tile * QT;
+    if (row0 >= end) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, dg = lane & 15, rg = tid >> 4;
+    const size_t head = g.head(b, l, h);
+    uint8_t *codes = const_cast<uint8_t *>(is_v ? g.v : g.k) + (head * g.cap + row0) * DH;
+    float *scales = const_cast<float *>(is_v ? g.vs : g.ks) + ((head * g.cap) >> g.bsh);
+    const uint16_t *src = (is_v ? vn : kn) + (size_t)hd * n * DH + (size_t)dg * E;
+
+    float x[4][E];
+    unsigned amax = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = row0 + rg * 4 + i;
+        if (row >= pos && row < end) {
+            uint16_t u[E];
+            __builtin_memcpy(u, __builtin_assume_aligned(src + (size_t)(row - pos) * DH, E * 2), E * 2);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                x[i][e] = __uint_as_float((unsigned)u[e] << 16);
+                amax = max(amax, __float_as_uint(x[i][e]) & 0x7fffffffu);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[i][e] = 0.f;
+        }
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) amax = max(amax, (unsigned)__shfl_xor((int)amax, o));
+    const int gw = 1 << (g.bsh - 4);                     // wavefronts of a block
+    const int first = row0 + wave / gw * gw * 16;        // the block's first row
+    const bool has_old = first < pos, has_new = first < end && first + gw * 16 > pos;
+    const float was = has_old ? scales[first >> g.bsh] : 0.f;
+    if (lane == 0) wmax[wave] = amax;
+    __syncthreads();
+    for (int w = wave / gw * gw; w < wave / gw * gw + gw; ++w) amax = max(amax, wmax[w]);
+    float s = quant_scale<FMT>(amax);
+    // a NaN on either side stays one
+    if (has_old) s = was != was || s != s ? __uint_as_float(0x7fc00000u) : fmaxf(was, s);
+    const bool good = s == s, grew = has_old && good && s > was;
+    if (has_new && lane == 0 && wave % gw == 0) scales[first >> g.bsh] = s;
+    const float inv = 1.f / s;
+
+    bool put[4], old[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = row0 + rg * 4 + i;
+        put[i] = row >= pos && row < end;
+        old[i] = has_new && grew && row < pos;
+    }
+    constexpr unsigned ZERO = FMT == WNW_QUANT_INT8 ? 0x80808080u : 0u;
+    if (!is_v) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint8_t *to = codes + (size_t)(rg * 4 + i) * DH + dg * E;
+            unsigned w[E / 4];
+            if (put[i]) {
+#pragma unroll
+                for (int e = 0; e < E; e += 4)
+                    w[e / 4] = good ? quant4<FMT>(x[i][e], x[i][e + 1], x[i][e + 2], x[i][e + 3], s, inv) : ZERO;
+            } else if (old[i]) {
+                __builtin_memcpy(w, __builtin_assume_aligned(to, E), E);
+#pragma unroll
+                for (int e = 0; e < E; e += 4) {
+                    unsigned r = 0;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) r |= requant<FMT>((w[e / 4] >> (8 * j)) & 255u, was, s) << (8 * j);
+                    w[e / 4] = r;
+                }
+            }
+            if (put[i] || old[i]) __builtin_memcpy(__builtin_assume_aligned(to, E), w, E);
+        }
+        return;
+    }
+    if (pos <= row0 && end >= row0 + QT) {   // a whole tile of new rows (uniform)
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            sm.t[sm.at(dg, e, rg)] = good ? quant4<FMT>(x[0][e], x[1][e], x[2][e], x[3][e], s, inv) : ZERO;
+        __syncthreads();
+#pragma unroll
+        for (int u = tid; u < DH * 4; u += Q_THREADS)
+            *(qu4_t *)(codes + (size_t)u * 16) = *(const qu4_t *)&sm.t[sm.unit(u >> 2, u & 3)];
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        unsigned *to = (unsigned *)(codes + (size_t)(dg * E + e) * QT) + (rg & 3) * 4 + (rg >> 2);
+        unsigned w = good ? quant4<FMT>(x[0][e], x[1][e], x[2][e], x[3][e], s, inv) : ZERO;
+        if (put[0] && put[1] && put[2] && put[3])
+            *to = w;
+        else {
+            // rows of the dword that are neither new nor rounded again are left alone
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint8_t *at = (uint8_t *)to + i;
+                if (put[i])
+                    *at = (uint8_t)(w >> (8 * i));
+                else if (old[i])
+                    *at = (uint8_t)requant<FMT>(*at, was, s);
+            }
+        }
+    }
+}
+
+// ---- reading back ----------------------------------------------------------------------------
+
+template <int E, bool BF16>
+__device__ inline void store_row(void *out, size_t elem, const float (&x)[E])
+{
+    if constexpr (BF16) {
+        uint16_t u[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) u[e] = to_bf16(x[e]);
+        __builtin_memcpy(__builtin_assume_aligned((uint16_t *)out + elem, E * 2), u, E * 2);
+    } else
+        __builtin_memcpy(__builtin_assume_aligned((float *)out + elem, 16), x, E * 4);
+}
+
+// Work-group and lanes as in quant_write_kernel.
+template <int DH, int FMT, bool BF16>
+__global__ __launch_bounds__(Q_THREADS) void quant_read_kernel(QuantGeo g, int n, int tiles, void *__restrict__ ko,
+                                                              void *__restrict__ vo, const int32_t *__restrict__ pos_dev,
+                                                              const int32_t *__restrict__ count_dev)
+{
+    constexpr int E = DH / 16;
+    __shared__ QuantTileSmem<DH> sm;
+    const bool both = ko && vo, is_v = both ? blockIdx.x & 1 : vo != nullptr;
+    const int item = both ? blockIdx.x >> 1 : blockIdx.x, hd = item / tiles, h = hd % g.H, bl = hd / g.H, l = bl % g.nl,
+              b = bl / g.nl;
+    const int pos = q_clamp(pos_dev[b], g.cap), cnt = count_dev ? q_clamp(count_dev[b], n) : n, end = min(pos + cnt, g.cap);
+    const int tile = pos / QT + (item - hd * tiles), row0 = tile * QT;
+    if (row0 >= end) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, dg = lane & 15, rg = tid >> 4;
+    const size_t head = g.head(b, l, h);
+    const uint8_t *codes = (is_v ? g.v : g.k) + (head * g.cap + row0) * DH;
+    const float s = (is_v ? g.vs : g.ks)[(head * g.cap + row0 + wave * 16) >> g.bsh];
+    void *out = is_v ? vo : ko;
+    const size_t to = (size_t)hd * n * DH + (size_t)dg * E;
+    unsigned w[4][E / 4];    // K: of the lane's four rows
+    if (!is_v) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            __builtin_memcpy(w[i], __builtin_assume_aligned(codes + (size_t)(rg * 4 + i) * DH + dg * E, E), E);
+    } else {
+#pragma unroll
+        for (int u = tid; u < DH * 4; u += Q_THREADS)
+            *(qu4_t *)&sm.t[sm.unit(u >> 2, u & 3)] = *(const qu4_t *)(codes + (size_t)u * 16);
+        __syncthreads();
+    }
+    unsigned t[E];           // V: of the lane's dimensions, a byte for each of its rows
+    if (is_v) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) t[e] = sm.t[sm.at(dg, e, rg)];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = row0 + rg * 4 + i;
+        if (row < pos || row >= end) continue;
+        float x[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = s * (is_v ? byte_value<FMT>(t[e], i) : byte_value<FMT>(w[i][e / 4], e & 3));
+        store_row<E, BF16>(out, to + (size_t)(row - pos) * DH, x);
+    }
+}
+
+// ---- attention -------------------------------------------------------------------------------
+
+struct QuantAttend {
+    QuantGeo g;
+    int G, n, R;               // q-heads per KV-head, tokens, rows G * n of a KV-head: row r is token r / G, q-head r % G
+    int splits;                // parts of a cache
+    const uint16_t *q;
+    const int32_t *len, *count;
+    void *out;
+    float *lse, *mass;
+    float *ws_o;               // [splits][B * nl * H * R][d]: a part's sum of weights times values
+    float2 *ws_ml;             // [splits][B * nl * H * R]: its maximum (base 2) and sum of weights
+    float *ws_m;               // [B * nl * H * R][cap / 64]: the maximum that a tile's masses are relative to
+    float scale;               // log2(e) / sqrt(d)
+};
+
+// Tiles per part of a sequence of len rows.
+__device__ inline int part_tiles(int len, int splits)
+{
+    const int tiles = (len + QT - 1) / QT;
+    return max((tiles + splits - 1) / splits, 4);
+}
+
+struct QuantRow {
+    int row_of;      // index into [B][nl][H_q][n] of row r
+    int vis;         // cache rows it sees; -1: not a row of this call
+};
+__device__ inline QuantRow quant_row(const QuantAttend &a, int hd, int r, int len, int cnt)
+{
+    const int i = r / a.G, j = r - i * a.G;
+    QuantRow q;
+    q.row_of = (hd * a.G + j) * a.n + i;      // hd = (b * nl + l) * H + h
+    q.vis = r < a.R && i < cnt ? max(0, min(len, len - cnt + i + 1)) : -1;
+    return q;
+}
+
+__device__ inline float pow2i(int e)   // 2^e, e in -126 .. 127 (clamped from below)
+{
+    return __uint_as_float((unsigned)(max(e, -126) + 127) << 23);
+}
+
+// Merge of the lane's running maximum m with a tile's
+__device__ inline float finite_or_zero(float m)
+{
+    return m == -INFINITY ? 0.f : m;
+}
+
+// Few query rows.  Grid: parts, then blocks of 16 rows, then heads.  Each wavefront takes tiles of 64 cache rows of
+// the part in turn:
+//   S^T (16 keys x 16 rows) = K Q^T, K bytes straight from registers: lane (key l % 16, quarter l / 16) has 16 bytes of a
+//   row per load, two matrix products of 32 dimensions; which dimensions is the same for Q;
+//   O^T (16 dimensions x 16 rows) += V^T P^T: result element i of S^T is key 4 (l / 16) + i, so that two blocks'
+//   results are P^T's operand as they stand, and the tile's layout gives V^T's: 16 bytes of one dimension.
+// The wavefronts' results meet in shared memory at the end.
+template <int DH, int FMT, bool F32>
+__global__ __launch_bounds__(Q_THREADS, 2) void quant_token_kernel(QuantAttend a)
+{
+    constexpr int NJ = DH / 64, ND = DH / 16;
+    const QuantGeo &g = a.g;
+    const int nrb = (a.R + 15) / 16;
+    const int part = blockIdx.x % a.splits, rest = blockIdx.x / a.splits, rb = rest % nrb, hd = rest / nrb;
+    const int h = hd % g.H, bl = hd / g.H, l = bl % g.nl, b = bl / g.nl;
+    const int len = q_clamp(a.len[b], g.cap), cnt = a.count ? q_clamp(a.count[b], a.n) : a.n;
+    const int per = part_tiles(len, a.splits), tiles = (len + QT - 1) / QT, nparts = (tiles + per - 1) / per;
+    if (rb * 16 / a.G >= cnt || (a.splits > 1 && part >= nparts)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 15, quarter = lane >> 4;
+    const size_t head = g.head(b, l, h);
+    const uint8_t *kh = g.k + head * g.cap * DH, *vh = g.v + head * g.cap * DH;
+    const float *ks = g.ks + ((head * g.cap) >> g.bsh), *vs = g.vs + ((head * g.cap) >> g.bsh);
+
+    const QuantRow qr = quant_row(a, hd, rb * 16 + col, len, cnt);
+    const int seen = min(len, max(0, len - cnt + min(cnt - 1, (min(rb * 16 + 15, a.R - 1)) / a.G) + 1));   // by the last row
+    const int full = len - cnt + rb * 16 / a.G + 1;                                                        // by the first row
+    const int t_end = min(min(tiles, (part + 1) * per), (seen + QT - 1) / QT);
+    int t = part * per + wave;
+
+    // Q^T: column col; quarter q has dimensions 64 j + 16 q .. + 16
+    h8_t qf[2 * NJ];
+    float crow;
+    {
+        qu4_t u[2 * NJ];
+        unsigned amax = 0;
+#pragma unroll
+        for (int j = 0; j < 2 * NJ; ++j) {
+            u[j] = qr.vis >= 0 ? *(const qu4_t *)(a.q + (size_t)qr.row_of * DH + (j >> 1) * 64 + quarter * 16 + (j & 1) * 8)
+                               : qu4_t{0, 0, 0, 0};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) amax = max(amax, max(u[j][e] & 0x7fffu, (u[j][e] >> 16) & 0x7fffu));
+        }
+        amax = max(amax, (unsigned)__shfl_xor((int)amax, 16));
+        amax = max(amax, (unsigned)__shfl_xor((int)amax, 32));
+        const int sh = min(141 - (int)(amax >> 7), 126);       // the largest magnitude goes to 2^14 .. 2^15
+        const float up = pow2i(sh);
+        crow = amax >= 0x7f80u ? __uint_as_float(0x7fc00000u) : a.scale * pow2i(-sh);
+#pragma unroll
+        for (int j = 0; j < 2 * NJ; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                qf[j][2 * e] = (_Float16)(__uint_as_float(u[j][e] << 16) * up);
+                qf[j][2 * e + 1] = (_Float16)(__uint_as_float(u[j][e] & 0xffff0000u) * up);
+            }
+    }
+
+    qu4_t kr[4][NJ], vr[ND];
+    float ksr[4], vsr[4];
+    auto load_k = [&](int t) {
+        const uint8_t *p = kh + (size_t)t * QT * DH + col * DH + quarter * 16;
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) kr[kb][j] = *(const qu4_t *)(p + kb * 16 * DH + j * 64);
+            ksr[kb] = ks[(t * QT + kb * 16) >> g.bsh];
+        }
+    };
+    auto load_v = [&](int t) {
+        const uint8_t *p = vh + (size_t)t * QT * DH + col * QT + quarter * 16;
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt) vr[dt] = *(const qu4_t *)(p + dt * 16 * QT);
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) vsr[kb] = vs[(t * QT + kb * 16) >> g.bsh];
+    };
+
+    qf4_t o[ND];
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt) o[dt] = qf4_t{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, sum = 0.f;
+    int vexp = -100;           // o is in units of 2^(vexp - 15); V scales seen so far are below 2^vexp
+    if (t < t_end) {
+        load_k(t);
+        load_v(t);
+    }
+    for (; t < t_end; t += 4) {
+        const int key0 = t * QT + quarter * 4;
+        float s[4][4];
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+            qf4_t c = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                c = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_to_h8<FMT>(kr[kb][j].x, kr[kb][j].y), qf[2 * j], c, 0, 0, 0);
+                c = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_to_h8<FMT>(kr[kb][j].z, kr[kb][j].w), qf[2 * j + 1], c, 0, 0, 0);
+            }
+            const float f = crow * ksr[kb];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[kb][i] = c[i] * f;
+        }
+        if (t + 4 < t_end) load_k(t + 4);
+        const bool masked = t * QT + QT > full;   // some row does not see all of the tile
+        if (masked) {
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[kb][i] = key0 + kb * 16 + i < qr.vis ? s[kb][i] : -INFINITY;
+        }
+        float mt = m;
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mt = fmaxf(mt, s[kb][i]);
+        mt = fmaxf(mt, __shfl_xor(mt, 16));
+        mt = fmaxf(mt, __shfl_xor(mt, 32));
+
+        // the largest V scale of the tile's blocks of live rows
+        float vmax = 0.f;
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+            if (t * QT + kb * 16 >= len) vsr[kb] = 0.f;
+            vmax = fmaxf(vmax, vsr[kb]);
+        }
+        const int ve = __builtin_amdgcn_readfirstlane((int)(__float_as_uint(vmax) >> 23) - 126);
+        float alpha = exp2f(m - finite_or_zero(mt));
+        if (ve > vexp || __any(mt > m)) {
+            const float f = alpha * (ve > vexp ? pow2i(vexp - ve) : 1.f);
+            vexp = max(vexp, ve);
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt) o[dt] *= f;
+            sum *= alpha;
+            m = mt;
+        }
+        const float mz = finite_or_zero(m), vf = pow2i(15 - vexp);
+        float bs[4];
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+            bs[kb] = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[kb][i] = exp2f(s[kb][i] - mz);
+                bs[kb] += s[kb][i];
+            }
+            sum += bs[kb];
+        }
+        if (a.mass) {
+            // block sums relative to m; the merge makes them shares
+            const int nb = QT >> g.bsh;
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb) {
+                bs[kb] += __shfl_xor(bs[kb], 16);
+                bs[kb] += __shfl_xor(bs[kb], 32);
+            }
+            if (quarter == 0 && qr.vis >= 0) {
+                float *to = a.mass + (size_t)qr.row_of * (g.cap >> g.bsh) + (size_t)t * nb;
+                if (nb == 1)
+                    to[0] = (bs[0] + bs[1]) + (bs[2] + bs[3]);
+                else if (nb == 2) {
+                    to[0] = bs[0] + bs[1];
+                    to[1] = bs[2] + bs[3];
+                } else {
+#pragma unroll
+                    for (int kb = 0; kb < 4; ++kb) to[kb] = bs[kb];
+                }
+                a.ws_m[(size_t)qr.row_of * (g.cap / QT) + t] = m;
+            }
+        }
+        // P^T, times the V scales; a masked weight is 0 whatever the scale is
+        h8_t ph[2], pl[2];
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+            const float f = vsr[kb] * vf;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[kb][i] *= f;
+        }
+        if (masked) {
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[kb][i] = key0 + kb * 16 + i < qr.vis ? s[kb][i] : 0.f;
+        }
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float p = s[kb][i];
+                const _Float16 hi = (_Float16)p;
+                ph[kb >> 1][(kb & 1) * 4 + i] = hi;
+                if constexpr (F32) pl[kb >> 1][(kb & 1) * 4 + i] = (_Float16)(p - (float)hi);
+            }
+        }
+        if (FMT == WNW_QUANT_E4M3 && t * QT + QT > len) {
+            // bytes of dead rows may be e4m3's NaN
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb) {
+                const int live = len - (key0 + kb * 16);
+                const unsigned mask = live >= 4 ? ~0u : live <= 0 ? 0u : (1u << (8 * live)) - 1;
+#pragma unroll
+                for (int dt = 0; dt < ND; ++dt) vr[dt][kb] &= mask;
+            }
+        }
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const h8_t v = bytes_to_h8<FMT>(vr[dt][2 * c], vr[dt][2 * c + 1]);
+                o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph[c], o[dt], 0, 0, 0);
+                if constexpr (F32) o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl[c], o[dt], 0, 0, 0);
+            }
+        if (t + 4 < t_end) load_v(t + 4);
+    }
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+
+    __shared__ float sm_m[4][16], sm_l[4][16];
+    __shared__ alignas(16) float sm_o[4][16][DH + 4];
+    {
+        const float unit = pow2i(vexp - 15);
+        if (quarter == 0) {
+            sm_m[wave][col] = m;
+            sm_l[wave][col] = sum;
+        }
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt) *(qf4_t *)&sm_o[wave][col][dt * 16 + quarter * 4] = o[dt] * unit;
+    }
+    __syncthreads();
+    const bool whole = a.splits == 1;
+    const int row = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * (DH / 16);
+    const QuantRow rr = quant_row(a, hd, rb * 16 + row, len, cnt);
+    if (rr.vis < 0) return;
+    float mm = -INFINITY, ll = 0.f, x[DH / 16];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) mm = fmaxf(mm, sm_m[w][row]);
+#pragma unroll
+    for (int e = 0; e < DH / 16; ++e) x[e] = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const float lw = sm_l[w][row];
+        if (lw == 0.f) continue;
+        const float f = exp2f(sm_m[w][row] - finite_or_zero(mm));
+        ll += f * lw;
+#pragma unroll
+        for (int e = 0; e < DH / 16; ++e) x[e] += f * sm_o[w][row][d0 + e];
+    }
+    const size_t NR = (size_t)g.B * g.nl * g.H * a.R, flat = (size_t)part * NR + rr.row_of;
+    if (!whole) {
+        __builtin_memcpy(a.ws_o + flat * DH + d0, x, sizeof(x));
+        if (d0 == 0) a.ws_ml[flat] = make_float2(mm, ll);
+        return;
+    }
+    const float inv = ll == 0.f ? 0.f : 1.f / ll;
+#pragma unroll
+    for (int e = 0; e < DH / 16; ++e) x[e] *= inv;
+    store_row<DH / 16, !F32>(a.out, (size_t)rr.row_of * DH + d0, x);
+    if (d0 == 0) {
+        if (a.lse) a.lse[rr.row_of] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * Q_LN2;
+        if (a.mass) a.ws_ml[rr.row_of] = make_float2(mm, ll);
+    }
+}
+
+// Joins the parts of every output row (one wavefront each) and makes the tiles' block sums shares of the whole.
+template <int DH, bool BF16>
+__global__ __launch_bounds__(Q_THREADS) void quant_merge_kernel(QuantAttend a)
+{
+    const QuantGeo &g = a.g;
+    const int64_t NR = (int64_t)g.B * g.nl * g.H * a.R, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= NR) return;
+    const int lane = threadIdx.x & 63, i = (int)(row % a.n), b = (int)(row / ((int64_t)g.nl * g.H * a.R));
+    const int len = q_clamp(a.len[b], g.cap), cnt = a.count ? q_clamp(a.count[b], a.n) : a.n;
+    if (i >= cnt) return;
+    const int tiles = (len + QT - 1) / QT, per = part_tiles(len, a.splits);
+    const int parts = a.splits == 1 ? 1 : (tiles + per - 1) / per;
+    float m = -INFINITY, sum = 0.f;
+    for (int p = 0; p < parts; ++p) m = fmaxf(m, a.ws_ml[p * NR + row].x);
+    const float mz = finite_or_zero(m);
+    float x[DH / 64] = {};
+    for (int p = 0; p < parts; ++p) {
+        const float2 ml = a.ws_ml[p * NR + row];
+        if (ml.y == 0.f) continue;          // saw nothing
+        const float f = exp2f(ml.x - mz);
+        sum += f * ml.y;
+        if (a.splits > 1) {
+#pragma unroll
+            for (int e = 0; e < DH / 64; ++e) x[e] += f * a.ws_o[(p * NR + row) * DH + lane * (DH / 64) + e];
+        }
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    if (a.splits > 1) {
+#pragma unroll
+        for (int e = 0; e < DH / 64; ++e) {
+            const size_t at = row * DH + lane * (DH / 64) + e;
+            if constexpr (BF16)
+                ((uint16_t *)a.out)[at] = to_bf16(x[e] * inv);
+            else
+                ((float *)a.out)[at] = x[e] * inv;
+        }
+        if (a.lse && lane == 0) a.lse[row] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * Q_LN2;
+    }
+    if (a.mass) {
+        const int blocks = g.cap >> g.bsh, live = (len + (1 << g.bsh) - 1) >> g.bsh, per_tile = QT >> g.bsh;
+        float *to = a.mass + row * blocks;
+        for (int j = lane; j < blocks; j += 64) {
+            float w = 0.f;
+            if (j < live) {
+                const float mt = a.ws_m[row * (g.cap / QT) + j / per_tile];
+                w = to[j] * (exp2f(mt - mz) * inv);
+            }
+            to[j] = w;
+        }
+    }
+}
+
+// ---- host ------------------------------------------------------------------------------------
+
+thread_local char q_msg[256] = "no error";
+
+wnw_status quant_fail(wnw_status st, const char *msg)
+{
+    strncpy(q_msg, msg, sizeof q_msg - 1);
+    return st;
+}
+wnw_status quant_hip()
+{
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? WNW_OK : quant_fail(WNW_ERR_HIP, hipGetErrorString(e));
+}
+
+bool aligned16(const void *p)
+{
+    return ((uintptr_t)p & 15) == 0;
+}
+
+wnw_status quant_config(const wnw_quant_config *c, int32_t first_layer, int32_t n_layers, int32_t n)
+{
+    if (!c) return quant_fail(WNW_ERR_INVALID, "NULL configuration");
+    if (c->batch < 1 || c->layers < 1 || c->kv_heads < 1) return quant_fail(WNW_ERR_INVALID, "batch, layers and kv_heads must be at least 1");
+    if (c->head_dim != 64 && c->head_dim != 128) return quant_fail(WNW_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
+    if (c->block != 16 && c->block != 32 && c->block != 64) return quant_fail(WNW_ERR_UNSUPPORTED, "block must be 16, 32 or 64");
+    if (c->capacity < QT || c->capacity % QT) return quant_fail(WNW_ERR_INVALID, "capacity must be a positive multiple of 64");
+    if (c->capacity > Q_MAX_CAP) return quant_fail(WNW_ERR_UNSUPPORTED, "capacity above 2^24 rows");
+    if (c->format != WNW_QUANT_INT8 && c->format != WNW_QUANT_E4M3) return quant_fail(WNW_ERR_INVALID, "unknown format");
+    if (c->flags & ~(uint32_t)WNW_F_OUT_BF16) return quant_fail(WNW_ERR_INVALID, "unknown flag bits");
+    if (first_layer < 0 || n_layers < 1 || first_layer > c->layers - n_layers)
+        return quant_fail(WNW_ERR_INVALID, "layers outside the cache's");
+    if (n < 0 || n > c->capacity) return quant_fail(WNW_ERR_INVALID, "n outside 0 .. capacity");
+    if ((int64_t)c->batch * n_layers > INT32_MAX / c->kv_heads) return quant_fail(WNW_ERR_UNSUPPORTED, "too many heads");
+    return WNW_OK;
+}
+
+wnw_status quant_cache(const wnw_quant_cache *c)
+{
+    if (!c || !c->k || !c->v || !c->k_scale || !c->v_scale) return quant_fail(WNW_ERR_INVALID, "NULL cache pointer");
+    if (!aligned16(c->k) || !aligned16(c->v)) return quant_fail(WNW_ERR_INVALID, "cache bytes must be aligned to 16 bytes");
+    if (((uintptr_t)c->k_scale | (uintptr_t)c->v_scale) & 3) return quant_fail(WNW_ERR_INVALID, "scales must be aligned to 4 bytes");
+    return WNW_OK;
+}
+
+QuantGeo quant_geo(const wnw_quant_config &c, const wnw_quant_cache &k, int32_t l0, int32_t nl)
+{
+    return QuantGeo{c.batch, c.layers, c.kv_heads, c.capacity, l0, nl, c.block == 16 ? 4 : c.block == 32 ? 5 : 6,
+                    k.k, k.v, k.k_scale, k.v_scale};
+}
+
+// Tiles that n rows from any position on can touch.
+int64_t touched_tiles(int32_t n)
+{
+    return ((int64_t)n + QT - 2) / QT + 1;
+}
+
+// Calls f with the configuration's head dimension and format as constants.
+template <typename F>
+void quant_dispatch(const wnw_quant_config &c, F f)
+{
+    using I0 = std::integral_constant<int, WNW_QUANT_INT8>;
+    using I1 = std::integral_constant<int, WNW_QUANT_E4M3>;
+    using D0 = std::integral_constant<int, 64>;
+    using D1 = std::integral_constant<int, 128>;
+    if (c.head_dim == 64)
+        c.format == WNW_QUANT_INT8 ? f(D0{}, I0{}) : f(D0{}, I1{});
+    else
+        c.format == WNW_QUANT_INT8 ? f(D1{}, I0{}) : f(D1{}, I1{});
+}
+
+// Sizes of an attention call: parts of a cache, output rows, and the workspace's three arrays.
+struct QuantPlan {
+    int splits;
+    int64_t rows, o_bytes, ml_bytes, m_bytes;
+    int64_t total() const { return o_bytes + ml_bytes + m_bytes; }
+};
+int64_t round16(int64_t x)
+{
+    return (x + 15) / 16 * 16;
+}
+QuantPlan quant_plan(const wnw_quant_config &c, int32_t n_layers, int32_t q_heads, int32_t n, int32_t max_len)
+{
+    const int64_t heads = (int64_t)c.batch * n_layers * c.kv_heads, R = (int64_t)q_heads / c.kv_heads * n;
+    const int64_t groups = heads * ((R + 15) / 16);
+    const int64_t tiles = ((max_len ? std::min(max_len, c.capacity) : c.capacity) + QT - 1) / QT;
+    QuantPlan p;
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(768 / std::max<int64_t>(groups, 1), (tiles + 3) / 4));
+    p.rows = heads * R;
+    p.o_bytes = p.splits > 1 ? p.splits * p.rows * c.head_dim * 4 : 0;
+    p.ml_bytes = p.splits > 1 || n == 1 ? round16(p.splits * p.rows * 8) : 0;
+    p.m_bytes = n == 1 ? round16(p.rows * (c.capacity / QT) * 4) : 0;
+    return p;
+}
+
+wnw_status quant_heads(const wnw_quant_config &c, int32_t n_layers, int32_t q_heads, int32_t n, int32_t max_len)
+{
+    if (q_heads < c.kv_heads || q_heads % c.kv_heads) return quant_fail(WNW_ERR_INVALID, "q_heads must be a multiple of kv_heads");
+    if (max_len < 0) return quant_fail(WNW_ERR_INVALID, "negative max_len");
+    if ((int64_t)c.batch * n_layers * q_heads > 4 * Q_MAX_GROUPS / std::max(n, 1))
+        return quant_fail(WNW_ERR_UNSUPPORTED, "too many query rows");
+    return WNW_OK;
+}
+
+}  // namespace
+
+}  // namespace wnw
+
+using namespace wnw;
+
+extern "C" {
+
+const char *wnw_quant_last_error(void)
+{
+    return q_msg;
+}
+
+wnw_status wnw_quant_write(const wnw_quant_config *cfg, const wnw_quant_cache *cache, int32_t first_layer, int32_t n_layers,
+                           int32_t n, const void *k_dev, const void *v_dev, const int32_t *pos_dev, const int32_t *count_dev,
+                           void *hip_stream)
+{
+    wnw_status st = quant_config(cfg, first_layer, n_layers, n);
+    if (st == WNW_OK) st = quant_cache(cache);
+    if (st != WNW_OK) return st;
+    if (n == 0) return WNW_OK;
+    if (!k_dev || !v_dev || !pos_dev) return quant_fail(WNW_ERR_INVALID, "NULL pointer");
+    if (!aligned16(k_dev) || !aligned16(v_dev)) return quant_fail(WNW_ERR_INVALID, "rows must be aligned to 16 bytes");
+    const int64_t tiles = touched_tiles(n), groups = 2 * tiles * cfg->batch * n_layers * cfg->kv_heads;
+    if (groups > Q_MAX_GROUPS) return quant_fail(WNW_ERR_UNSUPPORTED, "too many rows for one call");
+    const QuantGeo g = quant_geo(*cfg, *cache, first_layer, n_layers);
+    quant_dispatch(*cfg, [&](auto d, auto f) {
+        hipLaunchKernelGGL((quant_write_kernel<decltype(d)::value, decltype(f)::value>), dim3((unsigned)groups), dim3(Q_THREADS), 0,
+                           (hipStream_t)hip_stream, g, n, (int)tiles, (const uint16_t *)k_dev, (const uint16_t *)v_dev, pos_dev,
+                           count_dev);
+    });
+    return quant_hip();
+}
+
+wnw_status wnw_quant_read(const wnw_quant_config *cfg, const wnw_quant_cache *cache, int32_t first_layer, int32_t n_layers,
+                          int32_t n, void *k_out, void *v_out, const int32_t *pos_dev, const int32_t *count_dev, void *hip_stream)
+{
+    wnw_status st = quant_config(cfg, first_layer, n_layers, n);
+    if (st == WNW_OK) st = quant_cache(cache);
+    if (st != WNW_OK) return st;
+    if (n == 0 || (!k_out && !v_out)) return WNW_OK;
+    if (!pos_dev) return quant_fail(WNW_ERR_INVALID, "NULL pointer");
+    if (!aligned16(k_out) || !aligned16(v_out)) return quant_fail(WNW_ERR_INVALID, "outputs must be aligned to 16 bytes");
+    const int64_t tiles = touched_tiles(n), groups = (k_out && v_out ? 2 : 1) * tiles * cfg->batch * n_layers * cfg->kv_heads;
+    if (groups > Q_MAX_GROUPS) return quant_fail(WNW_ERR_UNSUPPORTED, "too many rows for one call");
+    const QuantGeo g = quant_geo(*cfg, *cache, first_layer, n_layers);
+    const bool bf16 = cfg->flags & WNW_F_OUT_BF16;
+    quant_dispatch(*cfg, [&](auto d, auto f) {
+        constexpr int DH = decltype(d)::value, FMT = decltype(f)::value;
+        hipLaunchKernelGGL((bf16 ? quant_read_kernel<DH, FMT, true> : quant_read_kernel<DH, FMT, false>), dim3((unsigned)groups),
+                           dim3(Q_THREADS), 0, (hipStream_t)hip_stream, g, n, (int)tiles, k_out, v_out, pos_dev, count_dev);
+    });
+    return quant_hip();
+}
+
+wnw_status wnw_quant_attend_workspace(const wnw_quant_config *cfg, int32_t n_layers, int32_t q_heads, int32_t n, int32_t max_len,
+                                      size_t *bytes)
+{
+    wnw_status st = quant_config(cfg, 0, n_layers, n);
+    if (st == WNW_OK) st = quant_heads(*cfg, n_layers, q_heads, n, max_len);
+    if (st != WNW_OK) return st;
+    if (!bytes) return quant_fail(WNW_ERR_INVALID, "NULL pointer");
+    *bytes = (size_t)quant_plan(*cfg, n_layers, q_heads, n, max_len).total();
+    return WNW_OK;
+}
+
+wnw_status wnw_quant_attend(const wnw_quant_config *cfg, const wnw_quant_cache *cache, int32_t first_layer, int32_t n_layers,
+                            int32_t q_heads, int32_t n, const void *q_dev, const int32_t *len_dev, const int32_t *count_dev,
+                            void *out_dev, float *lse_dev, float *mass_dev, int32_t max_len, void *workspace,
+                            size_t workspace_bytes, void *hip_stream)
+{
+    wnw_status st = quant_config(cfg, first_layer, n_layers, n);
+    if (st == WNW_OK) st = quant_cache(cache);
+    if (st == WNW_OK) st = quant_heads(*cfg, n_layers, q_heads, n, max_len);
+    if (st != WNW_OK) return st;
+    if (mass_dev && n > 1) return quant_fail(WNW_ERR_INVALID, "block masses are of single tokens (n = 1)");
+    if (n == 0) return WNW_OK;
+    if (!q_dev || !len_dev || !out_dev) return quant_fail(WNW_ERR_INVALID, "NULL pointer");
+    if (!aligned16(q_dev) || !aligned16(out_dev)) return quant_fail(WNW_ERR_INVALID, "queries and outputs must be aligned to 16 bytes");
+    const QuantPlan p = quant_plan(*cfg, n_layers, q_heads, n, max_len);
+    if (p.total() && (!workspace || !aligned16(workspace) || workspace_bytes < (size_t)p.total()))
+        return quant_fail(WNW_ERR_INVALID, "workspace missing, too small or not aligned to 16 bytes");
+    const int G = q_heads / cfg->kv_heads, R = G * n;
+    const int64_t groups = (int64_t)cfg->batch * n_layers * cfg->kv_heads * ((R + 15) / 16) * p.splits;
+    if (groups > Q_MAX_GROUPS) return quant_fail(WNW_ERR_UNSUPPORTED, "too many query rows");
+    char *ws = (char *)workspace;
+    QuantAttend a = {quant_geo(*cfg, *cache, first_layer, n_layers), G, n, R, p.splits, (const uint16_t *)q_dev, len_dev, count_dev,
+                     out_dev, lse_dev, mass_dev, (float *)ws, (float2 *)(ws + p.o_bytes), (float *)(ws + p.o_bytes + p.ml_bytes),
+                     Q_LOG2E / sqrtf((float)cfg->head_dim)};
+    const bool bf16 = cfg->flags & WNW_F_OUT_BF16;
+    quant_dispatch(*cfg, [&](auto d, auto f) {
+        constexpr int DH = decltype(d)::value, FMT = decltype(f)::value;
+        hipLaunchKernelGGL((bf16 ? quant_token_kernel<DH, FMT, false> : quant_token_kernel<DH, FMT, true>), dim3((unsigned)groups),
+                           dim3(Q_THREADS), 0, (hipStream_t)hip_stream, a);
+        if (p.splits > 1 || mass_dev)
+            hipLaunchKernelGGL((bf16 ? quant_merge_kernel<DH, true> : quant_merge_kernel<DH, false>),
+                               dim3((unsigned)((p.rows + 3) / 4)), dim3(Q_THREADS), 0, (hipStream_t)hip_stream, a);
+    });
+    return quant_hip();
+}
+
+}  // extern "C"

@@ -19,6 +19,7 @@ WNW_OK, WNW_ERR_INVALID, WNW_ERR_OOM, WNW_ERR_HIP, WNW_ERR_STATE, WNW_ERR_UNSUPP
 WNW_ANCHOR, WNW_TIDAL, WNW_FIXED = 0, 1, 2
 WNW_F_SELECT_NEXT_STEP, WNW_F_RECALL_MEMCPY, WNW_F_TIMING, WNW_F_OVERLAP_CHUNKS, WNW_F_PREFILL_GLOBAL = 1, 2, 4, 8, 16
 WNW_F_OUT_BF16 = 32
+WNW_QUANT_INT8, WNW_QUANT_E4M3 = 0, 1
 
 EXPORTS = ("wnw_init_cache", "wnw_set_retention", "wnw_set_roles", "wnw_prefill_scores", "wnw_prefill_scores_static",
            "wnw_set_roles_device",
@@ -27,7 +28,8 @@ EXPORTS = ("wnw_init_cache", "wnw_set_retention", "wnw_set_roles", "wnw_prefill_
            "wnw_set_selection_override", "wnw_debug_read_slot", "wnw_debug_read_host_chunk",
            "wnw_debug_set_slot_offset_limit", "wnw_debug_set_recall_delay",
            "wnw_debug_read_resident", "wnw_last_error", "wnw_destroy", "wnw_voice_hits", "wnw_key_sensitivity",
-           "wnw_triage", "wnw_triage_last_error")
+           "wnw_triage", "wnw_triage_last_error",
+           "wnw_quant_write", "wnw_quant_read", "wnw_quant_attend", "wnw_quant_attend_workspace", "wnw_quant_last_error")
 
 
 class wnw_config(C.Structure):
@@ -53,6 +55,15 @@ class wnw_stats(C.Structure):
         return {name: getattr(self, name) for name, _ in self._fields_}
 
 
+class wnw_quant_config(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("layers", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("capacity", C.c_int32), ("block", C.c_int32), ("format", C.c_int32), ("flags", C.c_uint32)]
+
+
+class wnw_quant_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
 class WnwError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"wnw status {status}: {msg}")
@@ -75,6 +86,11 @@ def _load():
         "wnw_key_sensitivity": ([I32, I32, I32, I32, P, P, P], C.c_int),
         "wnw_triage": ([I32, I32, I32, I32, P, P, I32, P, I32, I32, P, P, P, P], C.c_int),
         "wnw_triage_last_error": ([], C.c_char_p),
+        "wnw_quant_write": ([P, P, I32, I32, I32, P, P, P, P, P], C.c_int),
+        "wnw_quant_read": ([P, P, I32, I32, I32, P, P, P, P, P], C.c_int),
+        "wnw_quant_attend": ([P, P, I32, I32, I32, I32, P, P, P, P, P, P, I32, P, SZ, P], C.c_int),
+        "wnw_quant_attend_workspace": ([P, I32, I32, I32, I32, C.POINTER(SZ)], C.c_int),
+        "wnw_quant_last_error": ([], C.c_char_p),
         "wnw_set_roles_device": ([P, P, P], C.c_int),
         "wnw_query_head_keep": ([P, P], C.c_int),
         "wnw_decode_step": ([P, P, P, P, P, P], C.c_int),
@@ -115,8 +131,8 @@ def _ptr(t):
     return t.ctypes.data
 
 
-# element sizes the library reads or writes: bf16 bit patterns (any 2-byte dtype), fp32, int32
-_BF16, _F32, _I32 = "bf16", "f32", "i32"
+# element sizes the library reads or writes: bf16 bit patterns (any 2-byte dtype), fp32, int32, bytes
+_BF16, _F32, _I32, _U8 = "bf16", "f32", "i32", "u8"
 
 
 def _dev(t, kind, numel=None, what="tensor"):
@@ -128,7 +144,7 @@ def _dev(t, kind, numel=None, what="tensor"):
         raise TypeError(f"{what} must be a device tensor")
     import torch
     ok = {_BF16: t.element_size() == 2 and not t.dtype.is_complex,
-          _F32: t.dtype == torch.float32, _I32: t.dtype == torch.int32}[kind]
+          _F32: t.dtype == torch.float32, _I32: t.dtype == torch.int32, _U8: t.dtype == torch.uint8}[kind]
     if not ok:
         raise TypeError(f"{what}: expected {kind} elements, got {t.dtype}")
     if not t.is_contiguous():
@@ -235,6 +251,113 @@ def wnw_triage(hits, top_k, sens, sample, n_voice, n_anchor):
     _tcheck(lib.wnw_triage(L, Hkv, Hq // Hkv, n, _ptr(sample), _ptr(hits), top_k, _ptr(sens), n_voice, n_anchor,
                            _ptr(roles), _ptr(imp), _ptr(vs), _ptr(hs)))
     return roles, imp, vs, hs
+
+
+class QuantCache:
+    """The buffers of an 8-bit cache (see wnw.h): k uint8 [B][L][H_kv][capacity][d], v uint8
+    [B][L][H_kv][capacity / 64][d][64], scales fp32 [B][L][H_kv][capacity / block]."""
+
+    def __init__(self, k, v, k_scale, v_scale):
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+
+    def _struct(self, cfg, device):
+        n = cfg.batch * cfg.layers * cfg.kv_heads * cfg.capacity
+        scales = n // max(cfg.block, 1)
+        return wnw_quant_cache(_on(device, self.k, _U8, n * cfg.head_dim, "k"), _on(device, self.v, _U8, n * cfg.head_dim, "v"),
+                               _on(device, self.k_scale, _F32, scales, "k_scale"),
+                               _on(device, self.v_scale, _F32, scales, "v_scale"))
+
+
+def make_quant_config(batch, layers, kv_heads, capacity, block, format, head_dim=128, flags=0) -> wnw_quant_config:
+    return wnw_quant_config(batch, layers, kv_heads, head_dim, capacity, block, format, flags)
+
+
+def make_quant_cache(cfg, device="cuda") -> QuantCache:
+    """New buffers for cfg on a device, uninitialised: no row is meaningful before it is written."""
+    import torch
+    heads = (cfg.batch, cfg.layers, cfg.kv_heads)
+    scales = [torch.empty((*heads, cfg.capacity // cfg.block), dtype=torch.float32, device=device) for _ in range(2)]
+    return QuantCache(torch.empty((*heads, cfg.capacity, cfg.head_dim), dtype=torch.uint8, device=device),
+                      torch.empty((*heads, cfg.capacity // 64, cfg.head_dim, 64), dtype=torch.uint8, device=device), *scales)
+
+
+def _qcheck(status):
+    if status != WNW_OK:
+        raise WnwError(status, lib.wnw_quant_last_error().decode())
+
+
+def _on(device, t, kind, numel, what):
+    """_dev() for a tensor that must be on `device`, the one that the call's work runs on."""
+    if hasattr(t, "device") and t.device != device:
+        raise ValueError(f"{what} is on {t.device}, the call's work on {device}")
+    return _dev(t, kind, numel, what)
+
+
+def _quant_shape(cfg, t, heads, what):
+    """(layers, tokens) of rows [B][n_layers][heads][n][d]."""
+    if t.dim() != 5 or t.shape[0] != cfg.batch or t.shape[2] != heads or t.shape[4] != cfg.head_dim:
+        raise ValueError(f"{what}: expected [{cfg.batch}][n_layers][{heads}][n][{cfg.head_dim}], got {list(t.shape)}")
+    return t.shape[1], t.shape[3]
+
+
+def _quant_device():
+    import torch
+    return torch.device("cuda", torch.cuda.current_device())
+
+
+def wnw_quant_write(cfg, cache, k_dev, v_dev, pos_dev, count_dev=None, first_layer=0, stream=None):
+    """k_dev, v_dev bf16 [B][n_layers][H_kv][n][d] -> rows pos[b] .. pos[b] + count[b] - 1 of the cache
+    (pos_dev, count_dev: int32 [B])."""
+    nl, n = _quant_shape(cfg, k_dev, cfg.kv_heads, "k_dev")
+    if v_dev.shape != k_dev.shape:
+        raise ValueError(f"v_dev: expected {list(k_dev.shape)}, got {list(v_dev.shape)}")
+    dev = _quant_device()
+    _qcheck(lib.wnw_quant_write(C.byref(cfg), C.byref(cache._struct(cfg, dev)), first_layer, nl, n,
+                                _on(dev, k_dev, _BF16, None, "k_dev"), _on(dev, v_dev, _BF16, None, "v_dev"),
+                                _on(dev, pos_dev, _I32, cfg.batch, "pos_dev"), _on(dev, count_dev, _I32, cfg.batch, "count_dev"),
+                                _stream(stream)))
+
+
+def wnw_quant_read(cfg, cache, k_out, v_out, pos_dev, count_dev=None, first_layer=0, stream=None):
+    """Rows pos[b] .. pos[b] + count[b] - 1 -> k_out, v_out [B][n_layers][H_kv][n][d], fp32 or (WNW_F_OUT_BF16)
+    bf16; one of the two may be None."""
+    some = k_out if k_out is not None else v_out
+    if some is None:
+        raise ValueError("k_out or v_out must be given")
+    nl, n = _quant_shape(cfg, some, cfg.kv_heads, "k_out" if k_out is not None else "v_out")
+    if v_out is not None and v_out.shape != some.shape:
+        raise ValueError(f"v_out: expected {list(some.shape)}, got {list(v_out.shape)}")
+    dev, kind = _quant_device(), _BF16 if cfg.flags & WNW_F_OUT_BF16 else _F32
+    _qcheck(lib.wnw_quant_read(C.byref(cfg), C.byref(cache._struct(cfg, dev)), first_layer, nl, n,
+                               _on(dev, k_out, kind, None, "k_out"), _on(dev, v_out, kind, None, "v_out"),
+                               _on(dev, pos_dev, _I32, cfg.batch, "pos_dev"), _on(dev, count_dev, _I32, cfg.batch, "count_dev"),
+                               _stream(stream)))
+
+
+def wnw_quant_attend_workspace(cfg, n_layers, q_heads, n, max_len=0) -> int:
+    """Bytes of workspace that wnw_quant_attend needs for these sizes."""
+    need = C.c_size_t()
+    _qcheck(lib.wnw_quant_attend_workspace(C.byref(cfg), n_layers, q_heads, n, max_len, C.byref(need)))
+    return need.value
+
+
+def wnw_quant_attend(cfg, cache, q_dev, out_dev, len_dev, count_dev=None, lse_dev=None, mass_dev=None, workspace=None,
+                     max_len=0, first_layer=0, stream=None):
+    """q_dev bf16 [B][n_layers][H_q][n][d] -> out_dev (same shape, fp32 or bf16), lse_dev fp32 [B][n_layers][H_q][n],
+    mass_dev fp32 [B][n_layers][H_q][capacity / block] (n = 1); workspace: a uint8 tensor of
+    wnw_quant_attend_workspace() bytes or more."""
+    Hq = q_dev.shape[2] if q_dev.dim() == 5 else 0
+    nl, n = _quant_shape(cfg, q_dev, Hq, "q_dev")
+    if out_dev.shape != q_dev.shape:
+        raise ValueError(f"out_dev: expected {list(q_dev.shape)}, got {list(out_dev.shape)}")
+    dev, rows = _quant_device(), cfg.batch * nl * Hq
+    _qcheck(lib.wnw_quant_attend(
+        C.byref(cfg), C.byref(cache._struct(cfg, dev)), first_layer, nl, Hq, n, _on(dev, q_dev, _BF16, None, "q_dev"),
+        _on(dev, len_dev, _I32, cfg.batch, "len_dev"), _on(dev, count_dev, _I32, cfg.batch, "count_dev"),
+        _on(dev, out_dev, _BF16 if cfg.flags & WNW_F_OUT_BF16 else _F32, None, "out_dev"),
+        _on(dev, lse_dev, _F32, rows * n, "lse_dev"),
+        _on(dev, mass_dev, _F32, rows * (cfg.capacity // max(cfg.block, 1)), "mass_dev"), max_len,
+        _on(dev, workspace, _U8, None, "workspace"), 0 if workspace is None else workspace.numel(), _stream(stream)))
 
 
 def wnw_append_kv(ctx, k_new_dev, v_new_dev, stream=None):
