@@ -5,7 +5,7 @@
 //   quant_read_kernel    the same tiles back to fp32 / bf16
 //   quant_token_kernel   attention of few query rows: K and V bytes go from HBM to registers once and
 //                        straight into the matrix cores
-//   quant_merge_kernel   joins the parts of a cache split over work-groups, and finishes the block masses
+//   quant_merge_kernel   joins the pieces of a cache split over work-groups, and finishes the block masses
 //
 // Bytes become fp16 on the way to the matrix cores, exactly: integers up to 127 and e4m3 numbers both fit.
 // A query row is scaled by a power of two (its largest magnitude to 2^14 .. 2^15) and is then exact in fp16 as well, but
@@ -342,23 +342,146 @@ __global__ __launch_bounds__(Q_THREADS) void quant_read_kernel(QuantGeo g, int n
 struct QuantAttend {
     QuantGeo g;
     int G, n, R;               // q-heads per KV-head, tokens, rows G * n of a KV-head: row r is token r / G, q-head r % G
-    int splits;                // parts of a cache
+    int W, RB;                 // work-groups that share the batch's tiles, rows of a block
     const uint16_t *q;
     const int32_t *len, *count;
     void *out;
     float *lse, *mass;
-    float *ws_o;               // [splits][B * nl * H * R][d]: a part's sum of weights times values
-    float2 *ws_ml;             // [splits][B * nl * H * R]: its maximum (base 2) and sum of weights
-    float *ws_m;               // [B * nl * H * R][cap / 64]: the maximum that a tile's masses are relative to
+    float *ws_o;               // [W][2][RB][d]: sums of weights times values of a block of rows over a piece of its cache
+    float2 *ws_ml;             // [W][2][RB]: the piece's maximum (base 2) and sum of weights
+    float2 *ws_row;            // masses: [rows] maximum and sum of rows whose cache is one piece
+    float *ws_m;               // masses: [rows][cap / 64] the maximum that a tile's masses are relative to
     float scale;               // log2(e) / sqrt(d)
 };
 
-// Tiles per part of a sequence of len rows.
-__device__ inline int part_tiles(int len, int splits)
+// Work of a batch: every block of RB query rows of every head has its sequence's tiles (one at least, so that an
+// empty sequence's outputs are written).  W work-groups share them, whatever the lengths are, in one of two ways:
+//   pieces  a block's tiles are cut into pieces of at most `pp` tiles, a work-group each;
+//   line    all tiles in a line, in the order sequence, head, block of rows, tile, are cut into W equal parts (pp = 0), so that a
+//           work-group's part may end one block and begin another.
+// The line is even, but a second block costs a work-group about PIECE_COST tiles' time again (its queries, first tiles and
+// the join of its wavefronts).  A block that is not whole leaves its result in the workspace, in the work-group's slot 1
+// (its first tiles) or 0 (later ones), and quant_merge_kernel joins those.
+constexpr int MIN_PIECE = 4;    // tiles of a piece at least, one per wavefront
+constexpr int PIECE_COST = 3;
+
+struct QuantSeq {
+    int len, cnt, tiles, nrb;   // rows, tokens of this call, tiles and blocks of rows of a head (0: none)
+};
+__device__ inline QuantSeq quant_seq(const QuantAttend &a, int b)
 {
-    const int tiles = (len + QT - 1) / QT;
-    return max((tiles + splits - 1) / splits, 4);
+    QuantSeq q = {0, 0, 1, 0};
+    if (b < a.g.B) {
+        q.len = q_clamp(a.len[b], a.g.cap);
+        q.cnt = a.count ? q_clamp(a.count[b], a.n) : a.n;
+        q.tiles = max(1, (q.len + QT - 1) / QT);
+        q.nrb = (q.cnt * a.G + a.RB - 1) / a.RB;
+    }
+    return q;
 }
+
+__device__ inline unsigned wave_scan(unsigned v, int lane)   // sum over the lanes up to this one
+{
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const unsigned u = (unsigned)__shfl_up((int)v, o);
+        if (lane >= o) v += u;
+    }
+    return v;
+}
+__device__ inline unsigned uniform(unsigned v)
+{
+    return (unsigned)__builtin_amdgcn_readfirstlane((int)v);
+}
+__device__ inline float lane_f(float v, int lane)
+{
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+}
+__device__ inline unsigned lane_of(unsigned v, int lane)
+{
+    return (unsigned)__builtin_amdgcn_readlane((int)v, lane);
+}
+
+// How a batch is shared; every wavefront finds out by itself (lane i has the sequences i, i + 64, ...).
+struct QuantShare {
+    int heads, lane;
+    int pp;              // tiles of a piece, or 0: the line
+    unsigned per;        // items per work-group (tiles of the line, or 1 piece)
+    unsigned total;      // items
+    QuantSeq mine;       // sequence `lane`
+
+    __device__ QuantSeq seq(const QuantAttend &a, int b0) const { return b0 == 0 ? mine : quant_seq(a, b0 + lane); }
+    // items of a block of rows
+    __device__ unsigned span(const QuantSeq &q) const { return pp ? (unsigned)((q.tiles + pp - 1) / pp) : (unsigned)q.tiles; }
+    __device__ unsigned work(const QuantSeq &q) const { return span(q) * (unsigned)(q.nrb * heads); }
+
+    __device__ QuantShare(const QuantAttend &a, int lane_) : heads(a.g.nl * a.g.H), lane(lane_), pp(0)
+    {
+        mine = quant_seq(a, lane);
+        unsigned t = 0, units = 0, most = 0;
+        for (int b0 = 0; b0 < a.g.B; b0 += 64) {
+            const QuantSeq q = seq(a, b0);
+            t += work(q);
+            units += (unsigned)(q.nrb * heads);
+            most = max(most, q.nrb ? (unsigned)q.tiles : 0u);
+        }
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            t += (unsigned)__shfl_xor((int)t, o);
+            units += (unsigned)__shfl_xor((int)units, o);
+            most = max(most, (unsigned)__shfl_xor((int)most, o));
+        }
+        t = uniform(t), units = uniform(units), most = uniform(most);
+        total = t;
+        per = max((t + a.W - 1) / a.W, (unsigned)MIN_PIECE);
+        if (units < (unsigned)a.W) {
+            // pieces of at most p tiles are at most t / p + units
+            const unsigned p = min(max((t + a.W - units - 1) / (a.W - units), (unsigned)MIN_PIECE), most);
+            if (p && (most + (most + p - 1) / p - 1) / ((most + p - 1) / p) <= per + PIECE_COST) {
+                pp = (int)p;
+                per = 1;
+                t = 0;
+                for (int b0 = 0; b0 < a.g.B; b0 += 64) t += work(seq(a, b0));
+#pragma unroll
+                for (int o = 1; o < 64; o <<= 1) t += (unsigned)__shfl_xor((int)t, o);
+                total = uniform(t);
+            }
+        }
+    }
+    // The sequence that item f (< total) belongs to, and the first of its items.
+    __device__ int find(const QuantAttend &a, unsigned f, unsigned &start, QuantSeq &sq) const
+    {
+        unsigned base = 0;
+        for (int b0 = 0;; b0 += 64) {
+            const QuantSeq q = seq(a, b0);
+            const unsigned v = work(q), inc = wave_scan(v, lane);
+            const unsigned long long hit = __ballot(base + inc > f);
+            if (hit) {
+                const int at = __builtin_ctzll(hit);
+                start = base + lane_of(inc - v, at);
+                sq = {(int)lane_of(q.len, at), (int)lane_of(q.cnt, at), (int)lane_of(q.tiles, at), (int)lane_of(q.nrb, at)};
+                return b0 + at;
+            }
+            base += lane_of(inc, 63);
+        }
+    }
+    // Items of the sequences 0 .. end - 1.
+    __device__ unsigned before(const QuantAttend &a, int end) const
+    {
+        unsigned t = 0;
+        for (int b0 = 0; b0 < end; b0 += 64) t += b0 + lane < end ? work(seq(a, b0)) : 0u;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) t += (unsigned)__shfl_xor((int)t, o);
+        return uniform(t);
+    }
+    // Tiles of a block's item i: [first, first + count).
+    __device__ void piece(const QuantSeq &q, unsigned i, int &first, int &end) const
+    {
+        const int n = (q.tiles + pp - 1) / pp, len = (q.tiles + n - 1) / n;
+        first = (int)i * len;
+        end = min(q.tiles, first + len);
+    }
+};
 
 struct QuantRow {
     int row_of;      // index into [B][nl][H_q][n] of row r
@@ -378,203 +501,240 @@ __device__ inline float pow2i(int e)   // 2^e, e in -126 .. 127 (clamped from be
     return __uint_as_float((unsigned)(max(e, -126) + 127) << 23);
 }
 
-// Merge of the lane's running maximum m with a tile's
+// 2^x by the hardware instruction alone: results below 2^-126 flush to zero, which no sum here shows (every row's
+// holds a term of 2^0).
+__device__ inline float exp2_hw(float x)
+{
+    return __builtin_amdgcn_exp2f(x);
+}
+
+// What a logit is taken relative to when its maximum is m: a row that has seen nothing keeps -inf out of differences.
 __device__ inline float finite_or_zero(float m)
 {
     return m == -INFINITY ? 0.f : m;
 }
 
-// Few query rows.  Grid: parts, then blocks of 16 rows, then heads.  Each wavefront takes tiles of 64 cache rows of
-// the part in turn:
+// Few query rows.  A work-group has its part of the batch's tiles; within a block of RB = 16 MT rows each wavefront takes
+// tiles of 64 cache rows in turn, and MT times
 //   S^T (16 keys x 16 rows) = K Q^T, K bytes straight from registers: lane (key l % 16, quarter l / 16) has 16 bytes of a
 //   row per load, two matrix products of 32 dimensions; which dimensions is the same for Q;
 //   O^T (16 dimensions x 16 rows) += V^T P^T: result element i of S^T is key 4 (l / 16) + i, so that two blocks'
 //   results are P^T's operand as they stand, and the tile's layout gives V^T's: 16 bytes of one dimension.
 // The wavefronts' results meet in shared memory at the end.
-template <int DH, int FMT, bool F32>
-__global__ __launch_bounds__(Q_THREADS, 2) void quant_token_kernel(QuantAttend a)
+template <int DH, int MT>
+struct QuantTokenSmem {
+    float m[4][16 * MT], l[4][16 * MT];
+    alignas(16) float o[4][16 * MT][DH + 4];
+};
+
+template <bool NTL>
+__device__ inline qu4_t load16(const uint8_t *p)
 {
-    constexpr int NJ = DH / 64, ND = DH / 16;
+    if constexpr (NTL) return __builtin_nontemporal_load((const qu4_t *)p);
+    return *(const qu4_t *)p;
+}
+
+// Q^T of a block of rows as fp16: column (row) lane % 16, quarter q has dimensions 64 j + 16 q + 8 e .. + 8 in f[2 j + e].
+// Returns what turns products with bytes into base-2 logits, before K's scale.
+template <int NJ>
+__device__ inline float load_queries(const uint16_t *row, bool live, int quarter, float scale, h8_t (&f)[2 * NJ])
+{
+    qu4_t u[2 * NJ];
+    unsigned amax = 0;
+#pragma unroll
+    for (int j = 0; j < 2 * NJ; ++j) {
+        u[j] = live ? *(const qu4_t *)(row + (j >> 1) * 64 + quarter * 16 + (j & 1) * 8) : qu4_t{0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) amax = max(amax, max(u[j][e] & 0x7fffu, (u[j][e] >> 16) & 0x7fffu));
+    }
+    amax = max(amax, (unsigned)__shfl_xor((int)amax, 16));
+    amax = max(amax, (unsigned)__shfl_xor((int)amax, 32));
+    const int sh = min(141 - (int)(amax >> 7), 126);       // the largest magnitude goes to 2^14 .. 2^15
+    const float up = pow2i(sh);
+#pragma unroll
+    for (int j = 0; j < 2 * NJ; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            f[j][2 * e] = (_Float16)(__uint_as_float(u[j][e] << 16) * up);
+            f[j][2 * e + 1] = (_Float16)(__uint_as_float(u[j][e] & 0xffff0000u) * up);
+        }
+    return amax >= 0x7f80u ? __uint_as_float(0x7fc00000u) : scale * pow2i(-sh);
+}
+
+// Tiles ta .. tb - 1 of block rb of head (b, hd)'s rows; slot: where a piece's result goes (-1: the block is whole).
+template <int DH, int FMT, bool F32, int MT, bool NTL>
+__device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH, MT> &sm, const QuantSeq &sq, int b, int hd,
+                                         int rb, int ta, int tb, int slot)
+{
+    constexpr int NJ = DH / 64, ND = DH / 16, RB = 16 * MT;
     const QuantGeo &g = a.g;
-    const int nrb = (a.R + 15) / 16;
-    const int part = blockIdx.x % a.splits, rest = blockIdx.x / a.splits, rb = rest % nrb, hd = rest / nrb;
-    const int h = hd % g.H, bl = hd / g.H, l = bl % g.nl, b = bl / g.nl;
-    const int len = q_clamp(a.len[b], g.cap), cnt = a.count ? q_clamp(a.count[b], a.n) : a.n;
-    const int per = part_tiles(len, a.splits), tiles = (len + QT - 1) / QT, nparts = (tiles + per - 1) / per;
-    if (rb * 16 / a.G >= cnt || (a.splits > 1 && part >= nparts)) return;
+    const int len = sq.len, cnt = sq.cnt, h = hd % g.H, l = hd / g.H % g.nl;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quarter = lane >> 4;
     const size_t head = g.head(b, l, h);
     const uint8_t *kh = g.k + head * g.cap * DH, *vh = g.v + head * g.cap * DH;
     const float *ks = g.ks + ((head * g.cap) >> g.bsh), *vs = g.vs + ((head * g.cap) >> g.bsh);
 
-    const QuantRow qr = quant_row(a, hd, rb * 16 + col, len, cnt);
-    const int seen = min(len, max(0, len - cnt + min(cnt - 1, (min(rb * 16 + 15, a.R - 1)) / a.G) + 1));   // by the last row
-    const int full = len - cnt + rb * 16 / a.G + 1;                                                        // by the first row
-    const int t_end = min(min(tiles, (part + 1) * per), (seen + QT - 1) / QT);
-    int t = part * per + wave;
+    // cache rows that the block's last and first row see
+    const int seen = min(len, max(0, len - cnt + min(cnt - 1, min(rb * RB + RB - 1, a.R - 1) / a.G) + 1));
+    const int full = len - cnt + rb * RB / a.G + 1;
+    const int t_end = min(tb, (seen + QT - 1) / QT);
+    int t = ta + wave;
 
-    // Q^T: column col; quarter q has dimensions 64 j + 16 q .. + 16
-    h8_t qf[2 * NJ];
-    float crow;
-    {
-        qu4_t u[2 * NJ];
-        unsigned amax = 0;
-#pragma unroll
-        for (int j = 0; j < 2 * NJ; ++j) {
-            u[j] = qr.vis >= 0 ? *(const qu4_t *)(a.q + (size_t)qr.row_of * DH + (j >> 1) * 64 + quarter * 16 + (j & 1) * 8)
-                               : qu4_t{0, 0, 0, 0};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) amax = max(amax, max(u[j][e] & 0x7fffu, (u[j][e] >> 16) & 0x7fffu));
-        }
-        amax = max(amax, (unsigned)__shfl_xor((int)amax, 16));
-        amax = max(amax, (unsigned)__shfl_xor((int)amax, 32));
-        const int sh = min(141 - (int)(amax >> 7), 126);       // the largest magnitude goes to 2^14 .. 2^15
-        const float up = pow2i(sh);
-        crow = amax >= 0x7f80u ? __uint_as_float(0x7fc00000u) : a.scale * pow2i(-sh);
-#pragma unroll
-        for (int j = 0; j < 2 * NJ; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                qf[j][2 * e] = (_Float16)(__uint_as_float(u[j][e] << 16) * up);
-                qf[j][2 * e + 1] = (_Float16)(__uint_as_float(u[j][e] & 0xffff0000u) * up);
-            }
-    }
-
+    // a tile; the scales of its four 16-row blocks are in the lanes' registers, block lane % 4
     qu4_t kr[4][NJ], vr[ND];
-    float ksr[4], vsr[4];
+    float ksr = 0.f, vsr = 0.f;
     auto load_k = [&](int t) {
-        const uint8_t *p = kh + (size_t)t * QT * DH + col * DH + quarter * 16;
+        const uint8_t *p = kh + (size_t)t * QT * DH;
+        const unsigned off = col * DH + quarter * 16;
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb) {
+        for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) kr[kb][j] = *(const qu4_t *)(p + kb * 16 * DH + j * 64);
-            ksr[kb] = ks[(t * QT + kb * 16) >> g.bsh];
-        }
+            for (int j = 0; j < NJ; ++j) kr[kb][j] = load16<NTL>(p + (off + kb * 16 * DH + j * 64));
+        ksr = ks[(t * QT + (lane & 3) * 16) >> g.bsh];
     };
     auto load_v = [&](int t) {
-        const uint8_t *p = vh + (size_t)t * QT * DH + col * QT + quarter * 16;
+        const uint8_t *p = vh + (size_t)t * QT * DH;
+        const unsigned off = col * QT + quarter * 16;
 #pragma unroll
-        for (int dt = 0; dt < ND; ++dt) vr[dt] = *(const qu4_t *)(p + dt * 16 * QT);
-#pragma unroll
-        for (int kb = 0; kb < 4; ++kb) vsr[kb] = vs[(t * QT + kb * 16) >> g.bsh];
+        for (int dt = 0; dt < ND; ++dt) vr[dt] = load16<NTL>(p + (off + dt * 16 * QT));
+        vsr = vs[(t * QT + (lane & 3) * 16) >> g.bsh];
     };
-
-    qf4_t o[ND];
-#pragma unroll
-    for (int dt = 0; dt < ND; ++dt) o[dt] = qf4_t{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, sum = 0.f;
-    int vexp = -100;           // o is in units of 2^(vexp - 15); V scales seen so far are below 2^vexp
     if (t < t_end) {
         load_k(t);
         load_v(t);
     }
+    __builtin_amdgcn_sched_barrier(0);
+
+    QuantRow qr[MT];
+    h8_t qf[MT][2 * NJ];
+    float crow[MT], m[MT], sum[MT];
+    qf4_t o[MT][ND];
+#pragma unroll
+    for (int r = 0; r < MT; ++r) {
+        qr[r] = quant_row(a, hd, rb * RB + r * 16 + col, len, cnt);
+        crow[r] = load_queries<NJ>(a.q + (size_t)qr[r].row_of * DH, qr[r].vis >= 0, quarter, a.scale, qf[r]);
+        m[r] = -INFINITY;
+        sum[r] = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt) o[r][dt] = qf4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    int vexp = -100;           // o is in units of 2^(vexp - 15); V scales seen so far are below 2^vexp
     for (; t < t_end; t += 4) {
         const int key0 = t * QT + quarter * 4;
-        float s[4][4];
+        const bool masked = t * QT + QT > full;   // some row does not see all of the tile
+        float s[MT][4][4];
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb) {
-            qf4_t c = {0.f, 0.f, 0.f, 0.f};
+            qf4_t c[MT] = {};
 #pragma unroll
             for (int j = 0; j < NJ; ++j) {
-                c = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_to_h8<FMT>(kr[kb][j].x, kr[kb][j].y), qf[2 * j], c, 0, 0, 0);
-                c = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_to_h8<FMT>(kr[kb][j].z, kr[kb][j].w), qf[2 * j + 1], c, 0, 0, 0);
+                const h8_t k0 = bytes_to_h8<FMT>(kr[kb][j].x, kr[kb][j].y), k1 = bytes_to_h8<FMT>(kr[kb][j].z, kr[kb][j].w);
+#pragma unroll
+                for (int r = 0; r < MT; ++r) {
+                    c[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, qf[r][2 * j], c[r], 0, 0, 0);
+                    c[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, qf[r][2 * j + 1], c[r], 0, 0, 0);
+                }
             }
-            const float f = crow * ksr[kb];
+            const float kscale = lane_f(ksr, kb);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[kb][i] = c[i] * f;
+            for (int r = 0; r < MT; ++r) {
+                const float f = crow[r] * kscale;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[r][kb][i] = c[r][i] * f;
+            }
         }
+        // loads are issued here and not where they are used: about a round under way
+        __builtin_amdgcn_sched_barrier(0);
         if (t + 4 < t_end) load_k(t + 4);
-        const bool masked = t * QT + QT > full;   // some row does not see all of the tile
-        if (masked) {
-#pragma unroll
-            for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s[kb][i] = key0 + kb * 16 + i < qr.vis ? s[kb][i] : -INFINITY;
-        }
-        float mt = m;
-#pragma unroll
-        for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) mt = fmaxf(mt, s[kb][i]);
-        mt = fmaxf(mt, __shfl_xor(mt, 16));
-        mt = fmaxf(mt, __shfl_xor(mt, 32));
+        __builtin_amdgcn_sched_barrier(0);
 
         // the largest V scale of the tile's blocks of live rows
-        float vmax = 0.f;
+        float vmax = 0.f, vsc[4];
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb) {
-            if (t * QT + kb * 16 >= len) vsr[kb] = 0.f;
-            vmax = fmaxf(vmax, vsr[kb]);
+            vsc[kb] = t * QT + kb * 16 < len ? lane_f(vsr, kb) : 0.f;
+            vmax = fmaxf(vmax, vsc[kb]);
         }
-        const int ve = __builtin_amdgcn_readfirstlane((int)(__float_as_uint(vmax) >> 23) - 126);
-        float alpha = exp2f(m - finite_or_zero(mt));
-        if (ve > vexp || __any(mt > m)) {
-            const float f = alpha * (ve > vexp ? pow2i(vexp - ve) : 1.f);
-            vexp = max(vexp, ve);
+        const int ve = max(vexp, (int)(uniform(__float_as_uint(vmax)) >> 23) - 126);
+        h8_t ph[MT][2], pl[MT][2];
 #pragma unroll
-            for (int dt = 0; dt < ND; ++dt) o[dt] *= f;
-            sum *= alpha;
-            m = mt;
-        }
-        const float mz = finite_or_zero(m), vf = pow2i(15 - vexp);
-        float bs[4];
+        for (int r = 0; r < MT; ++r) {
+            float (&x)[4][4] = s[r];
+            if (masked) {
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb) {
-            bs[kb] = 0.f;
+                for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                s[kb][i] = exp2f(s[kb][i] - mz);
-                bs[kb] += s[kb][i];
+                    for (int i = 0; i < 4; ++i) x[kb][i] = key0 + kb * 16 + i < qr[r].vis ? x[kb][i] : -INFINITY;
             }
-            sum += bs[kb];
-        }
-        if (a.mass) {
-            // block sums relative to m; the merge makes them shares
-            const int nb = QT >> g.bsh;
-#pragma unroll
-            for (int kb = 0; kb < 4; ++kb) {
-                bs[kb] += __shfl_xor(bs[kb], 16);
-                bs[kb] += __shfl_xor(bs[kb], 32);
-            }
-            if (quarter == 0 && qr.vis >= 0) {
-                float *to = a.mass + (size_t)qr.row_of * (g.cap >> g.bsh) + (size_t)t * nb;
-                if (nb == 1)
-                    to[0] = (bs[0] + bs[1]) + (bs[2] + bs[3]);
-                else if (nb == 2) {
-                    to[0] = bs[0] + bs[1];
-                    to[1] = bs[2] + bs[3];
-                } else {
-#pragma unroll
-                    for (int kb = 0; kb < 4; ++kb) to[kb] = bs[kb];
-                }
-                a.ws_m[(size_t)qr.row_of * (g.cap / QT) + t] = m;
-            }
-        }
-        // P^T, times the V scales; a masked weight is 0 whatever the scale is
-        h8_t ph[2], pl[2];
-#pragma unroll
-        for (int kb = 0; kb < 4; ++kb) {
-            const float f = vsr[kb] * vf;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[kb][i] *= f;
-        }
-        if (masked) {
+            float mt = m[r];
 #pragma unroll
             for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[kb][i] = key0 + kb * 16 + i < qr.vis ? s[kb][i] : 0.f;
-        }
+                for (int i = 0; i < 4; ++i) mt = fmaxf(mt, x[kb][i]);
+            mt = fmaxf(mt, __shfl_xor(mt, 16));
+            mt = fmaxf(mt, __shfl_xor(mt, 32));
+            if (ve > vexp || __any(mt > m[r])) {
+                const float alpha = exp2_hw(m[r] - finite_or_zero(mt)), f = alpha * pow2i(vexp - ve);
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float p = s[kb][i];
-                const _Float16 hi = (_Float16)p;
-                ph[kb >> 1][(kb & 1) * 4 + i] = hi;
-                if constexpr (F32) pl[kb >> 1][(kb & 1) * 4 + i] = (_Float16)(p - (float)hi);
+                for (int dt = 0; dt < ND; ++dt) o[r][dt] *= f;
+                sum[r] *= alpha;
+                m[r] = mt;
             }
+            const float mz = finite_or_zero(m[r]), vf = pow2i(15 - ve);
+            float bs[4];
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[kb][i] = exp2_hw(x[kb][i] - mz);
+                bs[kb] = (x[kb][0] + x[kb][1]) + (x[kb][2] + x[kb][3]);
+            }
+            sum[r] += (bs[0] + bs[1]) + (bs[2] + bs[3]);
+            if (a.mass) {
+                // block sums relative to m; the merge makes them shares
+                const int nb = QT >> g.bsh;
+#pragma unroll
+                for (int kb = 0; kb < 4; ++kb) {
+                    bs[kb] += __shfl_xor(bs[kb], 16);
+                    bs[kb] += __shfl_xor(bs[kb], 32);
+                }
+                if (quarter == 0 && qr[r].vis >= 0) {
+                    float *to = a.mass + (size_t)qr[r].row_of * (g.cap >> g.bsh) + (size_t)t * nb;
+                    if (nb == 1)
+                        to[0] = (bs[0] + bs[1]) + (bs[2] + bs[3]);
+                    else if (nb == 2) {
+                        to[0] = bs[0] + bs[1];
+                        to[1] = bs[2] + bs[3];
+                    } else {
+#pragma unroll
+                        for (int kb = 0; kb < 4; ++kb) to[kb] = bs[kb];
+                    }
+                    a.ws_m[(size_t)qr[r].row_of * (g.cap / QT) + t] = m[r];
+                }
+            }
+            // P^T, times the V scales; a masked weight is 0 whatever the scale is
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb) {
+                const float f = vsc[kb] * vf;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[kb][i] *= f;
+            }
+            if (masked) {
+#pragma unroll
+                for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[kb][i] = key0 + kb * 16 + i < qr[r].vis ? x[kb][i] : 0.f;
+            }
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const _Float16 hi = (_Float16)x[kb][i];
+                    ph[r][kb >> 1][(kb & 1) * 4 + i] = hi;
+                    if constexpr (F32) pl[r][kb >> 1][(kb & 1) * 4 + i] = (_Float16)(x[kb][i] - (float)hi);
+                }
         }
+        vexp = ve;
         if (FMT == WNW_QUANT_E4M3 && t * QT + QT > len) {
             // bytes of dead rows may be e4m3's NaN
 #pragma unroll
@@ -590,109 +750,154 @@ __global__ __launch_bounds__(Q_THREADS, 2) void quant_token_kernel(QuantAttend a
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 const h8_t v = bytes_to_h8<FMT>(vr[dt][2 * c], vr[dt][2 * c + 1]);
-                o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph[c], o[dt], 0, 0, 0);
-                if constexpr (F32) o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl[c], o[dt], 0, 0, 0);
+#pragma unroll
+                for (int r = 0; r < MT; ++r) {
+                    o[r][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph[r][c], o[r][dt], 0, 0, 0);
+                    if constexpr (F32) o[r][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl[r][c], o[r][dt], 0, 0, 0);
+                }
             }
+        __builtin_amdgcn_sched_barrier(0);
         if (t + 4 < t_end) load_v(t + 4);
+        __builtin_amdgcn_sched_barrier(0);
     }
-    sum += __shfl_xor(sum, 16);
-    sum += __shfl_xor(sum, 32);
 
-    __shared__ float sm_m[4][16], sm_l[4][16];
-    __shared__ alignas(16) float sm_o[4][16][DH + 4];
-    {
-        const float unit = pow2i(vexp - 15);
+    const float unit = pow2i(vexp - 15);
+#pragma unroll
+    for (int r = 0; r < MT; ++r) {
+        sum[r] += __shfl_xor(sum[r], 16);
+        sum[r] += __shfl_xor(sum[r], 32);
         if (quarter == 0) {
-            sm_m[wave][col] = m;
-            sm_l[wave][col] = sum;
+            sm.m[wave][r * 16 + col] = m[r];
+            sm.l[wave][r * 16 + col] = sum[r];
         }
 #pragma unroll
-        for (int dt = 0; dt < ND; ++dt) *(qf4_t *)&sm_o[wave][col][dt * 16 + quarter * 4] = o[dt] * unit;
+        for (int dt = 0; dt < ND; ++dt) *(qf4_t *)&sm.o[wave][r * 16 + col][dt * 16 + quarter * 4] = o[r][dt] * unit;
     }
     __syncthreads();
-    const bool whole = a.splits == 1;
-    const int row = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * (DH / 16);
-    const QuantRow rr = quant_row(a, hd, rb * 16 + row, len, cnt);
-    if (rr.vis < 0) return;
-    float mm = -INFINITY, ll = 0.f, x[DH / 16];
+    for (int row = threadIdx.x >> 4; row < RB; row += Q_THREADS / 16) {
+        const int d0 = (threadIdx.x & 15) * (DH / 16);
+        const QuantRow rr = quant_row(a, hd, rb * RB + row, len, cnt);
+        if (rr.vis < 0) continue;
+        float mm = -INFINITY, ll = 0.f, x[DH / 16];
 #pragma unroll
-    for (int w = 0; w < 4; ++w) mm = fmaxf(mm, sm_m[w][row]);
+        for (int w = 0; w < 4; ++w) mm = fmaxf(mm, sm.m[w][row]);
 #pragma unroll
-    for (int e = 0; e < DH / 16; ++e) x[e] = 0.f;
+        for (int e = 0; e < DH / 16; ++e) x[e] = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        const float lw = sm_l[w][row];
-        if (lw == 0.f) continue;
-        const float f = exp2f(sm_m[w][row] - finite_or_zero(mm));
-        ll += f * lw;
+        for (int w = 0; w < 4; ++w) {
+            const float lw = sm.l[w][row], f = lw == 0.f ? 0.f : exp2f(sm.m[w][row] - finite_or_zero(mm));   // 0: saw nothing
+            ll += f * lw;
 #pragma unroll
-        for (int e = 0; e < DH / 16; ++e) x[e] += f * sm_o[w][row][d0 + e];
-    }
-    const size_t NR = (size_t)g.B * g.nl * g.H * a.R, flat = (size_t)part * NR + rr.row_of;
-    if (!whole) {
-        __builtin_memcpy(a.ws_o + flat * DH + d0, x, sizeof(x));
-        if (d0 == 0) a.ws_ml[flat] = make_float2(mm, ll);
-        return;
-    }
-    const float inv = ll == 0.f ? 0.f : 1.f / ll;
+            for (int e = 0; e < DH / 16; ++e) x[e] += f * sm.o[w][row][d0 + e];
+        }
+        if (slot >= 0) {
+            const size_t at = (size_t)(blockIdx.x * 2 + slot) * RB + row;
+            __builtin_memcpy(__builtin_assume_aligned(a.ws_o + at * DH + d0, 16), x, sizeof(x));
+            if (d0 == 0) a.ws_ml[at] = make_float2(mm, ll);
+        } else {
+            const float inv = ll == 0.f ? 0.f : 1.f / ll;
 #pragma unroll
-    for (int e = 0; e < DH / 16; ++e) x[e] *= inv;
-    store_row<DH / 16, !F32>(a.out, (size_t)rr.row_of * DH + d0, x);
-    if (d0 == 0) {
-        if (a.lse) a.lse[rr.row_of] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * Q_LN2;
-        if (a.mass) a.ws_ml[rr.row_of] = make_float2(mm, ll);
+            for (int e = 0; e < DH / 16; ++e) x[e] *= inv;
+            store_row<DH / 16, !F32>(a.out, (size_t)rr.row_of * DH + d0, x);
+            if (d0 == 0) {
+                if (a.lse) a.lse[rr.row_of] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * Q_LN2;
+                if (a.mass) a.ws_row[rr.row_of] = make_float2(mm, ll);
+            }
+        }
     }
 }
 
-// Joins the parts of every output row (one wavefront each) and makes the tiles' block sums shares of the whole.
+template <int DH, int FMT, bool F32, int MT, bool NTL>
+__global__ __launch_bounds__(Q_THREADS, MT == 2 ? 1 : DH == 64 ? 3 : 2) void quant_token_kernel(QuantAttend a)
+{
+    __shared__ QuantTokenSmem<DH, MT> sm;
+    const QuantShare sh(a, threadIdx.x & 63);
+    unsigned f = blockIdx.x * sh.per, start;
+    if (f >= sh.total) return;
+    const unsigned f1 = min(f + sh.per, sh.total);
+    QuantSeq sq;
+    int b = sh.find(a, f, start, sq);
+    for (;;) {
+        const unsigned off = f - start, span = sh.span(sq), unit = off / span, at = off - unit * span;
+        int ta = (int)at, tb = (int)min(span, at + (f1 - f));
+        f += tb - ta;
+        if (sh.pp) sh.piece(sq, at, ta, tb);
+        quant_token_block<DH, FMT, F32, MT, NTL>(a, sm, sq, b, b * sh.heads + (int)(unit / sq.nrb), (int)(unit % sq.nrb), ta, tb,
+                                                 ta > 0 ? 0 : tb < sq.tiles ? 1 : -1);
+        if (f >= f1) return;
+        if (f - start >= sh.work(sq)) b = sh.find(a, f, start, sq);
+        __syncthreads();
+    }
+}
+
+// One work-group per output row: joins the pieces of its cache, and makes the tiles' block sums shares of the whole.
 template <int DH, bool BF16>
 __global__ __launch_bounds__(Q_THREADS) void quant_merge_kernel(QuantAttend a)
 {
+    constexpr int E = DH / 64;
+    __shared__ float sm_m[4], sm_l[4], sm_o[4][DH];
     const QuantGeo &g = a.g;
-    const int64_t NR = (int64_t)g.B * g.nl * g.H * a.R, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= NR) return;
-    const int lane = threadIdx.x & 63, i = (int)(row % a.n), b = (int)(row / ((int64_t)g.nl * g.H * a.R));
-    const int len = q_clamp(a.len[b], g.cap), cnt = a.count ? q_clamp(a.count[b], a.n) : a.n;
-    if (i >= cnt) return;
-    const int tiles = (len + QT - 1) / QT, per = part_tiles(len, a.splits);
-    const int parts = a.splits == 1 ? 1 : (tiles + per - 1) / per;
+    const int heads = g.nl * g.H;
+    const unsigned row = blockIdx.x, hq = row / a.n, i = row % a.n, hd = hq / a.G, b = hd / heads;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const QuantSeq sq = quant_seq(a, b);
+    if ((int)i >= sq.cnt) return;
+    const unsigned r = i * a.G + hq % a.G;
+    const QuantShare sh(a, lane);
+    const unsigned span = sh.span(sq), s0 = sh.before(a, b) + ((hd - b * heads) * sq.nrb + r / a.RB) * span;
+    const unsigned w0 = s0 / sh.per, pieces = (s0 + span - 1) / sh.per - w0 + 1;
     float m = -INFINITY, sum = 0.f;
-    for (int p = 0; p < parts; ++p) m = fmaxf(m, a.ws_ml[p * NR + row].x);
-    const float mz = finite_or_zero(m);
-    float x[DH / 64] = {};
-    for (int p = 0; p < parts; ++p) {
-        const float2 ml = a.ws_ml[p * NR + row];
-        if (ml.y == 0.f) continue;          // saw nothing
-        const float f = exp2f(ml.x - mz);
-        sum += f * ml.y;
-        if (a.splits > 1) {
+    if (pieces == 1) {
+        if (!a.mass) return;
+        const float2 ml = a.ws_row[row];
+        m = ml.x;
+        sum = ml.y;
+    } else {
+        // piece p: the work-group w0 + p's slot 1 for the first, 0 for the others
+        auto at = [&](unsigned p) { return (size_t)((w0 + p) * 2 + (p == 0)) * a.RB + r % a.RB; };
+        for (unsigned p = wave; p < pieces; p += 4) m = fmaxf(m, a.ws_ml[at(p)].x);
+        const float mz = finite_or_zero(m);
+        float x[E] = {};
+#pragma unroll 4
+        for (unsigned p = wave; p < pieces; p += 4) {
+            const float2 ml = a.ws_ml[at(p)];
+            const float f = ml.y == 0.f ? 0.f : exp2f(ml.x - mz);    // 0: saw nothing
+            sum += f * ml.y;
 #pragma unroll
-            for (int e = 0; e < DH / 64; ++e) x[e] += f * a.ws_o[(p * NR + row) * DH + lane * (DH / 64) + e];
+            for (int e = 0; e < E; ++e) x[e] += f * a.ws_o[at(p) * DH + lane * E + e];
         }
-    }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    if (a.splits > 1) {
 #pragma unroll
-        for (int e = 0; e < DH / 64; ++e) {
-            const size_t at = row * DH + lane * (DH / 64) + e;
+        for (int e = 0; e < E; ++e) sm_o[wave][lane * E + e] = x[e];
+        if (lane == 0) {
+            sm_m[wave] = m;
+            sm_l[wave] = sum;
+        }
+        __syncthreads();
+        float mm = -INFINITY, y = 0.f;
+        for (int w = 0; w < 4; ++w) mm = fmaxf(mm, sm_m[w]);
+        sum = 0.f;
+        for (int w = 0; w < 4; ++w) {
+            if (sm_l[w] == 0.f) continue;
+            const float f = exp2f(sm_m[w] - finite_or_zero(mm));
+            sum += f * sm_l[w];
+            if (tid < DH) y += f * sm_o[w][tid];
+        }
+        m = mm;
+        if (tid < DH) {
+            y *= sum == 0.f ? 0.f : 1.f / sum;
             if constexpr (BF16)
-                ((uint16_t *)a.out)[at] = to_bf16(x[e] * inv);
+                ((uint16_t *)a.out)[(size_t)row * DH + tid] = to_bf16(y);
             else
-                ((float *)a.out)[at] = x[e] * inv;
+                ((float *)a.out)[(size_t)row * DH + tid] = y;
         }
-        if (a.lse && lane == 0) a.lse[row] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * Q_LN2;
+        if (a.lse && tid == 0) a.lse[row] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * Q_LN2;
     }
     if (a.mass) {
-        const int blocks = g.cap >> g.bsh, live = (len + (1 << g.bsh) - 1) >> g.bsh, per_tile = QT >> g.bsh;
-        float *to = a.mass + row * blocks;
-        for (int j = lane; j < blocks; j += 64) {
-            float w = 0.f;
-            if (j < live) {
-                const float mt = a.ws_m[row * (g.cap / QT) + j / per_tile];
-                w = to[j] * (exp2f(mt - mz) * inv);
-            }
-            to[j] = w;
-        }
+        const float inv = sum == 0.f ? 0.f : 1.f / sum, mz = finite_or_zero(m);
+        const int blocks = g.cap >> g.bsh, live = (sq.len + (1 << g.bsh) - 1) >> g.bsh, tsh = 6 - g.bsh;
+        float *to = a.mass + (size_t)row * blocks;
+        const float *mt = a.ws_m + (size_t)row * (g.cap / QT);
+        for (int j = tid; j < blocks; j += Q_THREADS) to[j] = j < live ? to[j] * (exp2f(mt[j >> tsh] - mz) * inv) : 0.f;
     }
 }
 
@@ -767,11 +972,12 @@ void quant_dispatch(const wnw_quant_config &c, F f)
         c.format == WNW_QUANT_INT8 ? f(D1{}, I0{}) : f(D1{}, I1{});
 }
 
-// Sizes of an attention call: parts of a cache, output rows, and the workspace's three arrays.
+// How an attention call runs: rows of a block, work-groups, loads past the caches; output rows; the workspace's arrays.
 struct QuantPlan {
-    int splits;
-    int64_t rows, o_bytes, ml_bytes, m_bytes;
-    int64_t total() const { return o_bytes + ml_bytes + m_bytes; }
+    int RB, W;
+    bool stream;
+    int64_t rows, o_bytes, ml_bytes, row_bytes, m_bytes;
+    int64_t total() const { return o_bytes + ml_bytes + row_bytes + m_bytes; }
 };
 int64_t round16(int64_t x)
 {
@@ -780,23 +986,40 @@ int64_t round16(int64_t x)
 QuantPlan quant_plan(const wnw_quant_config &c, int32_t n_layers, int32_t q_heads, int32_t n, int32_t max_len)
 {
     const int64_t heads = (int64_t)c.batch * n_layers * c.kv_heads, R = (int64_t)q_heads / c.kv_heads * n;
-    const int64_t groups = heads * ((R + 15) / 16);
-    const int64_t tiles = ((max_len ? std::min(max_len, c.capacity) : c.capacity) + QT - 1) / QT;
+    const int64_t len = max_len ? std::min(max_len, c.capacity) : c.capacity;
     QuantPlan p;
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(768 / std::max<int64_t>(groups, 1), (tiles + 3) / 4));
+    p.RB = R > 16 ? 32 : 16;
+    const int64_t blocks = heads * ((R + p.RB - 1) / p.RB), tiles = (len + QT - 1) / QT * blocks;
+    // as many as the chip's 256 compute units hold at once, or as many as pieces of MIN_PIECE tiles need
+    const int held = 256 * (p.RB == 32 ? 1 : c.head_dim == 64 ? 3 : 2);
+    p.W = (int)std::max<int64_t>(1, std::min<int64_t>(held, tiles / MIN_PIECE + blocks));
+    // Bytes that one pass reads once and the 256 MB of the last-level cache cannot keep for the next one
+    p.stream = R <= p.RB && heads * len * c.head_dim * 2 > (256ll << 20);
     p.rows = heads * R;
-    p.o_bytes = p.splits > 1 ? p.splits * p.rows * c.head_dim * 4 : 0;
-    p.ml_bytes = p.splits > 1 || n == 1 ? round16(p.splits * p.rows * 8) : 0;
+    p.o_bytes = (int64_t)p.W * 2 * p.RB * c.head_dim * 4;
+    p.ml_bytes = (int64_t)p.W * 2 * p.RB * 8;
+    p.row_bytes = n == 1 ? round16(p.rows * 8) : 0;
     p.m_bytes = n == 1 ? round16(p.rows * (c.capacity / QT) * 4) : 0;
     return p;
+}
+
+template <int DH, int FMT, bool F32>
+void launch_token(const QuantPlan &p, const QuantAttend &a, hipStream_t st)
+{
+    auto *k = p.RB == 16 ? (p.stream ? quant_token_kernel<DH, FMT, F32, 1, true> : quant_token_kernel<DH, FMT, F32, 1, false>)
+                         : (p.stream ? quant_token_kernel<DH, FMT, F32, 2, true> : quant_token_kernel<DH, FMT, F32, 2, false>);
+    hipLaunchKernelGGL(k, dim3(p.W), dim3(Q_THREADS), 0, st, a);
 }
 
 wnw_status quant_heads(const wnw_quant_config &c, int32_t n_layers, int32_t q_heads, int32_t n, int32_t max_len)
 {
     if (q_heads < c.kv_heads || q_heads % c.kv_heads) return quant_fail(WNW_ERR_INVALID, "q_heads must be a multiple of kv_heads");
     if (max_len < 0) return quant_fail(WNW_ERR_INVALID, "negative max_len");
-    if ((int64_t)c.batch * n_layers * q_heads > 4 * Q_MAX_GROUPS / std::max(n, 1))
+    if ((int64_t)c.batch * n_layers * q_heads > Q_MAX_GROUPS / std::max(n, 1))
         return quant_fail(WNW_ERR_UNSUPPORTED, "too many query rows");
+    // the line of tiles is counted in 32 bits
+    const int64_t blocks = ((int64_t)q_heads / c.kv_heads * n + 15) / 16 * c.batch * n_layers * c.kv_heads;
+    if (blocks > INT32_MAX / (c.capacity / QT)) return quant_fail(WNW_ERR_UNSUPPORTED, "too many tiles for one call");
     return WNW_OK;
 }
 
@@ -883,20 +1106,19 @@ wnw_status wnw_quant_attend(const wnw_quant_config *cfg, const wnw_quant_cache *
     if (p.total() && (!workspace || !aligned16(workspace) || workspace_bytes < (size_t)p.total()))
         return quant_fail(WNW_ERR_INVALID, "workspace missing, too small or not aligned to 16 bytes");
     const int G = q_heads / cfg->kv_heads, R = G * n;
-    const int64_t groups = (int64_t)cfg->batch * n_layers * cfg->kv_heads * ((R + 15) / 16) * p.splits;
-    if (groups > Q_MAX_GROUPS) return quant_fail(WNW_ERR_UNSUPPORTED, "too many query rows");
     char *ws = (char *)workspace;
-    QuantAttend a = {quant_geo(*cfg, *cache, first_layer, n_layers), G, n, R, p.splits, (const uint16_t *)q_dev, len_dev, count_dev,
-                     out_dev, lse_dev, mass_dev, (float *)ws, (float2 *)(ws + p.o_bytes), (float *)(ws + p.o_bytes + p.ml_bytes),
+    QuantAttend a = {quant_geo(*cfg, *cache, first_layer, n_layers), G, n, R, p.W, p.RB, (const uint16_t *)q_dev, len_dev, count_dev,
+                     out_dev, lse_dev, mass_dev, (float *)ws, (float2 *)(ws + p.o_bytes),
+                     (float2 *)(ws + p.o_bytes + p.ml_bytes), (float *)(ws + p.o_bytes + p.ml_bytes + p.row_bytes),
                      Q_LOG2E / sqrtf((float)cfg->head_dim)};
     const bool bf16 = cfg->flags & WNW_F_OUT_BF16;
     quant_dispatch(*cfg, [&](auto d, auto f) {
         constexpr int DH = decltype(d)::value, FMT = decltype(f)::value;
-        hipLaunchKernelGGL((bf16 ? quant_token_kernel<DH, FMT, false> : quant_token_kernel<DH, FMT, true>), dim3((unsigned)groups),
-                           dim3(Q_THREADS), 0, (hipStream_t)hip_stream, a);
-        if (p.splits > 1 || mass_dev)
+        bf16 ? launch_token<DH, FMT, false>(p, a, (hipStream_t)hip_stream) : launch_token<DH, FMT, true>(p, a, (hipStream_t)hip_stream);
+        // one work-group alone leaves no pieces
+        if (p.W > 1 || mass_dev)
             hipLaunchKernelGGL((bf16 ? quant_merge_kernel<DH, true> : quant_merge_kernel<DH, false>),
-                               dim3((unsigned)((p.rows + 3) / 4)), dim3(Q_THREADS), 0, (hipStream_t)hip_stream, a);
+                               dim3((unsigned)p.rows), dim3(Q_THREADS), 0, (hipStream_t)hip_stream, a);
     });
     return quant_hip();
 }
