@@ -14,6 +14,7 @@
 // to the sum of two fp16 (2^-23) where it is fp32.
 #include "wnw.h"
 #include "wnw_internal.h"
+#include "wnw_lds.h"
 
 #include <math.h>
 
@@ -393,10 +394,6 @@ __device__ inline unsigned uniform(unsigned v)
 {
     return (unsigned)__builtin_amdgcn_readfirstlane((int)v);
 }
-__device__ inline float lane_f(float v, int lane)
-{
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
-}
 __device__ inline unsigned lane_of(unsigned v, int lane)
 {
     return (unsigned)__builtin_amdgcn_readlane((int)v, lane);
@@ -520,18 +517,32 @@ __device__ inline float finite_or_zero(float m)
 //   row per load, two matrix products of 32 dimensions; which dimensions is the same for Q;
 //   O^T (16 dimensions x 16 rows) += V^T P^T: result element i of S^T is key 4 (l / 16) + i, so that two blocks'
 //   results are P^T's operand as they stand, and the tile's layout gives V^T's: 16 bytes of one dimension.
-// The wavefronts' results meet in shared memory at the end.
+// A wavefront's tile goes from global to shared memory without registers, each lane's bytes to a place that it alone reads:
+// K's of the next tile are under way from the end of the first products on, V's from the end of the second.  Registers are
+// left for two blocks of 16 rows and two wavefronts on every SIMD.
+// The wavefronts' results meet in shared memory at the end, in the tiles' place.
 template <int DH, int MT>
 struct QuantTokenSmem {
+    union {
+        alignas(16) qu4_t tile[4][2][DH / 16 * 64];    // [wavefront][K, V]
+        alignas(16) float o[4][32][DH];                // in the wavefront's own tile: others may still be reading theirs
+    };
     float m[4][16 * MT], l[4][16 * MT];
-    alignas(16) float o[4][16 * MT][DH + 4];
+    static_assert(sizeof(tile) == sizeof(o) && MT <= 2, "a wavefront's results fit its tile");
+    // 16-byte unit u of a row of o, spread over the banks
+    static __device__ int unit(int row, int u) { return (u ^ (row & (DH / 4 - 1) & 15)) * 4; }
 };
 
-template <bool NTL>
-__device__ inline qu4_t load16(const uint8_t *p)
+// As load_to_lds, past the caches that a stream does not fit.
+__device__ inline void stream_to_lds(const void *base, unsigned off, unsigned lds)
 {
-    if constexpr (NTL) return __builtin_nontemporal_load((const qu4_t *)p);
-    return *(const qu4_t *)p;
+    __asm__ volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(lds), "v"(off), "s"(base) : "m0", "memory");
+}
+
+// A wave-uniform scale by the scalar unit, whose loads do not count among those of the tiles.
+__device__ inline float scalar_load(const float *p, int i)
+{
+    return ((const __attribute__((address_space(4))) float *)p)[i];
 }
 
 // Q^T of a block of rows as fp16: column (row) lane % 16, quarter q has dimensions 64 j + 16 q + 8 e .. + 8 in f[2 j + e].
@@ -581,30 +592,28 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
     const int t_end = min(tb, (seen + QT - 1) / QT);
     int t = ta + wave;
 
-    // a tile; the scales of its four 16-row blocks are in the lanes' registers, block lane % 4
-    qu4_t kr[4][NJ], vr[ND];
-    float ksr = 0.f, vsr = 0.f;
+    const unsigned lds_k = __builtin_amdgcn_readfirstlane(lds_address(sm.tile[wave][0])),
+                   lds_v = __builtin_amdgcn_readfirstlane(lds_address(sm.tile[wave][1]));
+    const unsigned off_k = col * DH + quarter * 16, off_v = col * QT + quarter * 16;
+    auto load = [&](const uint8_t *base, unsigned off, unsigned lds) {
+        NTL ? stream_to_lds(base, off, lds) : load_to_lds(base, off, lds);
+    };
     auto load_k = [&](int t) {
         const uint8_t *p = kh + (size_t)t * QT * DH;
-        const unsigned off = col * DH + quarter * 16;
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) kr[kb][j] = load16<NTL>(p + (off + kb * 16 * DH + j * 64));
-        ksr = ks[(t * QT + (lane & 3) * 16) >> g.bsh];
+            for (int j = 0; j < NJ; ++j) load(p, off_k + kb * 16 * DH + j * 64, lds_k + (kb * NJ + j) * 1024);
     };
     auto load_v = [&](int t) {
         const uint8_t *p = vh + (size_t)t * QT * DH;
-        const unsigned off = col * QT + quarter * 16;
 #pragma unroll
-        for (int dt = 0; dt < ND; ++dt) vr[dt] = load16<NTL>(p + (off + dt * 16 * QT));
-        vsr = vs[(t * QT + (lane & 3) * 16) >> g.bsh];
+        for (int dt = 0; dt < ND; ++dt) load(p, off_v + dt * 16 * QT, lds_v + dt * 1024);
     };
     if (t < t_end) {
         load_k(t);
         load_v(t);
     }
-    __builtin_amdgcn_sched_barrier(0);
 
     QuantRow qr[MT];
     h8_t qf[MT][2 * NJ];
@@ -623,37 +632,44 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
     for (; t < t_end; t += 4) {
         const int key0 = t * QT + quarter * 4;
         const bool masked = t * QT + QT > full;   // some row does not see all of the tile
-        float s[MT][4][4];
+        const bool more = t + 4 < t_end;
+        float s[MT][4][4], ksc[4], vsc[4];
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+            ksc[kb] = scalar_load(ks, (t * QT + kb * 16) >> g.bsh);
+            vsc[kb] = scalar_load(vs, (t * QT + kb * 16) >> g.bsh);
+        }
+        lds_loads_wait<ND>();       // K is there, V's ND loads may be under way
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb) {
             qf4_t c[MT] = {};
 #pragma unroll
             for (int j = 0; j < NJ; ++j) {
-                const h8_t k0 = bytes_to_h8<FMT>(kr[kb][j].x, kr[kb][j].y), k1 = bytes_to_h8<FMT>(kr[kb][j].z, kr[kb][j].w);
+                const qu4_t u = sm.tile[wave][0][(kb * NJ + j) * 64 + lane];
+                const h8_t k0 = bytes_to_h8<FMT>(u.x, u.y), k1 = bytes_to_h8<FMT>(u.z, u.w);
 #pragma unroll
                 for (int r = 0; r < MT; ++r) {
                     c[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, qf[r][2 * j], c[r], 0, 0, 0);
                     c[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, qf[r][2 * j + 1], c[r], 0, 0, 0);
                 }
             }
-            const float kscale = lane_f(ksr, kb);
 #pragma unroll
             for (int r = 0; r < MT; ++r) {
-                const float f = crow[r] * kscale;
+                const float f = crow[r] * ksc[kb];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) s[r][kb][i] = c[r][i] * f;
             }
         }
-        // loads are issued here and not where they are used: about a round under way
         __builtin_amdgcn_sched_barrier(0);
-        if (t + 4 < t_end) load_k(t + 4);
+        __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the bytes have been read
+        if (more) load_k(t + 4);
         __builtin_amdgcn_sched_barrier(0);
 
         // the largest V scale of the tile's blocks of live rows
-        float vmax = 0.f, vsc[4];
+        float vmax = 0.f;
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb) {
-            vsc[kb] = t * QT + kb * 16 < len ? lane_f(vsr, kb) : 0.f;
+            vsc[kb] = t * QT + kb * 16 < len ? vsc[kb] : 0.f;
             vmax = fmaxf(vmax, vsc[kb]);
         }
         const int ve = max(vexp, (int)(uniform(__float_as_uint(vmax)) >> 23) - 126);
@@ -735,29 +751,37 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
                 }
         }
         vexp = ve;
-        if (FMT == WNW_QUANT_E4M3 && t * QT + QT > len) {
+        if (more)
+            lds_loads_wait<4 * NJ>();     // V is there, the next K may be under way
+        else
+            lds_loads_wait<0>();
+        unsigned live[4] = {~0u, ~0u, ~0u, ~0u};
+        const bool tail = FMT == WNW_QUANT_E4M3 && t * QT + QT > len;
+        if (tail) {
             // bytes of dead rows may be e4m3's NaN
 #pragma unroll
             for (int kb = 0; kb < 4; ++kb) {
-                const int live = len - (key0 + kb * 16);
-                const unsigned mask = live >= 4 ? ~0u : live <= 0 ? 0u : (1u << (8 * live)) - 1;
-#pragma unroll
-                for (int dt = 0; dt < ND; ++dt) vr[dt][kb] &= mask;
+                const int n = len - (key0 + kb * 16);
+                live[kb] = n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1;
             }
         }
 #pragma unroll
-        for (int dt = 0; dt < ND; ++dt)
+        for (int dt = 0; dt < ND; ++dt) {
+            qu4_t u = sm.tile[wave][1][dt * 64 + lane];
+            if (tail) u &= qu4_t{live[0], live[1], live[2], live[3]};
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const h8_t v = bytes_to_h8<FMT>(vr[dt][2 * c], vr[dt][2 * c + 1]);
+                const h8_t v = bytes_to_h8<FMT>(u[2 * c], u[2 * c + 1]);
 #pragma unroll
                 for (int r = 0; r < MT; ++r) {
                     o[r][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph[r][c], o[r][dt], 0, 0, 0);
                     if constexpr (F32) o[r][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl[r][c], o[r][dt], 0, 0, 0);
                 }
             }
+        }
         __builtin_amdgcn_sched_barrier(0);
-        if (t + 4 < t_end) load_v(t + 4);
+        __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (more) load_v(t + 4);
         __builtin_amdgcn_sched_barrier(0);
     }
 
@@ -771,7 +795,7 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
             sm.l[wave][r * 16 + col] = sum[r];
         }
 #pragma unroll
-        for (int dt = 0; dt < ND; ++dt) *(qf4_t *)&sm.o[wave][r * 16 + col][dt * 16 + quarter * 4] = o[r][dt] * unit;
+        for (int dt = 0; dt < ND; ++dt) *(qf4_t *)&sm.o[wave][r * 16 + col][sm.unit(r * 16 + col, dt * 4 + quarter)] = o[r][dt] * unit;
     }
     __syncthreads();
     for (int row = threadIdx.x >> 4; row < RB; row += Q_THREADS / 16) {
@@ -788,7 +812,11 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
             const float lw = sm.l[w][row], f = lw == 0.f ? 0.f : exp2f(sm.m[w][row] - finite_or_zero(mm));   // 0: saw nothing
             ll += f * lw;
 #pragma unroll
-            for (int e = 0; e < DH / 16; ++e) x[e] += f * sm.o[w][row][d0 + e];
+            for (int e = 0; e < DH / 16; e += 4) {
+                const qf4_t y = *(const qf4_t *)&sm.o[w][row][sm.unit(row, (d0 + e) / 4)];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[e + k] += f * y[k];
+            }
         }
         if (slot >= 0) {
             const size_t at = (size_t)(blockIdx.x * 2 + slot) * RB + row;
@@ -807,8 +835,15 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
     }
 }
 
+// Work-groups that a compute unit holds: of d = 128 two by shared memory, of d = 64 with one block of rows three by registers.
+template <int DH, int MT>
+constexpr int token_held()
+{
+    return DH == 64 && MT == 1 ? 3 : 2;
+}
+
 template <int DH, int FMT, bool F32, int MT, bool NTL>
-__global__ __launch_bounds__(Q_THREADS, MT == 2 ? 1 : DH == 64 ? 3 : 2) void quant_token_kernel(QuantAttend a)
+__global__ __launch_bounds__(Q_THREADS, (token_held<DH, MT>())) void quant_token_kernel(QuantAttend a)
 {
     __shared__ QuantTokenSmem<DH, MT> sm;
     const QuantShare sh(a, threadIdx.x & 63);
@@ -991,7 +1026,7 @@ QuantPlan quant_plan(const wnw_quant_config &c, int32_t n_layers, int32_t q_head
     p.RB = R > 16 ? 32 : 16;
     const int64_t blocks = heads * ((R + p.RB - 1) / p.RB), tiles = (len + QT - 1) / QT * blocks;
     // as many as the chip's 256 compute units hold at once, or as many as pieces of MIN_PIECE tiles need
-    const int held = 256 * (p.RB == 32 ? 1 : c.head_dim == 64 ? 3 : 2);
+    const int held = 256 * (c.head_dim == 64 && p.RB == 16 ? token_held<64, 1>() : 2);
     p.W = (int)std::max<int64_t>(1, std::min<int64_t>(held, tiles / MIN_PIECE + blocks));
     // Bytes that one pass reads once and the 256 MB of the last-level cache cannot keep for the next one
     p.stream = R <= p.RB && heads * len * c.head_dim * 2 > (256ll << 20);
