@@ -45,7 +45,8 @@ struct QuantGeo {
     int bsh;          // log2 of the rows per scale
     const uint8_t *k, *v;
     const float *ks, *vs;
-    __host__ __device__ size_t head(int b, int l, int h) const { return ((size_t)b * L + l0 + l) * H + h; }
+    // head hd (of nl * H) of a call's layers in sequence b
+    __host__ __device__ size_t head(int b, int hd) const { return ((size_t)b * L + l0) * H + hd; }
 };
 
 __device__ inline int q_clamp(int x, int hi)
@@ -172,12 +173,12 @@ __global__ __launch_bounds__(Q_THREADS) void quant_write_kernel(QuantGeo g, int 
     __shared__ QuantTileSmem<DH> sm;
     __shared__ unsigned wmax[4];
     const bool is_v = blockIdx.x & 1;
-    const int item = blockIdx.x >> 1, hd = item / tiles, h = hd % g.H, bl = hd / g.H, l = bl % g.nl, b = bl / g.nl;
+    const int item = blockIdx.x >> 1, hd = item / tiles, b = hd / (g.nl * g.H);
     const int pos = q_clamp(pos_dev[b], g.cap), cnt = count_dev ? q_clamp(count_dev[b], n) : n, end = min(pos + cnt, g.cap);
     const int tile = pos / QT + (item - hd * tiles), row0 = tile * QT;
     if (row0 >= end) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, dg = lane & 15, rg = tid >> 4;
-    const size_t head = g.head(b, l, h);
+    const size_t head = g.head(b, hd - b * g.nl * g.H);
     uint8_t *codes = const_cast<uint8_t *>(is_v ? g.v : g.k) + (head * g.cap + row0) * DH;
     float *scales = const_cast<float *>(is_v ? g.vs : g.ks) + ((head * g.cap) >> g.bsh);
     const uint16_t *src = (is_v ? vn : kn) + (size_t)hd * n * DH + (size_t)dg * E;
@@ -300,13 +301,12 @@ __global__ __launch_bounds__(Q_THREADS) void quant_read_kernel(QuantGeo g, int n
     constexpr int E = DH / 16;
     __shared__ QuantTileSmem<DH> sm;
     const bool both = ko && vo, is_v = both ? blockIdx.x & 1 : vo != nullptr;
-    const int item = both ? blockIdx.x >> 1 : blockIdx.x, hd = item / tiles, h = hd % g.H, bl = hd / g.H, l = bl % g.nl,
-              b = bl / g.nl;
+    const int item = both ? blockIdx.x >> 1 : blockIdx.x, hd = item / tiles, b = hd / (g.nl * g.H);
     const int pos = q_clamp(pos_dev[b], g.cap), cnt = count_dev ? q_clamp(count_dev[b], n) : n, end = min(pos + cnt, g.cap);
     const int tile = pos / QT + (item - hd * tiles), row0 = tile * QT;
     if (row0 >= end) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, dg = lane & 15, rg = tid >> 4;
-    const size_t head = g.head(b, l, h);
+    const size_t head = g.head(b, hd - b * g.nl * g.H);
     const uint8_t *codes = (is_v ? g.v : g.k) + (head * g.cap + row0) * DH;
     const float s = (is_v ? g.vs : g.ks)[(head * g.cap + row0 + wave * 16) >> g.bsh];
     void *out = is_v ? vo : ko;
@@ -364,7 +364,7 @@ struct QuantAttend {
 // the join of its wavefronts).  A block that is not whole leaves its result in the workspace, in the work-group's slot 1
 // (its first tiles) or 0 (later ones), and quant_merge_kernel joins those.
 constexpr int MIN_PIECE = 4;    // tiles of a piece at least, one per wavefront
-constexpr int PIECE_COST = 3;
+constexpr int PIECE_COST = 10;
 
 struct QuantSeq {
     int len, cnt, tiles, nrb;   // rows, tokens of this call, tiles and blocks of rows of a head (0: none)
@@ -381,14 +381,45 @@ __device__ inline QuantSeq quant_seq(const QuantAttend &a, int b)
     return q;
 }
 
-__device__ inline unsigned wave_scan(unsigned v, int lane)   // sum over the lanes up to this one
+// Inclusive scans over the wavefront's lanes by data-parallel moves: within rows of sixteen lanes, then across them.
+template <typename F>
+__device__ inline unsigned wave_scan_by(unsigned v, F f)
 {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const unsigned u = (unsigned)__shfl_up((int)v, o);
-        if (lane >= o) v += u;
-    }
-    return v;
+    v = f(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, false));
+    v = f(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, false));
+    v = f(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, false));
+    v = f(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, false));
+    v = f(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false));
+    return f(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false));
+}
+__device__ inline unsigned wave_scan(unsigned v)
+{
+    return wave_scan_by(v, [](unsigned a, unsigned b) { return a + b; });
+}
+__device__ inline unsigned wave_sum(unsigned v)
+{
+    return (unsigned)__builtin_amdgcn_readlane((int)wave_scan(v), 63);
+}
+__device__ inline unsigned wave_max(unsigned v)
+{
+    return (unsigned)__builtin_amdgcn_readlane((int)wave_scan_by(v, [](unsigned a, unsigned b) { return max(a, b); }), 63);
+}
+// f(x of this lane, x of lane ^ 16), and the same with lane ^ 32.
+template <typename F>
+__device__ inline float across_quarters(float x, F f)
+{
+    auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = f(__uint_as_float(p[0]), __uint_as_float(p[1]));
+    auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return f(__uint_as_float(q[0]), __uint_as_float(q[1]));
+}
+__device__ inline float quarters_max(float x)
+{
+    return across_quarters(x, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ inline float quarters_sum(float x)
+{
+    return across_quarters(x, [](float a, float b) { return a + b; });
 }
 __device__ inline unsigned uniform(unsigned v)
 {
@@ -422,13 +453,7 @@ struct QuantShare {
             units += (unsigned)(q.nrb * heads);
             most = max(most, q.nrb ? (unsigned)q.tiles : 0u);
         }
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            t += (unsigned)__shfl_xor((int)t, o);
-            units += (unsigned)__shfl_xor((int)units, o);
-            most = max(most, (unsigned)__shfl_xor((int)most, o));
-        }
-        t = uniform(t), units = uniform(units), most = uniform(most);
+        t = wave_sum(t), units = wave_sum(units), most = wave_max(most);
         total = t;
         per = max((t + a.W - 1) / a.W, (unsigned)MIN_PIECE);
         if (units < (unsigned)a.W) {
@@ -439,9 +464,7 @@ struct QuantShare {
                 per = 1;
                 t = 0;
                 for (int b0 = 0; b0 < a.g.B; b0 += 64) t += work(seq(a, b0));
-#pragma unroll
-                for (int o = 1; o < 64; o <<= 1) t += (unsigned)__shfl_xor((int)t, o);
-                total = uniform(t);
+                total = wave_sum(t);
             }
         }
     }
@@ -451,7 +474,7 @@ struct QuantShare {
         unsigned base = 0;
         for (int b0 = 0;; b0 += 64) {
             const QuantSeq q = seq(a, b0);
-            const unsigned v = work(q), inc = wave_scan(v, lane);
+            const unsigned v = work(q), inc = wave_scan(v);
             const unsigned long long hit = __ballot(base + inc > f);
             if (hit) {
                 const int at = __builtin_ctzll(hit);
@@ -467,9 +490,7 @@ struct QuantShare {
     {
         unsigned t = 0;
         for (int b0 = 0; b0 < end; b0 += 64) t += b0 + lane < end ? work(seq(a, b0)) : 0u;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) t += (unsigned)__shfl_xor((int)t, o);
-        return uniform(t);
+        return wave_sum(t);
     }
     // Tiles of a block's item i: [first, first + count).
     __device__ void piece(const QuantSeq &q, unsigned i, int &first, int &end) const
@@ -486,7 +507,7 @@ struct QuantRow {
 };
 __device__ inline QuantRow quant_row(const QuantAttend &a, int hd, int r, int len, int cnt)
 {
-    const int i = r / a.G, j = r - i * a.G;
+    const int i = a.n == 1 ? 0 : r / a.G, j = r - i * a.G;
     QuantRow q;
     q.row_of = (hd * a.G + j) * a.n + i;      // hd = (b * nl + l) * H + h
     q.vis = r < a.R && i < cnt ? max(0, min(len, len - cnt + i + 1)) : -1;
@@ -579,10 +600,10 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
 {
     constexpr int NJ = DH / 64, ND = DH / 16, RB = 16 * MT;
     const QuantGeo &g = a.g;
-    const int len = sq.len, cnt = sq.cnt, h = hd % g.H, l = hd / g.H % g.nl;
+    const int len = sq.len, cnt = sq.cnt;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quarter = lane >> 4;
-    const size_t head = g.head(b, l, h);
+    const size_t head = g.head(b, hd - b * g.nl * g.H);
     const uint8_t *kh = g.k + head * g.cap * DH, *vh = g.v + head * g.cap * DH;
     const float *ks = g.ks + ((head * g.cap) >> g.bsh), *vs = g.vs + ((head * g.cap) >> g.bsh);
 
@@ -688,8 +709,7 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
             for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) mt = fmaxf(mt, x[kb][i]);
-            mt = fmaxf(mt, __shfl_xor(mt, 16));
-            mt = fmaxf(mt, __shfl_xor(mt, 32));
+            mt = quarters_max(mt);
             if (ve > vexp || __any(mt > m[r])) {
                 const float alpha = exp2_hw(m[r] - finite_or_zero(mt)), f = alpha * pow2i(vexp - ve);
 #pragma unroll
@@ -710,10 +730,7 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
                 // block sums relative to m; the merge makes them shares
                 const int nb = QT >> g.bsh;
 #pragma unroll
-                for (int kb = 0; kb < 4; ++kb) {
-                    bs[kb] += __shfl_xor(bs[kb], 16);
-                    bs[kb] += __shfl_xor(bs[kb], 32);
-                }
+                for (int kb = 0; kb < 4; ++kb) bs[kb] = quarters_sum(bs[kb]);
                 if (quarter == 0 && qr[r].vis >= 0) {
                     float *to = a.mass + (size_t)qr[r].row_of * (g.cap >> g.bsh) + (size_t)t * nb;
                     if (nb == 1)
@@ -788,8 +805,7 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
     const float unit = pow2i(vexp - 15);
 #pragma unroll
     for (int r = 0; r < MT; ++r) {
-        sum[r] += __shfl_xor(sum[r], 16);
-        sum[r] += __shfl_xor(sum[r], 32);
+        sum[r] = quarters_sum(sum[r]);
         if (quarter == 0) {
             sm.m[wave][r * 16 + col] = m[r];
             sm.l[wave][r * 16 + col] = sum[r];
@@ -853,11 +869,12 @@ __global__ __launch_bounds__(Q_THREADS, (token_held<DH, MT>())) void quant_token
     QuantSeq sq;
     int b = sh.find(a, f, start, sq);
     for (;;) {
-        const unsigned off = f - start, span = sh.span(sq), unit = off / span, at = off - unit * span;
+        const unsigned off = f - start, span = sh.span(sq), unit = span == 1 ? off : off / span, at = off - unit * span;
         int ta = (int)at, tb = (int)min(span, at + (f1 - f));
         f += tb - ta;
         if (sh.pp) sh.piece(sq, at, ta, tb);
-        quant_token_block<DH, FMT, F32, MT, NTL>(a, sm, sq, b, b * sh.heads + (int)(unit / sq.nrb), (int)(unit % sq.nrb), ta, tb,
+        const int hd = sq.nrb == 1 ? (int)unit : (int)unit / sq.nrb;
+        quant_token_block<DH, FMT, F32, MT, NTL>(a, sm, sq, b, b * sh.heads + hd, (int)unit - hd * sq.nrb, ta, tb,
                                                  ta > 0 ? 0 : tb < sq.tiles ? 1 : -1);
         if (f >= f1) return;
         if (f - start >= sh.work(sq)) b = sh.find(a, f, start, sq);

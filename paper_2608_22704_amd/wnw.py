@@ -133,6 +133,8 @@ def _ptr(t):
 
 # element sizes the library reads or writes: bf16 bit patterns (any 2-byte dtype), fp32, int32, bytes
 _BF16, _F32, _I32, _U8 = "bf16", "f32", "i32", "u8"
+_NAME = {_BF16: ("torch.bfloat16", "torch.int16", "torch.uint16"), _F32: ("torch.float32",), _I32: ("torch.int32",),
+         _U8: ("torch.uint8",)}
 
 
 def _dev(t, kind, numel=None, what="tensor"):
@@ -262,8 +264,8 @@ class QuantCache:
 
     def _struct(self, cfg, device):
         n = cfg.batch * cfg.layers * cfg.kv_heads * cfg.capacity
-        scales = n // max(cfg.block, 1)
-        return wnw_quant_cache(_on(device, self.k, _U8, n * cfg.head_dim, "k"), _on(device, self.v, _U8, n * cfg.head_dim, "v"),
+        scales, n = n // max(cfg.block, 1), n * cfg.head_dim
+        return wnw_quant_cache(_on(device, self.k, _U8, n, "k"), _on(device, self.v, _U8, n, "v"),
                                _on(device, self.k_scale, _F32, scales, "k_scale"),
                                _on(device, self.v_scale, _F32, scales, "v_scale"))
 
@@ -287,10 +289,19 @@ def _qcheck(status):
 
 
 def _on(device, t, kind, numel, what):
-    """_dev() for a tensor that must be on `device`, the one that the call's work runs on."""
-    if hasattr(t, "device") and t.device != device:
-        raise ValueError(f"{what} is on {t.device}, the call's work on {device}")
-    return _dev(t, kind, numel, what)
+    """Address of a tensor that must be on the GPU `device` (its index), where the call's work runs, with the checks of
+    _dev(); half precision is not taken for bf16.  These calls are made for every layer and token: no detours."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.get_device() != device:
+        raise ValueError(f"{what} is on {t.device}, the call's work on cuda:{device}")
+    if str(t.dtype) not in _NAME[kind]:
+        raise TypeError(f"{what}: expected {kind} elements, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+    if numel is not None and t.numel() < numel:
+        raise ValueError(f"{what}: needs {numel} elements, got {t.numel()}")
+    return t.data_ptr()
 
 
 def _quant_shape(cfg, t, heads, what):
@@ -302,7 +313,7 @@ def _quant_shape(cfg, t, heads, what):
 
 def _quant_device():
     import torch
-    return torch.device("cuda", torch.cuda.current_device())
+    return torch.cuda.current_device()
 
 
 def wnw_quant_write(cfg, cache, k_dev, v_dev, pos_dev, count_dev=None, first_layer=0, stream=None):
