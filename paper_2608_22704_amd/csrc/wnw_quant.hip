@@ -5,6 +5,7 @@
 //   quant_read_kernel    the same tiles back to fp32 / bf16
 //   quant_token_kernel   attention of few query rows: K and V bytes go from HBM to registers once and
 //                        straight into the matrix cores
+//   quant_wide_kernel    attention of many query rows: tiles become fp16 in shared memory once for 128 rows
 //   quant_merge_kernel   joins the pieces of a cache split over work-groups, and finishes the block masses
 //
 // Bytes become fp16 on the way to the matrix cores, exactly: integers up to 127 and e4m3 numbers both fit.
@@ -566,6 +567,31 @@ __device__ inline float scalar_load(const float *p, int i)
     return ((const __attribute__((address_space(4))) float *)p)[i];
 }
 
+// A query row whose largest magnitude has the bf16 bits amax: the power of two that takes it to 2^14 .. 2^15, and what
+// turns its products with bytes into base-2 logits, before K's scale (NaN for a row that is not finite).
+__device__ inline int query_shift(unsigned amax)
+{
+    return min(141 - (int)(amax >> 7), 126);
+}
+__device__ inline float query_up(unsigned amax)
+{
+    return pow2i(query_shift(amax));
+}
+__device__ inline float query_scale(unsigned amax, float scale)
+{
+    return amax >= 0x7f80u ? __uint_as_float(0x7fc00000u) : scale * pow2i(-query_shift(amax));
+}
+__device__ inline h8_t query_half(qu4_t u, float up)
+{
+    h8_t f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        f[2 * e] = (_Float16)(__uint_as_float(u[e] << 16) * up);
+        f[2 * e + 1] = (_Float16)(__uint_as_float(u[e] & 0xffff0000u) * up);
+    }
+    return f;
+}
+
 // Q^T of a block of rows as fp16: column (row) lane % 16, quarter q has dimensions 64 j + 16 q + 8 e .. + 8 in f[2 j + e].
 // Returns what turns products with bytes into base-2 logits, before K's scale.
 template <int NJ>
@@ -581,16 +607,10 @@ __device__ inline float load_queries(const uint16_t *row, bool live, int quarter
     }
     amax = max(amax, (unsigned)__shfl_xor((int)amax, 16));
     amax = max(amax, (unsigned)__shfl_xor((int)amax, 32));
-    const int sh = min(141 - (int)(amax >> 7), 126);       // the largest magnitude goes to 2^14 .. 2^15
-    const float up = pow2i(sh);
+    const float up = query_up(amax);
 #pragma unroll
-    for (int j = 0; j < 2 * NJ; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            f[j][2 * e] = (_Float16)(__uint_as_float(u[j][e] << 16) * up);
-            f[j][2 * e + 1] = (_Float16)(__uint_as_float(u[j][e] & 0xffff0000u) * up);
-        }
-    return amax >= 0x7f80u ? __uint_as_float(0x7fc00000u) : scale * pow2i(-sh);
+    for (int j = 0; j < 2 * NJ; ++j) f[j] = query_half(u[j], up);
+    return query_scale(amax, scale);
 }
 
 // Tiles ta .. tb - 1 of block rb of head (b, hd)'s rows; slot: where a piece's result goes (-1: the block is whole).
@@ -882,6 +902,259 @@ __global__ __launch_bounds__(Q_THREADS, (token_held<DH, MT>())) void quant_token
     }
 }
 
+// Many query rows.  A work-group has blocks of RB = 128 rows, 32 for each of its four wavefronts; all of them use the same
+// tiles of 64 cache rows, which two buffers in shared memory hold as fp16, so that a byte is converted once per 128
+// rows.  While a tile is in use the next one's bytes, loaded a round before, are converted and written, and those of the
+// one after it are on their way to registers.
+//   S^T (32 keys x 32 rows) = K Q^T and O^T (32 dimensions x 32 rows) += V^T P^T by 32 x 32 x 16 products (see wnw_lds.h for
+//   operands): a lane has 16 keys of ONE row, elements 0 .. 7 in the tile's 16-row block 2 k and 8 .. 15 in 2 k + 1, so that S^T's
+//   elements are P^T's operand as they stand.
+// A row's maximum m is raised, and its output and sum scaled, only when a logit exceeds it by LAZY (base 2): weights
+// are up to 2^LAZY then, which fp16 has room for.
+constexpr int WIDE_ROWS = 128;
+constexpr int LAZY = 8;
+
+template <int DH>
+struct QuantWideSmem {
+    static constexpr int KU = DH / 8;     // 16-byte units of a row of K
+    alignas(16) qu4_t k[2][QT * KU];      // [key][dimension / 8]
+    alignas(16) qu4_t v[2][DH * 8];       // [dimension][2 (16-row block) + half]: rows 4 half .. + 4 and 8 + 4 half .. + 4 of the block
+    // eight neighbouring lanes read the same unit of eight rows: spread over the banks
+    static __device__ int k_at(int key, int u) { return key * KU + (u ^ (DH == 128 ? key & 15 : (key >> 1) & 7)); }
+    static __device__ int v_at(int d, int u) { return d * 8 + (u ^ ((d >> 1) & 7)); }
+};
+
+template <int FMT>
+__device__ inline qu4_t convert8(unsigned a, unsigned b)
+{
+    return __builtin_bit_cast(qu4_t, bytes_to_h8<FMT>(a, b));
+}
+
+template <int DH, int FMT, bool F32>
+__device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> &sm, const QuantSeq &sq, int b, int hd, int rb,
+                                        int ta, int tb, int slot)
+{
+    constexpr int NS = DH / 16, ND = DH / 32, RB = WIDE_ROWS;
+    const QuantGeo &g = a.g;
+    const int len = sq.len, cnt = sq.cnt;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, half = lane >> 5;
+    const size_t head = g.head(b, hd - b * g.nl * g.H);
+    const uint8_t *kh = g.k + head * g.cap * DH, *vh = g.v + head * g.cap * DH;
+    const float *ks = g.ks + ((head * g.cap) >> g.bsh), *vs = g.vs + ((head * g.cap) >> g.bsh);
+
+    // cache rows that the block's last row sees; those that the wavefront's first row sees
+    const int seen = min(len, max(0, len - cnt + min(cnt - 1, min(rb * RB + RB - 1, a.R - 1) / a.G) + 1));
+    const int full = len - cnt + (rb * RB + wave * 32) / a.G + 1;
+    const int t_end = min(tb, (seen + QT - 1) / QT);
+
+    // bytes of a tile: the thread has 32 (16) dimensions of one key, and 32 places of one dimension of V
+    constexpr int KL = DH / 64;
+    const int key_t = tid >> 2, part_t = tid & 3, d_t = tid >> 1, half_t = tid & 1;
+    const bool has_v = DH == 128 || tid < 2 * DH;
+    qu4_t kr[KL], vr[2];
+    auto load = [&](int t) {
+        const uint8_t *pk = kh + (size_t)t * QT * DH, *pv = vh + (size_t)t * QT * DH;
+#pragma unroll
+        for (int j = 0; j < KL; ++j) kr[j] = *(const qu4_t *)(pk + (key_t * DH + (part_t * KL + j) * 16));
+        if (has_v) {
+            vr[0] = *(const qu4_t *)(pv + (d_t * QT + half_t * 16));
+            vr[1] = *(const qu4_t *)(pv + (d_t * QT + half_t * 16 + 32));
+        }
+    };
+    auto store = [&](int t) {
+        const int buf = t & 1;
+#pragma unroll
+        for (int j = 0; j < KL; ++j) {
+            sm.k[buf][sm.k_at(key_t, (part_t * KL + j) * 2)] = convert8<FMT>(kr[j].x, kr[j].y);
+            sm.k[buf][sm.k_at(key_t, (part_t * KL + j) * 2 + 1)] = convert8<FMT>(kr[j].z, kr[j].w);
+        }
+        if (has_v) {
+            if (FMT == WNW_QUANT_E4M3 && t * QT + QT > len) {
+                // bytes of dead rows may be e4m3's NaN
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const int n = len - (t * QT + 16 * c + 4 * (half_t + 2 * j));
+                        vr[j][c] &= n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1;
+                    }
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) sm.v[buf][sm.v_at(d_t, 2 * c + half_t)] = convert8<FMT>(vr[0][c], vr[1][c]);
+        }
+    };
+    if (ta < t_end) load(ta);
+
+    const QuantRow qr = quant_row(a, hd, rb * RB + wave * 32 + col, len, cnt);
+    h8_t qf[NS];
+    float crow;
+    {
+        qu4_t u[NS];
+        unsigned amax = 0;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            u[s] = qr.vis >= 0 ? *(const qu4_t *)(a.q + (size_t)qr.row_of * DH + s * 16 + half * 8) : qu4_t{0, 0, 0, 0};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) amax = max(amax, max(u[s][e] & 0x7fffu, (u[s][e] >> 16) & 0x7fffu));
+        }
+        amax = max(amax, (unsigned)__shfl_xor((int)amax, 32));
+        crow = query_scale(amax, a.scale);
+        const float up = query_up(amax);
+#pragma unroll
+        for (int s = 0; s < NS; ++s) qf[s] = query_half(u[s], up);
+    }
+    float m = -INFINITY, sum = 0.f;
+    f32x16_t o[ND];
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+    int vexp = -100;           // o is in units of 2^(vexp + LAZY - 15); V scales seen so far are below 2^vexp
+    if (ta < t_end) {
+        store(ta);
+        if (ta + 1 < t_end) load(ta + 1);
+    }
+    __syncthreads();
+    for (int t = ta; t < t_end; ++t) {
+        const int buf = t & 1;
+        const bool masked = t * QT + QT > full;     // some row of the wavefront does not see all of the tile
+        float f[4], vsc[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            f[c] = crow * scalar_load(ks, (t * QT + c * 16) >> g.bsh);
+            vsc[c] = scalar_load(vs, (t * QT + c * 16) >> g.bsh);
+        }
+        f32x16_t x[2];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[kb][i] = 0.f;
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+                x[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                    __builtin_bit_cast(h8_t, sm.k[buf][sm.k_at(kb * 32 + col, 2 * s + half)]), qf[s], x[kb], 0, 0, 0);
+        }
+        const int key0 = t * QT + half * 4;         // element i of x[kb]: key0 + 32 kb + 8 (i / 4) + i % 4
+        if (masked) {
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    x[kb][i] = key0 + 32 * kb + 8 * (i / 4) + i % 4 < qr.vis ? x[kb][i] * f[2 * kb + i / 8] : -INFINITY;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) f[c] = 1.f;
+        }
+        float top = -INFINITY, vmax = 0.f;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            float y = x[c >> 1][8 * (c & 1)];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) y = fmaxf(y, x[c >> 1][8 * (c & 1) + i]);
+            top = fmaxf(top, y * f[c]);
+            vsc[c] = t * QT + c * 16 < len ? vsc[c] : 0.f;
+            vmax = fmaxf(vmax, vsc[c]);
+        }
+        {
+            auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+            top = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+        }
+        const int ve = max(vexp, (int)(uniform(__float_as_uint(vmax)) >> 23) - 126);
+        if (ve > vexp || __any(top > m + LAZY)) {
+            const float mn = fmaxf(m, top), alpha = exp2_hw(m - finite_or_zero(mn)), fo = alpha * pow2i(vexp - ve);
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt) o[dt] *= fo;
+            sum *= alpha;
+            m = mn;
+            vexp = ve;
+        }
+        const float mz = finite_or_zero(m), vf = pow2i(15 - LAZY - vexp);
+        h8_t ph[4], pl[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const float w = vsc[c] * vf;
+            float p[8], part = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                p[i] = exp2_hw(fmaf(x[c >> 1][8 * (c & 1) + i], f[c], -mz));
+                part += p[i];
+                p[i] *= w;
+            }
+            sum += part;
+            if (masked) {      // a masked weight is 0 whatever the scale is
+#pragma unroll
+                for (int i = 0; i < 8; ++i) p[i] = key0 + 16 * c + 8 * (i / 4) + i % 4 < qr.vis ? p[i] : 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const _Float16 hi = (_Float16)p[i];
+                ph[c][i] = hi;
+                if constexpr (F32) pl[c][i] = (_Float16)(p[i] - (float)hi);
+            }
+        }
+        if (t + 1 < t_end) {
+            store(t + 1);
+            if (t + 2 < t_end) load(t + 2);
+        }
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const h8_t v = __builtin_bit_cast(h8_t, sm.v[buf][sm.v_at(dt * 32 + col, 2 * c + half)]);
+                o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, ph[c], o[dt], 0, 0, 0);
+                if constexpr (F32) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pl[c], o[dt], 0, 0, 0);
+            }
+        __syncthreads();
+    }
+    sum += __shfl_xor(sum, 32);
+    if (qr.vis < 0) return;
+    // element i of o[dt]: dimension 32 dt + 8 (i / 4) + 4 half + i % 4 of row col
+    const float unit = pow2i(vexp + LAZY - 15), inv = sum == 0.f ? 0.f : 1.f / sum;
+    const size_t at = slot >= 0 ? (size_t)(blockIdx.x * 2 + slot) * RB + wave * 32 + col : (size_t)qr.row_of;
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            float y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = o[dt][i + e] * unit * (slot >= 0 ? 1.f : inv);
+            const size_t to = at * DH + dt * 32 + 2 * i + 4 * half;
+            if (slot >= 0)
+                *(qf4_t *)(a.ws_o + to) = qf4_t{y[0], y[1], y[2], y[3]};
+            else
+                store_row<4, !F32>(a.out, to, y);
+        }
+    if (half == 0) {
+        if (slot >= 0)
+            a.ws_ml[at] = make_float2(m, sum);
+        else if (a.lse)
+            a.lse[at] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * Q_LN2;
+    }
+}
+
+template <int DH, int FMT, bool F32>
+__global__ __launch_bounds__(Q_THREADS, 2) void quant_wide_kernel(QuantAttend a)
+{
+    __shared__ QuantWideSmem<DH> sm;
+    const QuantShare sh(a, threadIdx.x & 63);
+    unsigned f = blockIdx.x * sh.per, start;
+    if (f >= sh.total) return;
+    const unsigned f1 = min(f + sh.per, sh.total);
+    QuantSeq sq;
+    int b = sh.find(a, f, start, sq);
+    for (;;) {
+        const unsigned off = f - start, span = sh.span(sq), unit = span == 1 ? off : off / span, at = off - unit * span;
+        int ta = (int)at, tb = (int)min(span, at + (f1 - f));
+        f += tb - ta;
+        if (sh.pp) sh.piece(sq, at, ta, tb);
+        const int hd = sq.nrb == 1 ? (int)unit : (int)unit / sq.nrb;
+        quant_wide_block<DH, FMT, F32>(a, sm, sq, b, b * sh.heads + hd, (int)unit - hd * sq.nrb, ta, tb,
+                                       ta > 0 ? 0 : tb < sq.tiles ? 1 : -1);
+        if (f >= f1) return;
+        if (f - start >= sh.work(sq)) b = sh.find(a, f, start, sq);
+    }
+}
+
 // One work-group per output row: joins the pieces of its cache, and makes the tiles' block sums shares of the whole.
 template <int DH, bool BF16>
 __global__ __launch_bounds__(Q_THREADS) void quant_merge_kernel(QuantAttend a)
@@ -1040,7 +1313,7 @@ QuantPlan quant_plan(const wnw_quant_config &c, int32_t n_layers, int32_t q_head
     const int64_t heads = (int64_t)c.batch * n_layers * c.kv_heads, R = (int64_t)q_heads / c.kv_heads * n;
     const int64_t len = max_len ? std::min(max_len, c.capacity) : c.capacity;
     QuantPlan p;
-    p.RB = R > 16 ? 32 : 16;
+    p.RB = R > 32 ? WIDE_ROWS : R > 16 ? 32 : 16;
     const int64_t blocks = heads * ((R + p.RB - 1) / p.RB), tiles = (len + QT - 1) / QT * blocks;
     // as many as the chip's 256 compute units hold at once, or as many as pieces of MIN_PIECE tiles need
     const int held = 256 * (c.head_dim == 64 && p.RB == 16 ? token_held<64, 1>() : 2);
@@ -1058,6 +1331,10 @@ QuantPlan quant_plan(const wnw_quant_config &c, int32_t n_layers, int32_t q_head
 template <int DH, int FMT, bool F32>
 void launch_token(const QuantPlan &p, const QuantAttend &a, hipStream_t st)
 {
+    if (p.RB == WIDE_ROWS) {
+        hipLaunchKernelGGL((quant_wide_kernel<DH, FMT, F32>), dim3(p.W), dim3(Q_THREADS), 0, st, a);
+        return;
+    }
     auto *k = p.RB == 16 ? (p.stream ? quant_token_kernel<DH, FMT, F32, 1, true> : quant_token_kernel<DH, FMT, F32, 1, false>)
                          : (p.stream ? quant_token_kernel<DH, FMT, F32, 2, true> : quant_token_kernel<DH, FMT, F32, 2, false>);
     hipLaunchKernelGGL(k, dim3(p.W), dim3(Q_THREADS), 0, st, a);
