@@ -629,8 +629,8 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
 
     // cache rows that the block's last and first row see
     const int seen = min(len, max(0, len - cnt + min(cnt - 1, min(rb * RB + RB - 1, a.R - 1) / a.G) + 1));
-    const int full = len - cnt + rb * RB / a.G + 1;
-    const int t_end = min(tb, (seen + QT - 1) / QT);
+    const int full = (int)uniform(len - cnt + rb * RB / a.G + 1);
+    const int t_end = (int)uniform(min(tb, (seen + QT - 1) / QT));
     int t = ta + wave;
 
     const unsigned lds_k = __builtin_amdgcn_readfirstlane(lds_address(sm.tile[wave][0])),
@@ -914,15 +914,23 @@ __global__ __launch_bounds__(Q_THREADS, (token_held<DH, MT>())) void quant_token
 constexpr int WIDE_ROWS = 128;
 constexpr int LAZY = 8;
 
+// Tiles in shared memory: a row of K has its dimensions, a row of V (a dimension) the tile's rows, 16-byte unit 2 c + half
+// with rows 4 half .. + 4 and 8 + 4 half .. + 4 of 16-row block c.  Rows are 16 bytes longer than their content: the eight lanes of
+// a cycle, on one unit of eight rows, meet distinct banks, and every access of a lane is its base and a constant
+// (with the units permuted by an exclusive or instead, their addresses took a tenth of the vector instructions).
 template <int DH>
 struct QuantWideSmem {
-    static constexpr int KU = DH / 8;     // 16-byte units of a row of K
-    alignas(16) qu4_t k[2][QT * KU];      // [key][dimension / 8]
-    alignas(16) qu4_t v[2][DH * 8];       // [dimension][2 (16-row block) + half]: rows 4 half .. + 4 and 8 + 4 half .. + 4 of the block
-    // eight neighbouring lanes read the same unit of eight rows: spread over the banks
-    static __device__ int k_at(int key, int u) { return key * KU + (u ^ (DH == 128 ? key & 15 : (key >> 1) & 7)); }
-    static __device__ int v_at(int d, int u) { return d * 8 + (u ^ ((d >> 1) & 7)); }
+    static constexpr unsigned K_ROW = DH * 2 + 16, V_ROW = QT * 2 + 16, K_BYTES = QT * K_ROW, BUF = K_BYTES + DH * V_ROW;
+    alignas(256) unsigned char tile[2][BUF];   // K, then V
 };
+__device__ inline h8_t lds_read(unsigned at)
+{
+    return __builtin_bit_cast(h8_t, *(const __attribute__((address_space(3))) qu4_t *)(size_t)at);
+}
+__device__ inline void lds_write(unsigned at, qu4_t x)
+{
+    *(__attribute__((address_space(3))) qu4_t *)(size_t)at = x;
+}
 
 template <int FMT>
 __device__ inline qu4_t convert8(unsigned a, unsigned b)
@@ -943,10 +951,10 @@ __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> 
     const uint8_t *kh = g.k + head * g.cap * DH, *vh = g.v + head * g.cap * DH;
     const float *ks = g.ks + ((head * g.cap) >> g.bsh), *vs = g.vs + ((head * g.cap) >> g.bsh);
 
-    // cache rows that the block's last row sees; those that the wavefront's first row sees
+    // cache rows that the block's last and first row see
     const int seen = min(len, max(0, len - cnt + min(cnt - 1, min(rb * RB + RB - 1, a.R - 1) / a.G) + 1));
-    const int full = len - cnt + (rb * RB + wave * 32) / a.G + 1;
-    const int t_end = min(tb, (seen + QT - 1) / QT);
+    const int full = (int)uniform(max(0, len - cnt + rb * RB / a.G + 1));
+    const int t_end = (int)uniform(min(tb, (seen + QT - 1) / QT));
 
     // bytes of a tile: the thread has 32 (16) dimensions of one key, and 32 places of one dimension of V
     constexpr int KL = DH / 64;
@@ -962,12 +970,17 @@ __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> 
             vr[1] = *(const qu4_t *)(pv + (d_t * QT + half_t * 16 + 32));
         }
     };
-    auto store = [&](int t) {
-        const int buf = t & 1;
+    using SM = QuantWideSmem<DH>;
+    const unsigned lds = uniform(lds_address(sm.tile[0]));
+    const unsigned k_put = lds + key_t * SM::K_ROW + part_t * KL * 32,
+                   v_put = lds + SM::K_BYTES + d_t * SM::V_ROW + half_t * 16;
+    const unsigned k_get = lds + col * SM::K_ROW + half * 16,
+                   v_get = lds + SM::K_BYTES + col * SM::V_ROW + half * 16;
+    auto store = [&](int t, unsigned buf) {
 #pragma unroll
         for (int j = 0; j < KL; ++j) {
-            sm.k[buf][sm.k_at(key_t, (part_t * KL + j) * 2)] = convert8<FMT>(kr[j].x, kr[j].y);
-            sm.k[buf][sm.k_at(key_t, (part_t * KL + j) * 2 + 1)] = convert8<FMT>(kr[j].z, kr[j].w);
+            lds_write(k_put + j * 32 + buf, convert8<FMT>(kr[j].x, kr[j].y));
+            lds_write(k_put + j * 32 + 16 + buf, convert8<FMT>(kr[j].z, kr[j].w));
         }
         if (has_v) {
             if (FMT == WNW_QUANT_E4M3 && t * QT + QT > len) {
@@ -981,7 +994,7 @@ __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> 
                     }
             }
 #pragma unroll
-            for (int c = 0; c < 4; ++c) sm.v[buf][sm.v_at(d_t, 2 * c + half_t)] = convert8<FMT>(vr[0][c], vr[1][c]);
+            for (int c = 0; c < 4; ++c) lds_write(v_put + c * 32 + buf, convert8<FMT>(vr[0][c], vr[1][c]));
         }
     };
     if (ta < t_end) load(ta);
@@ -1012,13 +1025,14 @@ __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> 
         for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
     int vexp = -100;           // o is in units of 2^(vexp + LAZY - 15); V scales seen so far are below 2^vexp
     if (ta < t_end) {
-        store(ta);
+        store(ta, 0);
         if (ta + 1 < t_end) load(ta + 1);
     }
     __syncthreads();
-    for (int t = ta; t < t_end; ++t) {
-        const int buf = t & 1;
-        const bool masked = t * QT + QT > full;     // some row of the wavefront does not see all of the tile
+    // one tile, from the buffer at `buf`; the next one goes to the other.  MASKED: some row may not see all of the tile.
+    auto round = [&](int t, auto buf_c, auto masked_c) {
+        const unsigned buf = buf_c, other = SM::BUF - buf;
+        constexpr bool MASKED = decltype(masked_c)::value;
         float f[4], vsc[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -1027,23 +1041,27 @@ __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> 
         }
         f32x16_t x[2];
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[kb][i] = 0.f;
 #pragma unroll
-            for (int s = 0; s < NS; ++s)
-                x[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                    __builtin_bit_cast(h8_t, sm.k[buf][sm.k_at(kb * 32 + col, 2 * s + half)]), qf[s], x[kb], 0, 0, 0);
-        }
-        const int key0 = t * QT + half * 4;         // element i of x[kb]: key0 + 32 kb + 8 (i / 4) + i % 4
-        if (masked) {
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+                x[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds_read(k_get + s * 32 + kb * 32 * SM::K_ROW + buf), qf[s], x[kb], 0,
+                                                               0, 0);
+        // element i of x[kb] is of key 32 kb + 8 (i / 4) + i % 4 from here; `vis` is the row's limit from here
+        const int vis = qr.vis - (t * QT + half * 4);
+        if constexpr (MASKED) {
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    x[kb][i] = key0 + 32 * kb + 8 * (i / 4) + i % 4 < qr.vis ? x[kb][i] * f[2 * kb + i / 8] : -INFINITY;
+                for (int i = 0; i < 16; ++i) x[kb][i] = 32 * kb + 8 * (i / 4) + i % 4 < vis ? x[kb][i] * f[2 * kb + i / 8] : -INFINITY;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) f[c] = 1.f;
+            for (int c = 0; c < 4; ++c) {
+                f[c] = 1.f;
+                vsc[c] = t * QT + c * 16 < len ? vsc[c] : 0.f;
+            }
         }
         float top = -INFINITY, vmax = 0.f;
 #pragma unroll
@@ -1052,7 +1070,6 @@ __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> 
 #pragma unroll
             for (int i = 1; i < 8; ++i) y = fmaxf(y, x[c >> 1][8 * (c & 1) + i]);
             top = fmaxf(top, y * f[c]);
-            vsc[c] = t * QT + c * 16 < len ? vsc[c] : 0.f;
             vmax = fmaxf(vmax, vsc[c]);
         }
         {
@@ -1079,33 +1096,38 @@ __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> 
                 p[i] = exp2_hw(fmaf(x[c >> 1][8 * (c & 1) + i], f[c], -mz));
                 part += p[i];
                 p[i] *= w;
+                // a masked weight is 0 whatever the scale is
+                if constexpr (MASKED) p[i] = 16 * c + 8 * (i / 4) + i % 4 < vis ? p[i] : 0.f;
             }
             sum += part;
-            if (masked) {      // a masked weight is 0 whatever the scale is
-#pragma unroll
-                for (int i = 0; i < 8; ++i) p[i] = key0 + 16 * c + 8 * (i / 4) + i % 4 < qr.vis ? p[i] : 0.f;
-            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const _Float16 hi = (_Float16)p[i];
-                ph[c][i] = hi;
-                if constexpr (F32) pl[c][i] = (_Float16)(p[i] - (float)hi);
+                ph[c][i] = (_Float16)p[i];
+                if constexpr (F32) pl[c][i] = (_Float16)(p[i] - (float)ph[c][i]);
             }
         }
         if (t + 1 < t_end) {
-            store(t + 1);
+            store(t + 1, other);
             if (t + 2 < t_end) load(t + 2);
         }
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                const h8_t v = __builtin_bit_cast(h8_t, sm.v[buf][sm.v_at(dt * 32 + col, 2 * c + half)]);
+                const h8_t v = lds_read(v_get + c * 32 + dt * 32 * SM::V_ROW + buf);
                 o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, ph[c], o[dt], 0, 0, 0);
                 if constexpr (F32) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pl[c], o[dt], 0, 0, 0);
             }
         __syncthreads();
+    };
+    // tiles that every row sees, in pairs; then the others
+    const int t_full = min(t_end, full / QT);
+    int t = ta;
+    for (; t + 2 <= t_full; t += 2) {
+        round(t, std::integral_constant<unsigned, 0>{}, std::false_type{});
+        round(t + 1, std::integral_constant<unsigned, SM::BUF>{}, std::false_type{});
     }
+    for (; t < t_end; ++t) round(t, (t - ta) & 1 ? SM::BUF : 0u, std::true_type{});
     sum += __shfl_xor(sum, 32);
     if (qr.vis < 0) return;
     // element i of o[dt]: dimension 32 dt + 8 (i / 4) + 4 half + i % 4 of row col
