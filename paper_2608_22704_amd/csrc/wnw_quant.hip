@@ -382,6 +382,18 @@ __device__ inline QuantSeq quant_seq(const QuantAttend &a, int b)
     return q;
 }
 
+__device__ inline unsigned uniform(unsigned v)
+{
+    return (unsigned)__builtin_amdgcn_readfirstlane((int)v);
+}
+__device__ inline float lane_f(float v, int lane)
+{
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+}
+__device__ inline unsigned lane_of(unsigned v, int lane)
+{
+    return (unsigned)__builtin_amdgcn_readlane((int)v, lane);
+}
 // Inclusive scans over the wavefront's lanes by data-parallel moves: within rows of sixteen lanes, then across them.
 template <typename F>
 __device__ inline unsigned wave_scan_by(unsigned v, F f)
@@ -405,6 +417,29 @@ __device__ inline unsigned wave_max(unsigned v)
 {
     return (unsigned)__builtin_amdgcn_readlane((int)wave_scan_by(v, [](unsigned a, unsigned b) { return max(a, b); }), 63);
 }
+// Over the wavefront's lanes, for every lane.
+__device__ inline float wave_maxf(float v)
+{
+    auto step = [&](int u) { v = fmaxf(v, __int_as_float(u)); };
+    step(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), 0x111, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), 0x112, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), 0x114, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), 0x118, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), 0x142, 0xa, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), 0x143, 0xc, 0xf, false));
+    return lane_f(v, 63);
+}
+__device__ inline float wave_sumf(float v)
+{
+    auto step = [&](int u) { v += __int_as_float(u); };
+    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x111, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x112, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x114, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x118, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x142, 0xa, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x143, 0xc, 0xf, false));
+    return lane_f(v, 63);
+}
 // f(x of this lane, x of lane ^ 16), and the same with lane ^ 32.
 template <typename F>
 __device__ inline float across_quarters(float x, F f)
@@ -422,15 +457,6 @@ __device__ inline float quarters_sum(float x)
 {
     return across_quarters(x, [](float a, float b) { return a + b; });
 }
-__device__ inline unsigned uniform(unsigned v)
-{
-    return (unsigned)__builtin_amdgcn_readfirstlane((int)v);
-}
-__device__ inline unsigned lane_of(unsigned v, int lane)
-{
-    return (unsigned)__builtin_amdgcn_readlane((int)v, lane);
-}
-
 // How a batch is shared; every wavefront finds out by itself (lane i has the sequences i, i + 64, ...).
 struct QuantShare {
     int heads, lane;
@@ -1177,61 +1203,68 @@ __global__ __launch_bounds__(Q_THREADS, 2) void quant_wide_kernel(QuantAttend a)
     }
 }
 
-// One work-group per output row: joins the pieces of its cache, and makes the tiles' block sums shares of the whole.
+// Joins the pieces of a cache.  Which pieces of the workspace a block of rows has:
+struct QuantPieces {
+    unsigned w0, n;      // first work-group, pieces
+    int RB;
+    __device__ QuantPieces(const QuantAttend &a, const QuantShare &sh, const QuantSeq &sq, int b, unsigned hd, unsigned rb) : RB(a.RB)
+    {
+        const unsigned span = sh.span(sq), s0 = sh.before(a, b) + ((hd - b * sh.heads) * sq.nrb + rb) * span;
+        w0 = sh.per == 1 ? s0 : s0 / sh.per;
+        n = (sh.per == 1 ? s0 + span - 1 : (s0 + span - 1) / sh.per) - w0 + 1;
+    }
+    // row of piece p: slot 1 of its work-group for the first, 0 for the others
+    __device__ size_t at(unsigned p, unsigned r) const { return (size_t)((w0 + p) * 2 + (p == 0)) * RB + r % RB; }
+};
+
+// Single tokens: a work-group per output row.  A lane has a piece's statistics; the wavefronts share the pieces' sums.  Makes
+// the tiles' block sums shares of the whole as well.
 template <int DH, bool BF16>
 __global__ __launch_bounds__(Q_THREADS) void quant_merge_kernel(QuantAttend a)
 {
     constexpr int E = DH / 64;
-    __shared__ float sm_m[4], sm_l[4], sm_o[4][DH];
+    __shared__ float sm_o[4][DH];
     const QuantGeo &g = a.g;
-    const int heads = g.nl * g.H;
-    const unsigned row = blockIdx.x, hq = row / a.n, i = row % a.n, hd = hq / a.G, b = hd / heads;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const unsigned row = blockIdx.x, hd = row / a.G, r = row - hd * a.G;      // n = 1
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = hd / (g.nl * g.H);
     const QuantSeq sq = quant_seq(a, b);
-    if ((int)i >= sq.cnt) return;
-    const unsigned r = i * a.G + hq % a.G;
+    if (sq.cnt == 0) return;
     const QuantShare sh(a, lane);
-    const unsigned span = sh.span(sq), s0 = sh.before(a, b) + ((hd - b * heads) * sq.nrb + r / a.RB) * span;
-    const unsigned w0 = s0 / sh.per, pieces = (s0 + span - 1) / sh.per - w0 + 1;
+    const QuantPieces pc(a, sh, sq, b, hd, r / a.RB);
     float m = -INFINITY, sum = 0.f;
-    if (pieces == 1) {
+    if (pc.n == 1) {
         if (!a.mass) return;
         const float2 ml = a.ws_row[row];
         m = ml.x;
         sum = ml.y;
     } else {
-        // piece p: the work-group w0 + p's slot 1 for the first, 0 for the others
-        auto at = [&](unsigned p) { return (size_t)((w0 + p) * 2 + (p == 0)) * a.RB + r % a.RB; };
-        for (unsigned p = wave; p < pieces; p += 4) m = fmaxf(m, a.ws_ml[at(p)].x);
+        for (unsigned p0 = 0; p0 < pc.n; p0 += 64)
+            if (p0 + lane < pc.n) m = fmaxf(m, a.ws_ml[pc.at(p0 + lane, r)].x);
+        m = wave_maxf(m);
         const float mz = finite_or_zero(m);
         float x[E] = {};
+        for (unsigned p0 = 0; p0 < pc.n; p0 += 64) {
+            float f = 0.f;
+            if (p0 + lane < pc.n) {
+                const float2 ml = a.ws_ml[pc.at(p0 + lane, r)];
+                if (ml.y != 0.f) f = exp2f(ml.x - mz);         // 0: the piece saw nothing
+                sum += f * ml.y;
+            }
+            const int n = (int)min(64u, pc.n - p0);
 #pragma unroll 4
-        for (unsigned p = wave; p < pieces; p += 4) {
-            const float2 ml = a.ws_ml[at(p)];
-            const float f = ml.y == 0.f ? 0.f : exp2f(ml.x - mz);    // 0: saw nothing
-            sum += f * ml.y;
+            for (int p = wave; p < n; p += 4) {
+                const float fp = lane_f(f, p);
+                const float *o = a.ws_o + pc.at(p0 + p, r) * DH + lane * E;
 #pragma unroll
-            for (int e = 0; e < E; ++e) x[e] += f * a.ws_o[at(p) * DH + lane * E + e];
+                for (int e = 0; e < E; ++e) x[e] += fp * o[e];
+            }
         }
+        sum = wave_sumf(sum);
 #pragma unroll
         for (int e = 0; e < E; ++e) sm_o[wave][lane * E + e] = x[e];
-        if (lane == 0) {
-            sm_m[wave] = m;
-            sm_l[wave] = sum;
-        }
         __syncthreads();
-        float mm = -INFINITY, y = 0.f;
-        for (int w = 0; w < 4; ++w) mm = fmaxf(mm, sm_m[w]);
-        sum = 0.f;
-        for (int w = 0; w < 4; ++w) {
-            if (sm_l[w] == 0.f) continue;
-            const float f = exp2f(sm_m[w] - finite_or_zero(mm));
-            sum += f * sm_l[w];
-            if (tid < DH) y += f * sm_o[w][tid];
-        }
-        m = mm;
         if (tid < DH) {
-            y *= sum == 0.f ? 0.f : 1.f / sum;
+            const float y = ((sm_o[0][tid] + sm_o[1][tid]) + (sm_o[2][tid] + sm_o[3][tid])) * (sum == 0.f ? 0.f : 1.f / sum);
             if constexpr (BF16)
                 ((uint16_t *)a.out)[(size_t)row * DH + tid] = to_bf16(y);
             else
@@ -1246,6 +1279,41 @@ __global__ __launch_bounds__(Q_THREADS) void quant_merge_kernel(QuantAttend a)
         const float *mt = a.ws_m + (size_t)row * (g.cap / QT);
         for (int j = tid; j < blocks; j += Q_THREADS) to[j] = j < live ? to[j] * (exp2f(mt[j >> tsh] - mz) * inv) : 0.f;
     }
+}
+
+// Several tokens: a work-group per 16 rows of a head, sixteen threads a row.
+template <int DH, bool BF16>
+__global__ __launch_bounds__(Q_THREADS) void quant_merge_rows_kernel(QuantAttend a)
+{
+    constexpr int E = DH / 16;
+    const unsigned groups = (a.R + 15) / 16, hd = blockIdx.x / groups, r0 = (blockIdx.x - hd * groups) * 16;
+    const int b = hd / (a.g.nl * a.g.H);
+    const QuantSeq sq = quant_seq(a, b);
+    if ((int)r0 >= sq.cnt * a.G) return;
+    const QuantShare sh(a, threadIdx.x & 63);
+    const QuantPieces pc(a, sh, sq, b, hd, r0 / a.RB);
+    const unsigned r = r0 + (threadIdx.x >> 4), d0 = (threadIdx.x & 15) * E;
+    const QuantRow qr = quant_row(a, hd, r, sq.len, sq.cnt);
+    if (pc.n == 1 || qr.vis < 0) return;
+    float m = -INFINITY, sum = 0.f, x[E] = {};
+#pragma unroll 4
+    for (unsigned p = 0; p < pc.n; ++p) m = fmaxf(m, a.ws_ml[pc.at(p, r)].x);
+    const float mz = finite_or_zero(m);
+#pragma unroll 2
+    for (unsigned p = 0; p < pc.n; ++p) {
+        const float2 ml = a.ws_ml[pc.at(p, r)];
+        const float f = ml.y == 0.f ? 0.f : exp2f(ml.x - mz);
+        sum += f * ml.y;
+        float o[E];
+        __builtin_memcpy(o, __builtin_assume_aligned(a.ws_o + pc.at(p, r) * DH + d0, 16), sizeof(o));
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] += f * o[e];
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] *= inv;
+    store_row<E, BF16>(a.out, (size_t)qr.row_of * DH + d0, x);
+    if (a.lse && d0 == 0) a.lse[qr.row_of] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * Q_LN2;
 }
 
 // ---- host ------------------------------------------------------------------------------------
@@ -1467,9 +1535,12 @@ wnw_status wnw_quant_attend(const wnw_quant_config *cfg, const wnw_quant_cache *
         constexpr int DH = decltype(d)::value, FMT = decltype(f)::value;
         bf16 ? launch_token<DH, FMT, false>(p, a, (hipStream_t)hip_stream) : launch_token<DH, FMT, true>(p, a, (hipStream_t)hip_stream);
         // one work-group alone leaves no pieces
-        if (p.W > 1 || mass_dev)
-            hipLaunchKernelGGL((bf16 ? quant_merge_kernel<DH, true> : quant_merge_kernel<DH, false>),
-                               dim3((unsigned)p.rows), dim3(Q_THREADS), 0, (hipStream_t)hip_stream, a);
+        if (n == 1 && (p.W > 1 || mass_dev))
+            hipLaunchKernelGGL((bf16 ? quant_merge_kernel<DH, true> : quant_merge_kernel<DH, false>), dim3((unsigned)p.rows),
+                               dim3(Q_THREADS), 0, (hipStream_t)hip_stream, a);
+        else if (p.W > 1)
+            hipLaunchKernelGGL((bf16 ? quant_merge_rows_kernel<DH, true> : quant_merge_rows_kernel<DH, false>),
+                               dim3((unsigned)(p.rows / R * ((R + 15) / 16))), dim3(Q_THREADS), 0, (hipStream_t)hip_stream, a);
     });
     return quant_hip();
 }
