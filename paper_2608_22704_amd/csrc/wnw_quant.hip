@@ -55,6 +55,67 @@ __device__ inline int q_clamp(int x, int hi)
     return min(max(x, 0), hi);
 }
 
+// ---- lanes -----------------------------------------------------------------------------------
+
+__device__ inline unsigned uniform(unsigned v)
+{
+    return (unsigned)__builtin_amdgcn_readfirstlane((int)v);
+}
+__device__ inline float lane_f(float v, int lane)
+{
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+}
+__device__ inline unsigned lane_of(unsigned v, int lane)
+{
+    return (unsigned)__builtin_amdgcn_readlane((int)v, lane);
+}
+// Inclusive scans over the wavefront's lanes by data-parallel moves: within rows of sixteen lanes, then across them.
+template <typename F>
+__device__ inline unsigned wave_scan_by(unsigned v, F f)
+{
+    v = f(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, false));
+    v = f(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, false));
+    v = f(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, false));
+    v = f(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, false));
+    v = f(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false));
+    return f(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false));
+}
+__device__ inline unsigned wave_scan(unsigned v)
+{
+    return wave_scan_by(v, [](unsigned a, unsigned b) { return a + b; });
+}
+__device__ inline unsigned wave_sum(unsigned v)
+{
+    return (unsigned)__builtin_amdgcn_readlane((int)wave_scan(v), 63);
+}
+__device__ inline unsigned wave_max(unsigned v)
+{
+    return (unsigned)__builtin_amdgcn_readlane((int)wave_scan_by(v, [](unsigned a, unsigned b) { return max(a, b); }), 63);
+}
+// Over the wavefront's lanes, for every lane.
+__device__ inline float wave_maxf(float v)
+{
+    auto step = [&](int u) { v = fmaxf(v, __int_as_float(u)); };
+    step(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), 0x111, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), 0x112, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), 0x114, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), 0x118, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), 0x142, 0xa, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), 0x143, 0xc, 0xf, false));
+    return lane_f(v, 63);
+}
+__device__ inline float wave_sumf(float v)
+{
+    auto step = [&](int u) { v += __int_as_float(u); };
+    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x111, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x112, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x114, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x118, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x142, 0xa, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x143, 0xc, 0xf, false));
+    return lane_f(v, 63);
+}
+
 // ---- numbers ---------------------------------------------------------------------------------
 
 // Scale of a block whose largest magnitude has the (fp32) bits `amax`; NaN if that is not finite.
@@ -111,14 +172,25 @@ __device__ inline float byte_value(unsigned u, int i)
     return __builtin_amdgcn_cvt_f32_fp8((int)(u >> (8 * i)), 0);
 }
 
-// A byte held under scale `was`, rounded again under the larger scale `now`.  int8: quotients that are no tie differ from
-// one by 2^-25 or more, which a double shows.
+// Four bytes held under scale `was`, rounded again under the larger scale `now`.  int8: the fp32 product is off by 2^-16 at
+// most; next to a tie a double decides, as quotients that are no tie differ from one by 2^-25 or more.
 template <int FMT>
-__device__ inline unsigned requant(unsigned byte, float was, float now)
+__device__ inline unsigned requant4(unsigned u, float was, float now, float ratio)
 {
-    const float x = byte_value<FMT>(byte, 0);
-    if constexpr (FMT == WNW_QUANT_INT8) return (unsigned)((int)rint((double)x * (double)was / (double)now) + 128);
-    return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(x * (was / now), 0.f, 0, false) & 255u;
+    if constexpr (FMT == WNW_QUANT_E4M3) {
+        const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(byte_value<FMT>(u, 0) * ratio, byte_value<FMT>(u, 1) * ratio, 0, false);
+        return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(byte_value<FMT>(u, 2) * ratio, byte_value<FMT>(u, 3) * ratio, lo, true);
+    } else {
+        unsigned r = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float x = byte_value<FMT>(u, i), q = x * ratio;
+            float n = rintf(q);
+            if (fabsf(fabsf(q - n) - 0.5f) < 0x1p-14f) n = (float)rint((double)x * (double)was / (double)now);
+            r |= (unsigned)((int)n + 128) << (8 * i);
+        }
+        return r;
+    }
 }
 
 // Four bytes to four fp16, exactly.  int8: 0x64 in front of a byte u is the fp16 number 1024 + u.
@@ -164,6 +236,19 @@ struct QuantTileSmem {
     static __device__ int unit(int d, int h) { return d / E * ROW + d % E * 16 + h * 4; }
 };
 
+// E bf16 that are read once.
+template <int E>
+__device__ inline void load_row(uint16_t (&u)[E], const uint16_t *p)
+{
+    if constexpr (E == 8) {
+        const qu4_t v = __builtin_nontemporal_load((const qu4_t *)p);
+        __builtin_memcpy(u, &v, sizeof(u));
+    } else {
+        const qu2_t v = __builtin_nontemporal_load((const qu2_t *)p);
+        __builtin_memcpy(u, &v, sizeof(u));
+    }
+}
+
 template <int DH, int FMT>
 __global__ __launch_bounds__(Q_THREADS) void quant_write_kernel(QuantGeo g, int n, int tiles, const uint16_t *__restrict__ kn,
                                                                const uint16_t *__restrict__ vn,
@@ -184,14 +269,25 @@ __global__ __launch_bounds__(Q_THREADS) void quant_write_kernel(QuantGeo g, int 
     float *scales = const_cast<float *>(is_v ? g.vs : g.ks) + ((head * g.cap) >> g.bsh);
     const uint16_t *src = (is_v ? vn : kn) + (size_t)hd * n * DH + (size_t)dg * E;
 
+    const int gw = 1 << (g.bsh - 4);                     // wavefronts of a block
+    const int first = row0 + wave / gw * gw * 16;        // the block's first row
+    const bool has_old = first < pos, has_new = first < end && first + gw * 16 > pos;
+    const bool whole = pos <= row0 && end >= row0 + QT;  // the tile has new rows only (uniform)
+    const float was = has_old ? scales[first >> g.bsh] : 0.f;
+    bool put[4], old[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = row0 + rg * 4 + i;
+        put[i] = row >= pos && row < end;
+        old[i] = has_new && row < pos;
+    }
     float x[4][E];
     unsigned amax = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int row = row0 + rg * 4 + i;
-        if (row >= pos && row < end) {
+        if (put[i]) {
             uint16_t u[E];
-            __builtin_memcpy(u, __builtin_assume_aligned(src + (size_t)(row - pos) * DH, E * 2), E * 2);
+            load_row<E>(u, src + (size_t)(row0 + rg * 4 + i - pos) * DH);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 x[i][e] = __uint_as_float((unsigned)u[e] << 16);
@@ -202,12 +298,20 @@ __global__ __launch_bounds__(Q_THREADS) void quant_write_kernel(QuantGeo g, int 
             for (int e = 0; e < E; ++e) x[i][e] = 0.f;
         }
     }
+    // the lane's bytes of earlier rows, in case they are to be rounded again: K's four rows, or V's dwords of four rows
+    unsigned had[E];
+    const bool some_old = !whole && has_new && row0 + rg * 4 < pos;
+    if (some_old) {
+        if (!is_v) {
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) amax = max(amax, (unsigned)__shfl_xor((int)amax, o));
-    const int gw = 1 << (g.bsh - 4);                     // wavefronts of a block
-    const int first = row0 + wave / gw * gw * 16;        // the block's first row
-    const bool has_old = first < pos, has_new = first < end && first + gw * 16 > pos;
-    const float was = has_old ? scales[first >> g.bsh] : 0.f;
+            for (int i = 0; i < 4; ++i)
+                __builtin_memcpy(&had[i * (E / 4)], __builtin_assume_aligned(codes + (size_t)(rg * 4 + i) * DH + dg * E, E), E);
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) had[e] = *((const unsigned *)(codes + (size_t)(dg * E + e) * QT) + (rg & 3) * 4 + (rg >> 2));
+        }
+    }
+    amax = wave_max(amax);
     if (lane == 0) wmax[wave] = amax;
     __syncthreads();
     for (int w = wave / gw * gw; w < wave / gw * gw + gw; ++w) amax = max(amax, wmax[w]);
@@ -216,40 +320,27 @@ __global__ __launch_bounds__(Q_THREADS) void quant_write_kernel(QuantGeo g, int 
     if (has_old) s = was != was || s != s ? __uint_as_float(0x7fc00000u) : fmaxf(was, s);
     const bool good = s == s, grew = has_old && good && s > was;
     if (has_new && lane == 0 && wave % gw == 0) scales[first >> g.bsh] = s;
-    const float inv = 1.f / s;
+    const float inv = 1.f / s, ratio = was * inv;
 
-    bool put[4], old[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int row = row0 + rg * 4 + i;
-        put[i] = row >= pos && row < end;
-        old[i] = has_new && grew && row < pos;
-    }
     constexpr unsigned ZERO = FMT == WNW_QUANT_INT8 ? 0x80808080u : 0u;
     if (!is_v) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            uint8_t *to = codes + (size_t)(rg * 4 + i) * DH + dg * E;
             unsigned w[E / 4];
             if (put[i]) {
 #pragma unroll
                 for (int e = 0; e < E; e += 4)
                     w[e / 4] = good ? quant4<FMT>(x[i][e], x[i][e + 1], x[i][e + 2], x[i][e + 3], s, inv) : ZERO;
-            } else if (old[i]) {
-                __builtin_memcpy(w, __builtin_assume_aligned(to, E), E);
+            } else if (old[i] && grew) {
 #pragma unroll
-                for (int e = 0; e < E; e += 4) {
-                    unsigned r = 0;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) r |= requant<FMT>((w[e / 4] >> (8 * j)) & 255u, was, s) << (8 * j);
-                    w[e / 4] = r;
-                }
+                for (int e = 0; e < E / 4; ++e) w[e] = requant4<FMT>(had[i * (E / 4) + e], was, s, ratio);
             }
-            if (put[i] || old[i]) __builtin_memcpy(__builtin_assume_aligned(to, E), w, E);
+            if (put[i] || (old[i] && grew))
+                __builtin_memcpy(__builtin_assume_aligned(codes + (size_t)(rg * 4 + i) * DH + dg * E, E), w, E);
         }
         return;
     }
-    if (pos <= row0 && end >= row0 + QT) {   // a whole tile of new rows (uniform)
+    if (whole) {
 #pragma unroll
         for (int e = 0; e < E; ++e)
             sm.t[sm.at(dg, e, rg)] = good ? quant4<FMT>(x[0][e], x[1][e], x[2][e], x[3][e], s, inv) : ZERO;
@@ -259,22 +350,25 @@ __global__ __launch_bounds__(Q_THREADS) void quant_write_kernel(QuantGeo g, int 
             *(qu4_t *)(codes + (size_t)u * 16) = *(const qu4_t *)&sm.t[sm.unit(u >> 2, u & 3)];
         return;
     }
+    // a byte of the dword for each row: new, rounded again, or left alone
+    unsigned mask_put = 0, mask_old = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        mask_put |= put[i] ? 255u << (8 * i) : 0u;
+        mask_old |= old[i] && grew ? 255u << (8 * i) : 0u;
+    }
+    if (!(mask_put | mask_old)) return;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         unsigned *to = (unsigned *)(codes + (size_t)(dg * E + e) * QT) + (rg & 3) * 4 + (rg >> 2);
         unsigned w = good ? quant4<FMT>(x[0][e], x[1][e], x[2][e], x[3][e], s, inv) : ZERO;
-        if (put[0] && put[1] && put[2] && put[3])
+        if (mask_old) w = (w & mask_put) | (requant4<FMT>(had[e], was, s, ratio) & mask_old);
+        if ((mask_put | mask_old) == ~0u)
             *to = w;
         else {
-            // rows of the dword that are neither new nor rounded again are left alone
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint8_t *at = (uint8_t *)to + i;
-                if (put[i])
-                    *at = (uint8_t)(w >> (8 * i));
-                else if (old[i])
-                    *at = (uint8_t)requant<FMT>(*at, was, s);
-            }
+            for (int i = 0; i < 4; ++i)
+                if ((mask_put | mask_old) >> (8 * i) & 255u) *((uint8_t *)to + i) = (uint8_t)(w >> (8 * i));
         }
     }
 }
@@ -382,64 +476,6 @@ __device__ inline QuantSeq quant_seq(const QuantAttend &a, int b)
     return q;
 }
 
-__device__ inline unsigned uniform(unsigned v)
-{
-    return (unsigned)__builtin_amdgcn_readfirstlane((int)v);
-}
-__device__ inline float lane_f(float v, int lane)
-{
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
-}
-__device__ inline unsigned lane_of(unsigned v, int lane)
-{
-    return (unsigned)__builtin_amdgcn_readlane((int)v, lane);
-}
-// Inclusive scans over the wavefront's lanes by data-parallel moves: within rows of sixteen lanes, then across them.
-template <typename F>
-__device__ inline unsigned wave_scan_by(unsigned v, F f)
-{
-    v = f(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, false));
-    v = f(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, false));
-    v = f(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, false));
-    v = f(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, false));
-    v = f(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false));
-    return f(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false));
-}
-__device__ inline unsigned wave_scan(unsigned v)
-{
-    return wave_scan_by(v, [](unsigned a, unsigned b) { return a + b; });
-}
-__device__ inline unsigned wave_sum(unsigned v)
-{
-    return (unsigned)__builtin_amdgcn_readlane((int)wave_scan(v), 63);
-}
-__device__ inline unsigned wave_max(unsigned v)
-{
-    return (unsigned)__builtin_amdgcn_readlane((int)wave_scan_by(v, [](unsigned a, unsigned b) { return max(a, b); }), 63);
-}
-// Over the wavefront's lanes, for every lane.
-__device__ inline float wave_maxf(float v)
-{
-    auto step = [&](int u) { v = fmaxf(v, __int_as_float(u)); };
-    step(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), 0x111, 0xf, 0xf, false));
-    step(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), 0x112, 0xf, 0xf, false));
-    step(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), 0x114, 0xf, 0xf, false));
-    step(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), 0x118, 0xf, 0xf, false));
-    step(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), 0x142, 0xa, 0xf, false));
-    step(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), 0x143, 0xc, 0xf, false));
-    return lane_f(v, 63);
-}
-__device__ inline float wave_sumf(float v)
-{
-    auto step = [&](int u) { v += __int_as_float(u); };
-    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x111, 0xf, 0xf, false));
-    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x112, 0xf, 0xf, false));
-    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x114, 0xf, 0xf, false));
-    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x118, 0xf, 0xf, false));
-    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x142, 0xa, 0xf, false));
-    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x143, 0xc, 0xf, false));
-    return lane_f(v, 63);
-}
 // f(x of this lane, x of lane ^ 16), and the same with lane ^ 32.
 template <typename F>
 __device__ inline float across_quarters(float x, F f)

@@ -75,6 +75,7 @@ def _load():
         raise ImportError(f"{LIB_PATH} is missing: build the HIP library first (__graft_entry__.build())")
     lib = C.CDLL(LIB_PATH)
     P, I32, I64, SZ = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
+    QC, QK = C.POINTER(wnw_quant_config), C.POINTER(wnw_quant_cache)
     sig = {
         "wnw_init_cache": ([C.POINTER(wnw_config), P, P, P, C.POINTER(P)], C.c_int),
         "wnw_set_roles": ([P, P, P], C.c_int),
@@ -86,10 +87,10 @@ def _load():
         "wnw_key_sensitivity": ([I32, I32, I32, I32, P, P, P], C.c_int),
         "wnw_triage": ([I32, I32, I32, I32, P, P, I32, P, I32, I32, P, P, P, P], C.c_int),
         "wnw_triage_last_error": ([], C.c_char_p),
-        "wnw_quant_write": ([P, P, I32, I32, I32, P, P, P, P, P], C.c_int),
-        "wnw_quant_read": ([P, P, I32, I32, I32, P, P, P, P, P], C.c_int),
-        "wnw_quant_attend": ([P, P, I32, I32, I32, I32, P, P, P, P, P, P, I32, P, SZ, P], C.c_int),
-        "wnw_quant_attend_workspace": ([P, I32, I32, I32, I32, C.POINTER(SZ)], C.c_int),
+        "wnw_quant_write": ([QC, QK, I32, I32, I32, P, P, P, P, P], C.c_int),
+        "wnw_quant_read": ([QC, QK, I32, I32, I32, P, P, P, P, P], C.c_int),
+        "wnw_quant_attend": ([QC, QK, I32, I32, I32, I32, P, P, P, P, P, P, I32, P, SZ, P], C.c_int),
+        "wnw_quant_attend_workspace": ([QC, I32, I32, I32, I32, C.POINTER(SZ)], C.c_int),
         "wnw_quant_last_error": ([], C.c_char_p),
         "wnw_set_roles_device": ([P, P, P], C.c_int),
         "wnw_query_head_keep": ([P, P], C.c_int),
@@ -133,8 +134,6 @@ def _ptr(t):
 
 # element sizes the library reads or writes: bf16 bit patterns (any 2-byte dtype), fp32, int32, bytes
 _BF16, _F32, _I32, _U8 = "bf16", "f32", "i32", "u8"
-_NAME = {_BF16: ("torch.bfloat16", "torch.int16", "torch.uint16"), _F32: ("torch.float32",), _I32: ("torch.int32",),
-         _U8: ("torch.uint8",)}
 
 
 def _dev(t, kind, numel=None, what="tensor"):
@@ -262,12 +261,19 @@ class QuantCache:
     def __init__(self, k, v, k_scale, v_scale):
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
 
+    def __setattr__(self, name, t):
+        # checked once here, for calls that are made for every layer and token
+        _on(t.get_device(), t, _dtypes()[_F32 if name.endswith("scale") else _U8], None, name)
+        object.__setattr__(self, name, t)
+
     def _struct(self, cfg, device):
         n = cfg.batch * cfg.layers * cfg.kv_heads * cfg.capacity
-        scales, n = n // max(cfg.block, 1), n * cfg.head_dim
-        return wnw_quant_cache(_on(device, self.k, _U8, n, "k"), _on(device, self.v, _U8, n, "v"),
-                               _on(device, self.k_scale, _F32, scales, "k_scale"),
-                               _on(device, self.v_scale, _F32, scales, "v_scale"))
+        need = (n * cfg.head_dim, n * cfg.head_dim, n // max(cfg.block, 1), n // max(cfg.block, 1))
+        tensors = (self.k, self.v, self.k_scale, self.v_scale)
+        for t, numel, what in zip(tensors, need, ("k", "v", "k_scale", "v_scale")):
+            if t.get_device() != device or t.numel() < numel:
+                raise ValueError(f"{what}: needs {numel} elements on cuda:{device}, got {t.numel()} on {t.device}")
+        return wnw_quant_cache(*[t.data_ptr() for t in tensors])
 
 
 def make_quant_config(batch, layers, kv_heads, capacity, block, format, head_dim=128, flags=0) -> wnw_quant_config:
@@ -288,15 +294,27 @@ def _qcheck(status):
         raise WnwError(status, lib.wnw_quant_last_error().decode())
 
 
-def _on(device, t, kind, numel, what):
+_DTYPES = {}
+
+
+def _dtypes():
+    """Element kind -> the torch types that the calls below take for it."""
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({_BF16: (torch.bfloat16, torch.int16, torch.uint16), _F32: (torch.float32,), _I32: (torch.int32,),
+                        _U8: (torch.uint8,)})
+    return _DTYPES
+
+
+def _on(device, t, kinds, numel, what):
     """Address of a tensor that must be on the GPU `device` (its index), where the call's work runs, with the checks of
     _dev(); half precision is not taken for bf16.  These calls are made for every layer and token: no detours."""
     if t is None or isinstance(t, int):
         return t
     if t.get_device() != device:
         raise ValueError(f"{what} is on {t.device}, the call's work on cuda:{device}")
-    if str(t.dtype) not in _NAME[kind]:
-        raise TypeError(f"{what}: expected {kind} elements, got {t.dtype}")
+    if t.dtype not in kinds:
+        raise TypeError(f"{what}: expected {' or '.join(map(str, kinds))}, got {t.dtype}")
     if not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous")
     if numel is not None and t.numel() < numel:
@@ -306,9 +324,10 @@ def _on(device, t, kind, numel, what):
 
 def _quant_shape(cfg, t, heads, what):
     """(layers, tokens) of rows [B][n_layers][heads][n][d]."""
-    if t.dim() != 5 or t.shape[0] != cfg.batch or t.shape[2] != heads or t.shape[4] != cfg.head_dim:
-        raise ValueError(f"{what}: expected [{cfg.batch}][n_layers][{heads}][n][{cfg.head_dim}], got {list(t.shape)}")
-    return t.shape[1], t.shape[3]
+    shape = t.shape
+    if len(shape) != 5 or shape[0] != cfg.batch or shape[2] != heads or shape[4] != cfg.head_dim:
+        raise ValueError(f"{what}: expected [{cfg.batch}][n_layers][{heads}][n][{cfg.head_dim}], got {list(shape)}")
+    return shape[1], shape[3]
 
 
 def _quant_device():
@@ -322,11 +341,10 @@ def wnw_quant_write(cfg, cache, k_dev, v_dev, pos_dev, count_dev=None, first_lay
     nl, n = _quant_shape(cfg, k_dev, cfg.kv_heads, "k_dev")
     if v_dev.shape != k_dev.shape:
         raise ValueError(f"v_dev: expected {list(k_dev.shape)}, got {list(v_dev.shape)}")
-    dev = _quant_device()
-    _qcheck(lib.wnw_quant_write(C.byref(cfg), C.byref(cache._struct(cfg, dev)), first_layer, nl, n,
-                                _on(dev, k_dev, _BF16, None, "k_dev"), _on(dev, v_dev, _BF16, None, "v_dev"),
-                                _on(dev, pos_dev, _I32, cfg.batch, "pos_dev"), _on(dev, count_dev, _I32, cfg.batch, "count_dev"),
-                                _stream(stream)))
+    dev, k, B = _quant_device(), _dtypes(), cfg.batch
+    _qcheck(lib.wnw_quant_write(cfg, cache._struct(cfg, dev), first_layer, nl, n, _on(dev, k_dev, k[_BF16], None, "k_dev"),
+                                _on(dev, v_dev, k[_BF16], None, "v_dev"), _on(dev, pos_dev, k[_I32], B, "pos_dev"),
+                                _on(dev, count_dev, k[_I32], B, "count_dev"), _stream(stream)))
 
 
 def wnw_quant_read(cfg, cache, k_out, v_out, pos_dev, count_dev=None, first_layer=0, stream=None):
@@ -338,17 +356,17 @@ def wnw_quant_read(cfg, cache, k_out, v_out, pos_dev, count_dev=None, first_laye
     nl, n = _quant_shape(cfg, some, cfg.kv_heads, "k_out" if k_out is not None else "v_out")
     if v_out is not None and v_out.shape != some.shape:
         raise ValueError(f"v_out: expected {list(some.shape)}, got {list(v_out.shape)}")
-    dev, kind = _quant_device(), _BF16 if cfg.flags & WNW_F_OUT_BF16 else _F32
-    _qcheck(lib.wnw_quant_read(C.byref(cfg), C.byref(cache._struct(cfg, dev)), first_layer, nl, n,
-                               _on(dev, k_out, kind, None, "k_out"), _on(dev, v_out, kind, None, "v_out"),
-                               _on(dev, pos_dev, _I32, cfg.batch, "pos_dev"), _on(dev, count_dev, _I32, cfg.batch, "count_dev"),
-                               _stream(stream)))
+    dev, k, B = _quant_device(), _dtypes(), cfg.batch
+    out = k[_BF16 if cfg.flags & WNW_F_OUT_BF16 else _F32]
+    _qcheck(lib.wnw_quant_read(cfg, cache._struct(cfg, dev), first_layer, nl, n, _on(dev, k_out, out, None, "k_out"),
+                               _on(dev, v_out, out, None, "v_out"), _on(dev, pos_dev, k[_I32], B, "pos_dev"),
+                               _on(dev, count_dev, k[_I32], B, "count_dev"), _stream(stream)))
 
 
 def wnw_quant_attend_workspace(cfg, n_layers, q_heads, n, max_len=0) -> int:
     """Bytes of workspace that wnw_quant_attend needs for these sizes."""
     need = C.c_size_t()
-    _qcheck(lib.wnw_quant_attend_workspace(C.byref(cfg), n_layers, q_heads, n, max_len, C.byref(need)))
+    _qcheck(lib.wnw_quant_attend_workspace(cfg, n_layers, q_heads, n, max_len, C.byref(need)))
     return need.value
 
 
@@ -357,18 +375,20 @@ def wnw_quant_attend(cfg, cache, q_dev, out_dev, len_dev, count_dev=None, lse_de
     """q_dev bf16 [B][n_layers][H_q][n][d] -> out_dev (same shape, fp32 or bf16), lse_dev fp32 [B][n_layers][H_q][n],
     mass_dev fp32 [B][n_layers][H_q][capacity / block] (n = 1); workspace: a uint8 tensor of
     wnw_quant_attend_workspace() bytes or more."""
-    Hq = q_dev.shape[2] if q_dev.dim() == 5 else 0
+    shape = q_dev.shape
+    Hq = shape[2] if len(shape) == 5 else 0
     nl, n = _quant_shape(cfg, q_dev, Hq, "q_dev")
-    if out_dev.shape != q_dev.shape:
-        raise ValueError(f"out_dev: expected {list(q_dev.shape)}, got {list(out_dev.shape)}")
-    dev, rows = _quant_device(), cfg.batch * nl * Hq
+    if out_dev.shape != shape:
+        raise ValueError(f"out_dev: expected {list(shape)}, got {list(out_dev.shape)}")
+    dev, k, B = _quant_device(), _dtypes(), cfg.batch
+    rows = B * nl * Hq
     _qcheck(lib.wnw_quant_attend(
-        C.byref(cfg), C.byref(cache._struct(cfg, dev)), first_layer, nl, Hq, n, _on(dev, q_dev, _BF16, None, "q_dev"),
-        _on(dev, len_dev, _I32, cfg.batch, "len_dev"), _on(dev, count_dev, _I32, cfg.batch, "count_dev"),
-        _on(dev, out_dev, _BF16 if cfg.flags & WNW_F_OUT_BF16 else _F32, None, "out_dev"),
-        _on(dev, lse_dev, _F32, rows * n, "lse_dev"),
-        _on(dev, mass_dev, _F32, rows * (cfg.capacity // max(cfg.block, 1)), "mass_dev"), max_len,
-        _on(dev, workspace, _U8, None, "workspace"), 0 if workspace is None else workspace.numel(), _stream(stream)))
+        cfg, cache._struct(cfg, dev), first_layer, nl, Hq, n, _on(dev, q_dev, k[_BF16], None, "q_dev"),
+        _on(dev, len_dev, k[_I32], B, "len_dev"), _on(dev, count_dev, k[_I32], B, "count_dev"),
+        _on(dev, out_dev, k[_BF16 if cfg.flags & WNW_F_OUT_BF16 else _F32], None, "out_dev"),
+        _on(dev, lse_dev, k[_F32], rows * n, "lse_dev"),
+        _on(dev, mass_dev, k[_F32], rows * (cfg.capacity // max(cfg.block, 1)), "mass_dev"), max_len,
+        _on(dev, workspace, k[_U8], None, "workspace"), 0 if workspace is None else workspace.numel(), _stream(stream)))
 
 
 def wnw_append_kv(ctx, k_new_dev, v_new_dev, stream=None):

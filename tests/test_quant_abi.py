@@ -138,7 +138,9 @@ def test_binding_refuses_buffers(W):
     assert c.v.shape == (1, 1, 1, 1, 128, 64) and c.k_scale.shape == (1, 1, 1, 2)
     x = torch.zeros((1, 1, 1, 2, 128), dtype=torch.bfloat16)
     with pytest.raises(ValueError):
-        W._on(torch.device("cuda", 0), x, W._BF16, None, "x")
+        W._on(0, x, W._dtypes()[W._BF16], None, "x")
+    with pytest.raises(TypeError):          # half precision is no bf16
+        W._on(-1, x.half(), W._dtypes()[W._BF16], None, "x")
     for bad in (x[0], x[..., :64], x.expand(2, 1, 1, 2, 128)):
         with pytest.raises(ValueError):
             W._quant_shape(cfg, bad, 1, "x")
