@@ -298,15 +298,19 @@ __global__ __launch_bounds__(Q_THREADS) void quant_write_kernel(QuantGeo g, int 
             for (int e = 0; e < E; ++e) x[i][e] = 0.f;
         }
     }
-    // the lane's bytes of earlier rows, in case they are to be rounded again: K's four rows, or V's dwords of four rows
-    unsigned had[E];
-    const bool some_old = !whole && has_new && row0 + rg * 4 < pos;
-    if (some_old) {
+    // The lane's bytes of earlier rows, in case they are to be rounded again: K's four rows, or V's dwords of four rows (of
+    // one scale block), which are also what a dword with some new rows keeps.
+    unsigned had[E] = {};
+    const bool some_old = has_new && row0 + rg * 4 < pos, some_new = put[0] || put[1] || put[2] || put[3],
+               all_new = put[0] && put[1] && put[2] && put[3];
+    if (!whole) {
         if (!is_v) {
+            if (some_old) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                __builtin_memcpy(&had[i * (E / 4)], __builtin_assume_aligned(codes + (size_t)(rg * 4 + i) * DH + dg * E, E), E);
-        } else {
+                for (int i = 0; i < 4; ++i)
+                    __builtin_memcpy(&had[i * (E / 4)], __builtin_assume_aligned(codes + (size_t)(rg * 4 + i) * DH + dg * E, E), E);
+            }
+        } else if (some_old || (some_new && !all_new)) {
 #pragma unroll
             for (int e = 0; e < E; ++e) had[e] = *((const unsigned *)(codes + (size_t)(dg * E + e) * QT) + (rg & 3) * 4 + (rg >> 2));
         }
@@ -350,7 +354,7 @@ __global__ __launch_bounds__(Q_THREADS) void quant_write_kernel(QuantGeo g, int 
             *(qu4_t *)(codes + (size_t)u * 16) = *(const qu4_t *)&sm.t[sm.unit(u >> 2, u & 3)];
         return;
     }
-    // a byte of the dword for each row: new, rounded again, or left alone
+    // the dword's bytes: new, rounded again, or as they were
     unsigned mask_put = 0, mask_old = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -360,16 +364,10 @@ __global__ __launch_bounds__(Q_THREADS) void quant_write_kernel(QuantGeo g, int 
     if (!(mask_put | mask_old)) return;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        unsigned *to = (unsigned *)(codes + (size_t)(dg * E + e) * QT) + (rg & 3) * 4 + (rg >> 2);
-        unsigned w = good ? quant4<FMT>(x[0][e], x[1][e], x[2][e], x[3][e], s, inv) : ZERO;
-        if (mask_old) w = (w & mask_put) | (requant4<FMT>(had[e], was, s, ratio) & mask_old);
-        if ((mask_put | mask_old) == ~0u)
-            *to = w;
-        else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if ((mask_put | mask_old) >> (8 * i) & 255u) *((uint8_t *)to + i) = (uint8_t)(w >> (8 * i));
-        }
+        unsigned w = had[e];
+        if (mask_old) w = (w & ~mask_old) | (requant4<FMT>(w, was, s, ratio) & mask_old);
+        if (mask_put) w = (w & ~mask_put) | ((good ? quant4<FMT>(x[0][e], x[1][e], x[2][e], x[3][e], s, inv) : ZERO) & mask_put);
+        *((unsigned *)(codes + (size_t)(dg * E + e) * QT) + (rg & 3) * 4 + (rg >> 2)) = w;
     }
 }
 
