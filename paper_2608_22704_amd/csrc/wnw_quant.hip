@@ -466,6 +466,8 @@ struct QuantAttend {
     QuantGeo g;
     int G, n, R;               // q-heads per KV-head, tokens, rows G * n of a KV-head: row r is token r / G, q-head r % G
     int W, RB;                 // work-groups that share the batch's tiles, rows of a block
+    int nrb;                   // > 0: a work-group per block of rows, nrb blocks a head, nothing to join
+    float inv_w;               // 1 / W
     const uint16_t *q;
     const int32_t *len, *count;
     void *out;
@@ -477,6 +479,15 @@ struct QuantAttend {
     float scale;               // log2(e) / sqrt(d)
 };
 
+// The kernel's arguments once more, as memory: what only its last part needs is loaded there, and does not take scalar
+// registers from the start (fetching instructions is what a short call waits for, and spills are instructions).
+__device__ inline const QuantAttend &late_args()
+{
+    auto *p = (const __attribute__((address_space(4))) QuantAttend *)__builtin_amdgcn_kernarg_segment_ptr();
+    __asm__ volatile("" : "+s"(p));
+    return *(const QuantAttend *)p;
+}
+
 // Work of a batch: every block of RB query rows of every head has its sequence's tiles (one at least, so that an
 // empty sequence's outputs are written).  W work-groups share them, whatever the lengths are, in one of two ways:
 //   pieces  a block's tiles are cut into pieces of at most `pp` tiles, a work-group each;
@@ -484,9 +495,24 @@ struct QuantAttend {
 //           work-group's part may end one block and begin another.
 // The line is even, but a second block costs a work-group about PIECE_COST tiles' time again (its queries, first tiles and
 // the join of its wavefronts).  A block that is not whole leaves its result in the workspace, in the work-group's slot 1
-// (its first tiles) or 0 (later ones), and quant_merge_kernel joins those.
+// (its first tiles) or 0 (later ones), and a second kernel joins those.  With nrb > 0 there is none of this: every block has its
+// own work-group.
 constexpr int MIN_PIECE = 4;    // tiles of a piece at least, one per wavefront
 constexpr int PIECE_COST = 10;
+
+// a / b for 0 <= a < 2^24 and b > 0
+__device__ inline int div24(int a, int b)
+{
+    int q = (int)((float)a * __builtin_amdgcn_rcpf((float)b));
+    const int r = a - q * b;
+    q += r >= b ? 1 : 0;
+    return q - (r < 0 ? 1 : 0);
+}
+// At least x / y, given inv = 1 / y rounded, and the same in every kernel.
+__device__ inline unsigned at_least(unsigned x, float inv)
+{
+    return (unsigned)__fmul_rn(__fmul_rn((float)x, inv), 1.000001f) + 1;
+}
 
 struct QuantSeq {
     int len, cnt, tiles, nrb;   // rows, tokens of this call, tiles and blocks of rows of a head (0: none)
@@ -530,11 +556,12 @@ struct QuantShare {
 
     __device__ QuantSeq seq(const QuantAttend &a, int b0) const { return b0 == 0 ? mine : quant_seq(a, b0 + lane); }
     // items of a block of rows
-    __device__ unsigned span(const QuantSeq &q) const { return pp ? (unsigned)((q.tiles + pp - 1) / pp) : (unsigned)q.tiles; }
+    __device__ unsigned span(const QuantSeq &q) const { return pp ? (unsigned)div24(q.tiles + pp - 1, pp) : (unsigned)q.tiles; }
     __device__ unsigned work(const QuantSeq &q) const { return span(q) * (unsigned)(q.nrb * heads); }
 
-    __device__ QuantShare(const QuantAttend &a, int lane_) : heads(a.g.nl * a.g.H), lane(lane_), pp(0)
+    __device__ void init(const QuantAttend &a, int lane_)
     {
+        heads = a.g.nl * a.g.H, lane = lane_, pp = 0;
         mine = quant_seq(a, lane);
         unsigned t = 0, units = 0, most = 0;
         for (int b0 = 0; b0 < a.g.B; b0 += 64) {
@@ -545,11 +572,11 @@ struct QuantShare {
         }
         t = wave_sum(t), units = wave_sum(units), most = wave_max(most);
         total = t;
-        per = max((t + a.W - 1) / a.W, (unsigned)MIN_PIECE);
+        per = max(at_least(t, a.inv_w), (unsigned)MIN_PIECE);
         if (units < (unsigned)a.W) {
             // pieces of at most p tiles are at most t / p + units
-            const unsigned p = min(max((t + a.W - units - 1) / (a.W - units), (unsigned)MIN_PIECE), most);
-            if (p && (most + (most + p - 1) / p - 1) / ((most + p - 1) / p) <= per + PIECE_COST) {
+            const unsigned p = min(max(at_least(t, __builtin_amdgcn_rcpf((float)(a.W - units))), (unsigned)MIN_PIECE), most);
+            if (p && piece_len((int)most, (int)p) <= (int)per + PIECE_COST) {
                 pp = (int)p;
                 per = 1;
                 t = 0;
@@ -582,12 +609,11 @@ struct QuantShare {
         for (int b0 = 0; b0 < end; b0 += 64) t += b0 + lane < end ? work(seq(a, b0)) : 0u;
         return wave_sum(t);
     }
-    // Tiles of a block's item i: [first, first + count).
-    __device__ void piece(const QuantSeq &q, unsigned i, int &first, int &end) const
+    // Tiles of the pieces of a block of `tiles` tiles, cut evenly into pieces of at most p.
+    __device__ static int piece_len(int tiles, int p)
     {
-        const int n = (q.tiles + pp - 1) / pp, len = (q.tiles + n - 1) / n;
-        first = (int)i * len;
-        end = min(q.tiles, first + len);
+        const int n = div24(tiles + p - 1, p);
+        return div24(tiles + n - 1, n);
     }
 };
 
@@ -639,6 +665,7 @@ struct QuantTokenSmem {
         alignas(16) float o[4][32][DH];                // in the wavefront's own tile: others may still be reading theirs
     };
     float m[4][16 * MT], l[4][16 * MT];
+    float2 whole[16 * MT];                             // maximum and 1 / sum of a block that is not to be joined
     static_assert(sizeof(tile) == sizeof(o) && MT <= 2, "a wavefront's results fit its tile");
     // 16-byte unit u of a row of o, spread over the banks
     static __device__ int unit(int row, int u) { return (u ^ (row & (DH / 4 - 1) & 15)) * 4; }
@@ -700,6 +727,16 @@ __device__ inline float load_queries(const uint16_t *row, bool live, int quarter
 #pragma unroll
     for (int j = 0; j < 2 * NJ; ++j) f[j] = query_half(u[j], up);
     return query_scale(amax, scale);
+}
+
+// The raw block sums of a row, each relative to its tile's maximum, to shares of the whole: times 2^(tile's maximum - m) inv.
+__device__ inline void mass_shares(const QuantAttend &a, size_t row, int len, int blocks, int from, int step, float m, float inv)
+{
+    const float mz = finite_or_zero(m);
+    const int live = (len + (1 << a.g.bsh) - 1) >> a.g.bsh, tsh = 6 - a.g.bsh;
+    float *to = a.mass + row * blocks;
+    const float *mt = a.ws_m + row * (a.g.cap / QT);
+    for (int j = from; j < blocks; j += step) to[j] = j < live ? to[j] * (exp2f(mt[j >> tsh] - mz) * inv) : 0.f;
 }
 
 // Tiles ta .. tb - 1 of block rb of head (b, hd)'s rows; slot: where a piece's result goes (-1: the block is whole).
@@ -923,9 +960,10 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
         for (int dt = 0; dt < ND; ++dt) *(qf4_t *)&sm.o[wave][r * 16 + col][sm.unit(r * 16 + col, dt * 4 + quarter)] = o[r][dt] * unit;
     }
     __syncthreads();
+    const QuantAttend &z = late_args();
     for (int row = threadIdx.x >> 4; row < RB; row += Q_THREADS / 16) {
         const int d0 = (threadIdx.x & 15) * (DH / 16);
-        const QuantRow rr = quant_row(a, hd, rb * RB + row, len, cnt);
+        const QuantRow rr = quant_row(z, hd, rb * RB + row, len, cnt);
         if (rr.vis < 0) continue;
         float mm = -INFINITY, ll = 0.f, x[DH / 16];
 #pragma unroll
@@ -945,17 +983,31 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
         }
         if (slot >= 0) {
             const size_t at = (size_t)(blockIdx.x * 2 + slot) * RB + row;
-            __builtin_memcpy(__builtin_assume_aligned(a.ws_o + at * DH + d0, 16), x, sizeof(x));
-            if (d0 == 0) a.ws_ml[at] = make_float2(mm, ll);
+            __builtin_memcpy(__builtin_assume_aligned(z.ws_o + at * DH + d0, 16), x, sizeof(x));
+            if (d0 == 0) z.ws_ml[at] = make_float2(mm, ll);
         } else {
             const float inv = ll == 0.f ? 0.f : 1.f / ll;
 #pragma unroll
             for (int e = 0; e < DH / 16; ++e) x[e] *= inv;
-            store_row<DH / 16, !F32>(a.out, (size_t)rr.row_of * DH + d0, x);
+            store_row<DH / 16, !F32>(z.out, (size_t)rr.row_of * DH + d0, x);
             if (d0 == 0) {
-                if (a.lse) a.lse[rr.row_of] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * Q_LN2;
-                if (a.mass) a.ws_row[rr.row_of] = make_float2(mm, ll);
+                if (z.lse) z.lse[rr.row_of] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * Q_LN2;
+                if (z.mass) {
+                    if (z.nrb)
+                        sm.whole[row] = make_float2(mm, inv);
+                    else
+                        z.ws_row[rr.row_of] = make_float2(mm, ll);
+                }
             }
+        }
+    }
+    if (z.mass && z.nrb) {
+        // nobody joins this block: its tiles' sums become shares here (n = 1: row r is q-head r)
+        __syncthreads();
+        const int rows = min(RB, z.R - rb * RB), blocks = z.g.cap >> z.g.bsh;
+        for (int row = wave; row < rows; row += 4) {
+            const float2 mi = sm.whole[row];
+            mass_shares(z, (size_t)hd * z.G + rb * RB + row, len, blocks, lane, 64, mi.x, mi.y);
         }
     }
 }
@@ -967,28 +1019,60 @@ constexpr int token_held()
     return DH == 64 && MT == 1 ? 3 : 2;
 }
 
+// Runs f(sequence, b, head, block of rows, first tile, end tile, slot) for the work-group's part of a batch.
+template <typename F>
+__device__ inline void quant_parts(const QuantAttend &a, F f)
+{
+    QuantShare sh;
+    QuantSeq sq;
+    int b = 0, hd, rb, ta = 0, tb;
+    unsigned i = 0, i1 = 0, start = 0;
+    auto item = [&]() {
+        const unsigned off = i - start, span = sh.span(sq);
+        const unsigned unit = span == 1 ? off : sh.pp ? (unsigned)div24((int)off, (int)span) : off / span, at = off - unit * span;
+        ta = (int)at;
+        tb = (int)min(span, at + (i1 - i));
+        i += tb - ta;
+        if (sh.pp) {
+            const int len = QuantShare::piece_len(sq.tiles, sh.pp);
+            ta = min(sq.tiles, (int)at * len);
+            tb = min(sq.tiles, ta + len);
+        }
+        hd = sq.nrb == 1 ? (int)unit : (int)unit / sq.nrb;
+        rb = (int)unit - hd * sq.nrb;
+        hd += b * sh.heads;
+    };
+    if (a.nrb > 0) {
+        hd = a.nrb == 1 ? (int)blockIdx.x : (int)blockIdx.x / a.nrb;
+        rb = (int)blockIdx.x - hd * a.nrb;
+        if (a.g.B > 1) b = hd / (a.g.nl * a.g.H);
+        sq = quant_seq(a, b);
+        if (rb >= sq.nrb) return;
+        tb = sq.tiles;
+    } else {
+        sh.init(a, threadIdx.x & 63);
+        i = blockIdx.x * sh.per;
+        if (i >= sh.total) return;
+        i1 = min(i + sh.per, sh.total);
+        b = sh.find(a, i, start, sq);
+        item();
+    }
+    for (;;) {
+        f(sq, b, hd, rb, ta, tb, ta > 0 ? 0 : tb < sq.tiles ? 1 : -1);
+        if (i >= i1) return;
+        if (i - start >= sh.work(sq)) b = sh.find(a, i, start, sq);
+        item();
+        __syncthreads();
+    }
+}
+
 template <int DH, int FMT, bool F32, int MT, bool NTL>
 __global__ __launch_bounds__(Q_THREADS, (token_held<DH, MT>())) void quant_token_kernel(QuantAttend a)
 {
     __shared__ QuantTokenSmem<DH, MT> sm;
-    const QuantShare sh(a, threadIdx.x & 63);
-    unsigned f = blockIdx.x * sh.per, start;
-    if (f >= sh.total) return;
-    const unsigned f1 = min(f + sh.per, sh.total);
-    QuantSeq sq;
-    int b = sh.find(a, f, start, sq);
-    for (;;) {
-        const unsigned off = f - start, span = sh.span(sq), unit = span == 1 ? off : off / span, at = off - unit * span;
-        int ta = (int)at, tb = (int)min(span, at + (f1 - f));
-        f += tb - ta;
-        if (sh.pp) sh.piece(sq, at, ta, tb);
-        const int hd = sq.nrb == 1 ? (int)unit : (int)unit / sq.nrb;
-        quant_token_block<DH, FMT, F32, MT, NTL>(a, sm, sq, b, b * sh.heads + hd, (int)unit - hd * sq.nrb, ta, tb,
-                                                 ta > 0 ? 0 : tb < sq.tiles ? 1 : -1);
-        if (f >= f1) return;
-        if (f - start >= sh.work(sq)) b = sh.find(a, f, start, sq);
-        __syncthreads();
-    }
+    quant_parts(a, [&](const QuantSeq &sq, int b, int hd, int rb, int ta, int tb, int slot) {
+        quant_token_block<DH, FMT, F32, MT, NTL>(a, sm, sq, b, hd, rb, ta, tb, slot);
+    });
 }
 
 // Many query rows.  A work-group has blocks of RB = 128 rows, 32 for each of its four wavefronts; all of them use the same
@@ -1247,23 +1331,9 @@ template <int DH, int FMT, bool F32>
 __global__ __launch_bounds__(Q_THREADS, 2) void quant_wide_kernel(QuantAttend a)
 {
     __shared__ QuantWideSmem<DH> sm;
-    const QuantShare sh(a, threadIdx.x & 63);
-    unsigned f = blockIdx.x * sh.per, start;
-    if (f >= sh.total) return;
-    const unsigned f1 = min(f + sh.per, sh.total);
-    QuantSeq sq;
-    int b = sh.find(a, f, start, sq);
-    for (;;) {
-        const unsigned off = f - start, span = sh.span(sq), unit = span == 1 ? off : off / span, at = off - unit * span;
-        int ta = (int)at, tb = (int)min(span, at + (f1 - f));
-        f += tb - ta;
-        if (sh.pp) sh.piece(sq, at, ta, tb);
-        const int hd = sq.nrb == 1 ? (int)unit : (int)unit / sq.nrb;
-        quant_wide_block<DH, FMT, F32>(a, sm, sq, b, b * sh.heads + hd, (int)unit - hd * sq.nrb, ta, tb,
-                                       ta > 0 ? 0 : tb < sq.tiles ? 1 : -1);
-        if (f >= f1) return;
-        if (f - start >= sh.work(sq)) b = sh.find(a, f, start, sq);
-    }
+    quant_parts(a, [&](const QuantSeq &sq, int b, int hd, int rb, int ta, int tb, int slot) {
+        quant_wide_block<DH, FMT, F32>(a, sm, sq, b, hd, rb, ta, tb, slot);
+    });
 }
 
 // Joins the pieces of a cache.  Which pieces of the workspace a block of rows has:
@@ -1292,7 +1362,8 @@ __global__ __launch_bounds__(Q_THREADS) void quant_merge_kernel(QuantAttend a)
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = hd / (g.nl * g.H);
     const QuantSeq sq = quant_seq(a, b);
     if (sq.cnt == 0) return;
-    const QuantShare sh(a, lane);
+    QuantShare sh;
+    sh.init(a, lane);
     const QuantPieces pc(a, sh, sq, b, hd, r / a.RB);
     float m = -INFINITY, sum = 0.f;
     if (pc.n == 1) {
@@ -1335,13 +1406,7 @@ __global__ __launch_bounds__(Q_THREADS) void quant_merge_kernel(QuantAttend a)
         }
         if (a.lse && tid == 0) a.lse[row] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * Q_LN2;
     }
-    if (a.mass) {
-        const float inv = sum == 0.f ? 0.f : 1.f / sum, mz = finite_or_zero(m);
-        const int blocks = g.cap >> g.bsh, live = (sq.len + (1 << g.bsh) - 1) >> g.bsh, tsh = 6 - g.bsh;
-        float *to = a.mass + (size_t)row * blocks;
-        const float *mt = a.ws_m + (size_t)row * (g.cap / QT);
-        for (int j = tid; j < blocks; j += Q_THREADS) to[j] = j < live ? to[j] * (exp2f(mt[j >> tsh] - mz) * inv) : 0.f;
-    }
+    if (a.mass) mass_shares(a, row, sq.len, g.cap >> g.bsh, tid, Q_THREADS, m, sum == 0.f ? 0.f : 1.f / sum);
 }
 
 // Several tokens: a work-group per 16 rows of a head, sixteen threads a row.
@@ -1353,7 +1418,8 @@ __global__ __launch_bounds__(Q_THREADS) void quant_merge_rows_kernel(QuantAttend
     const int b = hd / (a.g.nl * a.g.H);
     const QuantSeq sq = quant_seq(a, b);
     if ((int)r0 >= sq.cnt * a.G) return;
-    const QuantShare sh(a, threadIdx.x & 63);
+    QuantShare sh;
+    sh.init(a, threadIdx.x & 63);
     const QuantPieces pc(a, sh, sq, b, hd, r0 / a.RB);
     const unsigned r = r0 + (threadIdx.x >> 4), d0 = (threadIdx.x & 15) * E;
     const QuantRow qr = quant_row(a, hd, r, sq.len, sq.cnt);
@@ -1450,10 +1516,29 @@ void quant_dispatch(const wnw_quant_config &c, F f)
         c.format == WNW_QUANT_INT8 ? f(D1{}, I0{}) : f(D1{}, I1{});
 }
 
+// Whether every block of rows gets a work-group of its own rather than blocks being cut into even parts and joined by a
+// second launch.  Times in us, measured: a tile of a work-group that has its compute unit nearly alone (`tile`: 0.45 in the token
+// kernels of d = 128, four wavefronts in turn; 1.5 in the wide kernel); a tile when the chip is full (`full`, a compute unit's time:
+// the token kernels' bytes at 6.5 TB/s; 1.3); the join with its launch and the parts' search (5, 6).  Measured whole and cut:
+// one token on 8 blocks of 12 tiles 10.6 and 11.6 us, of 20 14.3 and 13.2; on 72 of 16 14.0 and 16.1, of 32 21.8 and 19.5; on
+// 128 of 32 20.3 and 21.7, of 63 33.8 and 31.8; on 240 of 243 153 and 160, of 1423 848 and 866; a draft of five on
+// 720 of 147, 23 and 73 178 and 203; the wide kernel on 32 blocks of 4 12.6 and 15.6, of 16 30.8 and 21.9; on 256 of 32 59 and
+// 68, of 243 369 and 310; on 3840 of 32 563 and 617.
+bool whole_blocks(int RB, int head_dim, int64_t blocks, int64_t tiles)
+{
+    const double b = blocks / 256.0, t = (double)tiles;
+    if (RB == WIDE_ROWS) {
+        const double whole = blocks <= 256 ? 1.5 * t : 2.6 * t * (double)((blocks + 511) / 512);
+        return blocks >= 2048 || whole <= 6 + std::max(1.5 * MIN_PIECE, 1.3 * t * b);
+    }
+    const double tile = head_dim == 64 ? 0.3 : 0.45, full = head_dim == 64 ? 0.32 : 0.63;
+    return t * std::max(tile, full * b) <= 5 + std::max(tile * MIN_PIECE, full * t * b);
+}
+
 // How an attention call runs: rows of a block, work-groups, loads past the caches; output rows; the workspace's arrays.
 struct QuantPlan {
     int RB, W;
-    bool stream;
+    bool whole, stream;
     int64_t rows, o_bytes, ml_bytes, row_bytes, m_bytes;
     int64_t total() const { return o_bytes + ml_bytes + row_bytes + m_bytes; }
 };
@@ -1468,15 +1553,17 @@ QuantPlan quant_plan(const wnw_quant_config &c, int32_t n_layers, int32_t q_head
     QuantPlan p;
     p.RB = R > 32 ? WIDE_ROWS : R > 16 ? 32 : 16;
     const int64_t blocks = heads * ((R + p.RB - 1) / p.RB), tiles = (len + QT - 1) / QT * blocks;
-    // as many as the chip's 256 compute units hold at once, or as many as pieces of MIN_PIECE tiles need
+    // Work-groups: one for every block of rows; or as many as the chip's 256 compute units hold at once, or as pieces of
+    // MIN_PIECE tiles need.
     const int held = 256 * (c.head_dim == 64 && p.RB == 16 ? token_held<64, 1>() : 2);
-    p.W = (int)std::max<int64_t>(1, std::min<int64_t>(held, tiles / MIN_PIECE + blocks));
+    p.whole = whole_blocks(p.RB, c.head_dim, blocks, (len + QT - 1) / QT);
+    p.W = (int)std::max<int64_t>(1, p.whole ? blocks : std::min<int64_t>(held, tiles / MIN_PIECE + blocks));
     // Bytes that one pass reads once and the 256 MB of the last-level cache cannot keep for the next one
     p.stream = R <= p.RB && heads * len * c.head_dim * 2 > (256ll << 20);
     p.rows = heads * R;
-    p.o_bytes = (int64_t)p.W * 2 * p.RB * c.head_dim * 4;
-    p.ml_bytes = (int64_t)p.W * 2 * p.RB * 8;
-    p.row_bytes = n == 1 ? round16(p.rows * 8) : 0;
+    p.o_bytes = p.whole ? 0 : (int64_t)p.W * 2 * p.RB * c.head_dim * 4;
+    p.ml_bytes = p.whole ? 0 : (int64_t)p.W * 2 * p.RB * 8;
+    p.row_bytes = n == 1 && !p.whole ? round16(p.rows * 8) : 0;
     p.m_bytes = n == 1 ? round16(p.rows * (c.capacity / QT) * 4) : 0;
     return p;
 }
@@ -1501,7 +1588,7 @@ wnw_status quant_heads(const wnw_quant_config &c, int32_t n_layers, int32_t q_he
         return quant_fail(WNW_ERR_UNSUPPORTED, "too many query rows");
     // the line of tiles is counted in 32 bits
     const int64_t blocks = ((int64_t)q_heads / c.kv_heads * n + 15) / 16 * c.batch * n_layers * c.kv_heads;
-    if (blocks > INT32_MAX / (c.capacity / QT)) return quant_fail(WNW_ERR_UNSUPPORTED, "too many tiles for one call");
+    if (blocks > Q_MAX_GROUPS || blocks > INT32_MAX / (c.capacity / QT)) return quant_fail(WNW_ERR_UNSUPPORTED, "too many tiles for one call");
     return WNW_OK;
 }
 
@@ -1589,7 +1676,7 @@ wnw_status wnw_quant_attend(const wnw_quant_config *cfg, const wnw_quant_cache *
         return quant_fail(WNW_ERR_INVALID, "workspace missing, too small or not aligned to 16 bytes");
     const int G = q_heads / cfg->kv_heads, R = G * n;
     char *ws = (char *)workspace;
-    QuantAttend a = {quant_geo(*cfg, *cache, first_layer, n_layers), G, n, R, p.W, p.RB, (const uint16_t *)q_dev, len_dev, count_dev,
+    QuantAttend a = {quant_geo(*cfg, *cache, first_layer, n_layers), G, n, R, p.W, p.RB, p.whole ? (R + p.RB - 1) / p.RB : 0, 1.f / p.W, (const uint16_t *)q_dev, len_dev, count_dev,
                      out_dev, lse_dev, mass_dev, (float *)ws, (float2 *)(ws + p.o_bytes),
                      (float2 *)(ws + p.o_bytes + p.ml_bytes), (float *)(ws + p.o_bytes + p.ml_bytes + p.row_bytes),
                      Q_LOG2E / sqrtf((float)cfg->head_dim)};
@@ -1597,11 +1684,11 @@ wnw_status wnw_quant_attend(const wnw_quant_config *cfg, const wnw_quant_cache *
     quant_dispatch(*cfg, [&](auto d, auto f) {
         constexpr int DH = decltype(d)::value, FMT = decltype(f)::value;
         bf16 ? launch_token<DH, FMT, false>(p, a, (hipStream_t)hip_stream) : launch_token<DH, FMT, true>(p, a, (hipStream_t)hip_stream);
-        // one work-group alone leaves no pieces
-        if (n == 1 && (p.W > 1 || mass_dev))
+        if (p.whole) return;
+        if (n == 1)
             hipLaunchKernelGGL((bf16 ? quant_merge_kernel<DH, true> : quant_merge_kernel<DH, false>), dim3((unsigned)p.rows),
                                dim3(Q_THREADS), 0, (hipStream_t)hip_stream, a);
-        else if (p.W > 1)
+        else
             hipLaunchKernelGGL((bf16 ? quant_merge_rows_kernel<DH, true> : quant_merge_rows_kernel<DH, false>),
                                dim3((unsigned)(p.rows / R * ((R + 15) / 16))), dim3(Q_THREADS), 0, (hipStream_t)hip_stream, a);
     });
