@@ -648,6 +648,27 @@ __device__ inline float finite_or_zero(float m)
     return m == -INFINITY ? 0.f : m;
 }
 
+// Eight weights as matrix operands.  TWO: as the sum of two fp16.  The first is rounded towards zero by one instruction
+// whose result is also what the second is the rest of: with (_Float16) in both places the compiler rounded the product
+// with the V scale straight to fp16 in one of them, and where the other's fp32 value was a tie the two differed by a whole step.
+template <bool TWO>
+__device__ inline void weights_to_half(const float (&p)[8], h8_t &hi, h8_t &lo)
+{
+    if constexpr (TWO) {
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            const h2_t h = __builtin_bit_cast(h2_t, __builtin_amdgcn_cvt_pkrtz(p[i], p[i + 1]));
+            hi[i] = h.x;
+            hi[i + 1] = h.y;
+            lo[i] = (_Float16)(p[i] - (float)h.x);
+            lo[i + 1] = (_Float16)(p[i + 1] - (float)h.y);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) hi[i] = (_Float16)p[i];
+    }
+}
+
 // Few query rows.  A work-group has its part of the batch's tiles; within a block of RB = 16 MT rows each wavefront takes
 // tiles of 64 cache rows in turn, and MT times
 //   S^T (16 keys x 16 rows) = K Q^T, K bytes straight from registers: lane (key l % 16, quarter l / 16) has 16 bytes of a
@@ -905,13 +926,11 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
                     for (int i = 0; i < 4; ++i) x[kb][i] = key0 + kb * 16 + i < qr[r].vis ? x[kb][i] : 0.f;
             }
 #pragma unroll
-            for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const _Float16 hi = (_Float16)x[kb][i];
-                    ph[r][kb >> 1][(kb & 1) * 4 + i] = hi;
-                    if constexpr (F32) pl[r][kb >> 1][(kb & 1) * 4 + i] = (_Float16)(x[kb][i] - (float)hi);
-                }
+            for (int c = 0; c < 2; ++c) {
+                const float p[8] = {x[2 * c][0],     x[2 * c][1],     x[2 * c][2],     x[2 * c][3],
+                                    x[2 * c + 1][0], x[2 * c + 1][1], x[2 * c + 1][2], x[2 * c + 1][3]};
+                weights_to_half<F32>(p, ph[r][c], pl[r][c]);
+            }
         }
         vexp = ve;
         if (more)
@@ -1273,11 +1292,7 @@ __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> 
                 if constexpr (MASKED) p[i] = 16 * c + 8 * (i / 4) + i % 4 < vis ? p[i] : 0.f;
             }
             sum += part;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                ph[c][i] = (_Float16)p[i];
-                if constexpr (F32) pl[c][i] = (_Float16)(p[i] - (float)ph[c][i]);
-            }
+            weights_to_half<F32>(p, ph[c], pl[c]);
         }
         if (t + 1 < t_end) {
             store(t + 1, other);

@@ -140,3 +140,32 @@ def attend(q, k, v, lens, counts, block):
                     absq[b, :, hq, i] = (kk.abs() @ qq.abs().unsqueeze(-1)).squeeze(-1).amax(dim=-1) / math.sqrt(D)
                     sumv[b, :, hq, i] = see * vv.abs().amax(dim=(1, 2))
     return out, lse, mass, absv, absq, sumv
+
+
+def attend_fast(q, k, v, lens, counts, block):
+    """attend() with a product per sequence, on the tensors' device."""
+    B, L, Hq, n, D = q.shape
+    H, cap = k.shape[2], k.shape[3]
+    G = Hq // H
+    outs = [[] for _ in range(6)]
+    key = torch.arange(cap, device=q.device)
+    for b in range(B):
+        T, c = min(max(int(lens[b]), 0), cap), min(max(int(counts[b]), 0), n)
+        limit = (T - c + torch.arange(n, device=q.device) + 1).clamp(0, T)          # rows that token i sees
+        sees = key < limit[:, None]
+        qq = q[b].reshape(L, H, G * n, D)
+        dead = (key >= T)[:, None]
+        kk, vv = k[b].masked_fill(dead, 0.0), v[b].masked_fill(dead, 0.0)
+        x = (qq @ kk.transpose(-1, -2) / math.sqrt(D)).reshape(L, H, G, n, cap).masked_fill(~sees, -math.inf)
+        lse = torch.logsumexp(x, dim=-1)
+        p = torch.where(sees, torch.exp(x - lse.unsqueeze(-1)), 0.0)
+        absq = (qq.abs() @ kk.abs().transpose(-1, -2) / math.sqrt(D)).reshape(L, H, G, n, cap).masked_fill(~sees, 0.0).amax(dim=-1)
+        pr = p.reshape(L, H, G * n, cap)
+        got = ((pr @ vv), lse, p.unflatten(-1, (-1, block)).sum(dim=-1), (pr @ vv.abs()), absq,
+               (limit * vv.abs().amax(dim=(2, 3))[:, :, None, None]).expand(L, H, G, n))
+        token = torch.arange(n, device=q.device) < c
+        for o, t, width in zip(outs, got, (D, None, cap // block, D, None, None)):
+            t = t.reshape(L, Hq, n, *([width] if width else []))
+            gone = (~token).reshape(1, 1, n, *([1] if width else []))
+            o.append(t.masked_fill(gone, math.nan) if o is not outs[3] and o is not outs[4] and o is not outs[5] else t)
+    return tuple(torch.stack(o) for o in outs)

@@ -314,6 +314,57 @@ def test_attend_split_cache(W, fmt, n):
     check_attend(run_attend(W, cfg, c, q, lens, [n], count_dev=False), want, lens, [n], D, False, H)
 
 
+# How a call is shared out depends on its blocks of query rows and their tiles: a work-group per block, even pieces that
+# are joined, or equal parts of all tiles in a line.  (lens, n, counts, layers, KV heads, group, block, d)
+SHARED = {
+    "token, a block each": ([900, 0, 64, 333], 1, None, 6, 8, 4, 32, 128),
+    "token, pieces": ([5000, 63, 4097], 1, None, 2, 3, 2, 16, 128),
+    "token, pieces, many sequences": ([3000 - 23 * b if b % 7 else b for b in range(130)], 1, None, 1, 1, 2, 64, 128),
+    "token, a line": ([10240, 10000], 1, None, 5, 17, 3, 64, 128),
+    "token, a line, d = 64": ([36000, 35999], 1, None, 7, 10, 1, 32, 64),
+    "32 rows, pieces": ([4000, 700], 6, [6, 5], 2, 3, 4, 64, 128),
+    "32 rows, a block each": ([400, 70, 3], 6, [6, 5, 3], 10, 8, 5, 16, 64),
+    "many rows, pieces": ([2000, 900], 50, [50, 33], 2, 2, 3, 16, 128),
+    "many rows, a line": ([700], 41, [41], 20, 30, 1, 32, 64),
+    "many rows, a block each": ([200, 130], 140, [140, 100], 2, 2, 5, 32, 128),
+}
+
+
+@pytest.mark.parametrize("fmt", [R.INT8, R.E4M3])
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("name", SHARED)
+def test_attend_shared_out(W, fmt, bf16, name):
+    lens, n, counts, L, H, G, block, D = SHARED[name]
+    log(f"[case] quant attend, {name}, fmt={fmt} bf16={bf16}")
+    B = len(lens)
+    counts = counts or [1] * B
+    cap = (max(lens) + 63) // 64 * 64 + 64
+    cfg = W.make_quant_config(B, L, H, cap, block, fmt, head_dim=D, flags=W.WNW_F_OUT_BF16 if bf16 else 0)
+    g = torch.Generator(device="cuda").manual_seed(17)
+    c = W.make_quant_cache(cfg)
+    number = torch.from_numpy(np.nan_to_num(R.numbers(fmt))).cuda()
+    vals = []
+    for to, scale, is_v in ((c.k, c.k_scale, False), (c.v, c.v_scale, True)):
+        code = torch.randint(1, 256, (B, L, H, cap, D), generator=g, device="cuda", dtype=torch.uint8)
+        if fmt == R.E4M3:
+            code = torch.where((code & 127) == 127, 0, code)
+        mean = float(number[code.int()[0, 0, 0]].abs().mean())
+        s = torch.exp(0.5 * torch.randn(scale.shape, generator=g, device="cuda")) / mean
+        if not is_v:
+            s *= 0.5
+        vals.append(number[code.int()] * s.double().repeat_interleave(block, dim=3).unsqueeze(-1))
+        for b in range(B):
+            code[b, :, :, lens[b]:] = 0xFF
+            s[b, :, :, -(-lens[b] // block):] = math.nan
+        to.copy_(R.k_to_v(code) if is_v else code)
+        scale.copy_(s)
+        del code
+    q = rows(18, B, L, H * G, n, D, spread=0.3).cuda()
+    want = tuple(t.cpu() for t in R.attend_fast(q.double(), *vals, lens, counts, block))
+    del vals
+    check_attend(run_attend(W, cfg, c, q, lens, counts), want, lens, counts, D, bf16, H)
+
+
 @pytest.mark.parametrize("fmt", [R.INT8, R.E4M3])
 @pytest.mark.parametrize("n", [1, 9, 70])
 def test_attend_poisoned_block(W, fmt, n):

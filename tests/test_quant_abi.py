@@ -170,3 +170,13 @@ def test_reference_rounding():
     assert R.scale_of(127.0, R.INT8) == 1.0 and R.scale_of(0.0, R.INT8) == 2.0 ** -126
     assert R.scale_of(448.0, R.E4M3) == 1.0 and R.scale_of(448.5, R.E4M3) == 2.0 and R.scale_of(0.0, R.E4M3) == 2.0 ** -126
     assert np.isnan(R.scale_of(np.inf, R.INT8))
+
+
+def test_the_two_references_agree():
+    rng = np.random.default_rng(3)
+    k, v = (torch.from_numpy(rng.standard_normal((2, 1, 2, 64, 8))) for _ in range(2))
+    q = torch.from_numpy(rng.standard_normal((2, 1, 4, 3, 8)))
+    for lens, counts in (([64, 10], [3, 2]), ([0, 2], [1, 3])):
+        for a, b in zip(R.attend(q, k, v, lens, counts, 16)[:3], R.attend_fast(q, k, v, lens, counts, 16)[:3]):
+            assert torch.equal(torch.isnan(a), torch.isnan(b))
+            assert torch.allclose(a.nan_to_num(), b.nan_to_num(), rtol=1e-12, atol=1e-12)
