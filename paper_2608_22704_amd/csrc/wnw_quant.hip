@@ -842,11 +842,9 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
                 }
             }
 #pragma unroll
-            for (int r = 0; r < MT; ++r) {
-                const float f = crow[r] * ksc[kb];
+            for (int r = 0; r < MT; ++r)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[r][kb][i] = c[r][i] * f;
-            }
+                for (int i = 0; i < 4; ++i) s[r][kb][i] = c[r][i];
         }
         __builtin_amdgcn_sched_barrier(0);
         __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the bytes have been read
@@ -864,18 +862,22 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
         h8_t ph[MT][2], pl[MT][2];
 #pragma unroll
         for (int r = 0; r < MT; ++r) {
-            float (&x)[4][4] = s[r];
+            // logits are x[kb][.] f[kb]; where masks are needed they are made here, and f is 1
+            float (&x)[4][4] = s[r], f[4];
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb) f[kb] = crow[r] * ksc[kb];
             if (masked) {
 #pragma unroll
-                for (int kb = 0; kb < 4; ++kb)
+                for (int kb = 0; kb < 4; ++kb) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[kb][i] = key0 + kb * 16 + i < qr[r].vis ? x[kb][i] : -INFINITY;
+                    for (int i = 0; i < 4; ++i) x[kb][i] = key0 + kb * 16 + i < qr[r].vis ? x[kb][i] * f[kb] : -INFINITY;
+                    f[kb] = 1.f;
+                }
             }
             float mt = m[r];
 #pragma unroll
             for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) mt = fmaxf(mt, x[kb][i]);
+                mt = fmaxf(mt, fmaxf(fmaxf(x[kb][0], x[kb][1]), fmaxf(x[kb][2], x[kb][3])) * f[kb]);
             mt = quarters_max(mt);
             if (ve > vexp || __any(mt > m[r])) {
                 const float alpha = exp2_hw(m[r] - finite_or_zero(mt)), f = alpha * pow2i(vexp - ve);
@@ -889,7 +891,7 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
 #pragma unroll
             for (int kb = 0; kb < 4; ++kb) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[kb][i] = exp2_hw(x[kb][i] - mz);
+                for (int i = 0; i < 4; ++i) x[kb][i] = exp2_hw(fmaf(x[kb][i], f[kb], -mz));
                 bs[kb] = (x[kb][0] + x[kb][1]) + (x[kb][2] + x[kb][3]);
             }
             sum[r] += (bs[0] + bs[1]) + (bs[2] + bs[3]);
@@ -914,11 +916,9 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
             }
             // P^T, times the V scales; a masked weight is 0 whatever the scale is
 #pragma unroll
-            for (int kb = 0; kb < 4; ++kb) {
-                const float f = vsc[kb] * vf;
+            for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[kb][i] *= f;
-            }
+                for (int i = 0; i < 4; ++i) x[kb][i] *= vsc[kb] * vf;
             if (masked) {
 #pragma unroll
                 for (int kb = 0; kb < 4; ++kb)
