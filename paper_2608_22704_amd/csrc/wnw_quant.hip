@@ -562,15 +562,20 @@ struct QuantShare {
     __device__ void init(const QuantAttend &a, int lane_)
     {
         heads = a.g.nl * a.g.H, lane = lane_, pp = 0;
-        mine = quant_seq(a, lane);
         unsigned t = 0, units = 0, most = 0;
-        for (int b0 = 0; b0 < a.g.B; b0 += 64) {
-            const QuantSeq q = seq(a, b0);
-            t += work(q);
-            units += (unsigned)(q.nrb * heads);
-            most = max(most, q.nrb ? (unsigned)q.tiles : 0u);
+        if (a.g.B == 1) {       // (all of it scalar, and no other instructions to fetch)
+            mine = quant_seq(a, 0);
+            t = work(mine), units = (unsigned)(mine.nrb * heads), most = mine.nrb ? (unsigned)mine.tiles : 0u;
+        } else {
+            mine = quant_seq(a, lane);
+            for (int b0 = 0; b0 < a.g.B; b0 += 64) {
+                const QuantSeq q = seq(a, b0);
+                t += work(q);
+                units += (unsigned)(q.nrb * heads);
+                most = max(most, q.nrb ? (unsigned)q.tiles : 0u);
+            }
+            t = wave_sum(t), units = wave_sum(units), most = wave_max(most);
         }
-        t = wave_sum(t), units = wave_sum(units), most = wave_max(most);
         total = t;
         per = max(at_least(t, a.inv_w), (unsigned)MIN_PIECE);
         if (units < (unsigned)a.W) {
@@ -579,15 +584,25 @@ struct QuantShare {
             if (p && piece_len((int)most, (int)p) <= (int)per + PIECE_COST) {
                 pp = (int)p;
                 per = 1;
-                t = 0;
-                for (int b0 = 0; b0 < a.g.B; b0 += 64) t += work(seq(a, b0));
-                total = wave_sum(t);
+                if (a.g.B == 1)
+                    total = uniform(work(mine));
+                else {
+                    t = 0;
+                    for (int b0 = 0; b0 < a.g.B; b0 += 64) t += work(seq(a, b0));
+                    total = wave_sum(t);
+                }
             }
         }
+        per = uniform(per), pp = (int)uniform(pp);
     }
     // The sequence that item f (< total) belongs to, and the first of its items.
     __device__ int find(const QuantAttend &a, unsigned f, unsigned &start, QuantSeq &sq) const
     {
+        if (a.g.B == 1) {
+            start = 0;
+            sq = {(int)uniform(mine.len), (int)uniform(mine.cnt), (int)uniform(mine.tiles), (int)uniform(mine.nrb)};
+            return 0;
+        }
         unsigned base = 0;
         for (int b0 = 0;; b0 += 64) {
             const QuantSeq q = seq(a, b0);
@@ -605,6 +620,7 @@ struct QuantShare {
     // Items of the sequences 0 .. end - 1.
     __device__ unsigned before(const QuantAttend &a, int end) const
     {
+        if (end == 0) return 0;
         unsigned t = 0;
         for (int b0 = 0; b0 < end; b0 += 64) t += b0 + lane < end ? work(seq(a, b0)) : 0u;
         return wave_sum(t);
@@ -1047,7 +1063,7 @@ __device__ inline void quant_parts(const QuantAttend &a, F f)
     int b = 0, hd, rb, ta = 0, tb;
     unsigned i = 0, i1 = 0, start = 0;
     auto item = [&]() {
-        const unsigned off = i - start, span = sh.span(sq);
+        const unsigned off = i - start, span = uniform(sh.span(sq));
         const unsigned unit = span == 1 ? off : sh.pp ? (unsigned)div24((int)off, (int)span) : off / span, at = off - unit * span;
         ta = (int)at;
         tb = (int)min(span, at + (i1 - i));
@@ -1059,7 +1075,7 @@ __device__ inline void quant_parts(const QuantAttend &a, F f)
         }
         hd = sq.nrb == 1 ? (int)unit : (int)unit / sq.nrb;
         rb = (int)unit - hd * sq.nrb;
-        hd += b * sh.heads;
+        hd = (int)uniform(hd + b * sh.heads), rb = (int)uniform(rb), ta = (int)uniform(ta), tb = (int)uniform(tb);
     };
     if (a.nrb > 0) {
         hd = a.nrb == 1 ? (int)blockIdx.x : (int)blockIdx.x / a.nrb;
