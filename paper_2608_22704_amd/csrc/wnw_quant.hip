@@ -3,16 +3,15 @@
 //
 //   quant_write_kernel   a tile of 64 rows of one head's K or V per work-group
 //   quant_read_kernel    the same tiles back to fp32 / bf16
-//   quant_token_kernel   attention of few query rows: K and V bytes go from HBM to registers once and
-//                        straight into the matrix cores
+//   quant_token_kernel   attention of up to 32 query rows of a KV-head: every byte of K and V comes from HBM once
 //   quant_wide_kernel    attention of many query rows: tiles become fp16 in shared memory once for 128 rows
-//   quant_merge_kernel   joins the pieces of a cache split over work-groups, and finishes the block masses
+//   quant_merge_kernel, quant_merge_rows_kernel   join the parts of a cache that work-groups shared
 //
 // Bytes become fp16 on the way to the matrix cores, exactly: integers up to 127 and e4m3 numbers both fit.
 // A query row is scaled by a power of two (its largest magnitude to 2^14 .. 2^15) and is then exact in fp16 as well, but
 // for elements 2^28 times smaller than the largest, so logits carry fp32 rounding alone.  A softmax weight times its
-// block's V scale is rounded to fp16 once where the output is bf16 (2^-12 next to the output's 2^-9), and
-// to the sum of two fp16 (2^-23) where it is fp32.
+// block's V scale is rounded to fp16 once where the output is bf16 (by 2^-12 at most, next to the output's 2^-9), and
+// to the sum of two fp16 (2^-22) where it is fp32.  Sums, maxima and logits are fp32.
 #include "wnw.h"
 #include "wnw_internal.h"
 #include "wnw_lds.h"
@@ -465,7 +464,7 @@ __global__ __launch_bounds__(Q_THREADS) void quant_read_kernel(QuantGeo g, int n
 struct QuantAttend {
     QuantGeo g;
     int G, n, R;               // q-heads per KV-head, tokens, rows G * n of a KV-head: row r is token r / G, q-head r % G
-    int W, RB;                 // work-groups that share the batch's tiles, rows of a block
+    int W, RB, rsh;            // work-groups that share the batch's tiles, rows of a block and their log2
     int nrb;                   // > 0: a work-group per block of rows, nrb blocks a head, nothing to join
     float inv_w;               // 1 / W
     const uint16_t *q;
@@ -524,7 +523,7 @@ __device__ inline QuantSeq quant_seq(const QuantAttend &a, int b)
         q.len = q_clamp(a.len[b], a.g.cap);
         q.cnt = a.count ? q_clamp(a.count[b], a.n) : a.n;
         q.tiles = max(1, (q.len + QT - 1) / QT);
-        q.nrb = (q.cnt * a.G + a.RB - 1) / a.RB;
+        q.nrb = (q.cnt * a.G + a.RB - 1) >> a.rsh;
     }
     return q;
 }
@@ -1119,7 +1118,7 @@ __global__ __launch_bounds__(Q_THREADS, (token_held<DH, MT>())) void quant_token
 //   elements are P^T's operand as they stand.
 // A row's maximum m is raised, and its output and sum scaled, only when a logit exceeds it by LAZY (base 2): weights
 // are up to 2^LAZY then, which fp16 has room for.
-constexpr int WIDE_ROWS = 128;
+constexpr int WIDE_ROWS = 128;   // 2^7: see QuantAttend::rsh
 constexpr int LAZY = 8;
 
 // Tiles in shared memory: a row of K has its dimensions, a row of V (a dimension) the tile's rows, 16-byte unit 2 c + half
@@ -1378,7 +1377,7 @@ struct QuantPieces {
         n = (sh.per == 1 ? s0 + span - 1 : (s0 + span - 1) / sh.per) - w0 + 1;
     }
     // row of piece p: slot 1 of its work-group for the first, 0 for the others
-    __device__ size_t at(unsigned p, unsigned r) const { return (size_t)((w0 + p) * 2 + (p == 0)) * RB + r % RB; }
+    __device__ size_t at(unsigned p, unsigned r) const { return (size_t)((w0 + p) * 2 + (p == 0)) * RB + (r & (RB - 1)); }
 };
 
 // Single tokens: a work-group per output row.  A lane has a piece's statistics; the wavefronts share the pieces' sums.  Makes
@@ -1395,7 +1394,7 @@ __global__ __launch_bounds__(Q_THREADS) void quant_merge_kernel(QuantAttend a)
     if (sq.cnt == 0) return;
     QuantShare sh;
     sh.init(a, lane);
-    const QuantPieces pc(a, sh, sq, b, hd, r / a.RB);
+    const QuantPieces pc(a, sh, sq, b, hd, r >> a.rsh);
     float m = -INFINITY, sum = 0.f;
     if (pc.n == 1) {
         if (!a.mass) return;
@@ -1451,7 +1450,7 @@ __global__ __launch_bounds__(Q_THREADS) void quant_merge_rows_kernel(QuantAttend
     if ((int)r0 >= sq.cnt * a.G) return;
     QuantShare sh;
     sh.init(a, threadIdx.x & 63);
-    const QuantPieces pc(a, sh, sq, b, hd, r0 / a.RB);
+    const QuantPieces pc(a, sh, sq, b, hd, r0 >> a.rsh);
     const unsigned r = r0 + (threadIdx.x >> 4), d0 = (threadIdx.x & 15) * E;
     const QuantRow qr = quant_row(a, hd, r, sq.len, sq.cnt);
     if (pc.n == 1 || qr.vis < 0) return;
@@ -1549,18 +1548,20 @@ void quant_dispatch(const wnw_quant_config &c, F f)
 
 // Whether every block of rows gets a work-group of its own rather than blocks being cut into even parts and joined by a
 // second launch.  Times in us, measured: a tile of a work-group that has its compute unit nearly alone (`tile`: 0.45 in the token
-// kernels of d = 128, four wavefronts in turn; 1.5 in the wide kernel); a tile when the chip is full (`full`, a compute unit's time:
-// the token kernels' bytes at 6.5 TB/s; 1.3); the join with its launch and the parts' search (5, 6).  Measured whole and cut:
-// one token on 8 blocks of 12 tiles 10.6 and 11.6 us, of 20 14.3 and 13.2; on 72 of 16 14.0 and 16.1, of 32 21.8 and 19.5; on
-// 128 of 32 20.3 and 21.7, of 63 33.8 and 31.8; on 240 of 243 153 and 160, of 1423 848 and 866; a draft of five on
-// 720 of 147, 23 and 73 178 and 203; the wide kernel on 32 blocks of 4 12.6 and 15.6, of 16 30.8 and 21.9; on 256 of 32 59 and
-// 68, of 243 369 and 310; on 3840 of 32 563 and 617.
+// kernels of d = 128, four wavefronts in turn, 0.3 of d = 64; 1.5 in the wide kernel); a tile when the chip is full (`full`, a compute
+// unit's time: the token kernels' bytes at 6.5 TB/s; 1.3); and the join: its launch, the search for the parts (5, 6) and, in
+// the wide kernel, the parts' results to memory and back (8 for 512 of them).  Measured whole and cut, d = 128, tiles of one
+// token: 8 blocks of 12 10.6 and 11.6 us, of 20 14.3 and 13.2; 72 of 16 13.0 and 14.0, of 32 19.7 and 17.2; 128 of 32 20.3 and
+// 21.7, of 63 33.8 and 31.8; 240 of 243 153 and 160, of 1423 848 and 866; d = 64: 8 of 16 8.1 and 8.7, of 32 12.1 and 10.0; 128
+// of 32 13.7 and 15.3, of 63 22.1 and 19.0; a draft of five on 720 of 147, 23 and 73 178 and 203; the wide kernel: 16 blocks of 4
+// 12.7 and 14.9, of 12 24.5 and 19.1; 256 of 32 58 and 72, of 243 369 and 310; 1024 of 63 285 and 321.
 bool whole_blocks(int RB, int head_dim, int64_t blocks, int64_t tiles)
 {
     const double b = blocks / 256.0, t = (double)tiles;
     if (RB == WIDE_ROWS) {
         const double whole = blocks <= 256 ? 1.5 * t : 2.6 * t * (double)((blocks + 511) / 512);
-        return blocks >= 2048 || whole <= 6 + std::max(1.5 * MIN_PIECE, 1.3 * t * b);
+        const double join = 6 + 8 * std::min(1.0, t * b / (2 * MIN_PIECE));
+        return whole <= join + std::max(1.5 * MIN_PIECE, 1.3 * t * b);
     }
     const double tile = head_dim == 64 ? 0.3 : 0.45, full = head_dim == 64 ? 0.32 : 0.63;
     return t * std::max(tile, full * b) <= 5 + std::max(tile * MIN_PIECE, full * t * b);
@@ -1615,7 +1616,7 @@ wnw_status quant_heads(const wnw_quant_config &c, int32_t n_layers, int32_t q_he
 {
     if (q_heads < c.kv_heads || q_heads % c.kv_heads) return quant_fail(WNW_ERR_INVALID, "q_heads must be a multiple of kv_heads");
     if (max_len < 0) return quant_fail(WNW_ERR_INVALID, "negative max_len");
-    if ((int64_t)c.batch * n_layers * q_heads > Q_MAX_GROUPS / std::max(n, 1))
+    if ((int64_t)c.batch * n_layers * q_heads > (n > 1 ? INT32_MAX / n : Q_MAX_GROUPS))
         return quant_fail(WNW_ERR_UNSUPPORTED, "too many query rows");
     // the line of tiles is counted in 32 bits
     const int64_t blocks = ((int64_t)q_heads / c.kv_heads * n + 15) / 16 * c.batch * n_layers * c.kv_heads;
@@ -1707,7 +1708,7 @@ wnw_status wnw_quant_attend(const wnw_quant_config *cfg, const wnw_quant_cache *
         return quant_fail(WNW_ERR_INVALID, "workspace missing, too small or not aligned to 16 bytes");
     const int G = q_heads / cfg->kv_heads, R = G * n;
     char *ws = (char *)workspace;
-    QuantAttend a = {quant_geo(*cfg, *cache, first_layer, n_layers), G, n, R, p.W, p.RB, p.whole ? (R + p.RB - 1) / p.RB : 0, 1.f / p.W, (const uint16_t *)q_dev, len_dev, count_dev,
+    QuantAttend a = {quant_geo(*cfg, *cache, first_layer, n_layers), G, n, R, p.W, p.RB, p.RB == 16 ? 4 : p.RB == 32 ? 5 : 7, p.whole ? (R + p.RB - 1) / p.RB : 0, 1.f / p.W, (const uint16_t *)q_dev, len_dev, count_dev,
                      out_dev, lse_dev, mass_dev, (float *)ws, (float2 *)(ws + p.o_bytes),
                      (float2 *)(ws + p.o_bytes + p.ml_bytes), (float *)(ws + p.o_bytes + p.ml_bytes + p.row_bytes),
                      Q_LOG2E / sqrtf((float)cfg->head_dim)};
