@@ -1549,8 +1549,8 @@ void quant_dispatch(const wnw_quant_config &c, F f)
 // Whether every block of rows gets a work-group of its own rather than blocks being cut into even parts and joined by a
 // second launch.  Times in us, measured: a tile of a work-group that has its compute unit nearly alone (`tile`: 0.45 in the token
 // kernels of d = 128, four wavefronts in turn, 0.3 of d = 64; 1.5 in the wide kernel); a tile when the chip is full (`full`, a compute
-// unit's time: the token kernels' bytes at 6.5 TB/s; 1.3); and the join: its launch, the search for the parts (5, 6) and, in
-// the wide kernel, the parts' results to memory and back (8 for 512 of them).  Measured whole and cut, d = 128, tiles of one
+// unit's time: the token kernels' bytes at 6.5 TB/s; 1.3); and the join: its launch, which costs the host 3 as well, the search
+// for the parts (6) and, in the wide kernel, the parts' results to memory and back (8 for 512 of them).  Measured whole and cut, d = 128, tiles of one
 // token: 8 blocks of 12 10.6 and 11.6 us, of 20 14.3 and 13.2; 72 of 16 13.0 and 14.0, of 32 19.7 and 17.2; 128 of 32 20.3 and
 // 21.7, of 63 33.8 and 31.8; 240 of 243 153 and 160, of 1423 848 and 866; d = 64: 8 of 16 8.1 and 8.7, of 32 12.1 and 10.0; 128
 // of 32 13.7 and 15.3, of 63 22.1 and 19.0; a draft of five on 720 of 147, 23 and 73 178 and 203; the wide kernel: 16 blocks of 4
@@ -1564,7 +1564,7 @@ bool whole_blocks(int RB, int head_dim, int64_t blocks, int64_t tiles)
         return whole <= join + std::max(1.5 * MIN_PIECE, 1.3 * t * b);
     }
     const double tile = head_dim == 64 ? 0.3 : 0.45, full = head_dim == 64 ? 0.32 : 0.63;
-    return t * std::max(tile, full * b) <= 5 + std::max(tile * MIN_PIECE, full * t * b);
+    return t * std::max(tile, full * b) <= 6 + std::max(tile * MIN_PIECE, full * t * b);
 }
 
 // How an attention call runs: rows of a block, work-groups, loads past the caches; output rows; the workspace's arrays.

@@ -265,15 +265,21 @@ class QuantCache:
         # checked once here, for calls that are made for every layer and token
         _on(t.get_device(), t, _dtypes()[_F32 if name.endswith("scale") else _U8], None, name)
         object.__setattr__(self, name, t)
+        object.__setattr__(self, "_" + name, (t.get_device(), t.numel()))
 
     def _struct(self, cfg, device):
         n = cfg.batch * cfg.layers * cfg.kv_heads * cfg.capacity
-        need = (n * cfg.head_dim, n * cfg.head_dim, n // max(cfg.block, 1), n // max(cfg.block, 1))
-        tensors = (self.k, self.v, self.k_scale, self.v_scale)
-        for t, numel, what in zip(tensors, need, ("k", "v", "k_scale", "v_scale")):
+        need, scales = (device, n * cfg.head_dim), (device, n // (cfg.block or 1))
+        if self._k != need or self._v != need or self._k_scale != scales or self._v_scale != scales:
+            self._refuse(need, scales)
+        return wnw_quant_cache(self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr())
+
+    def _refuse(self, need, scales):
+        """Raises unless every buffer is on the device and has the elements it needs (or more)."""
+        for name, (device, numel) in (("k", need), ("v", need), ("k_scale", scales), ("v_scale", scales)):
+            t = getattr(self, name)
             if t.get_device() != device or t.numel() < numel:
-                raise ValueError(f"{what}: needs {numel} elements on cuda:{device}, got {t.numel()} on {t.device}")
-        return wnw_quant_cache(*[t.data_ptr() for t in tensors])
+                raise ValueError(f"{name}: needs {numel} elements on cuda:{device}, got {t.numel()} on {t.device}")
 
 
 def make_quant_config(batch, layers, kv_heads, capacity, block, format, head_dim=128, flags=0) -> wnw_quant_config:
@@ -330,9 +336,15 @@ def _quant_shape(cfg, t, heads, what):
     return shape[1], shape[3]
 
 
-def _quant_device():
+def _quant_place(stream):
+    """(index of the current device, stream handle): where a call's work runs."""
     import torch
-    return torch.cuda.current_device()
+    device = torch.cuda.current_device()
+    if stream is not None:
+        return device, getattr(stream, "cuda_stream", stream)
+    # the handle alone: a Stream object costs 2.5 us, as much as a launch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return device, raw(device) if raw else torch.cuda.current_stream().cuda_stream
 
 
 def wnw_quant_write(cfg, cache, k_dev, v_dev, pos_dev, count_dev=None, first_layer=0, stream=None):
@@ -341,10 +353,10 @@ def wnw_quant_write(cfg, cache, k_dev, v_dev, pos_dev, count_dev=None, first_lay
     nl, n = _quant_shape(cfg, k_dev, cfg.kv_heads, "k_dev")
     if v_dev.shape != k_dev.shape:
         raise ValueError(f"v_dev: expected {list(k_dev.shape)}, got {list(v_dev.shape)}")
-    dev, k, B = _quant_device(), _dtypes(), cfg.batch
+    (dev, st), k, B = _quant_place(stream), _DTYPES or _dtypes(), cfg.batch
     _qcheck(lib.wnw_quant_write(cfg, cache._struct(cfg, dev), first_layer, nl, n, _on(dev, k_dev, k[_BF16], None, "k_dev"),
                                 _on(dev, v_dev, k[_BF16], None, "v_dev"), _on(dev, pos_dev, k[_I32], B, "pos_dev"),
-                                _on(dev, count_dev, k[_I32], B, "count_dev"), _stream(stream)))
+                                _on(dev, count_dev, k[_I32], B, "count_dev"), st))
 
 
 def wnw_quant_read(cfg, cache, k_out, v_out, pos_dev, count_dev=None, first_layer=0, stream=None):
@@ -356,11 +368,11 @@ def wnw_quant_read(cfg, cache, k_out, v_out, pos_dev, count_dev=None, first_laye
     nl, n = _quant_shape(cfg, some, cfg.kv_heads, "k_out" if k_out is not None else "v_out")
     if v_out is not None and v_out.shape != some.shape:
         raise ValueError(f"v_out: expected {list(some.shape)}, got {list(v_out.shape)}")
-    dev, k, B = _quant_device(), _dtypes(), cfg.batch
+    (dev, st), k, B = _quant_place(stream), _DTYPES or _dtypes(), cfg.batch
     out = k[_BF16 if cfg.flags & WNW_F_OUT_BF16 else _F32]
     _qcheck(lib.wnw_quant_read(cfg, cache._struct(cfg, dev), first_layer, nl, n, _on(dev, k_out, out, None, "k_out"),
                                _on(dev, v_out, out, None, "v_out"), _on(dev, pos_dev, k[_I32], B, "pos_dev"),
-                               _on(dev, count_dev, k[_I32], B, "count_dev"), _stream(stream)))
+                               _on(dev, count_dev, k[_I32], B, "count_dev"), st))
 
 
 def wnw_quant_attend_workspace(cfg, n_layers, q_heads, n, max_len=0) -> int:
@@ -380,7 +392,7 @@ def wnw_quant_attend(cfg, cache, q_dev, out_dev, len_dev, count_dev=None, lse_de
     nl, n = _quant_shape(cfg, q_dev, Hq, "q_dev")
     if out_dev.shape != shape:
         raise ValueError(f"out_dev: expected {list(shape)}, got {list(out_dev.shape)}")
-    dev, k, B = _quant_device(), _dtypes(), cfg.batch
+    (dev, st), k, B = _quant_place(stream), _DTYPES or _dtypes(), cfg.batch
     rows = B * nl * Hq
     _qcheck(lib.wnw_quant_attend(
         cfg, cache._struct(cfg, dev), first_layer, nl, Hq, n, _on(dev, q_dev, k[_BF16], None, "q_dev"),
@@ -388,7 +400,7 @@ def wnw_quant_attend(cfg, cache, q_dev, out_dev, len_dev, count_dev=None, lse_de
         _on(dev, out_dev, k[_BF16 if cfg.flags & WNW_F_OUT_BF16 else _F32], None, "out_dev"),
         _on(dev, lse_dev, k[_F32], rows * n, "lse_dev"),
         _on(dev, mass_dev, k[_F32], rows * (cfg.capacity // max(cfg.block, 1)), "mass_dev"), max_len,
-        _on(dev, workspace, k[_U8], None, "workspace"), 0 if workspace is None else workspace.numel(), _stream(stream)))
+        _on(dev, workspace, k[_U8], None, "workspace"), 0 if workspace is None else workspace.numel(), st))
 
 
 def wnw_append_kv(ctx, k_new_dev, v_new_dev, stream=None):
