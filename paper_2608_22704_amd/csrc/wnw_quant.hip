@@ -694,13 +694,13 @@ __device__ inline void weights_to_half(const float (&p)[8], h8_t &hi, h8_t &lo)
 // K's of the next tile are under way from the end of the first products on, V's from the end of the second.  Registers are
 // left for two blocks of 16 rows and two wavefronts on every SIMD.
 // The wavefronts' results meet in shared memory at the end, in the tiles' place.
-template <int DH, int MT>
+template <int DH, int MT, int NW>
 struct QuantTokenSmem {
     union {
-        alignas(16) qu4_t tile[4][2][DH / 16 * 64];    // [wavefront][K, V]
-        alignas(16) float o[4][32][DH];                // in the wavefront's own tile: others may still be reading theirs
+        alignas(16) qu4_t tile[NW][2][DH / 16 * 64];    // [wavefront][K, V]
+        alignas(16) float o[NW][32][DH];                // in the wavefront's own tile: others may still be reading theirs
     };
-    float m[4][16 * MT], l[4][16 * MT];
+    float m[NW][16 * MT], l[NW][16 * MT];
     float2 whole[16 * MT];                             // maximum and 1 / sum of a block that is not to be joined
     static_assert(sizeof(tile) == sizeof(o) && MT <= 2, "a wavefront's results fit its tile");
     // 16-byte unit u of a row of o, spread over the banks
@@ -776,8 +776,8 @@ __device__ inline void mass_shares(const QuantAttend &a, size_t row, int len, in
 }
 
 // Tiles ta .. tb - 1 of block rb of head (b, hd)'s rows; slot: where a piece's result goes (-1: the block is whole).
-template <int DH, int FMT, bool F32, int MT, bool NTL>
-__device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH, MT> &sm, const QuantSeq &sq, int b, int hd,
+template <int DH, int FMT, bool F32, int MT, bool NTL, int NW>
+__device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH, MT, NW> &sm, const QuantSeq &sq, int b, int hd,
                                          int rb, int ta, int tb, int slot)
 {
     constexpr int NJ = DH / 64, ND = DH / 16, RB = 16 * MT;
@@ -832,10 +832,10 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
         for (int dt = 0; dt < ND; ++dt) o[r][dt] = qf4_t{0.f, 0.f, 0.f, 0.f};
     }
     int vexp = -100;           // o is in units of 2^(vexp - 15); V scales seen so far are below 2^vexp
-    for (; t < t_end; t += 4) {
+    for (; t < t_end; t += NW) {
         const int key0 = t * QT + quarter * 4;
         const bool masked = t * QT + QT > full;   // some row does not see all of the tile
-        const bool more = t + 4 < t_end;
+        const bool more = t + NW < t_end;
         float s[MT][4][4], ksc[4], vsc[4];
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb) {
@@ -863,7 +863,7 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
         }
         __builtin_amdgcn_sched_barrier(0);
         __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the bytes have been read
-        if (more) load_k(t + 4);
+        if (more) load_k(t + NW);
         __builtin_amdgcn_sched_barrier(0);
 
         // the largest V scale of the tile's blocks of live rows
@@ -978,7 +978,7 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
         }
         __builtin_amdgcn_sched_barrier(0);
         __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (more) load_v(t + 4);
+        if (more) load_v(t + NW);
         __builtin_amdgcn_sched_barrier(0);
     }
 
@@ -995,17 +995,17 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
     }
     __syncthreads();
     const QuantAttend &z = late_args();
-    for (int row = threadIdx.x >> 4; row < RB; row += Q_THREADS / 16) {
+    for (int row = threadIdx.x >> 4; row < RB; row += NW * 4) {
         const int d0 = (threadIdx.x & 15) * (DH / 16);
         const QuantRow rr = quant_row(z, hd, rb * RB + row, len, cnt);
         if (rr.vis < 0) continue;
         float mm = -INFINITY, ll = 0.f, x[DH / 16];
 #pragma unroll
-        for (int w = 0; w < 4; ++w) mm = fmaxf(mm, sm.m[w][row]);
+        for (int w = 0; w < NW; ++w) mm = fmaxf(mm, sm.m[w][row]);
 #pragma unroll
         for (int e = 0; e < DH / 16; ++e) x[e] = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < NW; ++w) {
             const float lw = sm.l[w][row], f = lw == 0.f ? 0.f : exp2f(sm.m[w][row] - finite_or_zero(mm));   // 0: saw nothing
             ll += f * lw;
 #pragma unroll
@@ -1039,14 +1039,16 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
         // nobody joins this block: its tiles' sums become shares here (n = 1: row r is q-head r)
         __syncthreads();
         const int rows = min(RB, z.R - rb * RB), blocks = z.g.cap >> z.g.bsh;
-        for (int row = wave; row < rows; row += 4) {
+        for (int row = wave; row < rows; row += NW) {
             const float2 mi = sm.whole[row];
             mass_shares(z, (size_t)hd * z.G + rb * RB + row, len, blocks, lane, 64, mi.x, mi.y);
         }
     }
 }
 
-// Work-groups that a compute unit holds: of d = 128 two by shared memory, of d = 64 with one block of rows three by registers.
+// Work-groups of NW wavefronts that a compute unit holds: of d = 128 two of four by shared memory, of d = 64 with one block of
+// rows three by registers.  Eight are for launches that leave a compute unit to each work-group: a round of tiles is one
+// wavefront's instructions one after the other, which two on a SIMD overlap.
 template <int DH, int MT>
 constexpr int token_held()
 {
@@ -1100,12 +1102,12 @@ __device__ inline void quant_parts(const QuantAttend &a, F f)
     }
 }
 
-template <int DH, int FMT, bool F32, int MT, bool NTL>
-__global__ __launch_bounds__(Q_THREADS, (token_held<DH, MT>())) void quant_token_kernel(QuantAttend a)
+template <int DH, int FMT, bool F32, int MT, bool NTL, int NW>
+__global__ __launch_bounds__(64 * NW, (NW == 8 ? 2 : token_held<DH, MT>())) void quant_token_kernel(QuantAttend a)
 {
-    __shared__ QuantTokenSmem<DH, MT> sm;
+    __shared__ QuantTokenSmem<DH, MT, NW> sm;
     quant_parts(a, [&](const QuantSeq &sq, int b, int hd, int rb, int ta, int tb, int slot) {
-        quant_token_block<DH, FMT, F32, MT, NTL>(a, sm, sq, b, hd, rb, ta, tb, slot);
+        quant_token_block<DH, FMT, F32, MT, NTL, NW>(a, sm, sq, b, hd, rb, ta, tb, slot);
     });
 }
 
@@ -1547,15 +1549,16 @@ void quant_dispatch(const wnw_quant_config &c, F f)
 }
 
 // Whether every block of rows gets a work-group of its own rather than blocks being cut into even parts and joined by a
-// second launch.  Times in us, measured: a tile of a work-group that has its compute unit nearly alone (`tile`: 0.45 in the token
-// kernels of d = 128, four wavefronts in turn, 0.3 of d = 64; 1.5 in the wide kernel); a tile when the chip is full (`full`, a compute
-// unit's time: the token kernels' bytes at 6.5 TB/s; 1.3); and the join: its launch, which costs the host 3 as well, the search
-// for the parts (6) and, in the wide kernel, the parts' results to memory and back (8 for 512 of them).  Measured whole and cut, d = 128, tiles of one
-// token: 8 blocks of 12 10.6 and 11.6 us, of 20 14.3 and 13.2; 72 of 16 13.0 and 14.0, of 32 19.7 and 17.2; 128 of 32 20.3 and
-// 21.7, of 63 33.8 and 31.8; 240 of 243 153 and 160, of 1423 848 and 866; d = 64: 8 of 16 8.1 and 8.7, of 32 12.1 and 10.0; 128
-// of 32 13.7 and 15.3, of 63 22.1 and 19.0; a draft of five on 720 of 147, 23 and 73 178 and 203; the wide kernel: 16 blocks of 4
-// 12.7 and 14.9, of 12 24.5 and 19.1; 256 of 32 58 and 72, of 243 369 and 310; 1024 of 63 285 and 321.
-bool whole_blocks(int RB, int head_dim, int64_t blocks, int64_t tiles)
+// second launch.  Times in us, measured: a tile of a work-group that has its compute unit nearly alone (`tile`, four
+// wavefronts in turn; `own`, as launched whole: eight of them, or four behind loads past the caches); a tile when the chip is
+// full (`full`, a compute unit's time: the token kernels' bytes at 6.5 TB/s); and the join: its launch, which costs the host 3
+// as well, the search for the parts (6) and, in the wide kernel, the parts' results to memory and back (8 for 512 of them).
+// Measured whole and cut, tiles of one token, d = 128: 8 blocks of 12 9.3 and 10.5 us, of 24 13.2 and 12.3; 72 of 16 11.9 and
+// 13.4, of 47 23.6 and 17.6; 128 of 32 18.4 and 20.8, of 63 29.4 and 30.5; 240 of 243 153 and 160, of 1423 848 and 866; d = 64:
+// 8 of 16 7.2 and 8.8, of 47 13.0 and 10.3; 72 of 32 10.9 and 12.6; five tokens of four heads: 8 of 8 12.6 and 13.6, of 32 23.8
+// and 19.1; 720 blocks of 147, 23 and 73 178 and 203; the wide kernel: 16 of 4 12.7 and 14.9, of 12 24.5 and 19.1; 256 of 32 58
+// and 72, of 243 369 and 310; 1024 of 63 285 and 321.
+bool whole_blocks(int RB, int head_dim, int64_t blocks, int64_t tiles, bool eight, bool stream)
 {
     const double b = blocks / 256.0, t = (double)tiles;
     if (RB == WIDE_ROWS) {
@@ -1563,14 +1566,16 @@ bool whole_blocks(int RB, int head_dim, int64_t blocks, int64_t tiles)
         const double join = 6 + 8 * std::min(1.0, t * b / (2 * MIN_PIECE));
         return whole <= join + std::max(1.5 * MIN_PIECE, 1.3 * t * b);
     }
-    const double tile = head_dim == 64 ? 0.3 : 0.45, full = head_dim == 64 ? 0.32 : 0.63;
-    return t * std::max(tile, full * b) <= 6 + std::max(tile * MIN_PIECE, full * t * b);
+    const bool half = head_dim == 64;
+    const double tile = half ? 0.3 : RB == 32 ? 0.6 : 0.45, full = half ? 0.32 : 0.63;
+    const double own = eight ? (half ? 0.18 : RB == 32 ? 0.47 : 0.35) : stream && !half ? 0.55 : tile;
+    return t * std::max(own, full * b) <= 6 + std::max(tile * MIN_PIECE, full * t * b);
 }
 
 // How an attention call runs: rows of a block, work-groups, loads past the caches; output rows; the workspace's arrays.
 struct QuantPlan {
     int RB, W;
-    bool whole, stream;
+    bool whole, eight, stream;
     int64_t rows, o_bytes, ml_bytes, row_bytes, m_bytes;
     int64_t total() const { return o_bytes + ml_bytes + row_bytes + m_bytes; }
 };
@@ -1588,10 +1593,16 @@ QuantPlan quant_plan(const wnw_quant_config &c, int32_t n_layers, int32_t q_head
     // Work-groups: one for every block of rows; or as many as the chip's 256 compute units hold at once, or as pieces of
     // MIN_PIECE tiles need.
     const int held = 256 * (c.head_dim == 64 && p.RB == 16 ? token_held<64, 1>() : 2);
-    p.whole = whole_blocks(p.RB, c.head_dim, blocks, (len + QT - 1) / QT);
-    p.W = (int)std::max<int64_t>(1, p.whole ? blocks : std::min<int64_t>(held, tiles / MIN_PIECE + blocks));
     // Bytes that one pass reads once and the 256 MB of the last-level cache cannot keep for the next one
     p.stream = R <= p.RB && heads * len * c.head_dim * 2 > (256ll << 20);
+    // Eight wavefronts instead of four for work-groups that have a compute unit each and a second round of tiles to share out
+    // (128 blocks of 63 tiles 33.9 -> 29.4 us, 72 of 63 with d = 64 21.7 -> 17.0, 8 of 8 no difference).  Loads past the caches
+    // that four wavefronts' instructions keep up with run 1 to 2 % faster with four (d = 128 and one block of 16 rows: 293.6
+    // and 299.0 us for 30000 rows of 240 blocks; 32 rows 337 and 315, d = 64 149 and 145).
+    p.eight = p.RB != WIDE_ROWS && blocks <= 256 && len > 8 * QT && !(p.stream && p.RB == 16 && c.head_dim == 128);
+    p.whole = whole_blocks(p.RB, c.head_dim, blocks, (len + QT - 1) / QT, p.eight, p.stream);
+    p.eight = p.eight && p.whole;
+    p.W = (int)std::max<int64_t>(1, p.whole ? blocks : std::min<int64_t>(held, tiles / MIN_PIECE + blocks));
     p.rows = heads * R;
     p.o_bytes = p.whole ? 0 : (int64_t)p.W * 2 * p.RB * c.head_dim * 4;
     p.ml_bytes = p.whole ? 0 : (int64_t)p.W * 2 * p.RB * 8;
@@ -1600,16 +1611,23 @@ QuantPlan quant_plan(const wnw_quant_config &c, int32_t n_layers, int32_t q_head
     return p;
 }
 
+template <int DH, int FMT, bool F32, int MT>
+void launch_few(const QuantPlan &p, const QuantAttend &a, hipStream_t st)
+{
+    constexpr bool both = DH == 64 || MT == 2;
+    auto *k = p.eight ? (p.stream ? quant_token_kernel<DH, FMT, F32, MT, both, 8> : quant_token_kernel<DH, FMT, F32, MT, false, 8>)
+                      : (p.stream ? quant_token_kernel<DH, FMT, F32, MT, true, 4> : quant_token_kernel<DH, FMT, F32, MT, false, 4>);
+    hipLaunchKernelGGL(k, dim3(p.W), dim3(p.eight ? 512 : 256), 0, st, a);
+}
 template <int DH, int FMT, bool F32>
 void launch_token(const QuantPlan &p, const QuantAttend &a, hipStream_t st)
 {
-    if (p.RB == WIDE_ROWS) {
+    if (p.RB == WIDE_ROWS)
         hipLaunchKernelGGL((quant_wide_kernel<DH, FMT, F32>), dim3(p.W), dim3(Q_THREADS), 0, st, a);
-        return;
-    }
-    auto *k = p.RB == 16 ? (p.stream ? quant_token_kernel<DH, FMT, F32, 1, true> : quant_token_kernel<DH, FMT, F32, 1, false>)
-                         : (p.stream ? quant_token_kernel<DH, FMT, F32, 2, true> : quant_token_kernel<DH, FMT, F32, 2, false>);
-    hipLaunchKernelGGL(k, dim3(p.W), dim3(Q_THREADS), 0, st, a);
+    else if (p.RB == 32)
+        launch_few<DH, FMT, F32, 2>(p, a, st);
+    else
+        launch_few<DH, FMT, F32, 1>(p, a, st);
 }
 
 wnw_status quant_heads(const wnw_quant_config &c, int32_t n_layers, int32_t q_heads, int32_t n, int32_t max_len)

@@ -318,12 +318,18 @@ def test_attend_split_cache(W, fmt, n):
 # are joined, or equal parts of all tiles in a line.  (lens, n, counts, layers, KV heads, group, block, d)
 SHARED = {
     "token, a block each": ([900, 0, 64, 333], 1, None, 6, 8, 4, 32, 128),
+    "token, a block each, d = 64": ([960, 577, 0], 1, None, 4, 8, 4, 32, 64),
+    "token, a block each, streamed": ([9000], 1, None, 30, 8, 4, 16, 64),
+    "token, many blocks": ([500, 30, 0, 449, 512], 1, None, 8, 8, 3, 16, 128),
     "token, pieces": ([5000, 63, 4097], 1, None, 2, 3, 2, 16, 128),
     "token, pieces, many sequences": ([3000 - 23 * b if b % 7 else b for b in range(130)], 1, None, 1, 1, 2, 64, 128),
     "token, a line": ([10240, 10000], 1, None, 5, 17, 3, 64, 128),
     "token, a line, d = 64": ([36000, 35999], 1, None, 7, 10, 1, 32, 64),
     "32 rows, pieces": ([4000, 700], 6, [6, 5], 2, 3, 4, 64, 128),
     "32 rows, a block each": ([400, 70, 3], 6, [6, 5, 3], 10, 8, 5, 16, 64),
+    "32 rows, a block each, many tiles": ([700, 130, 65], 6, [6, 5, 3], 10, 8, 5, 16, 64),
+    "32 rows, a block each, d = 128": ([640, 129], 5, [5, 2], 8, 8, 4, 64, 128),
+    "32 rows, a block each, streamed": ([4500], 5, [5], 30, 8, 4, 64, 128),
     "many rows, pieces": ([2000, 900], 50, [50, 33], 2, 2, 3, 16, 128),
     "many rows, a line": ([700], 41, [41], 20, 30, 1, 32, 64),
     "many rows, a block each": ([200, 130], 140, [140, 100], 2, 2, 5, 32, 128),
