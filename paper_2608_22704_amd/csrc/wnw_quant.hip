@@ -2,6 +2,7 @@
 // bytes.  Layout and formats as in wnw.h.
 //
 //   quant_write_kernel   a tile of 64 rows of one head's K or V per work-group
+//   quant_append_kernel  up to 16 new rows of one head's K or V per wavefront
 //   quant_read_kernel    the same tiles back to fp32 / bf16
 //   quant_token_kernel   attention of up to 32 query rows of a KV-head: every byte of K and V comes from HBM once
 //   quant_wide_kernel    attention of many query rows: tiles become fp16 in shared memory once for 128 rows
@@ -372,6 +373,140 @@ __global__ __launch_bounds__(Q_THREADS) void quant_write_kernel(QuantGeo g, int 
 
 // ---- reading back ----------------------------------------------------------------------------
 
+// A few rows: n <= APPEND_ROWS, which lie in two groups of 16 rows (that start at multiples of 16) and two scale blocks at most.
+// A wavefront has a head's K or V: what a launch of a work-group a tile spends its time on is starting wavefronts (the
+// chip starts one in about 0.5 ns), of which three or four of four had nothing to write.  Lanes as there, for each of the
+// groups; V's dwords of old and new rows take the new ones as bytes.  Old rows are only read when their scale grows.
+constexpr int APPEND_ROWS = 16;
+template <int DH, int FMT>
+__global__ __launch_bounds__(Q_THREADS) void quant_append_kernel(QuantGeo g, int n, int items, const uint16_t *__restrict__ kn,
+                                                                const uint16_t *__restrict__ vn,
+                                                                const int32_t *__restrict__ pos_dev,
+                                                                const int32_t *__restrict__ count_dev)
+{
+    constexpr int E = DH / 16;
+    constexpr unsigned ZERO = FMT == WNW_QUANT_INT8 ? 0x80808080u : 0u;
+    const int item = (int)uniform(blockIdx.x * 4 + (threadIdx.x >> 6));
+    if (item >= items) return;
+    const bool is_v = item & 1;
+    const int hd = item >> 1, b = hd / (g.nl * g.H);
+    const int pos = q_clamp(pos_dev[b], g.cap), cnt = count_dev ? q_clamp(count_dev[b], n) : n, end = min(pos + cnt, g.cap);
+    if (pos >= end) return;
+    const int lane = threadIdx.x & 63, dg = lane & 15, r4 = lane >> 4;
+    const size_t head = g.head(b, hd - b * g.nl * g.H);
+    uint8_t *codes = const_cast<uint8_t *>(is_v ? g.v : g.k) + head * g.cap * DH;
+    float *scales = const_cast<float *>(is_v ? g.vs : g.ks) + ((head * g.cap) >> g.bsh);
+    const uint16_t *src = (is_v ? vn : kn) + (size_t)hd * n * DH + (size_t)dg * E;
+
+    const int grp = pos >> 4, groups = end > (grp + 1) * 16 ? 2 : 1, block = pos >> g.bsh;
+    const bool has_old = (block << g.bsh) < pos, two = (end - 1) >> g.bsh != block;   // two blocks: the groups' own
+    const float was = has_old ? scales[block] : 0.f;
+    auto row_of = [&](int u, int i) { return (grp + u) * 16 + r4 * 4 + i; };
+    auto put = [&](int u, int i) { return row_of(u, i) >= pos && row_of(u, i) < end; };
+    // dword of the lane's four rows of a group at its dimension e, and bytes of its row i
+    auto at_v = [&](int group, int e) { return (size_t)(group >> 2) * QT * DH + (dg * E + e) * QT + r4 * 16 + (group & 3) * 4; };
+    auto at_k = [&](int group, int i) { return (size_t)(group * 16 + r4 * 4 + i) * DH + dg * E; };
+
+    uint16_t in[2][4][E];
+    unsigned amax[2] = {0, 0};
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        if (u < groups) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) in[u][i][e] = 0;
+                if (put(u, i)) load_row<E>(in[u][i], src + (size_t)(row_of(u, i) - pos) * DH);
+            }
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        if (u < groups) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int e = 0; e < E; ++e) amax[u] = max(amax[u], (unsigned)in[u][i][e] & 0x7fffu);
+            amax[u] = wave_max(amax[u]) << 16;
+        }
+    }
+    if (!two) amax[0] = amax[1] = max(amax[0], amax[1]);
+    float s[2] = {quant_scale<FMT>(amax[0]), quant_scale<FMT>(amax[1])};
+    // a NaN on either side stays one
+    if (has_old) s[0] = was != was || s[0] != s[0] ? __uint_as_float(0x7fc00000u) : fmaxf(was, s[0]);
+    if (!two) s[1] = s[0];
+    if (lane == 0) {
+        scales[block] = s[0];
+        if (two) scales[block + 1] = s[1];
+    }
+    if (has_old && s[0] > was) {      // (false for a NaN)
+        const float ratio = was * (1.f / s[0]);
+        const int first = block << (g.bsh - 4);
+        unsigned had[4][E];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const int group = first + w, row = group * 16 + r4 * 4;
+            if (row >= pos) continue;
+            if (is_v) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) had[w][e] = *(const unsigned *)(codes + at_v(group, e));
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    __builtin_memcpy(&had[w][i * (E / 4)], __builtin_assume_aligned(codes + at_k(group, i), E), E);
+            }
+        }
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const int group = first + w, row = group * 16 + r4 * 4, old = pos - row;
+            if (old <= 0) continue;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                unsigned x = requant4<FMT>(had[w][e], was, s[0], ratio);
+                if (is_v) {
+                    const unsigned keep = old >= 4 ? 0u : ~0u << (8 * old);
+                    *(unsigned *)(codes + at_v(group, e)) = (had[w][e] & keep) | (x & ~keep);
+                } else if (e / (E / 4) < old)
+                    *(unsigned *)(codes + at_k(group, e / (E / 4)) + e % (E / 4) * 4) = x;
+            }
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        if (u >= groups) break;
+        const float inv = 1.f / s[u];
+        const bool good = s[u] == s[u];
+        auto x = [&](int i, int e) { return __uint_as_float((unsigned)in[u][i][e] << 16); };
+        if (is_v) {
+            if (!(put(u, 0) || put(u, 1) || put(u, 2) || put(u, 3))) continue;
+            unsigned w[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) w[e] = good ? quant4<FMT>(x(0, e), x(1, e), x(2, e), x(3, e), s[u], inv) : ZERO;
+            if (put(u, 0) && put(u, 3)) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) *(unsigned *)(codes + at_v(grp + u, e)) = w[e];
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (put(u, i)) {
+#pragma unroll
+                        for (int e = 0; e < E; ++e) codes[at_v(grp + u, e) + i] = (uint8_t)(w[e] >> (8 * i));
+                    }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (!put(u, i)) continue;
+                unsigned w[E / 4];
+#pragma unroll
+                for (int e = 0; e < E; e += 4)
+                    w[e / 4] = good ? quant4<FMT>(x(i, e), x(i, e + 1), x(i, e + 2), x(i, e + 3), s[u], inv) : ZERO;
+                __builtin_memcpy(__builtin_assume_aligned(codes + at_k(grp + u, i), E), w, E);
+            }
+        }
+    }
+}
+
 template <int E, bool BF16>
 __device__ inline void store_row(void *out, size_t elem, const float (&x)[E])
 {
@@ -410,7 +545,8 @@ __global__ __launch_bounds__(Q_THREADS) void quant_read_kernel(QuantGeo g, int n
     unsigned t[E];           // V: of the lane's dimensions, a byte for each of its rows
     if (!is_v) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i) {
+            if (row0 + rg * 4 + i < pos || row0 + rg * 4 + i >= end) continue;
 #pragma unroll
             for (int j = 0; j < RUNS; ++j) {
                 const uint8_t *p = codes + (size_t)(rg * 4 + i) * DH + d0 + j * 64;
@@ -421,6 +557,7 @@ __global__ __launch_bounds__(Q_THREADS) void quant_read_kernel(QuantGeo g, int n
                 } else
                     w[i][j] = __builtin_nontemporal_load((const unsigned *)p);
             }
+        }
     } else {
 #pragma unroll
         for (int u = tid; u < DH * 4; u += Q_THREADS)
@@ -1669,9 +1806,15 @@ wnw_status wnw_quant_write(const wnw_quant_config *cfg, const wnw_quant_cache *c
     if (groups > Q_MAX_GROUPS) return quant_fail(WNW_ERR_UNSUPPORTED, "too many rows for one call");
     const QuantGeo g = quant_geo(*cfg, *cache, first_layer, n_layers);
     quant_dispatch(*cfg, [&](auto d, auto f) {
-        hipLaunchKernelGGL((quant_write_kernel<decltype(d)::value, decltype(f)::value>), dim3((unsigned)groups), dim3(Q_THREADS), 0,
-                           (hipStream_t)hip_stream, g, n, (int)tiles, (const uint16_t *)k_dev, (const uint16_t *)v_dev, pos_dev,
-                           count_dev);
+        constexpr int DH = decltype(d)::value, FMT = decltype(f)::value;
+        const uint16_t *k = (const uint16_t *)k_dev, *v = (const uint16_t *)v_dev;
+        const int heads = cfg->batch * n_layers * cfg->kv_heads;
+        if (n <= APPEND_ROWS)
+            hipLaunchKernelGGL((quant_append_kernel<DH, FMT>), dim3((unsigned)(heads + 1) / 2), dim3(Q_THREADS), 0, (hipStream_t)hip_stream, g,
+                               n, 2 * heads, k, v, pos_dev, count_dev);
+        else
+            hipLaunchKernelGGL((quant_write_kernel<DH, FMT>), dim3((unsigned)groups), dim3(Q_THREADS), 0, (hipStream_t)hip_stream, g, n,
+                               (int)tiles, k, v, pos_dev, count_dev);
     });
     return quant_hip();
 }

@@ -103,6 +103,34 @@ def test_writes(W, fmt, block, D, which):
 
 
 @pytest.mark.parametrize("fmt", [R.INT8, R.E4M3])
+@pytest.mark.parametrize("block,D", [(16, 64), (32, 128), (64, 128)])
+@pytest.mark.parametrize("n", [2, 5, 13, 16, 17])
+def test_a_few_rows_at_a_time(W, fmt, block, D, n):
+    """Up to n rows per call and sequence, across every boundary, until the cache is full; sizes that make scales grow."""
+    log(f"[case] quant write, {n} rows at a time, fmt={fmt} block={block} d={D}")
+    B, L, H, cap = 3, 1, 3, 192
+    cfg = W.make_quant_config(B, L, H, cap, block, fmt, head_dim=D)
+    c = new_cache(W, cfg)
+    refs = [R.Cache(B, L, H, cap, D, block, fmt) for _ in range(2)]
+    g = np.random.default_rng(n)
+    pos = [0, 0, 0]
+    written = np.zeros((B, L, H, cap), dtype=bool)
+    call = 0
+    while min(pos) < cap:
+        count = [int(k) for k in g.integers(0, n + 1, B)]
+        x = [rows(100 * call + j, B, L, H, n, D, spread=2.0) for j in range(2)]
+        W.wnw_quant_write(cfg, c, x[0].cuda(), x[1].cuda(), i32(pos), i32(count))
+        for ref, t in zip(refs, x):
+            ref.write(t.double().numpy(), pos, count)
+        for b in range(B):
+            written[b, ..., pos[b]: pos[b] + count[b]] = True
+            pos[b] += count[b]
+        call += 1
+    torch.cuda.synchronize()
+    check_cache(c, refs, written, fmt)
+
+
+@pytest.mark.parametrize("fmt", [R.INT8, R.E4M3])
 @pytest.mark.parametrize("block", [16, 64])
 def test_rows_one_by_one(W, fmt, block):
     """A row per call, of growing and shrinking sizes: a block's rows are rounded again as its scale grows."""
