@@ -223,7 +223,10 @@ __device__ inline uint16_t to_bf16(float f)
 // ---- writing ---------------------------------------------------------------------------------
 
 // Work-group: one tile of 64 rows of one head, K (even) or V (odd).  Wavefront w has rows 16 w .. + 16; its lane has rows
-// 4 rg .. + 4 (rg = 4 w + lane / 16) at dimensions E (lane % 16) .. + E.
+// 4 rg .. + 4 (rg = 4 w + lane / 16) at dimensions E (lane % 16) .. + E, so that a block's maximum is one of a wavefront or of
+// neighbours, and four of a lane's values are a dword of K or of V.
+// Bound by memory: two bytes of a value come, one goes.  15512 rows of 240 KV-heads (2.86 GB) 492 us, 5.8 TB/s; 7756 of 72
+// (429 MB) 90 us, 4.8 TB/s.  Stores past the caches made no difference.
 // Dwords of four rows at one dimension, transposed through shared memory for whole tiles of V.
 template <int DH>
 struct QuantTileSmem {
@@ -377,6 +380,8 @@ __global__ __launch_bounds__(Q_THREADS) void quant_write_kernel(QuantGeo g, int 
 // A wavefront has a head's K or V: what a launch of a work-group a tile spends its time on is starting wavefronts (the
 // chip starts one in about 0.5 ns), of which three or four of four had nothing to write.  Lanes as there, for each of the
 // groups; V's dwords of old and new rows take the new ones as bytes.  Old rows are only read when their scale grows.
+// 7 rows of 720 KV-heads 12-19 -> 6-8 us, one row of 3840 22-36 -> 15 us, of 240 4-5 either way, of 8 (int8) 3.9.  Small
+// calls wait for the chain position, rows, maximum, bytes; large ones for V's lines, of which a row has a byte each.
 constexpr int APPEND_ROWS = 16;
 template <int DH, int FMT>
 __global__ __launch_bounds__(Q_THREADS) void quant_append_kernel(QuantGeo g, int n, int items, const uint16_t *__restrict__ kn,
@@ -522,6 +527,8 @@ __device__ inline void store_row(void *out, size_t elem, const float (&x)[E])
 // Work-group and rows of a lane as in quant_write_kernel; its dimensions are E neighbours for bf16 and runs of four,
 // 64 apart, for fp32, so that every store of a wavefront fills whole lines.  Everything passes through once: streamed
 // (7756 rows of 72 KV-heads as bf16 77 -> 62 us; with eight neighbours as fp32, halves of lines, 185 -> 231 us).
+// Bound by memory: 15512 rows of 240 KV-heads as bf16 (2.86 GB) 494 us, 5.8 TB/s; four sequences of up to 7756 rows of 72
+// KV-heads as fp32 159 us; 64 rows of 720 KV-heads 13.5 us, of which starting 11520 wavefronts is 5.
 template <int DH, int FMT, bool BF16>
 __global__ __launch_bounds__(Q_THREADS) void quant_read_kernel(QuantGeo g, int n, int tiles, void *__restrict__ ko,
                                                               void *__restrict__ vo, const int32_t *__restrict__ pos_dev,
@@ -831,6 +838,12 @@ __device__ inline void weights_to_half(const float (&p)[8], h8_t &hi, h8_t &lo)
 // K's of the next tile are under way from the end of the first products on, V's from the end of the second.  Registers are
 // left for two blocks of 16 rows and two wavefronts on every SIMD.
 // The wavefronts' results meet in shared memory at the end, in the tiles' place.
+// Memory bounds long caches (two operations a byte and query row), and the bytes in flight decide, 64 KB a work-group: 15512
+// rows of 240 KV-heads, four query rows each, 151 us, 6.3 TB/s (a loop of loads alone reads 6.9), the matrix cores 8 % busy,
+// fetched bytes 1.006 of the cache's; 91024 rows 865 us, 6.45 TB/s; five tokens of three sequences (20 query rows) 171 us,
+// 5.6 TB/s.  Short calls wait for instructions, each fetched once, and for the chain length, tile, products, softmax,
+// products: 8 KV-heads of 1064 rows 13 us, of 512 rows 8.5.
+// Slower: tiles through registers instead of shared memory; two groups of wavefronts on a tile (a draft 269 -> 342 us).
 template <int DH, int MT, int NW>
 struct QuantTokenSmem {
     union {
@@ -1257,6 +1270,12 @@ __global__ __launch_bounds__(64 * NW, (NW == 8 ? 2 : token_held<DH, MT>())) void
 //   elements are P^T's operand as they stand.
 // A row's maximum m is raised, and its output and sum scaled, only when a logit exceeds it by LAZY (base 2): weights
 // are up to 2^LAZY then, which fp16 has room for.
+// Bound by the matrix cores and the vector unit taking turns within the card's power limit: a wavefront's tile is 32
+// products (1024 cycles) and about 280 vector instructions, which the two work-groups of a compute unit overlap.  512 tokens
+// of four heads over 15512 rows of 16 KV-heads 295 us and a join of 13, 836 TFLOP/s; 1024 tokens over 8000 rows of 32
+// KV-heads 564 us, 952 TFLOP/s (a large product of the library: 1149 in bf16, 1107 in fp16).  Fetched bytes are eight times
+// the cache's (every XCD reads all of it), from the last-level cache.  Conversions between the products instead of before them
+// gained 1.5 % (d = 64 lost 2), raised priority around the products 2 %: neither is kept.
 constexpr int WIDE_ROWS = 128;   // 2^7: see QuantAttend::rsh
 constexpr int LAZY = 8;
 
@@ -1520,7 +1539,8 @@ struct QuantPieces {
 };
 
 // Single tokens: a work-group per output row.  A lane has a piece's statistics; the wavefronts share the pieces' sums.  Makes
-// the tiles' block sums shares of the whole as well.
+// the tiles' block sums shares of the whole as well.  576 rows of 7 pieces 5.4 us, 512 of 16 sequences 7.6: a launch and three
+// dependent loads.
 template <int DH, bool BF16>
 __global__ __launch_bounds__(Q_THREADS) void quant_merge_kernel(QuantAttend a)
 {
@@ -1578,7 +1598,7 @@ __global__ __launch_bounds__(Q_THREADS) void quant_merge_kernel(QuantAttend a)
     if (a.mass) mass_shares(a, row, sq.len, g.cap >> g.bsh, tid, Q_THREADS, m, sum == 0.f ? 0.f : 1.f / sum);
 }
 
-// Several tokens: a work-group per 16 rows of a head, sixteen threads a row.
+// Several tokens: a work-group per 16 rows of a head, sixteen threads a row.  32768 rows of two or three pieces 12.6 us, 46 MB.
 template <int DH, bool BF16>
 __global__ __launch_bounds__(Q_THREADS) void quant_merge_rows_kernel(QuantAttend a)
 {
@@ -1869,8 +1889,9 @@ wnw_status wnw_quant_attend(const wnw_quant_config *cfg, const wnw_quant_cache *
         return quant_fail(WNW_ERR_INVALID, "workspace missing, too small or not aligned to 16 bytes");
     const int G = q_heads / cfg->kv_heads, R = G * n;
     char *ws = (char *)workspace;
-    QuantAttend a = {quant_geo(*cfg, *cache, first_layer, n_layers), G, n, R, p.W, p.RB, p.RB == 16 ? 4 : p.RB == 32 ? 5 : 7, p.whole ? (R + p.RB - 1) / p.RB : 0, 1.f / p.W, (const uint16_t *)q_dev, len_dev, count_dev,
-                     out_dev, lse_dev, mass_dev, (float *)ws, (float2 *)(ws + p.o_bytes),
+    QuantAttend a = {quant_geo(*cfg, *cache, first_layer, n_layers), G, n, R, p.W, p.RB, p.RB == 16 ? 4 : p.RB == 32 ? 5 : 7,
+                     p.whole ? (R + p.RB - 1) / p.RB : 0, 1.f / p.W, (const uint16_t *)q_dev, len_dev, count_dev, out_dev,
+                     lse_dev, mass_dev, (float *)ws, (float2 *)(ws + p.o_bytes),
                      (float2 *)(ws + p.o_bytes + p.ml_bytes), (float *)(ws + p.o_bytes + p.ml_bytes + p.row_bytes),
                      Q_LOG2E / sqrtf((float)cfg->head_dim)};
     const bool bf16 = cfg->flags & WNW_F_OUT_BF16;
