@@ -262,24 +262,20 @@ class QuantCache:
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
 
     def __setattr__(self, name, t):
-        # checked once here, for calls that are made for every layer and token
+        # type and layout are checked once here, device and size by every call
         _on(t.get_device(), t, _dtypes()[_F32 if name.endswith("scale") else _U8], None, name)
         object.__setattr__(self, name, t)
-        object.__setattr__(self, "_" + name, (t.get_device(), t.numel()))
 
     def _struct(self, cfg, device):
         n = cfg.batch * cfg.layers * cfg.kv_heads * cfg.capacity
-        need, scales = (device, n * cfg.head_dim), (device, n // (cfg.block or 1))
-        if self._k != need or self._v != need or self._k_scale != scales or self._v_scale != scales:
-            self._refuse(need, scales)
-        return wnw_quant_cache(self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr())
-
-    def _refuse(self, need, scales):
-        """Raises unless every buffer is on the device and has the elements it needs (or more)."""
-        for name, (device, numel) in (("k", need), ("v", need), ("k_scale", scales), ("v_scale", scales)):
-            t = getattr(self, name)
-            if t.get_device() != device or t.numel() < numel:
-                raise ValueError(f"{name}: needs {numel} elements on cuda:{device}, got {t.numel()} on {t.device}")
+        need, scales = n * cfg.head_dim, n // (cfg.block or 1)
+        k, v, ks, vs = self.k, self.v, self.k_scale, self.v_scale
+        if (k.numel() < need or v.numel() < need or ks.numel() < scales or vs.numel() < scales or k.get_device() != device
+                or v.get_device() != device or ks.get_device() != device or vs.get_device() != device):
+            for name, t, numel in (("k", k, need), ("v", v, need), ("k_scale", ks, scales), ("v_scale", vs, scales)):
+                if t.get_device() != device or t.numel() < numel:
+                    raise ValueError(f"{name}: needs {numel} elements on cuda:{device}, got {t.numel()} on {t.device}")
+        return wnw_quant_cache(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr())
 
 
 def make_quant_config(batch, layers, kv_heads, capacity, block, format, head_dim=128, flags=0) -> wnw_quant_config:

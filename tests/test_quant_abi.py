@@ -148,6 +148,18 @@ def test_binding_refuses_buffers(W):
         W.wnw_quant_read(cfg, c, None, None, None)
 
 
+@pytest.mark.parametrize("name", ["k", "v", "k_scale", "v_scale"])
+def test_binding_refuses_a_buffer_that_shrank(W, name):
+    """The size is read when a call is made, not when the cache was put together."""
+    cfg = W.make_quant_config(1, 2, 1, 128, 32, W.WNW_QUANT_INT8, head_dim=64)
+    c = W.make_quant_cache(cfg, device="cpu")
+    c._struct(cfg, -1)
+    t = getattr(c, name)
+    t.resize_(t.numel() - 1)
+    with pytest.raises(ValueError, match=name):
+        c._struct(cfg, -1)
+
+
 def test_places_of_a_v_tile():
     """Row 16 b + 4 h + i at 16 h + 4 b + i: a permutation, and what the reference encodes it decodes."""
     assert sorted(R.v_place(r) for r in range(64)) == list(range(64))
