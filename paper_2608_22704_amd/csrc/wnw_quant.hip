@@ -1745,7 +1745,7 @@ QuantPlan quant_plan(const wnw_quant_config &c, int32_t n_layers, int32_t q_head
     const int64_t heads = (int64_t)c.batch * n_layers * c.kv_heads, R = (int64_t)q_heads / c.kv_heads * n;
     const int64_t len = max_len ? std::min(max_len, c.capacity) : c.capacity;
     QuantPlan p;
-    p.RB = R > 32 ? WIDE_ROWS : R > 16 ? 32 : 16;
+    p.RB = R > 32 && n > 1 ? WIDE_ROWS : R > 16 ? 32 : 16;     // (only the token kernels make masses)
     const int64_t blocks = heads * ((R + p.RB - 1) / p.RB), tiles = (len + QT - 1) / QT * blocks;
     // Work-groups: one for every block of rows; or as many as the chip's 256 compute units hold at once, or as pieces of
     // MIN_PIECE tiles need.

@@ -301,6 +301,8 @@ SHAPES = [
     ([2500], 1, [1], 1, 16, 16, 128),
     ([700], 1, [1], 1, 20, 32, 64),
     ([700, 3], 1, [1, 1], 2, 5, 64, 128),
+    ([333, 70, 0], 1, [1, 1, 1], 1, 40, 32, 64),
+    ([500], 1, [1], 2, 71, 16, 128),
     ([300, 2, 64, 0], 4, [4, 2, 3, 4], 2, 2, 32, 128),
     ([515, 80], 5, [5, 3], 1, 8, 64, 128),
     ([200, 17], 17, [17, 17], 2, 3, 16, 64),
@@ -351,6 +353,7 @@ SHARED = {
     "token, many blocks": ([500, 30, 0, 449, 512], 1, None, 8, 8, 3, 16, 128),
     "token, pieces": ([5000, 63, 4097], 1, None, 2, 3, 2, 16, 128),
     "token, pieces, many sequences": ([3000 - 23 * b if b % 7 else b for b in range(130)], 1, None, 1, 1, 2, 64, 128),
+    "token, pieces, 37 q-heads": ([5000, 63], 1, None, 1, 1, 37, 64, 128),
     "token, a line": ([10240, 10000], 1, None, 5, 17, 3, 64, 128),
     "token, a line, d = 64": ([36000, 35999], 1, None, 7, 10, 1, 32, 64),
     "32 rows, pieces": ([4000, 700], 6, [6, 5], 2, 3, 4, 64, 128),
