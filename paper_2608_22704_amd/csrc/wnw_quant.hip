@@ -5,7 +5,7 @@
 //   quant_append_kernel  up to 16 new rows of one head's K or V per wavefront
 //   quant_read_kernel    the same tiles back to fp32 / bf16
 //   quant_token_kernel   attention of up to 32 query rows of a KV-head: every byte of K and V comes from HBM once
-//   quant_wide_kernel    attention of many query rows: tiles become fp16 in shared memory once for 128 rows
+//   quant_wide_kernel    attention of many query rows: tiles become fp16 in shared memory once for 128 (64) rows
 //   quant_merge_kernel, quant_merge_rows_kernel   join the parts of a cache that work-groups shared
 //
 // Bytes become fp16 on the way to the matrix cores, exactly: integers up to 127 and e4m3 numbers both fit.
@@ -1268,6 +1268,8 @@ __global__ __launch_bounds__(64 * NW, (NW == 8 ? 2 : token_held<DH, MT>())) void
 //   S^T (32 keys x 32 rows) = K Q^T and O^T (32 dimensions x 32 rows) += V^T P^T by 32 x 32 x 16 products (see wnw_lds.h for
 //   operands): a lane has 16 keys of ONE row, elements 0 .. 7 in the tile's 16-row block 2 k and 8 .. 15 in 2 k + 1, so that S^T's
 //   elements are P^T's operand as they stand.
+// KS = 2, for 33 to 64 rows: two wavefronts share 32 rows, each with half of every tile's keys, and join at the end (with
+// two of four wavefronts idle instead: 64 rows of 240 KV-heads over 15512 rows 300 -> 225 us, as fp32 367 -> 261).
 // A row's maximum m is raised, and its output and sum scaled, only when a logit exceeds it by LAZY (base 2): weights
 // are up to 2^LAZY then, which fp16 has room for.
 // Bound by the matrix cores and the vector unit taking turns within the card's power limit: a wavefront's tile is 32
@@ -1288,6 +1290,12 @@ struct QuantWideSmem {
     static constexpr unsigned K_ROW = DH * 2 + 16, V_ROW = QT * 2 + 16, K_BYTES = QT * K_ROW, BUF = K_BYTES + DH * V_ROW;
     alignas(256) unsigned char tile[2][BUF];   // K, then V
 };
+// In the tiles' place at the end, where two wavefronts share 32 rows: sums, maximum and sum of weights of the second.
+template <int DH>
+struct QuantWideJoin {
+    qf4_t o[2][DH / 8][64];
+    float2 ml[2][64];
+};
 __device__ inline h8_t lds_read(unsigned at)
 {
     return __builtin_bit_cast(h8_t, *(const __attribute__((address_space(3))) qu4_t *)(size_t)at);
@@ -1303,15 +1311,16 @@ __device__ inline qu4_t convert8(unsigned a, unsigned b)
     return __builtin_bit_cast(qu4_t, bytes_to_h8<FMT>(a, b));
 }
 
-template <int DH, int FMT, bool F32>
+template <int DH, int FMT, bool F32, int KS>
 __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> &sm, const QuantSeq &sq, int b, int hd, int rb,
                                         int ta, int tb, int slot)
 {
-    constexpr int NS = DH / 16, ND = DH / 32, RB = WIDE_ROWS;
+    constexpr int NS = DH / 16, ND = DH / 32, RB = WIDE_ROWS / KS, NB = 2 / KS;    // NB: blocks of 32 keys of a wavefront
     const QuantGeo &g = a.g;
     const int len = sq.len, cnt = sq.cnt;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, half = lane >> 5;
+    const int rows32 = KS == 2 ? wave & 1 : wave, key32 = KS == 2 ? wave >> 1 : 0;    // the wavefront's rows, and its keys of a tile
     const size_t head = g.head(b, hd - b * g.nl * g.H);
     const uint8_t *kh = g.k + head * g.cap * DH, *vh = g.v + head * g.cap * DH;
     const float *ks = g.ks + ((head * g.cap) >> g.bsh), *vs = g.vs + ((head * g.cap) >> g.bsh);
@@ -1339,8 +1348,8 @@ __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> 
     const unsigned lds = uniform(lds_address(sm.tile[0]));
     const unsigned k_put = lds + key_t * SM::K_ROW + part_t * KL * 32,
                    v_put = lds + SM::K_BYTES + d_t * SM::V_ROW + half_t * 16;
-    const unsigned k_get = lds + col * SM::K_ROW + half * 16,
-                   v_get = lds + SM::K_BYTES + col * SM::V_ROW + half * 16;
+    const unsigned k_get = lds + (col + key32 * 32) * SM::K_ROW + half * 16,
+                   v_get = lds + SM::K_BYTES + col * SM::V_ROW + half * 16 + key32 * 64;
     auto store = [&](int t, unsigned buf) {
 #pragma unroll
         for (int j = 0; j < KL; ++j) {
@@ -1364,7 +1373,7 @@ __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> 
     };
     if (ta < t_end) load(ta);
 
-    const QuantRow qr = quant_row(a, hd, rb * RB + wave * 32 + col, len, cnt);
+    const QuantRow qr = quant_row(a, hd, rb * RB + rows32 * 32 + col, len, cnt);
     h8_t qf[NS];
     float crow;
     {
@@ -1398,39 +1407,40 @@ __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> 
     auto round = [&](int t, auto buf_c, auto masked_c) {
         const unsigned buf = buf_c, other = SM::BUF - buf;
         constexpr bool MASKED = decltype(masked_c)::value;
-        float f[4], vsc[4];
+        const int row = t * QT + key32 * 32;      // of the cache, the wavefront's first
+        float f[2 * NB], vsc[2 * NB];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            f[c] = crow * scalar_load(ks, (t * QT + c * 16) >> g.bsh);
-            vsc[c] = scalar_load(vs, (t * QT + c * 16) >> g.bsh);
+        for (int c = 0; c < 2 * NB; ++c) {
+            f[c] = crow * scalar_load(ks, (row + c * 16) >> g.bsh);
+            vsc[c] = scalar_load(vs, (row + c * 16) >> g.bsh);
         }
-        f32x16_t x[2];
+        f32x16_t x[NB];
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+        for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[kb][i] = 0.f;
 #pragma unroll
         for (int s = 0; s < NS; ++s)
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
+            for (int kb = 0; kb < NB; ++kb)
                 x[kb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds_read(k_get + s * 32 + kb * 32 * SM::K_ROW + buf), qf[s], x[kb], 0,
                                                                0, 0);
         // element i of x[kb] is of key 32 kb + 8 (i / 4) + i % 4 from here; `vis` is the row's limit from here
-        const int vis = qr.vis - (t * QT + half * 4);
+        const int vis = qr.vis - (row + half * 4);
         if constexpr (MASKED) {
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
+            for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) x[kb][i] = 32 * kb + 8 * (i / 4) + i % 4 < vis ? x[kb][i] * f[2 * kb + i / 8] : -INFINITY;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < 2 * NB; ++c) {
                 f[c] = 1.f;
-                vsc[c] = t * QT + c * 16 < len ? vsc[c] : 0.f;
+                vsc[c] = row + c * 16 < len ? vsc[c] : 0.f;
             }
         }
         float top = -INFINITY, vmax = 0.f;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < 2 * NB; ++c) {
             float y = x[c >> 1][8 * (c & 1)];
 #pragma unroll
             for (int i = 1; i < 8; ++i) y = fmaxf(y, x[c >> 1][8 * (c & 1) + i]);
@@ -1451,9 +1461,9 @@ __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> 
             vexp = ve;
         }
         const float mz = finite_or_zero(m), vf = pow2i(15 - LAZY - vexp);
-        h8_t ph[4], pl[4];
+        h8_t ph[2 * NB], pl[2 * NB];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < 2 * NB; ++c) {
             const float w = vsc[c] * vf;
             float p[8], part = 0.f;
 #pragma unroll
@@ -1474,7 +1484,7 @@ __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> 
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < 2 * NB; ++c) {
                 const h8_t v = lds_read(v_get + c * 32 + dt * 32 * SM::V_ROW + buf);
                 o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, ph[c], o[dt], 0, 0, 0);
                 if constexpr (F32) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pl[c], o[dt], 0, 0, 0);
@@ -1490,10 +1500,37 @@ __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> 
     }
     for (; t < t_end; ++t) round(t, (t - ta) & 1 ? SM::BUF : 0u, std::true_type{});
     sum += __shfl_xor(sum, 32);
+    float unit = pow2i(vexp + LAZY - 15);
+    if constexpr (KS == 2) {
+        // the keys' halves meet: the second's result to the same lane of the first's wavefront
+        static_assert(sizeof(QuantWideJoin<DH>) <= sizeof(sm));
+        QuantWideJoin<DH> &jn = *(QuantWideJoin<DH> *)&sm;
+        if (key32) {
+#pragma unroll
+            for (int u = 0; u < ND * 4; ++u)
+                jn.o[rows32][u][lane] =
+                    qf4_t{o[u / 4][u % 4 * 4], o[u / 4][u % 4 * 4 + 1], o[u / 4][u % 4 * 4 + 2], o[u / 4][u % 4 * 4 + 3]} * unit;
+            jn.ml[rows32][lane] = make_float2(m, sum);
+        }
+        __syncthreads();
+        if (key32) return;
+        const float2 ml = jn.ml[rows32][lane];
+        const float mm = fmaxf(m, ml.x), mz = finite_or_zero(mm);
+        const float f0 = sum == 0.f ? 0.f : exp2f(m - mz), f1 = ml.y == 0.f ? 0.f : exp2f(ml.x - mz);    // 0: saw nothing
+        sum = f0 * sum + f1 * ml.y;
+        m = mm;
+#pragma unroll
+        for (int u = 0; u < ND * 4; ++u) {
+            const qf4_t y = jn.o[rows32][u][lane];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[u / 4][u % 4 * 4 + e] = f0 * (o[u / 4][u % 4 * 4 + e] * unit) + f1 * y[e];
+        }
+        unit = 1.f;
+    }
     if (qr.vis < 0) return;
     // element i of o[dt]: dimension 32 dt + 8 (i / 4) + 4 half + i % 4 of row col
-    const float unit = pow2i(vexp + LAZY - 15), inv = sum == 0.f ? 0.f : 1.f / sum;
-    const size_t at = slot >= 0 ? (size_t)(blockIdx.x * 2 + slot) * RB + wave * 32 + col : (size_t)qr.row_of;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const size_t at = slot >= 0 ? (size_t)(blockIdx.x * 2 + slot) * RB + rows32 * 32 + col : (size_t)qr.row_of;
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
@@ -1515,12 +1552,12 @@ __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> 
     }
 }
 
-template <int DH, int FMT, bool F32>
+template <int DH, int FMT, bool F32, int KS>
 __global__ __launch_bounds__(Q_THREADS, 2) void quant_wide_kernel(QuantAttend a)
 {
     __shared__ QuantWideSmem<DH> sm;
     quant_parts(a, [&](const QuantSeq &sq, int b, int hd, int rb, int ta, int tb, int slot) {
-        quant_wide_block<DH, FMT, F32>(a, sm, sq, b, hd, rb, ta, tb, slot);
+        quant_wide_block<DH, FMT, F32, KS>(a, sm, sq, b, hd, rb, ta, tb, slot);
     });
 }
 
@@ -1714,11 +1751,12 @@ void quant_dispatch(const wnw_quant_config &c, F f)
 // 13.4, of 47 23.6 and 17.6; 128 of 32 18.4 and 20.8, of 63 29.4 and 30.5; 240 of 243 153 and 160, of 1423 848 and 866; d = 64:
 // 8 of 16 7.2 and 8.8, of 47 13.0 and 10.3; 72 of 32 10.9 and 12.6; five tokens of four heads: 8 of 8 12.6 and 13.6, of 32 23.8
 // and 19.1; 720 blocks of 147, 23 and 73 178 and 203; the wide kernel: 16 of 4 12.7 and 14.9, of 12 24.5 and 19.1; 256 of 32 58
-// and 72, of 243 369 and 310; 1024 of 63 285 and 321.
+// and 72, of 243 369 and 310; 1024 of 63 285 and 321; its blocks of 64 rows: 8 of 5 10.6 and 12.8, of 16 20.4 and 14.9, 240 of 8
+// 16.4 and 19.3, of 63 84 and 85, of 243 254 and 228.
 bool whole_blocks(int RB, int head_dim, int64_t blocks, int64_t tiles, bool eight, bool stream)
 {
     const double b = blocks / 256.0, t = (double)tiles;
-    if (RB == WIDE_ROWS) {
+    if (RB > 32) {
         const double whole = blocks <= 256 ? 1.5 * t : 2.6 * t * (double)((blocks + 511) / 512);
         const double join = 6 + 8 * std::min(1.0, t * b / (2 * MIN_PIECE));
         return whole <= join + std::max(1.5 * MIN_PIECE, 1.3 * t * b);
@@ -1731,7 +1769,7 @@ bool whole_blocks(int RB, int head_dim, int64_t blocks, int64_t tiles, bool eigh
 
 // How an attention call runs: rows of a block, work-groups, loads past the caches; output rows; the workspace's arrays.
 struct QuantPlan {
-    int RB, W;
+    int RB, W;       // RB 16, 32, 64 or 128
     bool whole, eight, stream;
     int64_t rows, o_bytes, ml_bytes, row_bytes, m_bytes;
     int64_t total() const { return o_bytes + ml_bytes + row_bytes + m_bytes; }
@@ -1745,7 +1783,8 @@ QuantPlan quant_plan(const wnw_quant_config &c, int32_t n_layers, int32_t q_head
     const int64_t heads = (int64_t)c.batch * n_layers * c.kv_heads, R = (int64_t)q_heads / c.kv_heads * n;
     const int64_t len = max_len ? std::min(max_len, c.capacity) : c.capacity;
     QuantPlan p;
-    p.RB = R > 32 && n > 1 ? WIDE_ROWS : R > 16 ? 32 : 16;     // (only the token kernels make masses)
+    // (only the token kernel makes masses)
+    p.RB = n > 1 && R > 64 ? WIDE_ROWS : n > 1 && R > 32 ? WIDE_ROWS / 2 : R > 16 ? 32 : 16;
     const int64_t blocks = heads * ((R + p.RB - 1) / p.RB), tiles = (len + QT - 1) / QT * blocks;
     // Work-groups: one for every block of rows; or as many as the chip's 256 compute units hold at once, or as pieces of
     // MIN_PIECE tiles need.
@@ -1756,7 +1795,7 @@ QuantPlan quant_plan(const wnw_quant_config &c, int32_t n_layers, int32_t q_head
     // (128 blocks of 63 tiles 33.9 -> 29.4 us, 72 of 63 with d = 64 21.7 -> 17.0, 8 of 8 no difference).  Loads past the caches
     // that four wavefronts' instructions keep up with run 1 to 2 % faster with four (d = 128 and one block of 16 rows: 293.6
     // and 299.0 us for 30000 rows of 240 blocks; 32 rows 337 and 315, d = 64 149 and 145).
-    p.eight = p.RB != WIDE_ROWS && blocks <= 256 && len > 8 * QT && !(p.stream && p.RB == 16 && c.head_dim == 128);
+    p.eight = p.RB <= 32 && blocks <= 256 && len > 8 * QT && !(p.stream && p.RB == 16 && c.head_dim == 128);
     p.whole = whole_blocks(p.RB, c.head_dim, blocks, (len + QT - 1) / QT, p.eight, p.stream);
     p.eight = p.eight && p.whole;
     p.W = (int)std::max<int64_t>(1, p.whole ? blocks : std::min<int64_t>(held, tiles / MIN_PIECE + blocks));
@@ -1780,7 +1819,9 @@ template <int DH, int FMT, bool F32>
 void launch_token(const QuantPlan &p, const QuantAttend &a, hipStream_t st)
 {
     if (p.RB == WIDE_ROWS)
-        hipLaunchKernelGGL((quant_wide_kernel<DH, FMT, F32>), dim3(p.W), dim3(Q_THREADS), 0, st, a);
+        hipLaunchKernelGGL((quant_wide_kernel<DH, FMT, F32, 1>), dim3(p.W), dim3(Q_THREADS), 0, st, a);
+    else if (p.RB == WIDE_ROWS / 2)
+        hipLaunchKernelGGL((quant_wide_kernel<DH, FMT, F32, 2>), dim3(p.W), dim3(Q_THREADS), 0, st, a);
     else if (p.RB == 32)
         launch_few<DH, FMT, F32, 2>(p, a, st);
     else
@@ -1889,7 +1930,7 @@ wnw_status wnw_quant_attend(const wnw_quant_config *cfg, const wnw_quant_cache *
         return quant_fail(WNW_ERR_INVALID, "workspace missing, too small or not aligned to 16 bytes");
     const int G = q_heads / cfg->kv_heads, R = G * n;
     char *ws = (char *)workspace;
-    QuantAttend a = {quant_geo(*cfg, *cache, first_layer, n_layers), G, n, R, p.W, p.RB, p.RB == 16 ? 4 : p.RB == 32 ? 5 : 7,
+    QuantAttend a = {quant_geo(*cfg, *cache, first_layer, n_layers), G, n, R, p.W, p.RB, p.RB == 16 ? 4 : p.RB == 32 ? 5 : p.RB == 64 ? 6 : 7,
                      p.whole ? (R + p.RB - 1) / p.RB : 0, 1.f / p.W, (const uint16_t *)q_dev, len_dev, count_dev, out_dev,
                      lse_dev, mass_dev, (float *)ws, (float2 *)(ws + p.o_bytes),
                      (float2 *)(ws + p.o_bytes + p.ml_bytes), (float *)(ws + p.o_bytes + p.ml_bytes + p.row_bytes),

@@ -310,6 +310,7 @@ SHAPES = [
     ([300, 130], 130, [129, 130], 1, 4, 64, 128),
     ([130, 90], 130, [130, 130], 1, 2, 16, 128),
     ([1500, 3], 40, [40, 2], 1, 7, 32, 64),
+    ([70, 32, 33], 11, [11, 11, 3], 2, 3, 16, 128),
 ]
 
 
@@ -362,7 +363,10 @@ SHARED = {
     "32 rows, a block each, d = 128": ([640, 129], 5, [5, 2], 8, 8, 4, 64, 128),
     "32 rows, a block each, streamed": ([4500], 5, [5], 30, 8, 4, 64, 128),
     "many rows, pieces": ([2000, 900], 50, [50, 33], 2, 2, 3, 16, 128),
-    "many rows, a line": ([700], 41, [41], 20, 30, 1, 32, 64),
+    "64 rows, pieces": ([3000, 700], 12, [12, 7], 2, 2, 4, 64, 128),
+    "64 rows, a line": ([700], 41, [41], 20, 30, 1, 32, 64),
+    "64 rows, a block each": ([200, 130, 33, 0], 16, [16, 9, 16, 4], 4, 8, 4, 32, 128),
+    "many rows, a line": ([700], 90, [90], 20, 30, 1, 32, 64),
     "many rows, a block each": ([200, 130], 140, [140, 100], 2, 2, 5, 32, 128),
 }
 
