@@ -131,6 +131,31 @@ def test_a_few_rows_at_a_time(W, fmt, block, D, n):
 
 
 @pytest.mark.parametrize("fmt", [R.INT8, R.E4M3])
+@pytest.mark.parametrize("n", [1, 3, 20])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_writes_that_are_not_finite(W, fmt, n, bad):
+    """A block with such a row has the scale NaN, keeps it as rows join, and loses it when it is begun anew."""
+    log(f"[case] quant write, not finite, fmt={fmt} n={n} {bad}")
+    B, L, H, cap, D, block = 1, 1, 2, 128, 64, 32
+    cfg = W.make_quant_config(B, L, H, cap, block, fmt, head_dim=D)
+    c = new_cache(W, cfg)
+    refs = [R.Cache(B, L, H, cap, D, block, fmt) for _ in range(2)]
+    written = np.zeros((B, L, H, cap), dtype=bool)
+    # the bad value in head 1's K of the second call and V of the third; the last call begins the first block anew
+    for call, pos in enumerate((0, n, 2 * n, 3 * n, 0)):
+        x = [rows(10 * call + j, B, L, H, n, D) for j in range(2)]
+        if call in (1, 2):
+            x[call - 1][0, 0, 1, n - 1, 5] = bad
+        W.wnw_quant_write(cfg, c, x[0].cuda(), x[1].cuda(), i32([pos]))
+        for ref, t in zip(refs, x):
+            ref.write(t.double().numpy(), [pos], [n])
+        written[..., pos: pos + n] = True
+        torch.cuda.synchronize()
+        check_cache(c, refs, written, fmt)
+    assert not np.isnan(refs[0].scale[..., 0]).any()
+
+
+@pytest.mark.parametrize("fmt", [R.INT8, R.E4M3])
 @pytest.mark.parametrize("block", [16, 64])
 def test_rows_one_by_one(W, fmt, block):
     """A row per call, of growing and shrinking sizes: a block's rows are rounded again as its scale grows."""
@@ -343,6 +368,20 @@ def test_attend_split_cache(W, fmt, n):
     q = rows(91, 1, 1, H * G, n, D)
     want = R.attend(q.double(), k, v, lens, [n], block)
     check_attend(run_attend(W, cfg, c, q, lens, [n], count_dev=False), want, lens, [n], D, False, H)
+
+
+@pytest.mark.parametrize("n", [1, 4, 70])
+def test_lengths_and_counts_outside(W, n):
+    """Lengths and counts outside their ranges count as the nearer end."""
+    log(f"[case] quant attend, lengths outside, n={n}")
+    H, G, block, D, cap = 2, 2, 32, 64, 192
+    cfg = W.make_quant_config(4, 1, H, cap, block, R.INT8, head_dim=D)
+    c, _ = filled(W, cfg, [cap] * 4, R.INT8, 21, garbage=False)
+    q = rows(22, 4, 1, H * G, n, D)
+    got = run_attend(W, cfg, c, q, [-7, cap + 1, 2**31 - 1, 50], [n, n, n + 9, -2])
+    want = run_attend(W, cfg, c, q, [0, cap, cap, 50], [n, n, n, 0])
+    for a, b in zip(got, want):
+        assert a is b is None or torch.equal(a, b)
 
 
 # How a call is shared out depends on its blocks of query rows and their tiles: a work-group per block, even pieces that
