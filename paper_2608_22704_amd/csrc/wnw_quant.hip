@@ -265,7 +265,7 @@ __global__ __launch_bounds__(Q_THREADS) void quant_write_kernel(QuantGeo g, int 
     const int item = blockIdx.x >> 1, hd = item / tiles, b = hd / (g.nl * g.H);
     const int pos = q_clamp(pos_dev[b], g.cap), cnt = count_dev ? q_clamp(count_dev[b], n) : n, end = min(pos + cnt, g.cap);
     const int tile = pos / QT + (item - hd * tiles), row0 = tile * QT;
-    if (row0 >= end) return;
+    if (pos >= end || row0 >= end) return;      // (no rows: the scale of pos's block may be another call's to write)
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, dg = lane & 15, rg = tid >> 4;
     const size_t head = g.head(b, hd - b * g.nl * g.H);
     uint8_t *codes = const_cast<uint8_t *>(is_v ? g.v : g.k) + (head * g.cap + row0) * DH;
