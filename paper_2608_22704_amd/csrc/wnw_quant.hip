@@ -794,6 +794,13 @@ __device__ inline float pow2i(int e)   // 2^e, e in -126 .. 127 (clamped from be
     return __uint_as_float((unsigned)(max(e, -126) + 127) << 23);
 }
 
+// x 2^e for any e: one instruction, exact but for results below 2^-126.  V scales reach down to 2^-126, so that the factor
+// alone, 2^15 over a scale, can be more than fp32 holds.
+__device__ inline float times_pow2(float x, int e)
+{
+    return __builtin_amdgcn_ldexpf(x, e);
+}
+
 // 2^x by the hardware instruction alone: results below 2^-126 flush to zero, which no sum here shows (every row's
 // holds a term of 2^0).
 __device__ inline float exp2_hw(float x)
@@ -981,7 +988,7 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) o[r][dt] = qf4_t{0.f, 0.f, 0.f, 0.f};
     }
-    int vexp = -100;           // o is in units of 2^(vexp - 15); V scales seen so far are below 2^vexp
+    int vexp = -126;           // o is in units of 2^(vexp - 15); V scales seen so far are below 2^vexp
     for (; t < t_end; t += NW) {
         const int key0 = t * QT + quarter * 4;
         const bool masked = t * QT + QT > full;   // some row does not see all of the tile
@@ -1045,13 +1052,13 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
                 mt = fmaxf(mt, fmaxf(fmaxf(x[kb][0], x[kb][1]), fmaxf(x[kb][2], x[kb][3])) * f[kb]);
             mt = quarters_max(mt);
             if (ve > vexp || __any(mt > m[r])) {
-                const float alpha = exp2_hw(m[r] - finite_or_zero(mt)), f = alpha * pow2i(vexp - ve);
+                const float alpha = exp2_hw(m[r] - finite_or_zero(mt)), f = times_pow2(alpha, vexp - ve);
 #pragma unroll
                 for (int dt = 0; dt < ND; ++dt) o[r][dt] *= f;
                 sum[r] *= alpha;
                 m[r] = mt;
             }
-            const float mz = finite_or_zero(m[r]), vf = pow2i(15 - ve);
+            const float mz = finite_or_zero(m[r]);
             float bs[4];
 #pragma unroll
             for (int kb = 0; kb < 4; ++kb) {
@@ -1081,9 +1088,11 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
             }
             // P^T, times the V scales; a masked weight is 0 whatever the scale is
 #pragma unroll
-            for (int kb = 0; kb < 4; ++kb)
+            for (int kb = 0; kb < 4; ++kb) {
+                const float w = times_pow2(vsc[kb], 15 - ve);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[kb][i] *= vsc[kb] * vf;
+                for (int i = 0; i < 4; ++i) x[kb][i] *= w;
+            }
             if (masked) {
 #pragma unroll
                 for (int kb = 0; kb < 4; ++kb)
@@ -1132,7 +1141,6 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
         __builtin_amdgcn_sched_barrier(0);
     }
 
-    const float unit = pow2i(vexp - 15);
 #pragma unroll
     for (int r = 0; r < MT; ++r) {
         sum[r] = quarters_sum(sum[r]);
@@ -1141,7 +1149,12 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
             sm.l[wave][r * 16 + col] = sum[r];
         }
 #pragma unroll
-        for (int dt = 0; dt < ND; ++dt) *(qf4_t *)&sm.o[wave][r * 16 + col][sm.unit(r * 16 + col, dt * 4 + quarter)] = o[r][dt] * unit;
+        for (int dt = 0; dt < ND; ++dt) {
+            qf4_t y;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = times_pow2(o[r][dt][i], vexp - 15);
+            *(qf4_t *)&sm.o[wave][r * 16 + col][sm.unit(r * 16 + col, dt * 4 + quarter)] = y;
+        }
     }
     __syncthreads();
     const QuantAttend &z = late_args();
@@ -1397,7 +1410,7 @@ __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> 
     for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
-    int vexp = -100;           // o is in units of 2^(vexp + LAZY - 15); V scales seen so far are below 2^vexp
+    int vexp = -126;           // o is in units of 2^(vexp + LAZY - 15); V scales seen so far are below 2^vexp
     if (ta < t_end) {
         store(ta, 0);
         if (ta + 1 < t_end) load(ta + 1);
@@ -1453,18 +1466,18 @@ __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> 
         }
         const int ve = max(vexp, (int)(uniform(__float_as_uint(vmax)) >> 23) - 126);
         if (ve > vexp || __any(top > m + LAZY)) {
-            const float mn = fmaxf(m, top), alpha = exp2_hw(m - finite_or_zero(mn)), fo = alpha * pow2i(vexp - ve);
+            const float mn = fmaxf(m, top), alpha = exp2_hw(m - finite_or_zero(mn)), fo = times_pow2(alpha, vexp - ve);
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt) o[dt] *= fo;
             sum *= alpha;
             m = mn;
             vexp = ve;
         }
-        const float mz = finite_or_zero(m), vf = pow2i(15 - LAZY - vexp);
+        const float mz = finite_or_zero(m);
         h8_t ph[2 * NB], pl[2 * NB];
 #pragma unroll
         for (int c = 0; c < 2 * NB; ++c) {
-            const float w = vsc[c] * vf;
+            const float w = times_pow2(vsc[c], 15 - LAZY - vexp);
             float p[8], part = 0.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -1500,16 +1513,19 @@ __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> 
     }
     for (; t < t_end; ++t) round(t, (t - ta) & 1 ? SM::BUF : 0u, std::true_type{});
     sum += __shfl_xor(sum, 32);
-    float unit = pow2i(vexp + LAZY - 15);
+    int unit = vexp + LAZY - 15;
     if constexpr (KS == 2) {
         // the keys' halves meet: the second's result to the same lane of the first's wavefront
         static_assert(sizeof(QuantWideJoin<DH>) <= sizeof(sm));
         QuantWideJoin<DH> &jn = *(QuantWideJoin<DH> *)&sm;
         if (key32) {
 #pragma unroll
-            for (int u = 0; u < ND * 4; ++u)
-                jn.o[rows32][u][lane] =
-                    qf4_t{o[u / 4][u % 4 * 4], o[u / 4][u % 4 * 4 + 1], o[u / 4][u % 4 * 4 + 2], o[u / 4][u % 4 * 4 + 3]} * unit;
+            for (int u = 0; u < ND * 4; ++u) {
+                qf4_t y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = times_pow2(o[u / 4][u % 4 * 4 + e], unit);
+                jn.o[rows32][u][lane] = y;
+            }
             jn.ml[rows32][lane] = make_float2(m, sum);
         }
         __syncthreads();
@@ -1523,9 +1539,9 @@ __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> 
         for (int u = 0; u < ND * 4; ++u) {
             const qf4_t y = jn.o[rows32][u][lane];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[u / 4][u % 4 * 4 + e] = f0 * (o[u / 4][u % 4 * 4 + e] * unit) + f1 * y[e];
+            for (int e = 0; e < 4; ++e) o[u / 4][u % 4 * 4 + e] = f0 * times_pow2(o[u / 4][u % 4 * 4 + e], unit) + f1 * y[e];
         }
-        unit = 1.f;
+        unit = 0;
     }
     if (qr.vis < 0) return;
     // element i of o[dt]: dimension 32 dt + 8 (i / 4) + 4 half + i % 4 of row col
@@ -1537,7 +1553,7 @@ __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> 
         for (int i = 0; i < 16; i += 4) {
             float y[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = o[dt][i + e] * unit * (slot >= 0 ? 1.f : inv);
+            for (int e = 0; e < 4; ++e) y[e] = times_pow2(o[dt][i + e], unit) * (slot >= 0 ? 1.f : inv);
             const size_t to = at * DH + dt * 32 + 2 * i + 4 * half;
             if (slot >= 0)
                 *(qf4_t *)(a.ws_o + to) = qf4_t{y[0], y[1], y[2], y[3]};

@@ -1,9 +1,10 @@
-"""GPU tests of the 8-bit cache at the ends of what its header allows."""
+"""GPU tests of the 8-bit cache at the ends of what its header allows.  Tolerances of attention are those
+of test_gpu_quant.py, whose head derives them."""
 import pytest
 import torch
 
 from tests import quant_reference as R
-from tests.test_gpu_quant import i32, new_cache, rows
+from tests.test_gpu_quant import check_attend, filled, i32, new_cache, rows, run_attend
 from tests.wnw_harness import log
 
 pytestmark = pytest.mark.gpu
@@ -41,3 +42,31 @@ def test_a_sequence_that_writes_nothing(W, fmt, n):
             assert bool((t[b] == 0xA5).all()), b
         for t in (c.k_scale, c.v_scale):
             assert bool((t[b] == -7.0).all()), b
+
+
+# tokens a call of four query heads: 16, 32, 64 and 128 query rows to a block
+TOKENS = [1, 6, 12, 40]
+
+
+def scaled(c, vals, f, block):
+    """Multiplies V by 2^f[j] in block j."""
+    f = torch.pow(2.0, torch.as_tensor(f, dtype=torch.float64))
+    c.v_scale *= f.float().cuda()
+    vals[1].mul_(f.repeat_interleave(block).unsqueeze(-1))
+
+
+@pytest.mark.parametrize("fmt", [R.INT8, R.E4M3])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n", TOKENS)
+def test_smallest_v_scales(W, fmt, D, n):
+    """V scales from the smallest that a cache holds, 2^-126, on."""
+    log(f"[case] quant attend, smallest V scales, fmt={fmt} n={n} d={D}")
+    H, G, block, T, cap = 1, 4, 32, 330, 384
+    cfg = W.make_quant_config(1, 1, H, cap, block, fmt, head_dim=D)
+    c, vals = filled(W, cfg, [T], fmt, 41, garbage=False)
+    low = torch.floor(torch.log2(c.v_scale.double())).cpu().reshape(-1)
+    scaled(c, vals, -126 - low, block)
+    assert bool((c.v_scale >= 2.0 ** -126).all()) and bool((c.v_scale < 2.0 ** -125).all())
+    q = rows(42, 1, 1, H * G, n, D, spread=0.3)
+    want = R.attend(q.double(), *vals, [T], [n], block)
+    check_attend(run_attend(W, cfg, c, q, [T], [n]), want, [T], [n], D, False, H)
