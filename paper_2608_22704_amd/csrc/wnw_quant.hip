@@ -801,6 +801,16 @@ __device__ inline float times_pow2(float x, int e)
     return __builtin_amdgcn_ldexpf(x, e);
 }
 
+// The least e with all of the scales below 2^e, or -126 (a NaN, whose weights are NaN, has no say).
+template <int N>
+__device__ inline int scale_exp(const float (&s)[N])
+{
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) top = fmaxf(top, s[i]);
+    return (int)(__float_as_uint(top) >> 23) - 126;
+}
+
 // 2^x by the hardware instruction alone: results below 2^-126 flush to zero, which no sum here shows (every row's
 // holds a term of 2^0).
 __device__ inline float exp2_hw(float x)
@@ -978,6 +988,7 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
     QuantRow qr[MT];
     h8_t qf[MT][2 * NJ];
     float crow[MT], m[MT], sum[MT];
+    int vexp[MT];              // o is in units of 2^(vexp - 15); V scales of the rows that the lane's row has seen are below 2^vexp
     qf4_t o[MT][ND];
 #pragma unroll
     for (int r = 0; r < MT; ++r) {
@@ -985,10 +996,10 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
         crow[r] = load_queries<NJ>(a.q + (size_t)qr[r].row_of * DH, qr[r].vis >= 0, quarter, a.scale, qf[r]);
         m[r] = -INFINITY;
         sum[r] = 0.f;
+        vexp[r] = -126;
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) o[r][dt] = qf4_t{0.f, 0.f, 0.f, 0.f};
     }
-    int vexp = -126;           // o is in units of 2^(vexp - 15); V scales seen so far are below 2^vexp
     for (; t < t_end; t += NW) {
         const int key0 = t * QT + quarter * 4;
         const bool masked = t * QT + QT > full;   // some row does not see all of the tile
@@ -1023,22 +1034,20 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
         if (more) load_k(t + NW);
         __builtin_amdgcn_sched_barrier(0);
 
-        // the largest V scale of the tile's blocks of live rows
-        float vmax = 0.f;
-#pragma unroll
-        for (int kb = 0; kb < 4; ++kb) {
-            vsc[kb] = t * QT + kb * 16 < len ? vsc[kb] : 0.f;
-            vmax = fmaxf(vmax, vsc[kb]);
-        }
-        const int ve = max(vexp, (int)(uniform(__float_as_uint(vmax)) >> 23) - 126);
+        const int tile_exp = (int)uniform((unsigned)scale_exp(vsc));
         h8_t ph[MT][2], pl[MT][2];
 #pragma unroll
         for (int r = 0; r < MT; ++r) {
             // logits are x[kb][.] f[kb]; where masks are needed they are made here, and f is 1
-            float (&x)[4][4] = s[r], f[4];
+            float (&x)[4][4] = s[r], f[4], w[4];
+            int ve = tile_exp;
 #pragma unroll
-            for (int kb = 0; kb < 4; ++kb) f[kb] = crow[r] * ksc[kb];
+            for (int kb = 0; kb < 4; ++kb) f[kb] = crow[r] * ksc[kb], w[kb] = vsc[kb];
             if (masked) {
+                // only blocks that the row sees count: a later row's scale must not take bits from its weights
+#pragma unroll
+                for (int kb = 0; kb < 4; ++kb) w[kb] = t * QT + kb * 16 < qr[r].vis ? w[kb] : 0.f;
+                ve = scale_exp(w);
 #pragma unroll
                 for (int kb = 0; kb < 4; ++kb) {
 #pragma unroll
@@ -1051,12 +1060,14 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
             for (int kb = 0; kb < 4; ++kb)
                 mt = fmaxf(mt, fmaxf(fmaxf(x[kb][0], x[kb][1]), fmaxf(x[kb][2], x[kb][3])) * f[kb]);
             mt = quarters_max(mt);
-            if (ve > vexp || __any(mt > m[r])) {
-                const float alpha = exp2_hw(m[r] - finite_or_zero(mt)), f = times_pow2(alpha, vexp - ve);
+            ve = max(ve, vexp[r]);
+            if (__any(ve > vexp[r] || mt > m[r])) {
+                const float alpha = exp2_hw(m[r] - finite_or_zero(mt)), f = times_pow2(alpha, vexp[r] - ve);
 #pragma unroll
                 for (int dt = 0; dt < ND; ++dt) o[r][dt] *= f;
                 sum[r] *= alpha;
                 m[r] = mt;
+                vexp[r] = ve;
             }
             const float mz = finite_or_zero(m[r]);
             float bs[4];
@@ -1089,9 +1100,9 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
             // P^T, times the V scales; a masked weight is 0 whatever the scale is
 #pragma unroll
             for (int kb = 0; kb < 4; ++kb) {
-                const float w = times_pow2(vsc[kb], 15 - ve);
+                w[kb] = times_pow2(w[kb], 15 - ve);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[kb][i] *= w;
+                for (int i = 0; i < 4; ++i) x[kb][i] *= w[kb];
             }
             if (masked) {
 #pragma unroll
@@ -1106,7 +1117,6 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
                 weights_to_half<F32>(p, ph[r][c], pl[r][c]);
             }
         }
-        vexp = ve;
         if (more)
             lds_loads_wait<4 * NJ>();     // V is there, the next K may be under way
         else
@@ -1152,7 +1162,7 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
         for (int dt = 0; dt < ND; ++dt) {
             qf4_t y;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] = times_pow2(o[r][dt][i], vexp - 15);
+            for (int i = 0; i < 4; ++i) y[i] = times_pow2(o[r][dt][i], vexp[r] - 15);
             *(qf4_t *)&sm.o[wave][r * 16 + col][sm.unit(r * 16 + col, dt * 4 + quarter)] = y;
         }
     }
@@ -1410,7 +1420,7 @@ __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> 
     for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
-    int vexp = -126;           // o is in units of 2^(vexp + LAZY - 15); V scales seen so far are below 2^vexp
+    int vexp = -126;           // o is in units of 2^(vexp + LAZY - 15); V scales of the rows that the lane's row has seen are below 2^vexp
     if (ta < t_end) {
         store(ta, 0);
         if (ta + 1 < t_end) load(ta + 1);
@@ -1448,24 +1458,23 @@ __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> 
 #pragma unroll
             for (int c = 0; c < 2 * NB; ++c) {
                 f[c] = 1.f;
-                vsc[c] = row + c * 16 < len ? vsc[c] : 0.f;
+                vsc[c] = row + c * 16 < qr.vis ? vsc[c] : 0.f;      // only blocks that the row sees count, as there
             }
         }
-        float top = -INFINITY, vmax = 0.f;
+        float top = -INFINITY;
 #pragma unroll
         for (int c = 0; c < 2 * NB; ++c) {
             float y = x[c >> 1][8 * (c & 1)];
 #pragma unroll
             for (int i = 1; i < 8; ++i) y = fmaxf(y, x[c >> 1][8 * (c & 1) + i]);
             top = fmaxf(top, y * f[c]);
-            vmax = fmaxf(vmax, vsc[c]);
         }
         {
             auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
             top = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
         }
-        const int ve = max(vexp, (int)(uniform(__float_as_uint(vmax)) >> 23) - 126);
-        if (ve > vexp || __any(top > m + LAZY)) {
+        const int tile_exp = scale_exp(vsc), ve = max(vexp, MASKED ? tile_exp : (int)uniform((unsigned)tile_exp));
+        if (__any(top > m + LAZY) || __any(ve > vexp)) {
             const float mn = fmaxf(m, top), alpha = exp2_hw(m - finite_or_zero(mn)), fo = times_pow2(alpha, vexp - ve);
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt) o[dt] *= fo;

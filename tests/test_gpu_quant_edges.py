@@ -70,3 +70,23 @@ def test_smallest_v_scales(W, fmt, D, n):
     q = rows(42, 1, 1, H * G, n, D, spread=0.3)
     want = R.attend(q.double(), *vals, [T], [n], block)
     check_attend(run_attend(W, cfg, c, q, [T], [n]), want, [T], [n], D, False, H)
+
+
+@pytest.mark.parametrize("fmt", [R.INT8, R.E4M3])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n", [2, 6, 12, 40, 64])
+@pytest.mark.parametrize("before", [0, 1000])
+def test_v_scales_of_rows_not_seen(W, fmt, D, n, before):
+    """V scales that grow by 2^30 from block to block: a token's output knows nothing of the rows behind it, whose scales are
+    2^30 and more above those that it sees."""
+    log(f"[case] quant attend, V scales of later rows, fmt={fmt} n={n} d={D} rows in front {before}")
+    H, G, block = 1, 4, 16
+    T, first = before + n, before // block
+    cap = (T + 63) // 64 * 64
+    cfg = W.make_quant_config(1, 1, H, cap, block, fmt, head_dim=D)
+    c, vals = filled(W, cfg, [T], fmt, 43)
+    # (a token's own block and those behind it; all rows in front are alike)
+    scaled(c, vals, [30.0 * min(max(j - first, 0), 4) - 60 for j in range(cap // block)], block)
+    q = rows(44, 1, 1, H * G, n, D, spread=0.3)
+    want = R.attend(q.double(), *vals, [T], [n], block)
+    check_attend(run_attend(W, cfg, c, q, [T], [n]), want, [T], [n], D, False, H)
