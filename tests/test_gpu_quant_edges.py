@@ -1,10 +1,12 @@
 """GPU tests of the 8-bit cache at the ends of what its header allows.  Tolerances of attention are those
 of test_gpu_quant.py, whose head derives them."""
+import math
+
 import pytest
 import torch
 
 from tests import quant_reference as R
-from tests.test_gpu_quant import check_attend, filled, i32, new_cache, rows, run_attend
+from tests.test_gpu_quant import bound, check_attend, filled, i32, new_cache, rows, run_attend
 from tests.wnw_harness import log
 
 pytestmark = pytest.mark.gpu
@@ -90,3 +92,60 @@ def test_v_scales_of_rows_not_seen(W, fmt, D, n, before):
     q = rows(44, 1, 1, H * G, n, D, spread=0.3)
     want = R.attend(q.double(), *vals, [T], [n], block)
     check_attend(run_attend(W, cfg, c, q, [T], [n]), want, [T], [n], D, False, H)
+
+
+def check_not_finite(got, want, D, T, H):
+    """Every output has NaN and infinities exactly where the reference has, and is within its bound elsewhere."""
+    b_out, b_lse, b_mass = bound(D, [T], *want[3:], False, H)
+    checks = [("out", got[0], want[0], b_out), ("lse", got[1], want[1], b_lse + 2.0 ** -22 * want[1].abs())]
+    if got[2] is not None:       # single tokens
+        checks.append(("mass", got[2], want[2][..., 0, :], want[2][..., 0, :] * b_mass + 1e-37))
+    for name, g, w, tol in checks:
+        g = g.double().cpu()
+        assert torch.equal(torch.isnan(g), torch.isnan(w)), name
+        assert torch.equal(torch.isinf(g), torch.isinf(w)) and torch.equal(g[torch.isinf(w)], w[torch.isinf(w)]), name
+        fine = torch.isfinite(w)
+        assert bool(((g - w).abs()[fine] <= tol.expand_as(w)[fine]).all()), name
+
+
+@pytest.mark.parametrize("fmt", [R.INT8, R.E4M3])
+@pytest.mark.parametrize("n", [1, 9, 20, 70])
+@pytest.mark.parametrize("which", ["K", "V"])
+def test_a_nan_block_in_every_output(W, fmt, n, which):
+    """K's: the log-sum-exp and all masses of a token that sees it are NaN; V's: the output alone."""
+    log(f"[case] quant attend, NaN block of {which}, every output, fmt={fmt} n={n}")
+    H, G, block, D, T = 1, 3, 16, 64, 170
+    for bad in (T - n, 40, T - 1):
+        cfg = W.make_quant_config(1, 1, H, 192, block, fmt, head_dim=D)
+        c, vals = filled(W, cfg, [T], fmt, 11)
+        j = bad // block
+        (c.k_scale if which == "K" else c.v_scale)[..., j] = math.nan
+        vals[which == "V"][..., j * block: (j + 1) * block, :] = math.nan
+        q = rows(12, 1, 1, H * G, n, D)
+        want = list(R.attend(q.double(), *vals, [T], [n], block))
+        for e, t in zip((3, 4, 5), want[3:]):     # sizes for the bounds: without the block
+            clean = [v.nan_to_num(0.0) for v in vals]
+            want[e] = R.attend(q.double(), *clean, [T], [n], block)[e]
+        if which == "V":
+            assert torch.isfinite(want[1]).all() and torch.isnan(want[0]).any()
+        check_not_finite(run_attend(W, cfg, c, q, [T], [n]), want, D, T, H)
+
+
+@pytest.mark.parametrize("n", [1, 9, 20, 70])
+def test_queries_that_are_not_finite(W, n):
+    """A NaN or an infinity in a query: NaN in the outputs of its row alone, and -inf for a token that sees no row."""
+    log(f"[case] quant attend, queries that are not finite, n={n}")
+    H, G, block, D = 1, 3, 16, 64
+    T = 170 if n == 1 else n - 1        # the first token sees no row where there are several
+    cfg = W.make_quant_config(1, 1, H, 192, block, R.INT8, head_dim=D)
+    c, vals = filled(W, cfg, [T], R.INT8, 13)
+    q = rows(14, 1, 1, H * G, n, D)
+    want = list(R.attend(q.double(), *vals, [T], [n], block))
+    for hq, value in ((0, math.nan), (1, math.inf)):
+        q[0, 0, hq, n - 1, 5] = value
+        want[0][0, 0, hq, n - 1] = want[1][0, 0, hq, n - 1] = math.nan
+        want[2][0, 0, hq, n - 1, : -(-T // block)] = math.nan
+    got = run_attend(W, cfg, c, q, [T], [n])
+    if n > 1:
+        assert bool((want[1][..., 0] == -math.inf).all())
+    check_not_finite(got, want, D, max(T, 1), H)
