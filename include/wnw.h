@@ -409,9 +409,9 @@ const char *wnw_triage_last_error(void);
 /* ---- a KV cache in 8 bits.  A bf16 cache row costs a decode step 4 d bytes of HBM (K and V); these
  * calls hold it in half of that: rows are quantised as they are written, with one scale for every
  * `block` rows of a head, and attention reads the bytes.  The calls need no context; the caller owns
- * every buffer, and all of them only enqueue work on hip_stream (NULL = null stream) and allocate
- * nothing, so they can be captured into a graph; lengths and positions are read on the device when the
- * work runs.  Like the decode step's caches the buffers hold all layers; a call handles n_layers of
+ * every buffer, and all of them only enqueue work on hip_stream (NULL = null stream), a stream of the
+ * current device, and allocate nothing, so they can be captured into a graph; lengths and positions are read on
+ * the device when the work runs.  Like the decode step's caches the buffers hold all layers; a call handles n_layers of
  * them from first_layer on, so that a model can go layer by layer.  Sequences of a batch may have any
  * lengths.
  *

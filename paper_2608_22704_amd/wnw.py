@@ -333,10 +333,14 @@ def _quant_shape(cfg, t, heads, what):
 
 
 def _quant_place(stream):
-    """(index of the current device, stream handle): where a call's work runs."""
+    """(index of the current device, stream handle): where a call's work runs.  The library launches on the current device,
+    so a stream of another one is refused."""
     import torch
     device = torch.cuda.current_device()
     if stream is not None:
+        on = getattr(stream, "device", None)     # (a bare handle does not say)
+        if on is not None and on.index != device:
+            raise ValueError(f"stream is on {on}, the current device is cuda:{device}")
         return device, getattr(stream, "cuda_stream", stream)
     # the handle alone: a Stream object costs 2.5 us, as much as a launch
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)

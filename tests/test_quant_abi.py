@@ -160,6 +160,25 @@ def test_binding_refuses_a_buffer_that_shrank(W, name):
         c._struct(cfg, -1)
 
 
+def test_binding_refuses_a_stream_of_another_device(W, monkeypatch):
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+
+    class Stream:
+        cuda_stream = 4096
+
+        def __init__(self, device):
+            self.device = torch.device("cuda", device)
+    assert W._quant_place(Stream(0)) == (0, 4096) and W._quant_place(4096) == (0, 4096)
+    cfg = W.make_quant_config(1, 1, 1, 64, 32, W.WNW_QUANT_INT8)
+    c = W.make_quant_cache(cfg, device="cpu")
+    x, out = torch.zeros((1, 1, 1, 2, 128), dtype=torch.bfloat16), torch.zeros((1, 1, 1, 2, 128))
+    at = torch.zeros(1, dtype=torch.int32)
+    for call in (lambda s: W.wnw_quant_write(cfg, c, x, x, at, stream=s), lambda s: W.wnw_quant_read(cfg, c, out, out, at, stream=s),
+                 lambda s: W.wnw_quant_attend(cfg, c, x, out, at, stream=s)):
+        with pytest.raises(ValueError, match="stream is on cuda:1"):
+            call(Stream(1))
+
+
 def test_places_of_a_v_tile():
     """Row 16 b + 4 h + i at 16 h + 4 b + i: a permutation, and what the reference encodes it decodes."""
     assert sorted(R.v_place(r) for r in range(64)) == list(range(64))
