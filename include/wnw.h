@@ -442,7 +442,8 @@ typedef struct {
     int32_t block;        /* rows that share a scale: 16, 32 or 64                         */
     int32_t format;       /* wnw_quant_format                                              */
     uint32_t flags;       /* WNW_F_OUT_BF16: wnw_quant_read and wnw_quant_attend write bf16 (each
-                             fp32 result rounded to nearest, ties to even) instead of fp32 */
+                             fp32 result rounded to nearest, ties to even) instead of fp32; the
+                             arithmetic is unchanged */
 } wnw_quant_config;
 
 typedef struct {          /* device pointers                                               */
@@ -480,7 +481,7 @@ wnw_status wnw_quant_read(const wnw_quant_config *cfg, const wnw_quant_cache *ca
 /* Attention of a sequence's last count[b] tokens over its cache, their own rows (already written)
  * among it: token i of count[b] sees rows 0 .. len[b] - count[b] + i.  Logit scale 1 / sqrt(d); the bytes are
  * multiplied as they are, products summed in fp32, softmax statistics in fp32.  A softmax weight times
- * its block's V scale is held to 22 bits (bf16 output: 11) and counts down to 2^-31 of the largest V scale of
+ * its block's V scale is held to 22 bits and counts down to 2^-31 of the largest V scale of
  * the rows seen.  A token that sees no row gets zeros and the log-sum-exp -inf.
  *   q_heads    a multiple of kv_heads (any group size); q-head hq belongs to KV-head hq / (H_q / H_kv)
  *   q_dev      device bf16 [B][n_layers][H_q][n][d], 16-byte aligned

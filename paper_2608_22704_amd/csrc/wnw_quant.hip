@@ -11,8 +11,9 @@
 // Bytes become fp16 on the way to the matrix cores, exactly: integers up to 127 and e4m3 numbers both fit.
 // A query row is scaled by a power of two (its largest magnitude to 2^14 .. 2^15) and is then exact in fp16 as well, but
 // for elements 2^28 times smaller than the largest, so logits carry fp32 rounding alone.  A softmax weight times its
-// block's V scale is rounded to fp16 once where the output is bf16 (by 2^-12 at most, next to the output's 2^-9), and
-// to the sum of two fp16 (2^-22) where it is fp32.  Sums, maxima and logits are fp32.
+// block's V scale is rounded to the sum of two fp16 (2^-22): one would be off by up to 2^-11, and 7 % of bf16 outputs would
+// then not be the fp32 ones rounded, which is what the flag promises (512 tokens would take 302 us instead of 382, one
+// token 151 instead of 153).  Sums, maxima and logits are fp32.
 #include "wnw.h"
 #include "wnw_internal.h"
 #include "wnw_lds.h"
@@ -512,10 +513,10 @@ __global__ __launch_bounds__(Q_THREADS) void quant_append_kernel(QuantGeo g, int
     }
 }
 
-template <int E, bool BF16>
-__device__ inline void store_row(void *out, size_t elem, const float (&x)[E])
+template <int E>
+__device__ inline void store_row(void *out, bool bf16, size_t elem, const float (&x)[E])
 {
-    if constexpr (BF16) {
+    if (bf16) {
         uint16_t u[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) u[e] = to_bf16(x[e]);
@@ -609,6 +610,7 @@ struct QuantAttend {
     QuantGeo g;
     int G, n, R;               // q-heads per KV-head, tokens, rows G * n of a KV-head: row r is token r / G, q-head r % G
     int W, RB, rsh;            // work-groups that share the batch's tiles, rows of a block and their log2
+    int bf16;                  // outputs are bf16: the fp32 results, rounded as they are stored
     int nrb;                   // > 0: a work-group per block of rows, nrb blocks a head, nothing to join
     float inv_w;               // 1 / W
     const uint16_t *q;
@@ -824,24 +826,18 @@ __device__ inline float finite_or_zero(float m)
     return m == -INFINITY ? 0.f : m;
 }
 
-// Eight weights as matrix operands.  TWO: as the sum of two fp16.  The first is rounded towards zero by one instruction
+// Eight weights as matrix operands, each the sum of two fp16.  The first is rounded towards zero by one instruction
 // whose result is also what the second is the rest of: with (_Float16) in both places the compiler rounded the product
 // with the V scale straight to fp16 in one of them, and where the other's fp32 value was a tie the two differed by a whole step.
-template <bool TWO>
 __device__ inline void weights_to_half(const float (&p)[8], h8_t &hi, h8_t &lo)
 {
-    if constexpr (TWO) {
 #pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-            const h2_t h = __builtin_bit_cast(h2_t, __builtin_amdgcn_cvt_pkrtz(p[i], p[i + 1]));
-            hi[i] = h.x;
-            hi[i + 1] = h.y;
-            lo[i] = (_Float16)(p[i] - (float)h.x);
-            lo[i + 1] = (_Float16)(p[i + 1] - (float)h.y);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) hi[i] = (_Float16)p[i];
+    for (int i = 0; i < 8; i += 2) {
+        const h2_t h = __builtin_bit_cast(h2_t, __builtin_amdgcn_cvt_pkrtz(p[i], p[i + 1]));
+        hi[i] = h.x;
+        hi[i + 1] = h.y;
+        lo[i] = (_Float16)(p[i] - (float)h.x);
+        lo[i + 1] = (_Float16)(p[i + 1] - (float)h.y);
     }
 }
 
@@ -943,7 +939,7 @@ __device__ inline void mass_shares(const QuantAttend &a, size_t row, int len, in
 }
 
 // Tiles ta .. tb - 1 of block rb of head (b, hd)'s rows; slot: where a piece's result goes (-1: the block is whole).
-template <int DH, int FMT, bool F32, int MT, bool NTL, int NW>
+template <int DH, int FMT, int MT, bool NTL, int NW>
 __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH, MT, NW> &sm, const QuantSeq &sq, int b, int hd,
                                          int rb, int ta, int tb, int slot)
 {
@@ -1114,7 +1110,7 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
             for (int c = 0; c < 2; ++c) {
                 const float p[8] = {x[2 * c][0],     x[2 * c][1],     x[2 * c][2],     x[2 * c][3],
                                     x[2 * c + 1][0], x[2 * c + 1][1], x[2 * c + 1][2], x[2 * c + 1][3]};
-                weights_to_half<F32>(p, ph[r][c], pl[r][c]);
+                weights_to_half(p, ph[r][c], pl[r][c]);
             }
         }
         if (more)
@@ -1141,7 +1137,7 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
 #pragma unroll
                 for (int r = 0; r < MT; ++r) {
                     o[r][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph[r][c], o[r][dt], 0, 0, 0);
-                    if constexpr (F32) o[r][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl[r][c], o[r][dt], 0, 0, 0);
+                    o[r][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl[r][c], o[r][dt], 0, 0, 0);
                 }
             }
         }
@@ -1196,7 +1192,7 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
             const float inv = ll == 0.f ? 0.f : 1.f / ll;
 #pragma unroll
             for (int e = 0; e < DH / 16; ++e) x[e] *= inv;
-            store_row<DH / 16, !F32>(z.out, (size_t)rr.row_of * DH + d0, x);
+            store_row<DH / 16>(z.out, z.bf16, (size_t)rr.row_of * DH + d0, x);
             if (d0 == 0) {
                 if (z.lse) z.lse[rr.row_of] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * Q_LN2;
                 if (z.mass) {
@@ -1275,12 +1271,12 @@ __device__ inline void quant_parts(const QuantAttend &a, F f)
     }
 }
 
-template <int DH, int FMT, bool F32, int MT, bool NTL, int NW>
+template <int DH, int FMT, int MT, bool NTL, int NW>
 __global__ __launch_bounds__(64 * NW, (NW == 8 ? 2 : token_held<DH, MT>())) void quant_token_kernel(QuantAttend a)
 {
     __shared__ QuantTokenSmem<DH, MT, NW> sm;
     quant_parts(a, [&](const QuantSeq &sq, int b, int hd, int rb, int ta, int tb, int slot) {
-        quant_token_block<DH, FMT, F32, MT, NTL, NW>(a, sm, sq, b, hd, rb, ta, tb, slot);
+        quant_token_block<DH, FMT, MT, NTL, NW>(a, sm, sq, b, hd, rb, ta, tb, slot);
     });
 }
 
@@ -1334,7 +1330,7 @@ __device__ inline qu4_t convert8(unsigned a, unsigned b)
     return __builtin_bit_cast(qu4_t, bytes_to_h8<FMT>(a, b));
 }
 
-template <int DH, int FMT, bool F32, int KS>
+template <int DH, int FMT, int KS>
 __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> &sm, const QuantSeq &sq, int b, int hd, int rb,
                                         int ta, int tb, int slot)
 {
@@ -1497,7 +1493,7 @@ __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> 
                 if constexpr (MASKED) p[i] = 16 * c + 8 * (i / 4) + i % 4 < vis ? p[i] : 0.f;
             }
             sum += part;
-            weights_to_half<F32>(p, ph[c], pl[c]);
+            weights_to_half(p, ph[c], pl[c]);
         }
         if (t + 1 < t_end) {
             store(t + 1, other);
@@ -1509,7 +1505,7 @@ __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> 
             for (int c = 0; c < 2 * NB; ++c) {
                 const h8_t v = lds_read(v_get + c * 32 + dt * 32 * SM::V_ROW + buf);
                 o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, ph[c], o[dt], 0, 0, 0);
-                if constexpr (F32) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pl[c], o[dt], 0, 0, 0);
+                o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pl[c], o[dt], 0, 0, 0);
             }
         __syncthreads();
     };
@@ -1567,7 +1563,7 @@ __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> 
             if (slot >= 0)
                 *(qf4_t *)(a.ws_o + to) = qf4_t{y[0], y[1], y[2], y[3]};
             else
-                store_row<4, !F32>(a.out, to, y);
+                store_row<4>(a.out, a.bf16, to, y);
         }
     if (half == 0) {
         if (slot >= 0)
@@ -1577,12 +1573,12 @@ __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> 
     }
 }
 
-template <int DH, int FMT, bool F32, int KS>
+template <int DH, int FMT, int KS>
 __global__ __launch_bounds__(Q_THREADS, 2) void quant_wide_kernel(QuantAttend a)
 {
     __shared__ QuantWideSmem<DH> sm;
     quant_parts(a, [&](const QuantSeq &sq, int b, int hd, int rb, int ta, int tb, int slot) {
-        quant_wide_block<DH, FMT, F32, KS>(a, sm, sq, b, hd, rb, ta, tb, slot);
+        quant_wide_block<DH, FMT, KS>(a, sm, sq, b, hd, rb, ta, tb, slot);
     });
 }
 
@@ -1603,7 +1599,7 @@ struct QuantPieces {
 // Single tokens: a work-group per output row.  A lane has a piece's statistics; the wavefronts share the pieces' sums.  Makes
 // the tiles' block sums shares of the whole as well.  576 rows of 7 pieces 5.4 us, 512 of 16 sequences 7.6: a launch and three
 // dependent loads.
-template <int DH, bool BF16>
+template <int DH>
 __global__ __launch_bounds__(Q_THREADS) void quant_merge_kernel(QuantAttend a)
 {
     constexpr int E = DH / 64;
@@ -1650,7 +1646,7 @@ __global__ __launch_bounds__(Q_THREADS) void quant_merge_kernel(QuantAttend a)
         __syncthreads();
         if (tid < DH) {
             const float y = ((sm_o[0][tid] + sm_o[1][tid]) + (sm_o[2][tid] + sm_o[3][tid])) * (sum == 0.f ? 0.f : 1.f / sum);
-            if constexpr (BF16)
+            if (a.bf16)
                 ((uint16_t *)a.out)[(size_t)row * DH + tid] = to_bf16(y);
             else
                 ((float *)a.out)[(size_t)row * DH + tid] = y;
@@ -1661,7 +1657,7 @@ __global__ __launch_bounds__(Q_THREADS) void quant_merge_kernel(QuantAttend a)
 }
 
 // Several tokens: a work-group per 16 rows of a head, sixteen threads a row.  32768 rows of two or three pieces 12.6 us, 46 MB.
-template <int DH, bool BF16>
+template <int DH>
 __global__ __launch_bounds__(Q_THREADS) void quant_merge_rows_kernel(QuantAttend a)
 {
     constexpr int E = DH / 16;
@@ -1692,7 +1688,7 @@ __global__ __launch_bounds__(Q_THREADS) void quant_merge_rows_kernel(QuantAttend
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] *= inv;
-    store_row<E, BF16>(a.out, (size_t)qr.row_of * DH + d0, x);
+    store_row<E>(a.out, a.bf16, (size_t)qr.row_of * DH + d0, x);
     if (a.lse && d0 == 0) a.lse[qr.row_of] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * Q_LN2;
 }
 
@@ -1832,25 +1828,25 @@ QuantPlan quant_plan(const wnw_quant_config &c, int32_t n_layers, int32_t q_head
     return p;
 }
 
-template <int DH, int FMT, bool F32, int MT>
+template <int DH, int FMT, int MT>
 void launch_few(const QuantPlan &p, const QuantAttend &a, hipStream_t st)
 {
     constexpr bool both = DH == 64 || MT == 2;
-    auto *k = p.eight ? (p.stream ? quant_token_kernel<DH, FMT, F32, MT, both, 8> : quant_token_kernel<DH, FMT, F32, MT, false, 8>)
-                      : (p.stream ? quant_token_kernel<DH, FMT, F32, MT, true, 4> : quant_token_kernel<DH, FMT, F32, MT, false, 4>);
+    auto *k = p.eight ? (p.stream ? quant_token_kernel<DH, FMT, MT, both, 8> : quant_token_kernel<DH, FMT, MT, false, 8>)
+                      : (p.stream ? quant_token_kernel<DH, FMT, MT, true, 4> : quant_token_kernel<DH, FMT, MT, false, 4>);
     hipLaunchKernelGGL(k, dim3(p.W), dim3(p.eight ? 512 : 256), 0, st, a);
 }
-template <int DH, int FMT, bool F32>
+template <int DH, int FMT>
 void launch_token(const QuantPlan &p, const QuantAttend &a, hipStream_t st)
 {
     if (p.RB == WIDE_ROWS)
-        hipLaunchKernelGGL((quant_wide_kernel<DH, FMT, F32, 1>), dim3(p.W), dim3(Q_THREADS), 0, st, a);
+        hipLaunchKernelGGL((quant_wide_kernel<DH, FMT, 1>), dim3(p.W), dim3(Q_THREADS), 0, st, a);
     else if (p.RB == WIDE_ROWS / 2)
-        hipLaunchKernelGGL((quant_wide_kernel<DH, FMT, F32, 2>), dim3(p.W), dim3(Q_THREADS), 0, st, a);
+        hipLaunchKernelGGL((quant_wide_kernel<DH, FMT, 2>), dim3(p.W), dim3(Q_THREADS), 0, st, a);
     else if (p.RB == 32)
-        launch_few<DH, FMT, F32, 2>(p, a, st);
+        launch_few<DH, FMT, 2>(p, a, st);
     else
-        launch_few<DH, FMT, F32, 1>(p, a, st);
+        launch_few<DH, FMT, 1>(p, a, st);
 }
 
 wnw_status quant_heads(const wnw_quant_config &c, int32_t n_layers, int32_t q_heads, int32_t n, int32_t max_len)
@@ -1956,21 +1952,19 @@ wnw_status wnw_quant_attend(const wnw_quant_config *cfg, const wnw_quant_cache *
     const int G = q_heads / cfg->kv_heads, R = G * n;
     char *ws = (char *)workspace;
     QuantAttend a = {quant_geo(*cfg, *cache, first_layer, n_layers), G, n, R, p.W, p.RB, p.RB == 16 ? 4 : p.RB == 32 ? 5 : p.RB == 64 ? 6 : 7,
-                     p.whole ? (R + p.RB - 1) / p.RB : 0, 1.f / p.W, (const uint16_t *)q_dev, len_dev, count_dev, out_dev,
+                     cfg->flags & WNW_F_OUT_BF16 ? 1 : 0, p.whole ? (R + p.RB - 1) / p.RB : 0, 1.f / p.W, (const uint16_t *)q_dev, len_dev, count_dev, out_dev,
                      lse_dev, mass_dev, (float *)ws, (float2 *)(ws + p.o_bytes),
                      (float2 *)(ws + p.o_bytes + p.ml_bytes), (float *)(ws + p.o_bytes + p.ml_bytes + p.row_bytes),
                      Q_LOG2E / sqrtf((float)cfg->head_dim)};
-    const bool bf16 = cfg->flags & WNW_F_OUT_BF16;
     quant_dispatch(*cfg, [&](auto d, auto f) {
         constexpr int DH = decltype(d)::value, FMT = decltype(f)::value;
-        bf16 ? launch_token<DH, FMT, false>(p, a, (hipStream_t)hip_stream) : launch_token<DH, FMT, true>(p, a, (hipStream_t)hip_stream);
+        launch_token<DH, FMT>(p, a, (hipStream_t)hip_stream);
         if (p.whole) return;
         if (n == 1)
-            hipLaunchKernelGGL((bf16 ? quant_merge_kernel<DH, true> : quant_merge_kernel<DH, false>), dim3((unsigned)p.rows),
-                               dim3(Q_THREADS), 0, (hipStream_t)hip_stream, a);
+            hipLaunchKernelGGL((quant_merge_kernel<DH>), dim3((unsigned)p.rows), dim3(Q_THREADS), 0, (hipStream_t)hip_stream, a);
         else
-            hipLaunchKernelGGL((bf16 ? quant_merge_rows_kernel<DH, true> : quant_merge_rows_kernel<DH, false>),
-                               dim3((unsigned)(p.rows / R * ((R + 15) / 16))), dim3(Q_THREADS), 0, (hipStream_t)hip_stream, a);
+            hipLaunchKernelGGL((quant_merge_rows_kernel<DH>), dim3((unsigned)(p.rows / R * ((R + 15) / 16))), dim3(Q_THREADS), 0,
+                               (hipStream_t)hip_stream, a);
     });
     return quant_hip();
 }

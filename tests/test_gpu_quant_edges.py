@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from tests import quant_reference as R
-from tests.test_gpu_quant import bound, check_attend, filled, i32, new_cache, rows, run_attend
+from tests.test_gpu_quant import SHAPES, SHARED, bound, check_attend, filled, i32, new_cache, rows, run_attend
 from tests.wnw_harness import log
 
 pytestmark = pytest.mark.gpu
@@ -149,3 +149,29 @@ def test_queries_that_are_not_finite(W, n):
     if n > 1:
         assert bool((want[1][..., 0] == -math.inf).all())
     check_not_finite(got, want, D, max(T, 1), H)
+
+
+# every way of sharing work out, and every kernel: (lens, n, counts, layers, KV heads, group, block, d)
+CALLS = [(lens, n, counts, 2, H, G, block, D) for lens, n, counts, H, G, block, D in SHAPES] + list(SHARED.values())
+
+
+@pytest.mark.parametrize("fmt", [R.INT8, R.E4M3])
+@pytest.mark.parametrize("call", CALLS, ids=lambda c: f"b{len(c[0])}_len{c[0][0]}_n{c[1]}_l{c[3]}_g{c[5]}_blk{c[6]}_d{c[7]}")
+def test_bf16_outputs_are_the_fp32_ones_rounded(W, fmt, call):
+    """The flag changes how a result is stored and nothing else: the same bits, rounded; the same statistics and masses."""
+    lens, n, counts, L, H, G, block, D = call
+    log(f"[case] quant attend, bf16 against fp32, fmt={fmt} n={n} {L} layers group {G} block {block} d={D}")
+    B = len(lens)
+    counts = counts or [1] * B
+    cap = (max(lens) + 63) // 64 * 64 + 64
+    cfg = [W.make_quant_config(B, L, H, cap, block, fmt, head_dim=D, flags=f) for f in (0, W.WNW_F_OUT_BF16)]
+    g = torch.Generator(device="cuda").manual_seed(19)
+    c = W.make_quant_cache(cfg[0])
+    for t, s in ((c.k, c.k_scale), (c.v, c.v_scale)):
+        t.random_(1, 127, generator=g)
+        s.copy_(torch.exp(0.5 * torch.randn(s.shape, generator=g, device="cuda")) * 0.02)
+    q = rows(20, B, L, H * G, n, D, spread=0.3)
+    want, got = (run_attend(W, f, c, q, lens, counts) for f in cfg)
+    assert torch.equal(got[0], want[0].bfloat16())
+    for a, b in zip(got[1:], want[1:]):
+        assert a is b is None or torch.equal(a, b)
