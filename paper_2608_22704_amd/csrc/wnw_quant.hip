@@ -1771,16 +1771,21 @@ void quant_dispatch(const wnw_quant_config &c, F f)
 // Measured whole and cut, tiles of one token, d = 128: 8 blocks of 12 9.3 and 10.5 us, of 24 13.2 and 12.3; 72 of 16 11.9 and
 // 13.4, of 47 23.6 and 17.6; 128 of 32 18.4 and 20.8, of 63 29.4 and 30.5; 240 of 243 153 and 160, of 1423 848 and 866; d = 64:
 // 8 of 16 7.2 and 8.8, of 47 13.0 and 10.3; 72 of 32 10.9 and 12.6; five tokens of four heads: 8 of 8 12.6 and 13.6, of 32 23.8
-// and 19.1; 720 blocks of 147, 23 and 73 178 and 203; the wide kernel: 16 of 4 12.7 and 14.9, of 12 24.5 and 19.1; 256 of 32 58
-// and 72, of 243 369 and 310; 1024 of 63 285 and 321; its blocks of 64 rows: 8 of 5 10.6 and 12.8, of 16 20.4 and 14.9, 240 of 8
-// 16.4 and 19.3, of 63 84 and 85, of 243 254 and 228.
+// and 19.1; 720 blocks of 147, 23 and 73 178 and 203; the wide kernel's blocks of 128 rows: 16 of 4 13.8 and 16.2, of 8 20.8 and
+// 18.5, of 12 28.2 and 20.5; 64 of 8 21.8 and 22.9, of 32 64 and 38; 256 of 32 76 and 86, of 100 221 and 211, of 243 495 and 452;
+// 512 of 63 233 and 251; 1024 of 63 455 and 483; of 64 rows: 8 of 5 11.5 and 13.7, of 16 22.6 and 15.2; 64 of 16 23.7 and 20.5; 240
+// of 8 17.6 and 20.7, of 63 95 and 92, of 243 302 and 272.
+// Of a batch only the longest length is known here, and every sequence is priced at it: a ragged batch whose longest sequence is
+// walked whole waits for that sequence's blocks (16 ragged sequences of up to 20011 rows, d = 64, are cut, 30 us; 17 are
+// whole, 71; 32 of up to 15512 rows, d = 128, 122 for 320 MB).
 bool whole_blocks(int RB, int head_dim, int64_t blocks, int64_t tiles, bool eight, bool stream)
 {
     const double b = blocks / 256.0, t = (double)tiles;
     if (RB > 32) {
-        const double whole = blocks <= 256 ? 1.5 * t : 2.6 * t * (double)((blocks + 511) / 512);
+        const double alone = RB == WIDE_ROWS ? 2.0 : 1.5, part = RB == WIDE_ROWS ? 1.8 : 1.3;
+        const double whole = blocks <= 256 ? alone * t : 2 * part * t * (double)((blocks + 511) / 512);
         const double join = 6 + 8 * std::min(1.0, t * b / (2 * MIN_PIECE));
-        return whole <= join + std::max(1.5 * MIN_PIECE, 1.3 * t * b);
+        return whole <= join + std::max(alone * MIN_PIECE, part * t * b);
     }
     const bool half = head_dim == 64;
     const double tile = half ? 0.3 : RB == 32 ? 0.6 : 0.45, full = half ? 0.32 : 0.63;
