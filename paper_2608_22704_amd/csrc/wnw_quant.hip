@@ -12,8 +12,8 @@
 // A query row is scaled by a power of two (its largest magnitude to 2^14 .. 2^15) and is then exact in fp16 as well, but
 // for elements 2^28 times smaller than the largest, so logits carry fp32 rounding alone.  A softmax weight times its
 // block's V scale is rounded to the sum of two fp16 (2^-22): one would be off by up to 2^-11, and 7 % of bf16 outputs would
-// then not be the fp32 ones rounded, which is what the flag promises (512 tokens would take 302 us instead of 382, one
-// token 151 instead of 153).  Sums, maxima and logits are fp32.
+// then not be the fp32 ones rounded, which is what the flag promises (512 tokens would take 302 us instead of 377, 64 query
+// rows 223 instead of 260, five tokens of d = 64 82 instead of 96, single tokens as long).  Sums, maxima and logits are fp32.
 #include "wnw.h"
 #include "wnw_internal.h"
 #include "wnw_lds.h"
@@ -173,8 +173,11 @@ __device__ inline float byte_value(unsigned u, int i)
     return __builtin_amdgcn_cvt_f32_fp8((int)(u >> (8 * i)), 0);
 }
 
-// Four bytes held under scale `was`, rounded again under the larger scale `now`.  int8: the fp32 product is off by 2^-16 at
-// most; next to a tie a double decides, as quotients that are no tie differ from one by 2^-25 or more.
+// Four bytes held under scale `was`, rounded again under the larger scale `now`.  int8: the fp32 product has three roundings of
+// 2^-24 and is below 127, off by 2^-15 at most; next to a tie a double decides.  A quotient x was / now near a tie is 1/2 or more, so
+// that now < 2^8 was; with p the weight of was's last bit, 2 x was and (2 k + 1) now are multiples of p, and now < 2^32 p:
+// unless equal they differ by p or more, and the quotient from k + 1/2 by p / (2 now) > 2^-33.  x was is exact in double and the
+// division off by 2^-47 at most.
 template <int FMT>
 __device__ inline unsigned requant4(unsigned u, float was, float now, float ratio)
 {
@@ -375,8 +378,6 @@ __global__ __launch_bounds__(Q_THREADS) void quant_write_kernel(QuantGeo g, int 
     }
 }
 
-// ---- reading back ----------------------------------------------------------------------------
-
 // A few rows: n <= APPEND_ROWS, which lie in two groups of 16 rows (that start at multiples of 16) and two scale blocks at most.
 // A wavefront has a head's K or V: what a launch of a work-group a tile spends its time on is starting wavefronts (the
 // chip starts one in about 0.5 ns), of which three or four of four had nothing to write.  Lanes as there, for each of the
@@ -513,6 +514,9 @@ __global__ __launch_bounds__(Q_THREADS) void quant_append_kernel(QuantGeo g, int
     }
 }
 
+// ---- reading back ----------------------------------------------------------------------------
+
+// The second argument is the outputs' type: fp32 results, rounded to bf16 (nearest, ties to even) where it says so.
 template <int E>
 __device__ inline void store_row(void *out, bool bf16, size_t elem, const float (&x)[E])
 {
@@ -852,7 +856,7 @@ __device__ inline void weights_to_half(const float (&p)[8], h8_t &hi, h8_t &lo)
 // left for two blocks of 16 rows and two wavefronts on every SIMD.
 // The wavefronts' results meet in shared memory at the end, in the tiles' place.
 // Memory bounds long caches (two operations a byte and query row), and the bytes in flight decide, 64 KB a work-group: 15512
-// rows of 240 KV-heads, four query rows each, 151 us, 6.3 TB/s (a loop of loads alone reads 6.9), the matrix cores 8 % busy,
+// rows of 240 KV-heads, four query rows each, 151 us, 6.3 TB/s (a loop of loads alone reads 6.9), the matrix cores 12 % busy,
 // fetched bytes 1.006 of the cache's; 91024 rows 865 us, 6.45 TB/s; five tokens of three sequences (20 query rows) 171 us,
 // 5.6 TB/s.  Short calls wait for instructions, each fetched once, and for the chain length, tile, products, softmax,
 // products: 8 KV-heads of 1064 rows 13 us, of 512 rows 8.5.
@@ -1288,15 +1292,18 @@ __global__ __launch_bounds__(64 * NW, (NW == 8 ? 2 : token_held<DH, MT>())) void
 //   operands): a lane has 16 keys of ONE row, elements 0 .. 7 in the tile's 16-row block 2 k and 8 .. 15 in 2 k + 1, so that S^T's
 //   elements are P^T's operand as they stand.
 // KS = 2, for 33 to 64 rows: two wavefronts share 32 rows, each with half of every tile's keys, and join at the end (with
-// two of four wavefronts idle instead: 64 rows of 240 KV-heads over 15512 rows 300 -> 225 us, as fp32 367 -> 261).
+// two of four wavefronts idle instead: 64 rows of 240 KV-heads over 15512 rows 367 -> 260 us).
 // A row's maximum m is raised, and its output and sum scaled, only when a logit exceeds it by LAZY (base 2): weights
-// are up to 2^LAZY then, which fp16 has room for.
-// Bound by the matrix cores and the vector unit taking turns within the card's power limit: a wavefront's tile is 32
-// products (1024 cycles) and about 280 vector instructions, which the two work-groups of a compute unit overlap.  512 tokens
-// of four heads over 15512 rows of 16 KV-heads 295 us and a join of 13, 836 TFLOP/s; 1024 tokens over 8000 rows of 32
-// KV-heads 564 us, 952 TFLOP/s (a large product of the library: 1149 in bf16, 1107 in fp16).  Fetched bytes are eight times
-// the cache's (every XCD reads all of it), from the last-level cache.  Conversions between the products instead of before them
-// gained 1.5 % (d = 64 lost 2), raised priority around the products 2 %: neither is kept.
+// are up to 2^LAZY then, which fp16 has room for (a weight of 1 stands at 2^7 instead of 2^15, so that weights end at 2^-31 of the
+// largest V scale seen, where the kernel for few rows has 2^-39).
+// Bound by the matrix cores and the vector unit taking turns within the card's power limit: a wavefront's tile is 48
+// products (1536 cycles; weights are two operands) and about 340 vector instructions, which the two work-groups of a compute unit
+// overlap; the matrix cores are 47 % busy.  512 tokens of four heads over 15512 rows of 16 KV-heads 377-387 us with a join of 12, 665-680
+// TFLOP/s or 1000-1020 with the second product of every weight; 1024 tokens over 8000 rows of 32 KV-heads 710-727 us, 700 and 1050
+// TFLOP/s (a large product of the library: 1149 in bf16, 1107 in fp16).  After a pause the card's clocks take some milliseconds of
+// such work to settle, with calls up to a quarter longer.  Fetched bytes are eight times the cache's (every XCD reads all of
+// it), from the last-level cache.  Not kept, measured with one product for each weight: conversions between the products
+// instead of before them (1.5 % faster, d = 64 2 % slower), raised priority around the products (2 %).
 constexpr int WIDE_ROWS = 128;   // 2^7: see QuantAttend::rsh
 constexpr int LAZY = 8;
 
