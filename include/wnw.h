@@ -482,7 +482,9 @@ wnw_status wnw_quant_read(const wnw_quant_config *cfg, const wnw_quant_cache *ca
  * among it: token i of count[b] sees rows 0 .. len[b] - count[b] + i.  Logit scale 1 / sqrt(d); the bytes are
  * multiplied as they are, products summed in fp32, softmax statistics in fp32.  A softmax weight times
  * its block's V scale is held to 22 bits and counts down to 2^-31 of the largest V scale of
- * the rows seen.  A token that sees no row gets zeros and the log-sum-exp -inf.
+ * the rows seen.  A token that sees no row gets zeros and the log-sum-exp -inf; otherwise a query row with a
+ * NaN or an infinity gets NaN in all of its outputs, as does a token that sees a K block whose scale is NaN, and one
+ * that sees such a V block in out_dev alone.
  *   q_heads    a multiple of kv_heads (any group size); q-head hq belongs to KV-head hq / (H_q / H_kv)
  *   q_dev      device bf16 [B][n_layers][H_q][n][d], 16-byte aligned
  *   len_dev    device int32 [B], rows of the sequence (as the nearer end outside 0 .. capacity)
