@@ -16,7 +16,7 @@
 // rows 223 instead of 260, five tokens of d = 64 82 instead of 96, single tokens as long).  Sums, maxima and logits are fp32.
 #include "wnw.h"
 #include "wnw_internal.h"
-#include "wnw_lds.h"
+#include "wnw_parts.h"
 
 #include <math.h>
 
@@ -50,72 +50,6 @@ struct QuantGeo {
     // head hd (of nl * H) of a call's layers in sequence b
     __host__ __device__ size_t head(int b, int hd) const { return ((size_t)b * L + l0) * H + hd; }
 };
-
-__device__ inline int q_clamp(int x, int hi)
-{
-    return min(max(x, 0), hi);
-}
-
-// ---- lanes -----------------------------------------------------------------------------------
-
-__device__ inline unsigned uniform(unsigned v)
-{
-    return (unsigned)__builtin_amdgcn_readfirstlane((int)v);
-}
-__device__ inline float lane_f(float v, int lane)
-{
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
-}
-__device__ inline unsigned lane_of(unsigned v, int lane)
-{
-    return (unsigned)__builtin_amdgcn_readlane((int)v, lane);
-}
-// Inclusive scans over the wavefront's lanes by data-parallel moves: within rows of sixteen lanes, then across them.
-template <typename F>
-__device__ inline unsigned wave_scan_by(unsigned v, F f)
-{
-    v = f(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, false));
-    v = f(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, false));
-    v = f(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, false));
-    v = f(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, false));
-    v = f(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false));
-    return f(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false));
-}
-__device__ inline unsigned wave_scan(unsigned v)
-{
-    return wave_scan_by(v, [](unsigned a, unsigned b) { return a + b; });
-}
-__device__ inline unsigned wave_sum(unsigned v)
-{
-    return (unsigned)__builtin_amdgcn_readlane((int)wave_scan(v), 63);
-}
-__device__ inline unsigned wave_max(unsigned v)
-{
-    return (unsigned)__builtin_amdgcn_readlane((int)wave_scan_by(v, [](unsigned a, unsigned b) { return max(a, b); }), 63);
-}
-// Over the wavefront's lanes, for every lane.
-__device__ inline float wave_maxf(float v)
-{
-    auto step = [&](int u) { v = fmaxf(v, __int_as_float(u)); };
-    step(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), 0x111, 0xf, 0xf, false));
-    step(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), 0x112, 0xf, 0xf, false));
-    step(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), 0x114, 0xf, 0xf, false));
-    step(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), 0x118, 0xf, 0xf, false));
-    step(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), 0x142, 0xa, 0xf, false));
-    step(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), 0x143, 0xc, 0xf, false));
-    return lane_f(v, 63);
-}
-__device__ inline float wave_sumf(float v)
-{
-    auto step = [&](int u) { v += __int_as_float(u); };
-    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x111, 0xf, 0xf, false));
-    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x112, 0xf, 0xf, false));
-    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x114, 0xf, 0xf, false));
-    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x118, 0xf, 0xf, false));
-    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x142, 0xa, 0xf, false));
-    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x143, 0xc, 0xf, false));
-    return lane_f(v, 63);
-}
 
 // ---- numbers ---------------------------------------------------------------------------------
 
@@ -267,7 +201,7 @@ __global__ __launch_bounds__(Q_THREADS) void quant_write_kernel(QuantGeo g, int 
     __shared__ unsigned wmax[4];
     const bool is_v = blockIdx.x & 1;
     const int item = blockIdx.x >> 1, hd = item / tiles, b = hd / (g.nl * g.H);
-    const int pos = q_clamp(pos_dev[b], g.cap), cnt = count_dev ? q_clamp(count_dev[b], n) : n, end = min(pos + cnt, g.cap);
+    const int pos = clamp_to(pos_dev[b], g.cap), cnt = count_dev ? clamp_to(count_dev[b], n) : n, end = min(pos + cnt, g.cap);
     const int tile = pos / QT + (item - hd * tiles), row0 = tile * QT;
     if (pos >= end || row0 >= end) return;      // (no rows: the scale of pos's block may be another call's to write)
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, dg = lane & 15, rg = tid >> 4;
@@ -397,7 +331,7 @@ __global__ __launch_bounds__(Q_THREADS) void quant_append_kernel(QuantGeo g, int
     if (item >= items) return;
     const bool is_v = item & 1;
     const int hd = item >> 1, b = hd / (g.nl * g.H);
-    const int pos = q_clamp(pos_dev[b], g.cap), cnt = count_dev ? q_clamp(count_dev[b], n) : n, end = min(pos + cnt, g.cap);
+    const int pos = clamp_to(pos_dev[b], g.cap), cnt = count_dev ? clamp_to(count_dev[b], n) : n, end = min(pos + cnt, g.cap);
     if (pos >= end) return;
     const int lane = threadIdx.x & 63, dg = lane & 15, r4 = lane >> 4;
     const size_t head = g.head(b, hd - b * g.nl * g.H);
@@ -543,7 +477,7 @@ __global__ __launch_bounds__(Q_THREADS) void quant_read_kernel(QuantGeo g, int n
     __shared__ QuantTileSmem<DH> sm;
     const bool both = ko && vo, is_v = both ? blockIdx.x & 1 : vo != nullptr;
     const int item = both ? blockIdx.x >> 1 : blockIdx.x, hd = item / tiles, b = hd / (g.nl * g.H);
-    const int pos = q_clamp(pos_dev[b], g.cap), cnt = count_dev ? q_clamp(count_dev[b], n) : n, end = min(pos + cnt, g.cap);
+    const int pos = clamp_to(pos_dev[b], g.cap), cnt = count_dev ? clamp_to(count_dev[b], n) : n, end = min(pos + cnt, g.cap);
     const int tile = pos / QT + (item - hd * tiles), row0 = tile * QT;
     if (row0 >= end) return;
     const int tid = threadIdx.x, wave = tid >> 6, d0 = (tid & 15) * RUN, rg = tid >> 4;
@@ -626,174 +560,9 @@ struct QuantAttend {
     float2 *ws_row;            // masses: [rows] maximum and sum of rows whose cache is one piece
     float *ws_m;               // masses: [rows][cap / 64] the maximum that a tile's masses are relative to
     float scale;               // log2(e) / sqrt(d)
+    __device__ int cap() const { return g.cap; }
+    __device__ static int tiles_of(int rows) { return (rows + QT - 1) / QT; }
 };
-
-// The kernel's arguments once more, as memory: what only its last part needs is loaded there, and does not take scalar
-// registers from the start (fetching instructions is what a short call waits for, and spills are instructions).
-__device__ inline const QuantAttend &late_args()
-{
-    auto *p = (const __attribute__((address_space(4))) QuantAttend *)__builtin_amdgcn_kernarg_segment_ptr();
-    __asm__ volatile("" : "+s"(p));
-    return *(const QuantAttend *)p;
-}
-
-// Work of a batch: every block of RB query rows of every head has its sequence's tiles (one at least, so that an
-// empty sequence's outputs are written).  W work-groups share them, whatever the lengths are, in one of two ways:
-//   pieces  a block's tiles are cut into pieces of at most `pp` tiles, a work-group each;
-//   line    all tiles in a line, in the order sequence, head, block of rows, tile, are cut into W equal parts (pp = 0), so that a
-//           work-group's part may end one block and begin another.
-// The line is even, but a second block costs a work-group about PIECE_COST tiles' time again (its queries, first tiles and
-// the join of its wavefronts).  A block that is not whole leaves its result in the workspace, in the work-group's slot 1
-// (its first tiles) or 0 (later ones), and a second kernel joins those.  With nrb > 0 there is none of this: every block has its
-// own work-group.
-constexpr int MIN_PIECE = 4;    // tiles of a piece at least, one per wavefront
-constexpr int PIECE_COST = 10;
-
-// a / b for 0 <= a < 2^24 and b > 0
-__device__ inline int div24(int a, int b)
-{
-    int q = (int)((float)a * __builtin_amdgcn_rcpf((float)b));
-    const int r = a - q * b;
-    q += r >= b ? 1 : 0;
-    return q - (r < 0 ? 1 : 0);
-}
-// At least x / y, given inv = 1 / y rounded, and the same in every kernel.
-__device__ inline unsigned at_least(unsigned x, float inv)
-{
-    return (unsigned)__fmul_rn(__fmul_rn((float)x, inv), 1.000001f) + 1;
-}
-
-struct QuantSeq {
-    int len, cnt, tiles, nrb;   // rows, tokens of this call, tiles and blocks of rows of a head (0: none)
-};
-__device__ inline QuantSeq quant_seq(const QuantAttend &a, int b)
-{
-    QuantSeq q = {0, 0, 1, 0};
-    if (b < a.g.B) {
-        q.len = q_clamp(a.len[b], a.g.cap);
-        q.cnt = a.count ? q_clamp(a.count[b], a.n) : a.n;
-        q.tiles = max(1, (q.len + QT - 1) / QT);
-        q.nrb = (q.cnt * a.G + a.RB - 1) >> a.rsh;
-    }
-    return q;
-}
-
-// f(x of this lane, x of lane ^ 16), and the same with lane ^ 32.
-template <typename F>
-__device__ inline float across_quarters(float x, F f)
-{
-    auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = f(__uint_as_float(p[0]), __uint_as_float(p[1]));
-    auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return f(__uint_as_float(q[0]), __uint_as_float(q[1]));
-}
-__device__ inline float quarters_max(float x)
-{
-    return across_quarters(x, [](float a, float b) { return fmaxf(a, b); });
-}
-__device__ inline float quarters_sum(float x)
-{
-    return across_quarters(x, [](float a, float b) { return a + b; });
-}
-// How a batch is shared; every wavefront finds out by itself (lane i has the sequences i, i + 64, ...).
-struct QuantShare {
-    int heads, lane;
-    int pp;              // tiles of a piece, or 0: the line
-    unsigned per;        // items per work-group (tiles of the line, or 1 piece)
-    unsigned total;      // items
-    QuantSeq mine;       // sequence `lane`
-
-    __device__ QuantSeq seq(const QuantAttend &a, int b0) const { return b0 == 0 ? mine : quant_seq(a, b0 + lane); }
-    // items of a block of rows
-    __device__ unsigned span(const QuantSeq &q) const { return pp ? (unsigned)div24(q.tiles + pp - 1, pp) : (unsigned)q.tiles; }
-    __device__ unsigned work(const QuantSeq &q) const { return span(q) * (unsigned)(q.nrb * heads); }
-
-    __device__ void init(const QuantAttend &a, int lane_)
-    {
-        heads = a.g.nl * a.g.H, lane = lane_, pp = 0;
-        unsigned t = 0, units = 0, most = 0;
-        if (a.g.B == 1) {       // (all of it scalar, and no other instructions to fetch)
-            mine = quant_seq(a, 0);
-            t = work(mine), units = (unsigned)(mine.nrb * heads), most = mine.nrb ? (unsigned)mine.tiles : 0u;
-        } else {
-            mine = quant_seq(a, lane);
-            for (int b0 = 0; b0 < a.g.B; b0 += 64) {
-                const QuantSeq q = seq(a, b0);
-                t += work(q);
-                units += (unsigned)(q.nrb * heads);
-                most = max(most, q.nrb ? (unsigned)q.tiles : 0u);
-            }
-            t = wave_sum(t), units = wave_sum(units), most = wave_max(most);
-        }
-        total = t;
-        per = max(at_least(t, a.inv_w), (unsigned)MIN_PIECE);
-        if (units < (unsigned)a.W) {
-            // pieces of at most p tiles are at most t / p + units
-            const unsigned p = min(max(at_least(t, __builtin_amdgcn_rcpf((float)(a.W - units))), (unsigned)MIN_PIECE), most);
-            if (p && piece_len((int)most, (int)p) <= (int)per + PIECE_COST) {
-                pp = (int)p;
-                per = 1;
-                if (a.g.B == 1)
-                    total = uniform(work(mine));
-                else {
-                    t = 0;
-                    for (int b0 = 0; b0 < a.g.B; b0 += 64) t += work(seq(a, b0));
-                    total = wave_sum(t);
-                }
-            }
-        }
-        per = uniform(per), pp = (int)uniform(pp);
-    }
-    // The sequence that item f (< total) belongs to, and the first of its items.
-    __device__ int find(const QuantAttend &a, unsigned f, unsigned &start, QuantSeq &sq) const
-    {
-        if (a.g.B == 1) {
-            start = 0;
-            sq = {(int)uniform(mine.len), (int)uniform(mine.cnt), (int)uniform(mine.tiles), (int)uniform(mine.nrb)};
-            return 0;
-        }
-        unsigned base = 0;
-        for (int b0 = 0;; b0 += 64) {
-            const QuantSeq q = seq(a, b0);
-            const unsigned v = work(q), inc = wave_scan(v);
-            const unsigned long long hit = __ballot(base + inc > f);
-            if (hit) {
-                const int at = __builtin_ctzll(hit);
-                start = base + lane_of(inc - v, at);
-                sq = {(int)lane_of(q.len, at), (int)lane_of(q.cnt, at), (int)lane_of(q.tiles, at), (int)lane_of(q.nrb, at)};
-                return b0 + at;
-            }
-            base += lane_of(inc, 63);
-        }
-    }
-    // Items of the sequences 0 .. end - 1.
-    __device__ unsigned before(const QuantAttend &a, int end) const
-    {
-        if (end == 0) return 0;
-        unsigned t = 0;
-        for (int b0 = 0; b0 < end; b0 += 64) t += b0 + lane < end ? work(seq(a, b0)) : 0u;
-        return wave_sum(t);
-    }
-    // Tiles of the pieces of a block of `tiles` tiles, cut evenly into pieces of at most p.
-    __device__ static int piece_len(int tiles, int p)
-    {
-        const int n = div24(tiles + p - 1, p);
-        return div24(tiles + n - 1, n);
-    }
-};
-
-struct QuantRow {
-    int row_of;      // index into [B][nl][H_q][n] of row r
-    int vis;         // cache rows it sees; -1: not a row of this call
-};
-__device__ inline QuantRow quant_row(const QuantAttend &a, int hd, int r, int len, int cnt)
-{
-    const int i = a.n == 1 ? 0 : r / a.G, j = r - i * a.G;
-    QuantRow q;
-    q.row_of = (hd * a.G + j) * a.n + i;      // hd = (b * nl + l) * H + h
-    q.vis = r < a.R && i < cnt ? max(0, min(len, len - cnt + i + 1)) : -1;
-    return q;
-}
 
 __device__ inline float pow2i(int e)   // 2^e, e in -126 .. 127 (clamped from below)
 {
@@ -815,19 +584,6 @@ __device__ inline int scale_exp(const float (&s)[N])
 #pragma unroll
     for (int i = 0; i < N; ++i) top = fmaxf(top, s[i]);
     return (int)(__float_as_uint(top) >> 23) - 126;
-}
-
-// 2^x by the hardware instruction alone: results below 2^-126 flush to zero, which no sum here shows (every row's
-// holds a term of 2^0).
-__device__ inline float exp2_hw(float x)
-{
-    return __builtin_amdgcn_exp2f(x);
-}
-
-// What a logit is taken relative to when its maximum is m: a row that has seen nothing keeps -inf out of differences.
-__device__ inline float finite_or_zero(float m)
-{
-    return m == -INFINITY ? 0.f : m;
 }
 
 // Eight weights as matrix operands, each the sum of two fp16.  The first is rounded towards zero by one instruction
@@ -873,12 +629,6 @@ struct QuantTokenSmem {
     // 16-byte unit u of a row of o, spread over the banks
     static __device__ int unit(int row, int u) { return (u ^ (row & (DH / 4 - 1) & 15)) * 4; }
 };
-
-// As load_to_lds, past the caches that a stream does not fit.
-__device__ inline void stream_to_lds(const void *base, unsigned off, unsigned lds)
-{
-    __asm__ volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(lds), "v"(off), "s"(base) : "m0", "memory");
-}
 
 // A wave-uniform scale by the scalar unit, whose loads do not count among those of the tiles.
 __device__ inline float scalar_load(const float *p, int i)
@@ -944,7 +694,7 @@ __device__ inline void mass_shares(const QuantAttend &a, size_t row, int len, in
 
 // Tiles ta .. tb - 1 of block rb of head (b, hd)'s rows; slot: where a piece's result goes (-1: the block is whole).
 template <int DH, int FMT, int MT, bool NTL, int NW>
-__device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH, MT, NW> &sm, const QuantSeq &sq, int b, int hd,
+__device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH, MT, NW> &sm, const PartSeq &sq, int b, int hd,
                                          int rb, int ta, int tb, int slot)
 {
     constexpr int NJ = DH / 64, ND = DH / 16, RB = 16 * MT;
@@ -985,14 +735,14 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
         load_v(t);
     }
 
-    QuantRow qr[MT];
+    PartRow qr[MT];
     h8_t qf[MT][2 * NJ];
     float crow[MT], m[MT], sum[MT];
     int vexp[MT];              // o is in units of 2^(vexp - 15); V scales of the rows that the lane's row has seen are below 2^vexp
     qf4_t o[MT][ND];
 #pragma unroll
     for (int r = 0; r < MT; ++r) {
-        qr[r] = quant_row(a, hd, rb * RB + r * 16 + col, len, cnt);
+        qr[r] = part_row(a, hd, rb * RB + r * 16 + col, len, cnt);
         crow[r] = load_queries<NJ>(a.q + (size_t)qr[r].row_of * DH, qr[r].vis >= 0, quarter, a.scale, qf[r]);
         m[r] = -INFINITY;
         sum[r] = 0.f;
@@ -1167,10 +917,10 @@ __device__ inline void quant_token_block(const QuantAttend &a, QuantTokenSmem<DH
         }
     }
     __syncthreads();
-    const QuantAttend &z = late_args();
+    const QuantAttend &z = late_args<QuantAttend>();
     for (int row = threadIdx.x >> 4; row < RB; row += NW * 4) {
         const int d0 = (threadIdx.x & 15) * (DH / 16);
-        const QuantRow rr = quant_row(z, hd, rb * RB + row, len, cnt);
+        const PartRow rr = part_row(z, hd, rb * RB + row, len, cnt);
         if (rr.vis < 0) continue;
         float mm = -INFINITY, ll = 0.f, x[DH / 16];
 #pragma unroll
@@ -1228,58 +978,11 @@ constexpr int token_held()
     return DH == 64 && MT == 1 ? 3 : 2;
 }
 
-// Runs f(sequence, b, head, block of rows, first tile, end tile, slot) for the work-group's part of a batch.
-template <typename F>
-__device__ inline void quant_parts(const QuantAttend &a, F f)
-{
-    QuantShare sh;
-    QuantSeq sq;
-    int b = 0, hd, rb, ta = 0, tb;
-    unsigned i = 0, i1 = 0, start = 0;
-    auto item = [&]() {
-        const unsigned off = i - start, span = uniform(sh.span(sq));
-        const unsigned unit = span == 1 ? off : sh.pp ? (unsigned)div24((int)off, (int)span) : off / span, at = off - unit * span;
-        ta = (int)at;
-        tb = (int)min(span, at + (i1 - i));
-        i += tb - ta;
-        if (sh.pp) {
-            const int len = QuantShare::piece_len(sq.tiles, sh.pp);
-            ta = min(sq.tiles, (int)at * len);
-            tb = min(sq.tiles, ta + len);
-        }
-        hd = sq.nrb == 1 ? (int)unit : (int)unit / sq.nrb;
-        rb = (int)unit - hd * sq.nrb;
-        hd = (int)uniform(hd + b * sh.heads), rb = (int)uniform(rb), ta = (int)uniform(ta), tb = (int)uniform(tb);
-    };
-    if (a.nrb > 0) {
-        hd = a.nrb == 1 ? (int)blockIdx.x : (int)blockIdx.x / a.nrb;
-        rb = (int)blockIdx.x - hd * a.nrb;
-        if (a.g.B > 1) b = hd / (a.g.nl * a.g.H);
-        sq = quant_seq(a, b);
-        if (rb >= sq.nrb) return;
-        tb = sq.tiles;
-    } else {
-        sh.init(a, threadIdx.x & 63);
-        i = blockIdx.x * sh.per;
-        if (i >= sh.total) return;
-        i1 = min(i + sh.per, sh.total);
-        b = sh.find(a, i, start, sq);
-        item();
-    }
-    for (;;) {
-        f(sq, b, hd, rb, ta, tb, ta > 0 ? 0 : tb < sq.tiles ? 1 : -1);
-        if (i >= i1) return;
-        if (i - start >= sh.work(sq)) b = sh.find(a, i, start, sq);
-        item();
-        __syncthreads();
-    }
-}
-
 template <int DH, int FMT, int MT, bool NTL, int NW>
 __global__ __launch_bounds__(64 * NW, (NW == 8 ? 2 : token_held<DH, MT>())) void quant_token_kernel(QuantAttend a)
 {
     __shared__ QuantTokenSmem<DH, MT, NW> sm;
-    quant_parts(a, [&](const QuantSeq &sq, int b, int hd, int rb, int ta, int tb, int slot) {
+    run_parts(a, [&](const PartSeq &sq, int b, int hd, int rb, int ta, int tb, int slot) {
         quant_token_block<DH, FMT, MT, NTL, NW>(a, sm, sq, b, hd, rb, ta, tb, slot);
     });
 }
@@ -1338,7 +1041,7 @@ __device__ inline qu4_t convert8(unsigned a, unsigned b)
 }
 
 template <int DH, int FMT, int KS>
-__device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> &sm, const QuantSeq &sq, int b, int hd, int rb,
+__device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> &sm, const PartSeq &sq, int b, int hd, int rb,
                                         int ta, int tb, int slot)
 {
     constexpr int NS = DH / 16, ND = DH / 32, RB = WIDE_ROWS / KS, NB = 2 / KS;    // NB: blocks of 32 keys of a wavefront
@@ -1399,7 +1102,7 @@ __device__ inline void quant_wide_block(const QuantAttend &a, QuantWideSmem<DH> 
     };
     if (ta < t_end) load(ta);
 
-    const QuantRow qr = quant_row(a, hd, rb * RB + rows32 * 32 + col, len, cnt);
+    const PartRow qr = part_row(a, hd, rb * RB + rows32 * 32 + col, len, cnt);
     h8_t qf[NS];
     float crow;
     {
@@ -1584,24 +1287,10 @@ template <int DH, int FMT, int KS>
 __global__ __launch_bounds__(Q_THREADS, 2) void quant_wide_kernel(QuantAttend a)
 {
     __shared__ QuantWideSmem<DH> sm;
-    quant_parts(a, [&](const QuantSeq &sq, int b, int hd, int rb, int ta, int tb, int slot) {
+    run_parts(a, [&](const PartSeq &sq, int b, int hd, int rb, int ta, int tb, int slot) {
         quant_wide_block<DH, FMT, KS>(a, sm, sq, b, hd, rb, ta, tb, slot);
     });
 }
-
-// Joins the pieces of a cache.  Which pieces of the workspace a block of rows has:
-struct QuantPieces {
-    unsigned w0, n;      // first work-group, pieces
-    int RB;
-    __device__ QuantPieces(const QuantAttend &a, const QuantShare &sh, const QuantSeq &sq, int b, unsigned hd, unsigned rb) : RB(a.RB)
-    {
-        const unsigned span = sh.span(sq), s0 = sh.before(a, b) + ((hd - b * sh.heads) * sq.nrb + rb) * span;
-        w0 = sh.per == 1 ? s0 : s0 / sh.per;
-        n = (sh.per == 1 ? s0 + span - 1 : (s0 + span - 1) / sh.per) - w0 + 1;
-    }
-    // row of piece p: slot 1 of its work-group for the first, 0 for the others
-    __device__ size_t at(unsigned p, unsigned r) const { return (size_t)((w0 + p) * 2 + (p == 0)) * RB + (r & (RB - 1)); }
-};
 
 // Single tokens: a work-group per output row.  A lane has a piece's statistics; the wavefronts share the pieces' sums.  Makes
 // the tiles' block sums shares of the whole as well.  576 rows of 7 pieces 5.4 us, 512 of 16 sequences 7.6: a launch and three
@@ -1614,11 +1303,11 @@ __global__ __launch_bounds__(Q_THREADS) void quant_merge_kernel(QuantAttend a)
     const QuantGeo &g = a.g;
     const unsigned row = blockIdx.x, hd = row / a.G, r = row - hd * a.G;      // n = 1
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = hd / (g.nl * g.H);
-    const QuantSeq sq = quant_seq(a, b);
+    const PartSeq sq = part_seq(a, b);
     if (sq.cnt == 0) return;
-    QuantShare sh;
+    PartShare<QuantAttend> sh;
     sh.init(a, lane);
-    const QuantPieces pc(a, sh, sq, b, hd, r >> a.rsh);
+    const PartPieces<QuantAttend> pc(a, sh, sq, b, hd, r >> a.rsh);
     float m = -INFINITY, sum = 0.f;
     if (pc.n == 1) {
         if (!a.mass) return;
@@ -1670,13 +1359,13 @@ __global__ __launch_bounds__(Q_THREADS) void quant_merge_rows_kernel(QuantAttend
     constexpr int E = DH / 16;
     const unsigned groups = (a.R + 15) / 16, hd = blockIdx.x / groups, r0 = (blockIdx.x - hd * groups) * 16;
     const int b = hd / (a.g.nl * a.g.H);
-    const QuantSeq sq = quant_seq(a, b);
+    const PartSeq sq = part_seq(a, b);
     if ((int)r0 >= sq.cnt * a.G) return;
-    QuantShare sh;
+    PartShare<QuantAttend> sh;
     sh.init(a, threadIdx.x & 63);
-    const QuantPieces pc(a, sh, sq, b, hd, r0 >> a.rsh);
+    const PartPieces<QuantAttend> pc(a, sh, sq, b, hd, r0 >> a.rsh);
     const unsigned r = r0 + (threadIdx.x >> 4), d0 = (threadIdx.x & 15) * E;
-    const QuantRow qr = quant_row(a, hd, r, sq.len, sq.cnt);
+    const PartRow qr = part_row(a, hd, r, sq.len, sq.cnt);
     if (pc.n == 1 || qr.vis < 0) return;
     float m = -INFINITY, sum = 0.f, x[E] = {};
 #pragma unroll 4
