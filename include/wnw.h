@@ -514,6 +514,171 @@ wnw_status wnw_quant_attend_workspace(const wnw_quant_config *cfg, int32_t n_lay
 /* Error reporting, no passage behind it.  Message of the last failed call of this thread on an 8-bit cache. */
 const char *wnw_quant_last_error(void);
 
+/* ---- a paged KV cache, and drafted decoding over it.  Rows of K and V are bf16 and live in pages of `page` rows, which
+ * hold every layer and KV-head; a table gives the pages of every sequence, so that sequences grow, shrink and share
+ * without copies.  One step of drafted decoding: wnw_draft_tree (which drafted tokens see each other, and their
+ * positions), for every layer (or all at once) wnw_paged_append and wnw_paged_attend, then wnw_draft_verify, and
+ * wnw_paged_keep.  A prompt is appended and attended to likewise (n its tokens, no mask), a single token with n = 1.
+ * The calls need no context; the caller owns every buffer, and all of them only enqueue work on hip_stream (NULL = null
+ * stream), a stream of the current device, and allocate nothing, so they can be captured into a graph; tables, lengths and
+ * positions are read on the device when the work runs.  A call handles n_layers layers from first_layer on.
+ *
+ * Layout (cfg->head_dim = d): k, v  bf16 [pages][L][H_kv][page][d], aligned to 16 bytes;
+ * table  int32 [B][table_width]: row r of sequence b is row r % page of page table[b][r / page].  An entry outside
+ * 0 .. pages - 1 (say -1) has no page: its rows are neither written nor seen.  The rows of a sequence may be up to
+ * capacity = table_width * page; positions, lengths and counts outside their ranges count as the nearer end.
+ * Errors: WNW_ERR_INVALID / _UNSUPPORTED / _HIP, message from wnw_paged_last_error(). */
+typedef struct {
+    int32_t batch;        /* B >= 1                                                        */
+    int32_t layers;       /* L >= 1 layers of a page                                       */
+    int32_t kv_heads;     /* H_kv >= 1                                                     */
+    int32_t head_dim;     /* d: 64 or 128                                                  */
+    int32_t page;         /* rows of a page: 16, 32, 64, 128 or 256                        */
+    int32_t pages;        /* pages of the buffers, >= 1                                    */
+    int32_t table_width;  /* pages of a sequence at most, >= 1; capacity <= 2^24           */
+    uint32_t flags;       /* WNW_F_OUT_BF16: wnw_paged_attend writes bf16 instead of fp32  */
+} wnw_paged_config;
+
+typedef struct {          /* device pointers                                               */
+    void *k, *v;
+    const int32_t *table;
+} wnw_paged_cache;
+
+/* Rotary positions: the first `dim` elements of a head's vector are dim / 2 pairs; pair i of a vector at position p is
+ * turned by the angle p * freq[i] and multiplied by `amplitude`; the other elements stay as they are, bit for bit:
+ *   y0 = amplitude * (x0 cos - x1 sin), y1 = amplitude * (x1 cos + x0 sin)
+ * with angles in 64 bits, cos, sin and products in fp32 and one rounding to bf16 (nearest, ties to even). */
+typedef enum { WNW_ROTARY_HALVES = 0,   /* pair i is elements i and i + dim / 2 */
+               WNW_ROTARY_PAIRS = 1     /* pair i is elements 2 i and 2 i + 1   */
+} wnw_rotary_layout;
+
+typedef struct {
+    const float *freq;    /* device fp32 [dim / 2], radians per position; may be NULL with dim 0 */
+    int32_t dim;          /* even, 0 .. d                                                  */
+    int32_t layout;       /* wnw_rotary_layout                                             */
+    float amplitude;      /* finite                                                        */
+} wnw_rotary;
+
+/* Frequencies of the usual kinds (host): f_i = base^(-2 i / dim), for a context longer than the model was trained on
+ * slowed down by `factor` where a pair turns seldom: with r_i = original_len f_i / (2 pi) turns over the original context,
+ * f_i / factor where r_i < low, f_i where r_i > high, and in between the mean of the two with the weights
+ * (high - r_i) / (high - low) and (r_i - low) / (high - low).  factor 1 changes nothing; low = high = infinity slows down
+ * every pair (positions divided by factor).  Computed in 64 bits.
+ *   freq   host fp32 [dim / 2], written
+ * base > 0, factor >= 1, original_len >= 0, 0 <= low <= high. */
+wnw_status wnw_rotary_frequencies(int32_t dim, double base, double factor, double low, double high, int64_t original_len,
+                                  float *freq);
+
+/* Append rows: row i < count[b] of k_dev and v_dev becomes row at[b] + i of sequence b in every head, K rotated by the
+ * token's position; queries are rotated on the way.
+ *   k_dev, v_dev  device bf16 [B][n_layers][H_kv][n][d], 16-byte aligned; both may be NULL where q_dev is given (queries
+ *                 alone)
+ *   q_dev, q_out  device bf16 [B][n_layers][q_heads][n][d], 16-byte aligned, q_out may be q_dev; or both NULL.  q_out's rows
+ *                 at or after count[b] are left as they were; rows without a place in the cache are rotated all the same
+ *   at_dev        device int32 [B]: rows that the sequence has
+ *   count_dev     device int32 [B], 0 .. n; NULL = n for every sequence
+ *   position_dev  device int32 [B][n], any values; NULL = at[b] + i
+ *   rotary        NULL: nothing is rotated
+ * Two calls whose work overlaps must not write the same rows. */
+wnw_status wnw_paged_append(const wnw_paged_config *cfg, const wnw_paged_cache *cache, const wnw_rotary *rotary,
+                            int32_t first_layer, int32_t n_layers, int32_t q_heads, int32_t n, const void *k_dev,
+                            const void *v_dev, const void *q_dev, void *q_out, const int32_t *at_dev,
+                            const int32_t *count_dev, const int32_t *position_dev, void *hip_stream);
+
+/* Attention of a sequence's last count[b] tokens over its rows, their own (already appended) among them: token i of count[b]
+ * sees rows 0 .. len[b] - count[b] - 1, and of the tokens' own rows those that the mask says (row len[b] - count[b] + j is token
+ * j's), without a mask those of tokens 0 .. i.  Logit scale 1 / sqrt(d); products of bf16 summed in fp32, softmax statistics
+ * in fp32.  fp32 outputs: softmax weights to 24 bits.  bf16 outputs (WNW_F_OUT_BF16): up to 32 query rows n * H_q / H_kv the
+ * fp32 results rounded (nearest, ties to even); with more, weights are rounded to bf16 before they multiply V, and
+ * normalised by the sum of the rounded ones.  What a token does not see has no part in its outputs, infinities and NaN
+ * included.  A token that sees no row (or whose logits are all -inf) gets zeros and the log-sum-exp -inf; otherwise a query
+ * row with a NaN or an infinity gets NaN in all of its outputs, and an element of out_dev for which a row seen has a V
+ * element that is not finite is not finite.
+ *   q_heads    a multiple of kv_heads (any group size); q-head hq belongs to KV-head hq / (H_q / H_kv)
+ *   q_dev      device bf16 [B][n_layers][H_q][n][d], 16-byte aligned
+ *   len_dev    device int32 [B], rows of the sequence, the tokens' own among them (count[b] is taken as len[b] where it is more)
+ *   count_dev  device int32 [B], 0 .. n; NULL = n for every sequence
+ *   mask_dev   device uint64 [B][n][(n + 63) / 64]: bit j % 64 of word j / 64 of row i: token i sees token j's row (its own only if
+ *              bit i is set); NULL: causal
+ *   out_dev    device fp32 / bf16 [B][n_layers][H_q][n][d], 16-byte aligned
+ *   lse_dev    device fp32 [B][n_layers][H_q][n], natural log of the sum of exp(logit); may be NULL
+ *   max_len    upper bound of the lengths, 0 = capacity.  It only shapes the launch: a longer sequence is still attended to
+ *              in full
+ *   workspace  device memory, 16-byte aligned, of at least the bytes that wnw_paged_attend_workspace gives for the same cfg,
+ *              n_layers, q_heads, n and max_len; may be NULL where that is 0.  It holds nothing between calls; calls whose work
+ *              overlaps (two streams, two graphs replayed at once) need one each
+ * Outputs of tokens at or after count[b] are left as they were. */
+wnw_status wnw_paged_attend(const wnw_paged_config *cfg, const wnw_paged_cache *cache, int32_t first_layer,
+                            int32_t n_layers, int32_t q_heads, int32_t n, const void *q_dev, const int32_t *len_dev,
+                            const int32_t *count_dev, const uint64_t *mask_dev, void *out_dev, float *lse_dev,
+                            int32_t max_len, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Workspace of wnw_paged_attend for these sizes, in bytes (with or without mask and lse_dev). */
+wnw_status wnw_paged_attend_workspace(const wnw_paged_config *cfg, int32_t n_layers, int32_t q_heads, int32_t n,
+                                      int32_t max_len, size_t *bytes);
+
+/* Keep the rows of the drafted tokens that stand: row base[b] + path[b][i] becomes row base[b] + i, for i < count[b], in the
+ * layers from first_layer on; K rows keep the rotation of their positions.  A path ascends (as wnw_draft_verify gives it): it
+ * ends in front of the first entry that is not larger than the one before it, is negative or lies past the capacity.
+ *   base_dev   device int32 [B]: rows of the sequence without its draft
+ *   n          entries of a path, 0 <= n <= 1024
+ *   path_dev   device int32 [B][n]
+ *   count_dev  device int32 [B], 0 .. n; NULL = n for every sequence */
+wnw_status wnw_paged_keep(const wnw_paged_config *cfg, const wnw_paged_cache *cache, int32_t first_layer, int32_t n_layers,
+                          int32_t n, const int32_t *base_dev, const int32_t *path_dev, const int32_t *count_dev,
+                          void *hip_stream);
+
+/* Error reporting, no passage behind it.  Message of the last failed call of this thread on a paged cache. */
+const char *wnw_paged_last_error(void);
+
+/* A draft's tree: token i < count[b] follows token parent[b][i] (an earlier one; -1 or anything else outside 0 .. i - 1: the
+ * sequence as it is).  Token i sees itself and the tokens on its path, and its position is base[b] and the tokens before it on its
+ * path.
+ *   batch >= 1, 0 <= n <= 1024
+ *   parent_dev    device int32 [B][n]
+ *   base_dev      device int32 [B]: position of the draft's first token
+ *   count_dev     device int32 [B], 0 .. n; NULL = n for every sequence
+ *   mask_dev      device uint64 [B][n][(n + 63) / 64], as wnw_paged_attend takes it; may be NULL
+ *   position_dev  device int32 [B][n], as wnw_paged_append takes it; may be NULL
+ * Entries of tokens at or after count[b] are left as they were.  Errors of this and the next call: WNW_ERR_INVALID /
+ * _UNSUPPORTED / _HIP, message from wnw_draft_last_error(); both only enqueue work, as the calls above do. */
+wnw_status wnw_draft_tree(int32_t batch, int32_t n, const int32_t *parent_dev, const int32_t *base_dev,
+                          const int32_t *count_dev, uint64_t *mask_dev, int32_t *position_dev, void *hip_stream);
+
+/* Which drafted tokens stand, and the token after them, so that what comes out is distributed as the target says.
+ * From the sequence as it is on: the tokens that follow the last one that stands are tried in the order of their indexes, with
+ * p the target's probabilities behind it and q the draft's.  Token i, drawn from q, stands if
+ *   uniform[i] * q[token] < p[token];
+ * otherwise p becomes max(p - q, 0) divided by its sum, and the next one is tried.  Without draft_dev the draft is taken to
+ * have chosen its tokens, not drawn them: token i stands if uniform[i] * s < p[token], s = 1 at first; otherwise s becomes less by
+ * p[token], and p[token] 0.  When no token is left to try, the token after the path is drawn from p as it is then (from the
+ * target's row itself, if nothing of p is left): the first one at which the running sum of p, in the order of tokens, exceeds
+ * uniform[n] times its total (the last one with p > 0 if none does; -1 where the total is not a positive finite number).  Sums and
+ * comparisons are in 64 bits; a token whose p or q is NaN has nothing left.  Tokens outside 0 .. vocab - 1 never stand.
+ *   batch >= 1, 0 <= n <= 1024, vocab 1 .. 2^24
+ *   token_dev     device int32 [B][n]; may be NULL with n = 0
+ *   parent_dev    device int32 [B][n], as above; NULL: each follows the one before it
+ *   count_dev     device int32 [B], 0 .. n; NULL = n for every sequence
+ *   target_dev    device fp32 [B][n + 1][vocab]: probabilities (they are taken to add up to 1) behind the sequence as it is
+ *                 (row 0) and behind token i (row i + 1)
+ *   draft_dev     device fp32 [B][n + 1][vocab]: the draft's, row i + 1 for the tokens that follow token i; rows that no token
+ *                 follows are not read; may be NULL
+ *   uniform_dev   device fp32 [B][n + 1], in [0, 1)
+ *   path_dev      device int32 [B][n], written: the tokens that stand, ascending, then -1; may be NULL with n = 0
+ *   accepted_dev  device int32 [B], written: how many stand
+ *   next_dev      device int32 [B], written: the token after them
+ *   workspace     as wnw_paged_attend's; wnw_draft_verify_workspace gives its size */
+wnw_status wnw_draft_verify(int32_t batch, int32_t n, int32_t vocab, const int32_t *token_dev, const int32_t *parent_dev,
+                            const int32_t *count_dev, const float *target_dev, const float *draft_dev,
+                            const float *uniform_dev, int32_t *path_dev, int32_t *accepted_dev, int32_t *next_dev,
+                            void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Workspace of wnw_draft_verify for these sizes, in bytes. */
+wnw_status wnw_draft_verify_workspace(int32_t batch, int32_t n, int32_t vocab, size_t *bytes);
+
+/* Error reporting, no passage behind it.  Message of the last failed call of this thread on a draft. */
+const char *wnw_draft_last_error(void);
+
 #ifdef __cplusplus
 }
 #endif

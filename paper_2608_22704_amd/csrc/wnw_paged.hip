@@ -1,0 +1,943 @@
+// A paged KV cache in bf16: appending rows with the rotation of their positions, attention over the pages for single tokens,
+// drafts, their trees and prompts, and moving the rows of accepted tokens.  Layout and definitions as in wnw.h.
+//
+//   paged_append_kernel  new rows of K and V to their pages and queries to their place, rotated on the way
+//   paged_keep_kernel    accepted rows to the end of their sequence, a wavefront per head's K or V
+//   paged_token_kernel   attention in blocks of 16 or 32 query rows of a KV-head, every wavefront with tiles of its own
+//   paged_join_kernel    joins the parts of a cache that work-groups shared
+#include "wnw.h"
+#include "wnw_internal.h"
+#include "wnw_parts.h"
+
+#include <math.h>
+
+#include <algorithm>
+#include <cstring>
+#include <type_traits>
+
+namespace wnw {
+
+namespace {
+
+constexpr int P_THREADS = 256;
+constexpr int P_MAX_CAP = 1 << 24;
+constexpr int64_t P_MAX_GROUPS = 0xffffffffll / P_THREADS;   // a launch has fewer than 2^32 threads
+constexpr float P_LOG2E = 1.4426950408889634f;
+constexpr float P_LN2 = 0.6931471805599453f;
+
+typedef float pf4_t __attribute__((ext_vector_type(4)));
+typedef unsigned pu2_t __attribute__((ext_vector_type(2)));
+typedef unsigned pu4_t __attribute__((ext_vector_type(4)));
+typedef short ps4_t __attribute__((ext_vector_type(4)));
+
+// The pages and the layers of them that a call handles.
+struct PagedGeo {
+    int B, L, H, l0, nl;
+    int pages, width, psh;    // pages of the buffers and of a sequence, log2 of a page's rows
+    uint16_t *k, *v;
+    const int32_t *table;
+    __host__ __device__ int cap() const { return width << psh; }
+    // first row, in rows of d elements, that page `id` has for layer l0 + l and KV-head h
+    __device__ size_t page_row(int id, int l, int h) const { return (((size_t)id * L + l0 + l) * H + h) << psh; }
+    __device__ bool has(int id) const { return (unsigned)id < (unsigned)pages; }
+};
+
+__device__ inline uint16_t to_bf16(float f)
+{
+    return __builtin_bit_cast(uint16_t, (__bf16)f);   // nearest, ties to even
+}
+__device__ inline float bf16_at(pu4_t u, int e)
+{
+    return __uint_as_float(e & 1 ? u[e >> 1] & 0xffff0000u : u[e >> 1] << 16);
+}
+
+// ---- appending -------------------------------------------------------------------------------
+
+struct PagedAppend {
+    PagedGeo g;
+    int Hq, n, tiles, split;     // tiles: groups of tokens; split: work-groups that share a layer's vectors
+    int dim, vectors;            // vectors of a token and layer: K and V of every KV-head, then the queries
+    float amplitude;
+    const float *freq;
+    const uint16_t *kn, *vn, *q;
+    uint16_t *q_out;
+    const int32_t *at, *count, *position;
+};
+
+// How a pair's two elements lie.
+enum { TURN_NONE, TURN_PAIRS, TURN_HALVES, TURN_HALVES_ODD };
+
+// A lane has 16 bytes (eight elements) of a vector: neighbours d / 8 lanes one vector, and the work-group TT tokens' vectors of
+// HH heads at a time, going through the layer's heads with the angles of its lanes in registers.  An element's partner is in
+// the lane itself (pairs) or comes from the lane that has it, halves of a multiple of eight elements by four moves, others by two
+// for each element.
+template <int DH, int TURN>
+__global__ __launch_bounds__(P_THREADS) void paged_append_kernel(PagedAppend a, int TT)
+{
+    constexpr int UN = DH / 8, SLOTS = P_THREADS / UN;
+    const PagedGeo &g = a.g;
+    const int HH = SLOTS / TT, tid = threadIdx.x, u = tid % UN, slot = tid / UN, lane = tid & 63;
+    int item = blockIdx.x;
+    const int part = item % a.split;
+    item /= a.split;
+    const int tile = item % a.tiles;
+    item /= a.tiles;
+    const int l = item % g.nl, b = item / g.nl;
+    const int i = tile * TT + slot % TT, cnt = a.count ? clamp_to(a.count[b], a.n) : a.n;
+    if (tile * TT >= cnt) return;
+    const bool live = i < cnt;
+    const int at = clamp_to(a.at[b], g.cap()), row = at + i;
+    int id = -1;
+    if (live && row < g.cap()) id = g.table[(size_t)b * g.width + (row >> g.psh)];
+    const bool place = g.has(id);
+    // the lane's angles
+    float cs[8], sn[8];
+    const int half = a.dim >> 1;
+    if constexpr (TURN != TURN_NONE) {
+        const double pos = a.position && live ? (double)a.position[(size_t)b * a.n + i] : (double)row;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int x = u * 8 + e;
+            if (TURN == TURN_PAIRS && (e & 1)) {
+                cs[e] = cs[e - 1], sn[e] = -sn[e - 1];
+                continue;
+            }
+            cs[e] = 1.f, sn[e] = 0.f;
+            if (x < a.dim) {
+                const int pair = TURN == TURN_PAIRS ? x >> 1 : x < half ? x : x - half;
+                // turns, and without the whole ones: the product of position and frequency is exact in a double
+                const double turns = pos * (double)a.freq[pair] * 0.15915494309189535;
+                const float rest = (float)(turns - rint(turns));
+                float s, c;
+                sincospif(2.f * rest, &s, &c);
+                cs[e] = c * a.amplitude;
+                sn[e] = s * a.amplitude;
+                if (TURN == TURN_PAIRS || x < half) sn[e] = -sn[e];
+            }
+        }
+    }
+    for (int v = part * HH + slot / TT; v < a.vectors; v += a.split * HH) {
+        const int kv = a.kn ? 2 * g.H : 0;
+        const bool is_v = v >= g.H && v < kv, is_q = v >= kv;
+        const int h = is_q ? v - kv : is_v ? v - g.H : v;
+        const uint16_t *src = is_q ? a.q : is_v ? a.vn : a.kn;
+        uint16_t *dst;
+        bool put = live;
+        if (is_q)
+            dst = a.q_out + ((((size_t)b * g.nl + l) * a.Hq + h) * a.n + i) * DH;
+        else {
+            put = place;
+            dst = (is_v ? g.v : g.k) + (g.page_row(place ? id : 0, l, h) + (row & ((1 << g.psh) - 1))) * DH;
+        }
+        pu4_t x = {0, 0, 0, 0};
+        if (put) x = *(const pu4_t *)(src + ((((size_t)b * g.nl + l) * (is_q ? a.Hq : g.H) + h) * a.n + i) * DH + u * 8);
+        if constexpr (TURN != TURN_NONE) {
+            pu4_t o = x;     // partners
+            if constexpr (TURN == TURN_PAIRS) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = x[e] << 16 | x[e] >> 16;
+            } else if constexpr (TURN == TURN_HALVES) {
+                const int hu = half >> 3, other = u < hu ? u + hu : u < 2 * hu ? u - hu : u;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = (unsigned)__shfl((int)x[e], lane - u + other);
+            } else {
+                const int up = half & 7, down = 8 - up;      // half = 8 hu + up
+                uint16_t y[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    // from u + hu (+ 1) or from u - hu (- 1); the words to send are the same for all lanes
+                    const int e0 = (e + up) & 7, e1 = (e + down) & 7, hu = half >> 3;
+                    unsigned w0 = x[0], w1 = x[0];
+#pragma unroll
+                    for (int k = 1; k < 4; ++k) {
+                        w0 = e0 >> 1 == k ? x[k] : w0;
+                        w1 = e1 >> 1 == k ? x[k] : w1;
+                    }
+                    const int l0 = u + hu + (e + up >= 8), l1 = u - hu - (e < up);
+                    const unsigned g0 = (unsigned)__shfl((int)w0, lane - u + min(max(l0, 0), UN - 1)),
+                                   g1 = (unsigned)__shfl((int)w1, lane - u + min(max(l1, 0), UN - 1));
+                    const bool first = u * 8 + e < half;
+                    const unsigned w = first ? g0 : g1;
+                    y[e] = (uint16_t)((first ? e0 : e1) & 1 ? w >> 16 : w);
+                }
+                __builtin_memcpy(&o, y, sizeof(o));
+            }
+            if (!is_v) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float y0 = fmaf(bf16_at(o, 2 * e), sn[2 * e], bf16_at(x, 2 * e) * cs[2 * e]),
+                                y1 = fmaf(bf16_at(o, 2 * e + 1), sn[2 * e + 1], bf16_at(x, 2 * e + 1) * cs[2 * e + 1]);
+                    const unsigned r0 = u * 8 + 2 * e < a.dim ? to_bf16(y0) : x[e] & 0xffffu,
+                                   r1 = u * 8 + 2 * e + 1 < a.dim ? to_bf16(y1) : x[e] >> 16;
+                    x[e] = r0 | r1 << 16;
+                }
+            }
+        }
+        if (put) *(pu4_t *)(dst + u * 8) = x;
+    }
+}
+
+// ---- keeping ---------------------------------------------------------------------------------
+
+// A wavefront has a head's K or V.  A path ascends, so that row base + i is no source of a later entry, and the rows of one step
+// are read before any of them is written.
+template <int DH>
+__global__ __launch_bounds__(P_THREADS) void paged_keep_kernel(PagedGeo g, int n, int items, const int32_t *__restrict__ base_dev,
+                                                               const int32_t *__restrict__ path_dev,
+                                                               const int32_t *__restrict__ count_dev)
+{
+    constexpr int UN = DH / 8, ROWS = 64 / UN, STEP = 4;
+    const int item = blockIdx.x * (P_THREADS / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (item >= items) return;
+    const bool is_v = item & 1;
+    const int hd = item >> 1, b = hd / (g.nl * g.H), lh = hd - b * g.nl * g.H, l = lh / g.H, h = lh - l * g.H;
+    const int cap = g.cap(), base = clamp_to(base_dev[b], cap);
+    const int32_t *path = path_dev + (size_t)b * n, *table = g.table + (size_t)b * g.width;
+    int cnt = count_dev ? clamp_to(count_dev[b], n) : n;
+    for (int i0 = 0; i0 < cnt; i0 += 64) {
+        const int i = i0 + lane;
+        bool ends = false;
+        if (i < cnt) ends = path[i] < 0 || path[i] >= cap - base || (i > 0 && path[i] <= path[i - 1]);
+        const unsigned long long some = __ballot(ends);
+        if (some) cnt = i0 + __builtin_ctzll(some);
+    }
+    uint16_t *pool = is_v ? g.v : g.k;
+    const int u = lane % UN, r = lane / UN, mask = (1 << g.psh) - 1;
+    for (int i0 = 0; i0 < cnt; i0 += ROWS * STEP) {
+        pu4_t x[STEP];
+        uint16_t *to[STEP];
+#pragma unroll
+        for (int j = 0; j < STEP; ++j) {
+            const int i = i0 + j * ROWS + r;
+            to[j] = nullptr;
+            if (i >= cnt || path[i] == i) continue;
+            const int from = base + path[i], into = base + i, id0 = table[from >> g.psh], id1 = table[into >> g.psh];
+            if (!g.has(id0) || !g.has(id1)) continue;
+            x[j] = *(const pu4_t *)(pool + (g.page_row(id0, l, h) + (from & mask)) * DH + u * 8);
+            to[j] = pool + (g.page_row(id1, l, h) + (into & mask)) * DH + u * 8;
+        }
+#pragma unroll
+        for (int j = 0; j < STEP; ++j)
+            if (to[j]) *(pu4_t *)to[j] = x[j];
+    }
+}
+
+// ---- attention -------------------------------------------------------------------------------
+
+struct PagedAttend {
+    PagedGeo g;
+    int G, n, R;               // q-heads per KV-head, tokens, rows G * n of a KV-head: row r is token r / G, q-head r % G
+    int W, RB, rsh;            // work-groups that share the batch's tiles, rows of a block and their log2
+    int tsh;                   // log2 of the cache rows of a tile
+    int bf16;                  // outputs are bf16
+    int nrb;                   // > 0: a work-group per block of rows, nrb blocks a head, nothing to join
+    float inv_w;               // 1 / W
+    const uint16_t *q;
+    const int32_t *len, *count;
+    const unsigned long long *mask;
+    void *out;
+    float *lse;
+    float *ws_o;               // [W][2][RB][d]: sums of weights times values of a block of rows over a piece of its cache
+    float2 *ws_ml;             // [W][2][RB]: the piece's maximum (base 2) and sum of weights
+    float scale;               // log2(e) / sqrt(d)
+    __device__ int cap() const { return g.cap(); }
+    __device__ int tiles_of(int rows) const { return (rows + (1 << tsh) - 1) >> tsh; }
+};
+
+template <int E>
+__device__ inline void store_out(void *out, bool bf16, size_t elem, const float (&x)[E])
+{
+    if (bf16) {
+        uint16_t u[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) u[e] = to_bf16(x[e]);
+        __builtin_memcpy(__builtin_assume_aligned((uint16_t *)out + elem, E * 2), u, sizeof(u));
+    } else
+        __builtin_memcpy(__builtin_assume_aligned((float *)out + elem, 16), x, sizeof(x));
+}
+
+// What a query row sees of the drafted tokens' own rows.
+struct PagedRow {
+    int row_of;      // index into [B][nl][H_q][n] of row r
+    int token;       // of the call, or -1: not a row of it
+};
+__device__ inline PagedRow paged_row(const PagedAttend &a, int hd, int r, int cnt)
+{
+    const int i = a.n == 1 ? 0 : r / a.G, j = r - i * a.G;
+    return {(hd * a.G + j) * a.n + i, r < a.R && i < cnt ? i : -1};      // hd = (b * nl + l) * H + h
+}
+
+// The lowest n bits.
+__device__ inline unsigned long long low_bits(int n)
+{
+    return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1;
+}
+// Which of the rows t0 .. t0 + 63 of sequence b token i sees; base: the first of the tokens' own rows, len: the rows there are.
+__device__ inline unsigned long long sees(const PagedAttend &a, int b, int i, int t0, int base, int len)
+{
+    if (i < 0) return 0;
+    if (!a.mask) return low_bits(min(base + i + 1, len) - t0);
+    unsigned long long s = low_bits(base - t0);
+    const int words = (a.n + 63) >> 6, j0 = t0 - base;       // bit j of the mask is row t0 + (j - j0)
+    const unsigned long long *m = a.mask + ((size_t)b * a.n + i) * words;
+    if (j0 >= 0) {
+        const int w = j0 >> 6, sh = j0 & 63;
+        if (w < words) s |= m[w] >> sh;
+        if (sh && w + 1 < words) s |= m[w + 1] << (64 - sh);
+    } else if (j0 > -64)
+        s |= m[0] << -j0;
+    return s & low_bits(len - t0);
+}
+
+// A wave-uniform table entry by the scalar unit, whose loads do not count among those of the tiles.
+__device__ inline int scalar_entry(const int32_t *p, int i)
+{
+    return ((const __attribute__((address_space(4))) int32_t *)p)[i];
+}
+
+// Eight weights as three matrix operands whose sum they are, exactly: 8 bits of the 24 each.
+__device__ inline unsigned high_halves(float a, float b)
+{
+    return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+__device__ inline float top8(float x)
+{
+    return __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+}
+__device__ inline void weights_to_bf16(const float (&p)[8], bf16x8_t (&t)[3])
+{
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = p[i];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        pu4_t u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) u[i] = high_halves(x[2 * i], x[2 * i + 1]);
+        t[k] = __builtin_bit_cast(bf16x8_t, u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] -= top8(x[i]);
+    }
+}
+
+// 16 rows of the lane's 16-lane group, four elements each, as columns: lane n gives the address of elements 4 (n % 4) .. + 4 of row
+// n / 4 of four rows of 16, and gets element n of each of them.
+__device__ inline pu2_t column_read(unsigned lds)
+{
+    return __builtin_bit_cast(pu2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) ps4_t *)(size_t)lds));
+}
+
+__device__ inline bool some_not_finite(pu4_t u)
+{
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) bad |= (u[e] & 0x7f80u) == 0x7f80u || (u[e] & 0x7f800000u) == 0x7f800000u;
+    return bad;
+}
+// Elements that are not finite, as ones; or the finite ones, the others zero.
+__device__ inline pu4_t not_finite_or_rest(pu4_t u, bool ones)
+{
+    pu4_t y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const unsigned lo = (u[e] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u, hi = (u[e] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
+        y[e] = ones ? (lo | hi) & 0x3f803f80u : u[e] & ~(lo | hi);
+    }
+    return y;
+}
+
+// Tiles of TR rows of d elements, 8 KB, in a wavefront's own shared memory.  16-byte unit u of row r stands at position u ^ swz(r)
+// of the row, so that eight lanes reading one unit of eight rows, and sixteen reading two units of four rows, meet distinct banks.
+template <int DH>
+struct PagedTile {
+    static constexpr int UN = DH / 8, TR = 4096 / DH, SUB = TR / 16;   // units of a row, rows, 16-row parts
+    static constexpr int ROW = DH * 2, PART = 16 * ROW;                // bytes
+    static __device__ unsigned swz(unsigned r) { return DH == 128 ? (r & 7) * 2 : (r >> 1 & 3) * 2; }
+};
+template <int DH, int MT, int NW>
+struct PagedTokenSmem {
+    union {
+        alignas(256) unsigned char tile[NW][2][8192];   // [wavefront][K, V]
+        alignas(16) float o[NW][4096];                  // rows of d, in the wavefront's own tiles: others may still be reading theirs
+    };
+    float m[NW][16 * MT], l[NW][16 * MT];
+    static_assert(sizeof(tile) == sizeof(o) && 16 * MT * DH <= 4096, "a wavefront's results lie in its tiles");
+    // 16-byte unit u of row `row` of o, spread over the banks
+    static __device__ int unit(int row, int u) { return row * DH + (u ^ (row & (DH / 4 - 1) & 15)) * 4; }
+};
+
+// Tiles ta .. tb - 1 of block rb of head (b, hd)'s rows; slot: where a piece's result goes (-1: the block is whole).
+template <int DH, int MT, bool NTL, int NW>
+__device__ inline void paged_token_block(const PagedAttend &a, PagedTokenSmem<DH, MT, NW> &sm, const PartSeq &sq, int b, int hd, int rb,
+                                         int ta, int tb, int slot)
+{
+    using T = PagedTile<DH>;
+    constexpr int NS = DH / 32, ND = DH / 16, RB = 16 * MT, LOADS = 4096 * 2 / 1024;
+    const PagedGeo &g = a.g;
+    const int len = sq.len, cnt = min(sq.cnt, len), base = len - cnt;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 15, quarter = lane >> 4;
+    const int lh = hd - b * g.nl * g.H, l = lh / g.H, h = lh - l * g.H;
+    const int32_t *table = g.table + (size_t)b * g.width;
+
+    // cache rows that the block's last and first row may see
+    const int last = min(cnt - 1, min(rb * RB + RB - 1, a.R - 1) / a.G), first = rb * RB / a.G;
+    const int seen = cnt <= first ? 0 : a.mask ? len : base + last + 1;
+    const int full = (int)uniform(a.mask ? base : base + first + 1);
+    const int t_end = (int)uniform(min(tb, (seen + T::TR - 1) / T::TR));
+    int t = ta + wave;
+
+    const unsigned lds_k = __builtin_amdgcn_readfirstlane(lds_address(sm.tile[wave][0])),
+                   lds_v = __builtin_amdgcn_readfirstlane(lds_address(sm.tile[wave][1]));
+    // lane i's 16 bytes of a load of 1 KB land at 16 i: which unit of which row that is
+    unsigned off[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const unsigned r = j * (64 / T::UN) + lane / T::UN, u = lane % T::UN;
+        off[j] = r * T::ROW + (u ^ T::swz(r)) * 16;
+    }
+    // The pages of a tile's 16-row parts, as the first row of d elements that they have for the head; parts that are not there
+    // or past the sequence's end read page 0.
+    struct Parts {
+        size_t row[T::SUB];
+        unsigned gone;       // bit s: part s has no page
+    };
+    auto parts_of = [&](int t) {
+        Parts p;
+        p.gone = 0;
+#pragma unroll
+        for (int s = 0; s < T::SUB; ++s) {
+            const int r = t * T::TR + s * 16;
+            const int id = r < len ? scalar_entry(table, r >> g.psh) : 0;
+            const bool has = g.has(id);
+            if (!has) p.gone |= 1u << s;
+            p.row[s] = g.page_row(has ? id : 0, l, h) + (r & ((1 << g.psh) - 1));
+        }
+        return p;
+    };
+    auto load = [&](const uint16_t *pool, const Parts &p, unsigned lds) {
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+            constexpr int PER = LOADS / T::SUB;       // loads of a part
+            const uint16_t *from = pool + p.row[j / PER] * DH + (j % PER & ~1) * 512;
+            const unsigned o = off[j % PER & 1];
+            NTL ? stream_to_lds(from, o, lds + j * 1024) : load_to_lds(from, o, lds + j * 1024);
+        }
+    };
+    Parts now, next;
+    if (t < t_end) {
+        now = parts_of(t);
+        load(g.k, now, lds_k);
+        load(g.v, now, lds_v);
+        next = parts_of(min(t + NW, t_end - 1));
+    }
+
+    PagedRow qr[MT];
+    bf16x8_t qf[MT][NS];
+    float crow[MT], m[MT], sum[MT];
+    pf4_t o[MT][ND];
+#pragma unroll
+    for (int r = 0; r < MT; ++r) {
+        qr[r] = paged_row(a, hd, rb * RB + r * 16 + col, cnt);
+        bool bad = false;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            pu4_t u = {0, 0, 0, 0};
+            if (qr[r].token >= 0) u = *(const pu4_t *)(a.q + (size_t)qr[r].row_of * DH + s * 32 + quarter * 8);
+            bad |= some_not_finite(u);
+            qf[r][s] = __builtin_bit_cast(bf16x8_t, u);
+        }
+        bad = quarters_max(bad ? 1.f : 0.f) > 0.f;
+        crow[r] = bad ? __uint_as_float(0x7fc00000u) : a.scale;
+        m[r] = -INFINITY;
+        sum[r] = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt) o[r][dt] = pf4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    // K: row col of a part, unit 4 s + quarter; V: row 4 quarter + col / 4, two units of 16 elements dt, of which the lane reads 8 bytes
+    const unsigned k_at = lds_k + col * T::ROW + (quarter ^ T::swz(col)) * 16;
+    const unsigned v_row = quarter * 4 + col / 4, v_at = lds_v + v_row * T::ROW + T::swz(v_row) * 16 + (col & 3) * 8;
+
+    for (; t < t_end; t += NW) {
+        const bool masked = t * T::TR + T::TR > full || now.gone;   // some row does not see all of the tile
+        const bool more = t + NW < t_end;
+        const unsigned gone = now.gone;
+        float x[MT][T::SUB][4];
+        lds_loads_wait<LOADS>();       // K is there, V may be under way
+#pragma unroll
+        for (int kb = 0; kb < T::SUB; ++kb) {
+            pf4_t c[MT] = {};
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                const bf16x8_t k = frag_read((k_at ^ s * 64) + kb * T::PART);
+#pragma unroll
+                for (int r = 0; r < MT; ++r) c[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[r][s], c[r], 0, 0, 0);
+            }
+#pragma unroll
+            for (int r = 0; r < MT; ++r)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[r][kb][i] = c[r][i] * crow[r];
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the bytes have been read
+        if (more) load(g.k, next, lds_k);
+        __builtin_amdgcn_sched_barrier(0);
+
+        unsigned long long here = 0;       // rows of the tile that there are
+        if (masked) {
+            here = low_bits(len - t * T::TR);
+#pragma unroll
+            for (int s = 0; s < T::SUB; ++s)
+                if (gone >> s & 1) here &= ~(0xffffull << (16 * s));
+        }
+        unsigned long long see[MT];
+        bf16x8_t p[MT][T::SUB / 2][3];
+#pragma unroll
+        for (int r = 0; r < MT; ++r) {
+            if (masked) {
+                see[r] = (sees(a, b, qr[r].token, t * T::TR, base, len) & here) >> (quarter * 4);
+#pragma unroll
+                for (int kb = 0; kb < T::SUB; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[r][kb][i] = see[r] >> (kb * 16 + i) & 1 ? x[r][kb][i] : -INFINITY;
+            }
+            float mt = m[r];
+#pragma unroll
+            for (int kb = 0; kb < T::SUB; ++kb) mt = fmaxf(mt, fmaxf(fmaxf(x[r][kb][0], x[r][kb][1]), fmaxf(x[r][kb][2], x[r][kb][3])));
+            mt = quarters_max(mt);
+            if (__any(mt > m[r])) {
+                const float alpha = exp2_hw(m[r] - finite_or_zero(mt));
+#pragma unroll
+                for (int dt = 0; dt < ND; ++dt) o[r][dt] *= alpha;
+                sum[r] *= alpha;
+                m[r] = mt;
+            }
+            const float mz = finite_or_zero(m[r]);
+#pragma unroll
+            for (int kb = 0; kb < T::SUB; ++kb) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[r][kb][i] = exp2_hw(x[r][kb][i] - mz);
+                sum[r] += (x[r][kb][0] + x[r][kb][1]) + (x[r][kb][2] + x[r][kb][3]);
+            }
+#pragma unroll
+            for (int c = 0; c < T::SUB / 2; ++c) {
+                const float w[8] = {x[r][2 * c][0],     x[r][2 * c][1],     x[r][2 * c][2],     x[r][2 * c][3],
+                                    x[r][2 * c + 1][0], x[r][2 * c + 1][1], x[r][2 * c + 1][2], x[r][2 * c + 1][3]};
+                weights_to_bf16(w, p[r][c]);
+            }
+        }
+        if (more)
+            lds_loads_wait<LOADS>();     // V is there, the next K may be under way
+        else
+            lds_loads_wait<0>();
+        auto v_read = [&](int dt, int c) {
+            const unsigned at = (v_at ^ dt * 32) + 2 * c * T::PART;
+            const pu2_t y0 = column_read(at), y1 = column_read(at + T::PART);
+            return pu4_t{y0.x, y0.y, y1.x, y1.y};
+        };
+        if (masked) {
+            // Rows that are not there may hold anything: zeros instead.  An element that is not finite makes that of the output
+            // NaN for the rows that see it, and is zero for the others: a weight of zero would not be enough.
+            bool bad = false;
+#pragma unroll 1
+            for (int j = 0; j < LOADS; ++j) {
+                const unsigned at = lds_v + j * 1024 + lane * 16, r = (unsigned)(j * 64 + lane) / T::UN;
+                pu4_t u = __builtin_bit_cast(pu4_t, frag_read(at));
+                if (!(here >> r & 1)) {
+                    u = pu4_t{0, 0, 0, 0};
+                    *(__attribute__((address_space(3))) pu4_t *)(size_t)at = u;
+                }
+                bad |= some_not_finite(u);
+            }
+            __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (a.n > 1 && __any(bad)) {
+#pragma unroll
+                for (int r = 0; r < MT; ++r) {
+                    bf16x8_t ones[T::SUB / 2];
+#pragma unroll
+                    for (int c = 0; c < T::SUB / 2; ++c) {
+                        pu4_t u;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const unsigned two = (unsigned)(see[r] >> (32 * c + 16 * (i / 2) + 2 * (i % 2))) & 3u;
+                            u[i] = (two & 1 ? 0x3f80u : 0u) | (two & 2 ? 0x3f800000u : 0u);
+                        }
+                        ones[c] = __builtin_bit_cast(bf16x8_t, u);
+                    }
+#pragma unroll
+                    for (int dt = 0; dt < ND; ++dt) {
+                        pf4_t y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int c = 0; c < T::SUB / 2; ++c)
+                            y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, not_finite_or_rest(v_read(dt, c), true)),
+                                                                        ones[c], y, 0, 0, 0);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (y[i] > 0.f) o[r][dt][i] = __uint_as_float(0x7fc00000u);
+                    }
+                }
+                __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll 1
+                for (int j = 0; j < LOADS; ++j) {
+                    const unsigned at = lds_v + j * 1024 + lane * 16;
+                    *(__attribute__((address_space(3))) pu4_t *)(size_t)at =
+                        not_finite_or_rest(__builtin_bit_cast(pu4_t, frag_read(at)), false);
+                }
+                __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            }
+        }
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+            for (int c = 0; c < T::SUB / 2; ++c) {
+                const bf16x8_t v = __builtin_bit_cast(bf16x8_t, v_read(dt, c));
+#pragma unroll
+                for (int r = 0; r < MT; ++r)
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) o[r][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[r][c][k], o[r][dt], 0, 0, 0);
+            }
+        __builtin_amdgcn_sched_barrier(0);
+        __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (more) {
+            load(g.v, next, lds_v);
+            now = next;
+            next = parts_of(min(t + 2 * NW, t_end - 1));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+
+#pragma unroll
+    for (int r = 0; r < MT; ++r) {
+        sum[r] = quarters_sum(sum[r]);
+        if (quarter == 0) {
+            sm.m[wave][r * 16 + col] = m[r];
+            sm.l[wave][r * 16 + col] = sum[r];
+        }
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt) *(pf4_t *)&sm.o[wave][sm.unit(r * 16 + col, dt * 4 + quarter)] = o[r][dt];
+    }
+    __syncthreads();
+    const PagedAttend &z = late_args<PagedAttend>();
+    for (int row = threadIdx.x >> 4; row < RB; row += NW * 4) {
+        const int d0 = (threadIdx.x & 15) * (DH / 16);
+        const PagedRow rr = paged_row(z, hd, rb * RB + row, cnt);
+        if (rr.token < 0) continue;
+        float mm = -INFINITY, ll = 0.f, x[DH / 16];
+#pragma unroll
+        for (int w = 0; w < NW; ++w) mm = fmaxf(mm, sm.m[w][row]);
+#pragma unroll
+        for (int e = 0; e < DH / 16; ++e) x[e] = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float lw = sm.l[w][row], f = lw == 0.f ? 0.f : exp2f(sm.m[w][row] - finite_or_zero(mm));   // 0: saw nothing
+            ll += f * lw;
+#pragma unroll
+            for (int e = 0; e < DH / 16; e += 4) {
+                const pf4_t y = *(const pf4_t *)&sm.o[w][sm.unit(row, (d0 + e) / 4)];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[e + k] += f * y[k];
+            }
+        }
+        if (slot >= 0) {
+            const size_t at = (size_t)(blockIdx.x * 2 + slot) * RB + row;
+            __builtin_memcpy(__builtin_assume_aligned(z.ws_o + at * DH + d0, 16), x, sizeof(x));
+            if (d0 == 0) z.ws_ml[at] = make_float2(mm, ll);
+        } else {
+            const float inv = ll == 0.f ? 0.f : 1.f / ll;
+#pragma unroll
+            for (int e = 0; e < DH / 16; ++e) x[e] *= inv;
+            store_out<DH / 16>(z.out, z.bf16, (size_t)rr.row_of * DH + d0, x);
+            if (d0 == 0 && z.lse) z.lse[rr.row_of] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * P_LN2;
+        }
+    }
+}
+
+template <int DH, int MT, bool NTL, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void paged_token_kernel(PagedAttend a)
+{
+    __shared__ PagedTokenSmem<DH, MT, NW> sm;
+    run_parts(a, [&](const PartSeq &sq, int b, int hd, int rb, int ta, int tb, int slot) {
+        paged_token_block<DH, MT, NTL, NW>(a, sm, sq, b, hd, rb, ta, tb, slot);
+    });
+}
+
+// Joins the pieces of a cache: a work-group per 16 rows of a head, sixteen threads a row.
+template <int DH>
+__global__ __launch_bounds__(P_THREADS) void paged_join_kernel(PagedAttend a)
+{
+    constexpr int E = DH / 16;
+    const unsigned groups = (a.R + 15) / 16, hd = blockIdx.x / groups, r0 = (blockIdx.x - hd * groups) * 16;
+    const int b = hd / (a.g.nl * a.g.H);
+    const PartSeq sq = part_seq(a, b);
+    const int cnt = min(sq.cnt, sq.len);
+    if ((int)r0 >= cnt * a.G) return;
+    PartShare<PagedAttend> sh;
+    sh.init(a, threadIdx.x & 63);
+    const PartPieces<PagedAttend> pc(a, sh, sq, b, hd, r0 >> a.rsh);
+    const unsigned r = r0 + (threadIdx.x >> 4), d0 = (threadIdx.x & 15) * E;
+    const PagedRow row = paged_row(a, hd, r, cnt);
+    if (pc.n == 1 || row.token < 0) return;
+    float m = -INFINITY, sum = 0.f, x[E] = {};
+#pragma unroll 4
+    for (unsigned p = 0; p < pc.n; ++p) m = fmaxf(m, a.ws_ml[pc.at(p, r)].x);
+    const float mz = finite_or_zero(m);
+#pragma unroll 2
+    for (unsigned p = 0; p < pc.n; ++p) {
+        const float2 ml = a.ws_ml[pc.at(p, r)];
+        const float f = ml.y == 0.f ? 0.f : exp2f(ml.x - mz);       // 0: the piece saw nothing
+        sum += f * ml.y;
+        float o[E];
+        __builtin_memcpy(o, __builtin_assume_aligned(a.ws_o + pc.at(p, r) * DH + d0, 16), sizeof(o));
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] += f * o[e];
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] *= inv;
+    store_out<E>(a.out, a.bf16, (size_t)row.row_of * DH + d0, x);
+    if (a.lse && d0 == 0) a.lse[row.row_of] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * P_LN2;
+}
+
+// ---- host ------------------------------------------------------------------------------------
+
+thread_local char p_msg[256] = "no error";
+
+wnw_status paged_fail(wnw_status st, const char *msg)
+{
+    strncpy(p_msg, msg, sizeof p_msg - 1);
+    return st;
+}
+wnw_status paged_hip()
+{
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? WNW_OK : paged_fail(WNW_ERR_HIP, hipGetErrorString(e));
+}
+bool off16(const void *p)
+{
+    return (uintptr_t)p & 15;
+}
+bool off4(const void *p)
+{
+    return (uintptr_t)p & 3;
+}
+
+wnw_status paged_config(const wnw_paged_config *c, int32_t first_layer, int32_t n_layers, int32_t n)
+{
+    if (!c) return paged_fail(WNW_ERR_INVALID, "NULL configuration");
+    if (c->batch < 1 || c->layers < 1 || c->kv_heads < 1 || c->pages < 1 || c->table_width < 1)
+        return paged_fail(WNW_ERR_INVALID, "batch, layers, kv_heads, pages and table_width must be at least 1");
+    if (c->head_dim != 64 && c->head_dim != 128) return paged_fail(WNW_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
+    if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128 && c->page != 256)
+        return paged_fail(WNW_ERR_UNSUPPORTED, "page must be 16, 32, 64, 128 or 256");
+    if (c->table_width > P_MAX_CAP / c->page) return paged_fail(WNW_ERR_UNSUPPORTED, "capacity above 2^24 rows");
+    if (c->flags & ~(uint32_t)WNW_F_OUT_BF16) return paged_fail(WNW_ERR_INVALID, "unknown flag bits");
+    if (first_layer < 0 || n_layers < 1 || first_layer > c->layers - n_layers)
+        return paged_fail(WNW_ERR_INVALID, "layers outside the cache's");
+    if (n < 0 || n > c->table_width * c->page) return paged_fail(WNW_ERR_INVALID, "n outside 0 .. capacity");
+    if ((int64_t)c->batch * n_layers > INT32_MAX / 2 / c->kv_heads) return paged_fail(WNW_ERR_UNSUPPORTED, "too many heads");
+    if ((int64_t)c->pages * c->layers > INT64_MAX / (256 * 128 * 2) / c->kv_heads) return paged_fail(WNW_ERR_UNSUPPORTED, "too many pages");
+    return WNW_OK;
+}
+wnw_status paged_cache(const wnw_paged_cache *c)
+{
+    if (!c || !c->k || !c->v || !c->table) return paged_fail(WNW_ERR_INVALID, "NULL cache pointer");
+    if (off16(c->k) || off16(c->v)) return paged_fail(WNW_ERR_INVALID, "pages must be aligned to 16 bytes");
+    if (off4(c->table)) return paged_fail(WNW_ERR_INVALID, "the table must be aligned to 4 bytes");
+    return WNW_OK;
+}
+PagedGeo paged_geo(const wnw_paged_config &c, const wnw_paged_cache &k, int32_t l0, int32_t nl)
+{
+    return PagedGeo{c.batch, c.layers, c.kv_heads, l0, nl, c.pages, c.table_width, __builtin_ctz((unsigned)c.page),
+                    (uint16_t *)k.k, (uint16_t *)k.v, k.table};
+}
+
+template <typename F>
+void paged_dispatch(const wnw_paged_config &c, F f)
+{
+    c.head_dim == 64 ? f(std::integral_constant<int, 64>{}) : f(std::integral_constant<int, 128>{});
+}
+
+// How an attention call runs.
+struct PagedPlan {
+    int RB, W, tsh;
+    bool whole, eight, stream;
+    int64_t rows, o_bytes, ml_bytes;
+    int64_t total() const { return o_bytes + ml_bytes; }
+};
+PagedPlan paged_plan(const wnw_paged_config &c, int32_t n_layers, int32_t q_heads, int32_t n, int32_t max_len)
+{
+    const int64_t cap = (int64_t)c.table_width * c.page, heads = (int64_t)c.batch * n_layers * c.kv_heads, R = (int64_t)q_heads / c.kv_heads * n;
+    const int64_t len = max_len ? std::min<int64_t>(max_len, cap) : cap;
+    PagedPlan p;
+    p.RB = R > 16 ? 32 : 16;
+    p.tsh = c.head_dim == 64 ? 6 : 5;
+    const int64_t blocks = heads * ((R + p.RB - 1) / p.RB), per = (len + (1 << p.tsh) - 1) >> p.tsh, tiles = per * blocks;
+    p.stream = R <= p.RB && heads * len * c.head_dim * 4 > (256ll << 20);
+    p.whole = blocks >= 512;
+    p.eight = false;
+    p.W = (int)std::max<int64_t>(1, p.whole ? blocks : std::min<int64_t>(512, tiles / MIN_PIECE + blocks));
+    p.rows = heads * R;
+    p.o_bytes = p.whole ? 0 : (int64_t)p.W * 2 * p.RB * c.head_dim * 4;
+    p.ml_bytes = p.whole ? 0 : (int64_t)p.W * 2 * p.RB * 8;
+    return p;
+}
+
+template <int DH, int MT>
+void launch_tokens(const PagedPlan &p, const PagedAttend &a, hipStream_t st)
+{
+    auto *k = p.eight ? (p.stream ? paged_token_kernel<DH, MT, true, 8> : paged_token_kernel<DH, MT, false, 8>)
+                      : (p.stream ? paged_token_kernel<DH, MT, true, 4> : paged_token_kernel<DH, MT, false, 4>);
+    hipLaunchKernelGGL(k, dim3(p.W), dim3(p.eight ? 512 : 256), 0, st, a);
+}
+
+wnw_status paged_heads(const wnw_paged_config &c, int32_t n_layers, int32_t q_heads, int32_t n, int32_t max_len)
+{
+    if (q_heads < c.kv_heads || q_heads % c.kv_heads) return paged_fail(WNW_ERR_INVALID, "q_heads must be a multiple of kv_heads");
+    if (max_len < 0) return paged_fail(WNW_ERR_INVALID, "negative max_len");
+    if ((int64_t)c.batch * n_layers * q_heads > INT32_MAX / std::max(n, 1)) return paged_fail(WNW_ERR_UNSUPPORTED, "too many query rows");
+    // the line of tiles is counted in 32 bits
+    const int64_t blocks = ((int64_t)q_heads / c.kv_heads * n + 15) / 16 * c.batch * n_layers * c.kv_heads;
+    const int64_t tiles = ((int64_t)c.table_width * c.page + 31) / 32;
+    if (blocks > P_MAX_GROUPS || blocks > INT32_MAX / tiles) return paged_fail(WNW_ERR_UNSUPPORTED, "too many tiles for one call");
+    return WNW_OK;
+}
+
+}  // namespace
+
+}  // namespace wnw
+
+using namespace wnw;
+
+extern "C" {
+
+const char *wnw_paged_last_error(void)
+{
+    return p_msg;
+}
+
+wnw_status wnw_rotary_frequencies(int32_t dim, double base, double factor, double low, double high, int64_t original_len, float *freq)
+{
+    if (dim < 0 || dim % 2) return paged_fail(WNW_ERR_INVALID, "dim must be even");
+    if (!(base > 0.0) || !(factor >= 1.0) || std::isinf(base) || std::isinf(factor) || !(low >= 0.0) || !(high >= low) || original_len < 0)
+        return paged_fail(WNW_ERR_INVALID, "base > 0, factor >= 1, 0 <= low <= high and original_len >= 0 are wanted");
+    if (dim && !freq) return paged_fail(WNW_ERR_INVALID, "NULL pointer");
+    for (int32_t i = 0; i < dim / 2; ++i) {
+        const double f = pow(base, -2.0 * i / dim), turns = (double)original_len * f / 6.283185307179586;
+        // (low = high = infinity: every pair turns seldom)
+        const double keep = turns < low ? 0.0 : turns > high ? 1.0 : high > low ? (turns - low) / (high - low) : 1.0;
+        freq[i] = (float)(f * keep + f / factor * (1.0 - keep));
+    }
+    return WNW_OK;
+}
+
+wnw_status wnw_paged_append(const wnw_paged_config *cfg, const wnw_paged_cache *cache, const wnw_rotary *rotary, int32_t first_layer,
+                            int32_t n_layers, int32_t q_heads, int32_t n, const void *k_dev, const void *v_dev, const void *q_dev,
+                            void *q_out, const int32_t *at_dev, const int32_t *count_dev, const int32_t *position_dev, void *hip_stream)
+{
+    wnw_status st = paged_config(cfg, first_layer, n_layers, n);
+    if (st == WNW_OK) st = paged_cache(cache);
+    if (st != WNW_OK) return st;
+    if (!k_dev != !v_dev || !q_dev != !q_out) return paged_fail(WNW_ERR_INVALID, "keys and values, and queries and their place, come together");
+    if (!k_dev && !q_dev) return paged_fail(WNW_ERR_INVALID, "NULL pointer");
+    if (q_dev && (q_heads < 1 || q_heads > (1 << 20))) return paged_fail(WNW_ERR_INVALID, "q_heads must be at least 1");
+    if (rotary) {
+        if (rotary->dim < 0 || rotary->dim % 2 || rotary->dim > cfg->head_dim) return paged_fail(WNW_ERR_INVALID, "rotary: dim must be even, 0 .. head_dim");
+        if (rotary->layout != WNW_ROTARY_HALVES && rotary->layout != WNW_ROTARY_PAIRS) return paged_fail(WNW_ERR_INVALID, "rotary: unknown layout");
+        if (!std::isfinite(rotary->amplitude)) return paged_fail(WNW_ERR_INVALID, "rotary: the amplitude is not finite");
+        if (rotary->dim && (!rotary->freq || off4(rotary->freq))) return paged_fail(WNW_ERR_INVALID, "rotary: NULL or misaligned frequencies");
+    }
+    if (n == 0) return WNW_OK;
+    if (!at_dev) return paged_fail(WNW_ERR_INVALID, "NULL pointer");
+    if (off16(k_dev) || off16(v_dev) || off16(q_dev) || off16(q_out)) return paged_fail(WNW_ERR_INVALID, "rows must be aligned to 16 bytes");
+    if (off4(at_dev) || off4(count_dev) || off4(position_dev)) return paged_fail(WNW_ERR_INVALID, "a pointer is not aligned to its elements");
+    const int Hq = q_dev ? q_heads : 0, vectors = (k_dev ? 2 * cfg->kv_heads : 0) + Hq;
+    const int dim = rotary ? rotary->dim : 0;
+    int TT = 1;
+    const int slots = P_THREADS / (cfg->head_dim / 8);
+    while (TT < slots && TT < n) TT *= 2;
+    const int64_t tiles = (n + TT - 1) / TT, layers = (int64_t)cfg->batch * n_layers;
+    if (tiles * layers > P_MAX_GROUPS) return paged_fail(WNW_ERR_UNSUPPORTED, "too many rows for one call");
+    // few work-groups: share a layer's vectors out to several
+    const int rounds = (vectors + slots / TT - 1) / (slots / TT);
+    const int64_t split = std::max<int64_t>(1, std::min<int64_t>(rounds, 2048 / (tiles * layers)));
+    const PagedAppend a = {paged_geo(*cfg, *cache, first_layer, n_layers), Hq, n, (int)tiles, (int)split, dim, vectors, rotary ? rotary->amplitude : 1.f,
+                           rotary ? rotary->freq : nullptr, (const uint16_t *)k_dev, (const uint16_t *)v_dev, (const uint16_t *)q_dev, (uint16_t *)q_out,
+                           at_dev, count_dev, position_dev};
+    const int turn = !dim ? TURN_NONE : rotary->layout == WNW_ROTARY_PAIRS ? TURN_PAIRS : dim % 16 ? TURN_HALVES_ODD : TURN_HALVES;
+    paged_dispatch(*cfg, [&](auto d) {
+        constexpr int DH = decltype(d)::value;
+        auto *k = turn == TURN_NONE ? paged_append_kernel<DH, TURN_NONE> : turn == TURN_PAIRS ? paged_append_kernel<DH, TURN_PAIRS>
+                  : turn == TURN_HALVES ? paged_append_kernel<DH, TURN_HALVES> : paged_append_kernel<DH, TURN_HALVES_ODD>;
+        hipLaunchKernelGGL(k, dim3((unsigned)(tiles * layers * split)), dim3(P_THREADS), 0, (hipStream_t)hip_stream, a, TT);
+    });
+    return paged_hip();
+}
+
+wnw_status wnw_paged_keep(const wnw_paged_config *cfg, const wnw_paged_cache *cache, int32_t first_layer, int32_t n_layers, int32_t n,
+                          const int32_t *base_dev, const int32_t *path_dev, const int32_t *count_dev, void *hip_stream)
+{
+    wnw_status st = paged_config(cfg, first_layer, n_layers, 0);
+    if (st == WNW_OK) st = paged_cache(cache);
+    if (st != WNW_OK) return st;
+    if (n < 0) return paged_fail(WNW_ERR_INVALID, "negative n");
+    if (n > 1024) return paged_fail(WNW_ERR_UNSUPPORTED, "paths of more than 1024 tokens");
+    if (n == 0) return WNW_OK;
+    if (!base_dev || !path_dev) return paged_fail(WNW_ERR_INVALID, "NULL pointer");
+    if (off4(base_dev) || off4(path_dev) || off4(count_dev)) return paged_fail(WNW_ERR_INVALID, "a pointer is not aligned to its elements");
+    const int items = 2 * cfg->batch * n_layers * cfg->kv_heads, per = P_THREADS / 64;
+    const int64_t groups = ((int64_t)items + per - 1) / per;
+    if (groups > P_MAX_GROUPS) return paged_fail(WNW_ERR_UNSUPPORTED, "too many heads for one call");
+    const PagedGeo g = paged_geo(*cfg, *cache, first_layer, n_layers);
+    paged_dispatch(*cfg, [&](auto d) {
+        hipLaunchKernelGGL((paged_keep_kernel<decltype(d)::value>), dim3((unsigned)groups), dim3(P_THREADS), 0, (hipStream_t)hip_stream, g, n, items,
+                           base_dev, path_dev, count_dev);
+    });
+    return paged_hip();
+}
+
+wnw_status wnw_paged_attend_workspace(const wnw_paged_config *cfg, int32_t n_layers, int32_t q_heads, int32_t n, int32_t max_len, size_t *bytes)
+{
+    wnw_status st = paged_config(cfg, 0, n_layers, n);
+    if (st == WNW_OK) st = paged_heads(*cfg, n_layers, q_heads, n, max_len);
+    if (st != WNW_OK) return st;
+    if (!bytes) return paged_fail(WNW_ERR_INVALID, "NULL pointer");
+    *bytes = n ? (size_t)paged_plan(*cfg, n_layers, q_heads, n, max_len).total() : 0;
+    return WNW_OK;
+}
+
+wnw_status wnw_paged_attend(const wnw_paged_config *cfg, const wnw_paged_cache *cache, int32_t first_layer, int32_t n_layers, int32_t q_heads,
+                            int32_t n, const void *q_dev, const int32_t *len_dev, const int32_t *count_dev, const uint64_t *mask_dev,
+                            void *out_dev, float *lse_dev, int32_t max_len, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    wnw_status st = paged_config(cfg, first_layer, n_layers, n);
+    if (st == WNW_OK) st = paged_cache(cache);
+    if (st == WNW_OK) st = paged_heads(*cfg, n_layers, q_heads, n, max_len);
+    if (st != WNW_OK) return st;
+    if (n == 0) return WNW_OK;
+    if (!q_dev || !len_dev || !out_dev) return paged_fail(WNW_ERR_INVALID, "NULL pointer");
+    if (off16(q_dev) || off16(out_dev)) return paged_fail(WNW_ERR_INVALID, "queries and outputs must be aligned to 16 bytes");
+    if (off4(len_dev) || off4(count_dev) || off4(lse_dev) || (uintptr_t)mask_dev & 7)
+        return paged_fail(WNW_ERR_INVALID, "a pointer is not aligned to its elements");
+    const PagedPlan p = paged_plan(*cfg, n_layers, q_heads, n, max_len);
+    if (p.total() && (!workspace || off16(workspace) || workspace_bytes < (size_t)p.total()))
+        return paged_fail(WNW_ERR_INVALID, "workspace missing, too small or not aligned to 16 bytes");
+    const int G = q_heads / cfg->kv_heads, R = G * n;
+    char *ws = (char *)workspace;
+    const PagedAttend a = {paged_geo(*cfg, *cache, first_layer, n_layers), G, n, R, p.W, p.RB, __builtin_ctz((unsigned)p.RB), p.tsh,
+                           cfg->flags & WNW_F_OUT_BF16 ? 1 : 0, p.whole ? (R + p.RB - 1) / p.RB : 0, 1.f / p.W, (const uint16_t *)q_dev, len_dev,
+                           count_dev, (const unsigned long long *)mask_dev, out_dev, lse_dev, (float *)ws, (float2 *)(ws + p.o_bytes),
+                           P_LOG2E / sqrtf((float)cfg->head_dim)};
+    paged_dispatch(*cfg, [&](auto d) {
+        constexpr int DH = decltype(d)::value;
+        if (p.RB == 32)
+            launch_tokens<DH, 2>(p, a, (hipStream_t)hip_stream);
+        else
+            launch_tokens<DH, 1>(p, a, (hipStream_t)hip_stream);
+        if (!p.whole)
+            hipLaunchKernelGGL((paged_join_kernel<DH>), dim3((unsigned)(p.rows / R * ((R + 15) / 16))), dim3(P_THREADS), 0,
+                               (hipStream_t)hip_stream, a);
+    });
+    return paged_hip();
+}
+
+}  // extern "C"

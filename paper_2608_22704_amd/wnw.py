@@ -20,6 +20,7 @@ WNW_ANCHOR, WNW_TIDAL, WNW_FIXED = 0, 1, 2
 WNW_F_SELECT_NEXT_STEP, WNW_F_RECALL_MEMCPY, WNW_F_TIMING, WNW_F_OVERLAP_CHUNKS, WNW_F_PREFILL_GLOBAL = 1, 2, 4, 8, 16
 WNW_F_OUT_BF16 = 32
 WNW_QUANT_INT8, WNW_QUANT_E4M3 = 0, 1
+WNW_ROTARY_HALVES, WNW_ROTARY_PAIRS = 0, 1
 
 EXPORTS = ("wnw_init_cache", "wnw_set_retention", "wnw_set_roles", "wnw_prefill_scores", "wnw_prefill_scores_static",
            "wnw_set_roles_device",
@@ -29,7 +30,9 @@ EXPORTS = ("wnw_init_cache", "wnw_set_retention", "wnw_set_roles", "wnw_prefill_
            "wnw_debug_set_slot_offset_limit", "wnw_debug_set_recall_delay",
            "wnw_debug_read_resident", "wnw_last_error", "wnw_destroy", "wnw_voice_hits", "wnw_key_sensitivity",
            "wnw_triage", "wnw_triage_last_error",
-           "wnw_quant_write", "wnw_quant_read", "wnw_quant_attend", "wnw_quant_attend_workspace", "wnw_quant_last_error")
+           "wnw_quant_write", "wnw_quant_read", "wnw_quant_attend", "wnw_quant_attend_workspace", "wnw_quant_last_error",
+           "wnw_rotary_frequencies", "wnw_paged_append", "wnw_paged_attend", "wnw_paged_attend_workspace", "wnw_paged_keep",
+           "wnw_paged_last_error", "wnw_draft_tree", "wnw_draft_verify", "wnw_draft_verify_workspace", "wnw_draft_last_error")
 
 
 class wnw_config(C.Structure):
@@ -64,6 +67,19 @@ class wnw_quant_cache(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
 
 
+class wnw_paged_config(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("layers", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("page", C.c_int32), ("pages", C.c_int32), ("table_width", C.c_int32), ("flags", C.c_uint32)]
+
+
+class wnw_paged_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("table", C.c_void_p)]
+
+
+class wnw_rotary(C.Structure):
+    _fields_ = [("freq", C.c_void_p), ("dim", C.c_int32), ("layout", C.c_int32), ("amplitude", C.c_float)]
+
+
 class WnwError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"wnw status {status}: {msg}")
@@ -76,6 +92,7 @@ def _load():
     lib = C.CDLL(LIB_PATH)
     P, I32, I64, SZ = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
     QC, QK = C.POINTER(wnw_quant_config), C.POINTER(wnw_quant_cache)
+    PC, PK = C.POINTER(wnw_paged_config), C.POINTER(wnw_paged_cache)
     sig = {
         "wnw_init_cache": ([C.POINTER(wnw_config), P, P, P, C.POINTER(P)], C.c_int),
         "wnw_set_roles": ([P, P, P], C.c_int),
@@ -92,6 +109,16 @@ def _load():
         "wnw_quant_attend": ([QC, QK, I32, I32, I32, I32, P, P, P, P, P, P, I32, P, SZ, P], C.c_int),
         "wnw_quant_attend_workspace": ([QC, I32, I32, I32, I32, C.POINTER(SZ)], C.c_int),
         "wnw_quant_last_error": ([], C.c_char_p),
+        "wnw_rotary_frequencies": ([I32, C.c_double, C.c_double, C.c_double, C.c_double, I64, P], C.c_int),
+        "wnw_paged_append": ([PC, PK, C.POINTER(wnw_rotary), I32, I32, I32, I32, P, P, P, P, P, P, P, P], C.c_int),
+        "wnw_paged_attend": ([PC, PK, I32, I32, I32, I32, P, P, P, P, P, P, I32, P, SZ, P], C.c_int),
+        "wnw_paged_attend_workspace": ([PC, I32, I32, I32, I32, C.POINTER(SZ)], C.c_int),
+        "wnw_paged_keep": ([PC, PK, I32, I32, I32, P, P, P, P], C.c_int),
+        "wnw_paged_last_error": ([], C.c_char_p),
+        "wnw_draft_tree": ([I32, I32, P, P, P, P, P, P], C.c_int),
+        "wnw_draft_verify": ([I32, I32, I32, P, P, P, P, P, P, P, P, P, P, SZ, P], C.c_int),
+        "wnw_draft_verify_workspace": ([I32, I32, I32, C.POINTER(SZ)], C.c_int),
+        "wnw_draft_last_error": ([], C.c_char_p),
         "wnw_set_roles_device": ([P, P, P], C.c_int),
         "wnw_query_head_keep": ([P, P], C.c_int),
         "wnw_decode_step": ([P, P, P, P, P, P], C.c_int),
@@ -133,7 +160,7 @@ def _ptr(t):
 
 
 # element sizes the library reads or writes: bf16 bit patterns (any 2-byte dtype), fp32, int32, bytes
-_BF16, _F32, _I32, _U8 = "bf16", "f32", "i32", "u8"
+_BF16, _F32, _I32, _U8, _I64 = "bf16", "f32", "i32", "u8", "i64"
 
 
 def _dev(t, kind, numel=None, what="tensor"):
@@ -304,7 +331,7 @@ def _dtypes():
     if not _DTYPES:
         import torch
         _DTYPES.update({_BF16: (torch.bfloat16, torch.int16, torch.uint16), _F32: (torch.float32,), _I32: (torch.int32,),
-                        _U8: (torch.uint8,)})
+                        _U8: (torch.uint8,), _I64: (torch.int64, torch.uint64)})
     return _DTYPES
 
 
@@ -401,6 +428,181 @@ def wnw_quant_attend(cfg, cache, q_dev, out_dev, len_dev, count_dev=None, lse_de
         _on(dev, lse_dev, k[_F32], rows * n, "lse_dev"),
         _on(dev, mass_dev, k[_F32], rows * (cfg.capacity // max(cfg.block, 1)), "mass_dev"), max_len,
         _on(dev, workspace, k[_U8], None, "workspace"), 0 if workspace is None else workspace.numel(), st))
+
+
+class PagedCache:
+    """The buffers of a paged cache (see wnw.h): k, v bf16 [pages][L][H_kv][page][d], table int32 [B][table_width]."""
+
+    def __init__(self, k, v, table):
+        self.k, self.v, self.table = k, v, table
+
+    def __setattr__(self, name, t):
+        # type and layout are checked once here, device and size by every call
+        _on(t.get_device(), t, _dtypes()[_I32 if name == "table" else _BF16], None, name)
+        object.__setattr__(self, name, t)
+
+    def _struct(self, cfg, device):
+        need, entries = cfg.pages * cfg.layers * cfg.kv_heads * cfg.page * cfg.head_dim, cfg.batch * cfg.table_width
+        k, v, table = self.k, self.v, self.table
+        if (k.numel() < need or v.numel() < need or table.numel() < entries or k.get_device() != device
+                or v.get_device() != device or table.get_device() != device):
+            for name, t, numel in (("k", k, need), ("v", v, need), ("table", table, entries)):
+                if t.get_device() != device or t.numel() < numel:
+                    raise ValueError(f"{name}: needs {numel} elements on cuda:{device}, got {t.numel()} on {t.device}")
+        return wnw_paged_cache(k.data_ptr(), v.data_ptr(), table.data_ptr())
+
+
+def make_paged_config(batch, layers, kv_heads, page, pages, table_width, head_dim=128, flags=0) -> wnw_paged_config:
+    return wnw_paged_config(batch, layers, kv_heads, head_dim, page, pages, table_width, flags)
+
+
+def make_paged_cache(cfg, device="cuda") -> PagedCache:
+    """New pages for cfg on a device, uninitialised, and a table without pages (-1): the caller hands them out."""
+    import torch
+    k, v = (torch.empty((cfg.pages, cfg.layers, cfg.kv_heads, cfg.page, cfg.head_dim), dtype=torch.bfloat16, device=device)
+            for _ in range(2))
+    return PagedCache(k, v, torch.full((cfg.batch, cfg.table_width), -1, dtype=torch.int32, device=device))
+
+
+class Rotary:
+    """How wnw_paged_append rotates (see wnw.h): freq fp32 [dim / 2] on the device, radians per position."""
+
+    def __init__(self, freq, dim, layout, amplitude):
+        if freq is None and dim:
+            raise ValueError("freq must be given where dim is not 0")
+        if freq is not None:
+            _on(freq.get_device(), freq, _dtypes()[_F32], dim // 2, "freq")
+        self.freq, self.dim, self.layout, self.amplitude = freq, dim, layout, amplitude
+
+    def _struct(self, device):
+        return wnw_rotary(_on(device, self.freq, _dtypes()[_F32], self.dim // 2, "freq"), self.dim, self.layout, self.amplitude)
+
+
+def make_rotary(freq, dim, layout=WNW_ROTARY_HALVES, amplitude=1.0) -> Rotary:
+    return Rotary(freq, dim, layout, amplitude)
+
+
+def wnw_rotary_frequencies(dim, base, factor=1.0, low=0.0, high=0.0, original_len=0) -> np.ndarray:
+    """Host fp32 [dim / 2], radians per position; for contexts longer than original_len by factor see wnw.h."""
+    freq = np.empty(max(dim, 0) // 2, dtype=np.float32)
+    _pcheck(lib.wnw_rotary_frequencies(dim, base, factor, low, high, original_len, _ptr(freq)))
+    return freq
+
+
+def _pcheck(status):
+    if status != WNW_OK:
+        raise WnwError(status, lib.wnw_paged_last_error().decode())
+
+
+def wnw_paged_append(cfg, cache, k_dev, v_dev, at_dev, count_dev=None, q_dev=None, q_out=None, rotary=None, position_dev=None,
+                     first_layer=0, stream=None):
+    """k_dev, v_dev bf16 [B][n_layers][H_kv][n][d] -> rows at[b] .. at[b] + count[b] - 1 of the pages, K rotated; q_dev bf16
+    [B][n_layers][H_q][n][d] -> q_out, rotated (at_dev, count_dev: int32 [B]; position_dev: int32 [B][n])."""
+    some = k_dev if k_dev is not None else q_dev
+    if some is None:
+        raise ValueError("k_dev or q_dev must be given")
+    if (k_dev is None) != (v_dev is None) or (q_dev is None) != (q_out is None):
+        raise ValueError("k_dev and v_dev, and q_dev and q_out, are given together")
+    shape = some.shape
+    Hq = 0
+    if k_dev is not None:
+        nl, n = _quant_shape(cfg, k_dev, cfg.kv_heads, "k_dev")
+        if v_dev.shape != shape:
+            raise ValueError(f"v_dev: expected {list(shape)}, got {list(v_dev.shape)}")
+    if q_dev is not None:
+        Hq = q_dev.shape[2] if len(q_dev.shape) == 5 else 0
+        q_nl, q_n = _quant_shape(cfg, q_dev, Hq, "q_dev")
+        if k_dev is None:
+            nl, n = q_nl, q_n
+        if (q_nl, q_n) != (nl, n) or q_out.shape != q_dev.shape:
+            raise ValueError(f"q_dev, q_out: expected {nl} layers and {n} tokens each, got {list(q_dev.shape)}, {list(q_out.shape)}")
+    (dev, st), k, B = _quant_place(stream), _DTYPES or _dtypes(), cfg.batch
+    _pcheck(lib.wnw_paged_append(
+        cfg, cache._struct(cfg, dev), None if rotary is None else rotary._struct(dev), first_layer, nl, Hq, n,
+        _on(dev, k_dev, k[_BF16], None, "k_dev"), _on(dev, v_dev, k[_BF16], None, "v_dev"), _on(dev, q_dev, k[_BF16], None, "q_dev"),
+        _on(dev, q_out, k[_BF16], None, "q_out"), _on(dev, at_dev, k[_I32], B, "at_dev"), _on(dev, count_dev, k[_I32], B, "count_dev"),
+        _on(dev, position_dev, k[_I32], B * n, "position_dev"), st))
+
+
+def wnw_paged_attend_workspace(cfg, n_layers, q_heads, n, max_len=0) -> int:
+    """Bytes of workspace that wnw_paged_attend needs for these sizes."""
+    need = C.c_size_t()
+    _pcheck(lib.wnw_paged_attend_workspace(cfg, n_layers, q_heads, n, max_len, C.byref(need)))
+    return need.value
+
+
+def wnw_paged_attend(cfg, cache, q_dev, out_dev, len_dev, count_dev=None, mask_dev=None, lse_dev=None, workspace=None, max_len=0,
+                     first_layer=0, stream=None):
+    """q_dev bf16 [B][n_layers][H_q][n][d] -> out_dev (same shape, fp32 or bf16), lse_dev fp32 [B][n_layers][H_q][n];
+    mask_dev int64 [B][n][(n + 63) // 64] (None: causal); workspace: a uint8 tensor of wnw_paged_attend_workspace() bytes or more."""
+    shape = q_dev.shape
+    Hq = shape[2] if len(shape) == 5 else 0
+    nl, n = _quant_shape(cfg, q_dev, Hq, "q_dev")
+    if out_dev.shape != shape:
+        raise ValueError(f"out_dev: expected {list(shape)}, got {list(out_dev.shape)}")
+    (dev, st), k, B = _quant_place(stream), _DTYPES or _dtypes(), cfg.batch
+    _pcheck(lib.wnw_paged_attend(
+        cfg, cache._struct(cfg, dev), first_layer, nl, Hq, n, _on(dev, q_dev, k[_BF16], None, "q_dev"),
+        _on(dev, len_dev, k[_I32], B, "len_dev"), _on(dev, count_dev, k[_I32], B, "count_dev"),
+        _on(dev, mask_dev, k[_I64], B * n * ((n + 63) // 64), "mask_dev"),
+        _on(dev, out_dev, k[_BF16 if cfg.flags & WNW_F_OUT_BF16 else _F32], None, "out_dev"),
+        _on(dev, lse_dev, k[_F32], B * nl * Hq * n, "lse_dev"), max_len, _on(dev, workspace, k[_U8], None, "workspace"),
+        0 if workspace is None else workspace.numel(), st))
+
+
+def wnw_paged_keep(cfg, cache, base_dev, path_dev, count_dev=None, first_layer=0, n_layers=None, stream=None):
+    """Rows base[b] + path[b][i] -> base[b] + i, i < count[b], of n_layers layers (None: all from first_layer on); path_dev int32
+    [B][n], ascending."""
+    if len(path_dev.shape) != 2 or path_dev.shape[0] != cfg.batch:
+        raise ValueError(f"path_dev: expected [{cfg.batch}][n], got {list(path_dev.shape)}")
+    (dev, st), k, B = _quant_place(stream), _DTYPES or _dtypes(), cfg.batch
+    _pcheck(lib.wnw_paged_keep(cfg, cache._struct(cfg, dev), first_layer, cfg.layers - first_layer if n_layers is None else n_layers,
+                               path_dev.shape[1], _on(dev, base_dev, k[_I32], B, "base_dev"), _on(dev, path_dev, k[_I32], None, "path_dev"),
+                               _on(dev, count_dev, k[_I32], B, "count_dev"), st))
+
+
+def _dcheck(status):
+    if status != WNW_OK:
+        raise WnwError(status, lib.wnw_draft_last_error().decode())
+
+
+def wnw_draft_tree(parent_dev, base_dev, mask_dev=None, position_dev=None, count_dev=None, stream=None):
+    """parent_dev int32 [B][n] -> mask_dev int64 [B][n][(n + 63) // 64], position_dev int32 [B][n] (either may be None);
+    base_dev, count_dev int32 [B]."""
+    B, n = parent_dev.shape
+    (dev, st), k = _quant_place(stream), _DTYPES or _dtypes()
+    _dcheck(lib.wnw_draft_tree(B, n, _on(dev, parent_dev, k[_I32], None, "parent_dev"), _on(dev, base_dev, k[_I32], B, "base_dev"),
+                               _on(dev, count_dev, k[_I32], B, "count_dev"),
+                               _on(dev, mask_dev, k[_I64], B * n * ((n + 63) // 64), "mask_dev"),
+                               _on(dev, position_dev, k[_I32], B * n, "position_dev"), st))
+
+
+def wnw_draft_verify_workspace(batch, n, vocab) -> int:
+    """Bytes of workspace that wnw_draft_verify needs for these sizes."""
+    need = C.c_size_t()
+    _dcheck(lib.wnw_draft_verify_workspace(batch, n, vocab, C.byref(need)))
+    return need.value
+
+
+def wnw_draft_verify(token_dev, target_dev, uniform_dev, path_dev, accepted_dev, next_dev, draft_dev=None, parent_dev=None,
+                     count_dev=None, workspace=None, stream=None):
+    """token_dev int32 [B][n], target_dev fp32 [B][n + 1][vocab], uniform_dev fp32 [B][n + 1] -> path_dev int32 [B][n],
+    accepted_dev, next_dev int32 [B]; draft_dev like target_dev; parent_dev int32 [B][n]; workspace: a uint8 tensor of
+    wnw_draft_verify_workspace() bytes or more."""
+    B, n = token_dev.shape
+    shape = target_dev.shape
+    if len(shape) != 3 or shape[0] != B or shape[1] != n + 1:
+        raise ValueError(f"target_dev: expected [{B}][{n + 1}][vocab], got {list(shape)}")
+    if draft_dev is not None and draft_dev.shape != shape:
+        raise ValueError(f"draft_dev: expected {list(shape)}, got {list(draft_dev.shape)}")
+    (dev, st), k = _quant_place(stream), _DTYPES or _dtypes()
+    _dcheck(lib.wnw_draft_verify(
+        B, n, shape[2], _on(dev, token_dev, k[_I32], None, "token_dev"), _on(dev, parent_dev, k[_I32], B * n, "parent_dev"),
+        _on(dev, count_dev, k[_I32], B, "count_dev"), _on(dev, target_dev, k[_F32], None, "target_dev"),
+        _on(dev, draft_dev, k[_F32], None, "draft_dev"), _on(dev, uniform_dev, k[_F32], B * (n + 1), "uniform_dev"),
+        _on(dev, path_dev, k[_I32], B * n, "path_dev"), _on(dev, accepted_dev, k[_I32], B, "accepted_dev"),
+        _on(dev, next_dev, k[_I32], B, "next_dev"), _on(dev, workspace, k[_U8], None, "workspace"),
+        0 if workspace is None else workspace.numel(), st))
 
 
 def wnw_append_kv(ctx, k_new_dev, v_new_dev, stream=None):
