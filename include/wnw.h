@@ -589,8 +589,8 @@ wnw_status wnw_paged_append(const wnw_paged_config *cfg, const wnw_paged_cache *
  * sees rows 0 .. len[b] - count[b] - 1, and of the tokens' own rows those that the mask says (row len[b] - count[b] + j is token
  * j's), without a mask those of tokens 0 .. i.  Logit scale 1 / sqrt(d); products of bf16 summed in fp32, softmax statistics
  * in fp32.  fp32 outputs: softmax weights to 24 bits.  bf16 outputs (WNW_F_OUT_BF16): up to 32 query rows n * H_q / H_kv the
- * fp32 results rounded (nearest, ties to even); with more, weights are rounded to bf16 before they multiply V, and
- * normalised by the sum of the rounded ones.  What a token does not see has no part in its outputs, infinities and NaN
+ * fp32 results rounded (nearest, ties to even); with more, weights are rounded to bf16 before they multiply V.
+ * What a token does not see has no part in its outputs, infinities and NaN
  * included.  A token that sees no row (or whose logits are all -inf) gets zeros and the log-sum-exp -inf; otherwise a query
  * row with a NaN or an infinity gets NaN in all of its outputs, and an element of out_dev for which a row seen has a V
  * element that is not finite is not finite.

@@ -4,6 +4,7 @@
 //   paged_append_kernel  new rows of K and V to their pages and queries to their place, rotated on the way
 //   paged_keep_kernel    accepted rows to the end of their sequence, a wavefront per head's K or V
 //   paged_token_kernel   attention in blocks of 16 or 32 query rows of a KV-head, every wavefront with tiles of its own
+//   paged_wide_kernel    attention in blocks of 64 or 128 query rows, whose wavefronts share tiles
 //   paged_join_kernel    joins the parts of a cache that work-groups shared
 #include "wnw.h"
 #include "wnw_internal.h"
@@ -241,6 +242,13 @@ struct PagedAttend {
     float2 *ws_ml;             // [W][2][RB]: the piece's maximum (base 2) and sum of weights
     float scale;               // log2(e) / sqrt(d)
     __device__ int cap() const { return g.cap(); }
+    // Work-groups go to the eight dies in turn; those that follow each other here are on one die, whose cache then serves the blocks of
+    // rows of one head.
+    __device__ unsigned group() const
+    {
+        const unsigned die = blockIdx.x & 7, each = (unsigned)W >> 3, more = (unsigned)W & 7;
+        return die * each + min(die, more) + (blockIdx.x >> 3);
+    }
     __device__ int tiles_of(int rows) const { return (rows + (1 << tsh) - 1) >> tsh; }
 };
 
@@ -289,11 +297,36 @@ __device__ inline unsigned long long sees(const PagedAttend &a, int b, int i, in
     return s & low_bits(len - t0);
 }
 
-// A wave-uniform table entry by the scalar unit, whose loads do not count among those of the tiles.
-__device__ inline int scalar_entry(const int32_t *p, int i)
+// x where the bit of `word` is set, otherwise -inf; two vector instructions, and no scalar registers for conditions.
+__device__ inline float seen_or_none(unsigned word, int bit, float x)
 {
-    return ((const __attribute__((address_space(4))) int32_t *)p)[i];
+    const unsigned all = (unsigned)__builtin_amdgcn_sbfe((int)word, bit, 1);
+    return __uint_as_float((all & __float_as_uint(x)) | (~all & 0xff800000u));
 }
+
+// Where the 16-row parts of a head's cache are: scalar code, whose loads of table entries do not count among those of the tiles.
+struct PageWalk {
+    const char *k, *v;                 // the head's rows of page 0
+    const int32_t *table;              // the sequence's
+    size_t stride;                     // bytes from a page to the next
+    int pages, psh, last, row_bytes;   // last: the sequence's last row
+    __device__ PageWalk(const PagedGeo &g, int b, int hd, int len, int row_bytes_)
+        : table(g.table + (size_t)b * g.width), pages(g.pages), psh(g.psh), last(max(len - 1, 0)), row_bytes(row_bytes_)
+    {
+        const size_t head = ((size_t)(g.l0 * g.H + (hd - b * g.nl * g.H)) << g.psh) * row_bytes_;
+        k = (const char *)g.k + head;
+        v = (const char *)g.v + head;
+        stride = ((size_t)g.L * g.H << g.psh) * row_bytes_;
+    }
+    // the page of row r, or of the last one where r is behind it; its entry may name none
+    __device__ int entry(int r) const { return ((const __attribute__((address_space(4))) int32_t *)table)[min(r, last) >> psh]; }
+    __device__ bool has(int id) const { return (unsigned)id < (unsigned)pages; }
+    // bytes from k or v to row r of that page; of page 0 if there is none
+    __device__ size_t offset(int id, int r) const
+    {
+        return (has(id) ? (unsigned)id : 0u) * stride + (unsigned)((r & ((1 << psh) - 1)) * row_bytes);
+    }
+};
 
 // Eight weights as three matrix operands whose sum they are, exactly: 8 bits of the 24 each.
 __device__ inline unsigned high_halves(float a, float b)
@@ -327,12 +360,14 @@ __device__ inline pu2_t column_read(unsigned lds)
     return __builtin_bit_cast(pu2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) ps4_t *)(size_t)lds));
 }
 
-__device__ inline bool some_not_finite(pu4_t u)
+// Bits 15 and 31 set where the halves are bf16 numbers that are not finite; other bits may be set too.
+__device__ inline unsigned not_finite(unsigned u)
 {
-    bool bad = false;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) bad |= (u[e] & 0x7f80u) == 0x7f80u || (u[e] & 0x7f800000u) == 0x7f800000u;
-    return bad;
+    return (u & 0x7fff7fffu) + 0x00800080u;
+}
+__device__ inline unsigned not_finite(pu4_t u)
+{
+    return not_finite(u.x) | not_finite(u.y) | not_finite(u.z) | not_finite(u.w);
 }
 // Elements that are not finite, as ones; or the finite ones, the others zero.
 __device__ inline pu4_t not_finite_or_rest(pu4_t u, bool ones)
@@ -340,8 +375,8 @@ __device__ inline pu4_t not_finite_or_rest(pu4_t u, bool ones)
     pu4_t y;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const unsigned lo = (u[e] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u, hi = (u[e] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
-        y[e] = ones ? (lo | hi) & 0x3f803f80u : u[e] & ~(lo | hi);
+        const unsigned top = not_finite(u[e]) & 0x80008000u, all = (top - (top >> 15)) | top;
+        y[e] = ones ? all & 0x3f803f80u : u[e] & ~all;
     }
     return y;
 }
@@ -377,8 +412,7 @@ __device__ inline void paged_token_block(const PagedAttend &a, PagedTokenSmem<DH
     const int len = sq.len, cnt = min(sq.cnt, len), base = len - cnt;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quarter = lane >> 4;
-    const int lh = hd - b * g.nl * g.H, l = lh / g.H, h = lh - l * g.H;
-    const int32_t *table = g.table + (size_t)b * g.width;
+    const PageWalk pages(g, b, hd, len, T::ROW);
 
     // cache rows that the block's last and first row may see
     const int last = min(cnt - 1, min(rb * RB + RB - 1, a.R - 1) / a.G), first = rb * RB / a.G;
@@ -396,30 +430,29 @@ __device__ inline void paged_token_block(const PagedAttend &a, PagedTokenSmem<DH
         const unsigned r = j * (64 / T::UN) + lane / T::UN, u = lane % T::UN;
         off[j] = r * T::ROW + (u ^ T::swz(r)) * 16;
     }
-    // The pages of a tile's 16-row parts, as the first row of d elements that they have for the head; parts that are not there
-    // or past the sequence's end read page 0.
+    // The pages of a tile's 16-row parts, as bytes from the head's rows of page 0.
     struct Parts {
-        size_t row[T::SUB];
+        size_t at[T::SUB];
         unsigned gone;       // bit s: part s has no page
     };
     auto parts_of = [&](int t) {
         Parts p;
+        int id[T::SUB];
         p.gone = 0;
 #pragma unroll
+        for (int s = 0; s < T::SUB; ++s) id[s] = pages.entry(t * T::TR + s * 16);
+#pragma unroll
         for (int s = 0; s < T::SUB; ++s) {
-            const int r = t * T::TR + s * 16;
-            const int id = r < len ? scalar_entry(table, r >> g.psh) : 0;
-            const bool has = g.has(id);
-            if (!has) p.gone |= 1u << s;
-            p.row[s] = g.page_row(has ? id : 0, l, h) + (r & ((1 << g.psh) - 1));
+            p.gone |= pages.has(id[s]) ? 0u : 1u << s;
+            p.at[s] = pages.offset(id[s], t * T::TR + s * 16);
         }
         return p;
     };
-    auto load = [&](const uint16_t *pool, const Parts &p, unsigned lds) {
+    auto load = [&](const char *pool, const Parts &p, unsigned lds) {
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
             constexpr int PER = LOADS / T::SUB;       // loads of a part
-            const uint16_t *from = pool + p.row[j / PER] * DH + (j % PER & ~1) * 512;
+            const char *from = pool + p.at[j / PER] + (j % PER & ~1) * 1024;
             const unsigned o = off[j % PER & 1];
             NTL ? stream_to_lds(from, o, lds + j * 1024) : load_to_lds(from, o, lds + j * 1024);
         }
@@ -427,8 +460,8 @@ __device__ inline void paged_token_block(const PagedAttend &a, PagedTokenSmem<DH
     Parts now, next;
     if (t < t_end) {
         now = parts_of(t);
-        load(g.k, now, lds_k);
-        load(g.v, now, lds_v);
+        load(pages.k, now, lds_k);
+        load(pages.v, now, lds_v);
         next = parts_of(min(t + NW, t_end - 1));
     }
 
@@ -439,16 +472,15 @@ __device__ inline void paged_token_block(const PagedAttend &a, PagedTokenSmem<DH
 #pragma unroll
     for (int r = 0; r < MT; ++r) {
         qr[r] = paged_row(a, hd, rb * RB + r * 16 + col, cnt);
-        bool bad = false;
+        unsigned odd = 0;
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
             pu4_t u = {0, 0, 0, 0};
             if (qr[r].token >= 0) u = *(const pu4_t *)(a.q + (size_t)qr[r].row_of * DH + s * 32 + quarter * 8);
-            bad |= some_not_finite(u);
+            odd |= not_finite(u);
             qf[r][s] = __builtin_bit_cast(bf16x8_t, u);
         }
-        bad = quarters_max(bad ? 1.f : 0.f) > 0.f;
-        crow[r] = bad ? __uint_as_float(0x7fc00000u) : a.scale;
+        crow[r] = quarters_max(odd & 0x80008000u ? 1.f : 0.f) > 0.f ? __uint_as_float(0x7fc00000u) : a.scale;
         m[r] = -INFINITY;
         sum[r] = 0.f;
 #pragma unroll
@@ -480,7 +512,7 @@ __device__ inline void paged_token_block(const PagedAttend &a, PagedTokenSmem<DH
         }
         __builtin_amdgcn_sched_barrier(0);
         __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the bytes have been read
-        if (more) load(g.k, next, lds_k);
+        if (more) load(pages.k, next, lds_k);
         __builtin_amdgcn_sched_barrier(0);
 
         unsigned long long here = 0;       // rows of the tile that there are
@@ -499,7 +531,8 @@ __device__ inline void paged_token_block(const PagedAttend &a, PagedTokenSmem<DH
 #pragma unroll
                 for (int kb = 0; kb < T::SUB; ++kb)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[r][kb][i] = see[r] >> (kb * 16 + i) & 1 ? x[r][kb][i] : -INFINITY;
+                    for (int i = 0; i < 4; ++i)
+                        x[r][kb][i] = seen_or_none((unsigned)(see[r] >> (kb / 2 * 32)), kb % 2 * 16 + i, x[r][kb][i]);
             }
             float mt = m[r];
 #pragma unroll
@@ -538,7 +571,7 @@ __device__ inline void paged_token_block(const PagedAttend &a, PagedTokenSmem<DH
         if (masked) {
             // Rows that are not there may hold anything: zeros instead.  An element that is not finite makes that of the output
             // NaN for the rows that see it, and is zero for the others: a weight of zero would not be enough.
-            bool bad = false;
+            unsigned odd = 0;
 #pragma unroll 1
             for (int j = 0; j < LOADS; ++j) {
                 const unsigned at = lds_v + j * 1024 + lane * 16, r = (unsigned)(j * 64 + lane) / T::UN;
@@ -547,10 +580,10 @@ __device__ inline void paged_token_block(const PagedAttend &a, PagedTokenSmem<DH
                     u = pu4_t{0, 0, 0, 0};
                     *(__attribute__((address_space(3))) pu4_t *)(size_t)at = u;
                 }
-                bad |= some_not_finite(u);
+                odd |= not_finite(u);
             }
             __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            if (a.n > 1 && __any(bad)) {
+            if (a.n > 1 && __any(odd & 0x80008000u)) {
 #pragma unroll
                 for (int r = 0; r < MT; ++r) {
                     bf16x8_t ones[T::SUB / 2];
@@ -599,7 +632,7 @@ __device__ inline void paged_token_block(const PagedAttend &a, PagedTokenSmem<DH
         __builtin_amdgcn_sched_barrier(0);
         __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (more) {
-            load(g.v, next, lds_v);
+            load(pages.v, next, lds_v);
             now = next;
             next = parts_of(min(t + 2 * NW, t_end - 1));
         }
@@ -639,7 +672,7 @@ __device__ inline void paged_token_block(const PagedAttend &a, PagedTokenSmem<DH
             }
         }
         if (slot >= 0) {
-            const size_t at = (size_t)(blockIdx.x * 2 + slot) * RB + row;
+            const size_t at = (size_t)(z.group() * 2 + slot) * RB + row;
             __builtin_memcpy(__builtin_assume_aligned(z.ws_o + at * DH + d0, 16), x, sizeof(x));
             if (d0 == 0) z.ws_ml[at] = make_float2(mm, ll);
         } else {
@@ -658,6 +691,311 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_token_kernel(PagedAttend a)
     __shared__ PagedTokenSmem<DH, MT, NW> sm;
     run_parts(a, [&](const PartSeq &sq, int b, int hd, int rb, int ta, int tb, int slot) {
         paged_token_block<DH, MT, NTL, NW>(a, sm, sq, b, hd, rb, ta, tb, slot);
+    });
+}
+
+// Many query rows.  A work-group has blocks of RB = 128 rows, 32 for each of its four wavefronts, and all of them use the same
+// tiles of 64 cache rows, which go straight from global to one of two buffers in shared memory while the tile in the other is
+// in use; wavefront w loads part w of 16 rows.
+//   S^T (32 keys x 32 rows) = K Q^T and O^T (32 dimensions x 32 rows) += V^T P^T by 32 x 32 x 16 products (see wnw_lds.h for
+//   operands): a lane has 16 keys of ONE row, elements 0 .. 7 in the 16-row part 2 k and 8 .. 15 in 2 k + 1, so that S^T's elements are P^T's
+//   operand as they stand, and V^T's is read from the rows as columns.
+// KS = 2, for 33 to 64 rows: two wavefronts share 32 rows, each with half of every tile's keys, and join at the end.
+// A row's maximum m is raised, and its output and sum scaled, only when a logit exceeds it by LAZY_P (base 2).
+// NT: operands of a weight: 1, rounded to bf16, for bf16 outputs; 3, all of its 24 bits, for fp32 ones.
+constexpr int WIDE_P = 128;
+constexpr float LAZY_P = 8.f;
+
+template <int DH>
+struct PagedWideSmem {
+    alignas(256) unsigned char tile[2][2][64 * DH * 2];   // [buffer][K, V]
+    unsigned dirty[2][4];      // a wavefront's part of V has a number that is not finite
+};
+// In the tiles' place at the end, where two wavefronts share 32 rows: sums, maximum and sum of weights of the second.
+template <int DH>
+struct PagedWideJoin {
+    pf4_t o[2][DH / 8][64];
+    float2 ml[2][64];
+};
+
+template <int NT>
+__device__ inline void weights_to_terms(const float (&p)[8], bf16x8_t (&t)[NT])
+{
+    if constexpr (NT == 1) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[0][i] = (__bf16)p[i];
+    } else
+        weights_to_bf16(p, t);
+}
+
+template <int DH, int NT, int KS>
+__device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> &sm, const PartSeq &sq, int b, int hd, int rb, int ta,
+                                        int tb, int slot)
+{
+    using T = PagedTile<DH>;
+    constexpr int NS = DH / 16, ND = DH / 32, RB = WIDE_P / KS, NB = 2 / KS, PL = 16 * T::ROW / 1024;   // PL: loads of a part
+    constexpr unsigned V_OFF = 64 * DH * 2, BUF = 2 * V_OFF;
+    const PagedGeo &g = a.g;
+    const int len = sq.len, cnt = min(sq.cnt, len), base = len - cnt;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, half = lane >> 5;
+    const int rows32 = KS == 2 ? wave & 1 : wave, key32 = KS == 2 ? wave >> 1 : 0;    // the wavefront's rows, and its keys of a tile
+    const PageWalk pages(g, b, hd, len, T::ROW);
+
+    // cache rows that the block's last and first row may see
+    const int last = min(cnt - 1, min(rb * RB + RB - 1, a.R - 1) / a.G), first = rb * RB / a.G;
+    const int seen = cnt <= first ? 0 : a.mask ? len : base + last + 1;
+    const int full = (int)uniform(a.mask ? base : base + first + 1);
+    const int t_end = (int)uniform(min(tb, (seen + 63) / 64));
+
+    const unsigned lds = uniform(lds_address(sm.tile[0][0]));
+    unsigned off[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const unsigned r = j * (64 / T::UN) + lane / T::UN, u = lane % T::UN;
+        off[j] = r * T::ROW + (u ^ T::swz(r)) * 16;
+    }
+    // the wavefront's part of a tile, as bytes from the head's rows of page 0, and which of the four parts have no page
+    struct Parts {
+        size_t at;
+        unsigned gone;
+    };
+    auto parts_of = [&](int t) {
+        int id[4];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) id[s] = pages.entry(t * 64 + s * 16);
+        Parts p = {pages.offset(wave & 2 ? (wave & 1 ? id[3] : id[2]) : (wave & 1 ? id[1] : id[0]), t * 64 + wave * 16), 0};
+#pragma unroll
+        for (int s = 0; s < 4; ++s) p.gone |= pages.has(id[s]) ? 0u : 1u << s;
+        return p;
+    };
+    auto load = [&](const Parts &p, unsigned buf) {
+        const unsigned to = lds + buf + wave * T::PART;
+#pragma unroll
+        for (int j = 0; j < PL; ++j) load_to_lds(pages.k + p.at + (j & ~1) * 1024, off[j & 1], to + j * 1024);
+#pragma unroll
+        for (int j = 0; j < PL; ++j) load_to_lds(pages.v + p.at + (j & ~1) * 1024, off[j & 1], to + V_OFF + j * 1024);
+    };
+    Parts now, next;
+    if (ta < t_end) {
+        now = parts_of(ta);
+        load(now, 0);
+        next = parts_of(min(ta + 1, t_end - 1));
+    }
+
+    const PagedRow qr = paged_row(a, hd, rb * RB + rows32 * 32 + col, cnt);
+    bf16x8_t qf[NS];
+    unsigned odd = 0;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        pu4_t u = {0, 0, 0, 0};
+        if (qr.token >= 0) u = *(const pu4_t *)(a.q + (size_t)qr.row_of * DH + s * 16 + half * 8);
+        odd |= not_finite(u);
+        qf[s] = __builtin_bit_cast(bf16x8_t, u);
+    }
+    odd |= (unsigned)__shfl_xor((int)odd, 32);
+    const float crow = odd & 0x80008000u ? __uint_as_float(0x7fc00000u) : a.scale;
+    float m = -INFINITY, sum = 0.f;
+    f32x16_t o[ND];
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+    // K: row col, unit 2 s + half; V: rows 4 half + col16 / 4 and 8 more, two units of dimensions 16 (lane / 16 % 2) .. + 16
+    const unsigned k_get = lds + (key32 * 32 + col) * T::ROW + (half ^ T::swz(col)) * 16;
+    const unsigned n16 = lane & 15, v_row = half * 4 + n16 / 4;
+    const unsigned v_get = lds + V_OFF + (key32 * 32 + v_row) * T::ROW + ((2 * (lane >> 4 & 1)) ^ T::swz(v_row)) * 16 + (n16 & 3) * 8;
+
+    // one tile, from the buffer at `buf`; the next one goes to the other.  MASKED: some row may not see all of the tile.
+    auto round = [&](int t, auto buf_c, auto masked_c) {
+        const unsigned buf = buf_c, other = BUF - buf;
+        constexpr bool MASKED = decltype(masked_c)::value;
+        const int side = buf ? 1 : 0;
+        unsigned long long here = ~0ull;       // rows of the tile that there are
+        lds_loads_wait<0>();
+        if constexpr (MASKED) {
+            here = low_bits(len - t * 64);
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+                if (now.gone >> s & 1) here &= ~(0xffffull << (16 * s));
+            // Rows that are not there may hold anything: zeros instead.
+            unsigned odd = 0;
+#pragma unroll 1
+            for (int j = 0; j < PL; ++j) {
+                const unsigned at = lds + buf + V_OFF + wave * T::PART + j * 1024 + lane * 16, r = wave * 16 + (unsigned)(j * 64 + lane) / T::UN;
+                pu4_t u = __builtin_bit_cast(pu4_t, frag_read(at));
+                if (!(here >> r & 1)) {
+                    u = pu4_t{0, 0, 0, 0};
+                    *(__attribute__((address_space(3))) pu4_t *)(size_t)at = u;
+                }
+                odd |= not_finite(u);
+            }
+            const bool any = __any(odd & 0x80008000u);
+            if (lane == 0) sm.dirty[side][wave] = any;
+        }
+        lds_tile_barrier();
+        if (t + 1 < t_end) load(next, other);
+        f32x16_t x[NB];
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+            for (int kb = 0; kb < NB; ++kb) {
+                const f32x16_t zero = {};
+                x[kb] = mfma32(frag_read((k_get ^ s * 32) + kb * 32 * T::ROW + buf), qf[s], s ? x[kb] : zero);
+            }
+        // element i of x[kb] is of the wavefront's key 32 kb + 8 (i / 4) + 4 half + i % 4; base-2 logits relative to m from here
+        float mz = finite_or_zero(m);
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[kb][i] = fmaf(x[kb][i], crow, -mz);
+        unsigned long long see = ~0ull;
+        if constexpr (MASKED) {
+            see = (sees(a, b, qr.token, t * 64, base, len) & here) >> (key32 * 32 + half * 4);
+#pragma unroll
+            for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[kb][i] = seen_or_none((unsigned)(see >> 32 * kb), 8 * (i / 4) + i % 4, x[kb][i]);
+        }
+        float top = x[0][0];
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, x[kb][i]);
+        {
+            auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+            top = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+        }
+        if (__any(top > (m == -INFINITY ? -INFINITY : LAZY_P))) {
+            const float mn = fmaxf(m, mz + top), rise = finite_or_zero(mn) - mz, alpha = m == -INFINITY ? 0.f : exp2_hw(-rise);
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt) o[dt] *= alpha;
+#pragma unroll
+            for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[kb][i] -= rise;
+            sum *= alpha;
+            m = mn;
+        }
+        bf16x8_t p[2 * NB][NT];
+#pragma unroll
+        for (int c = 0; c < 2 * NB; ++c) {
+            float w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = exp2_hw(x[c >> 1][8 * (c & 1) + i]);
+            sum += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+            weights_to_terms<NT>(w, p[c]);
+        }
+        auto v_read = [&](int dt, int c) {
+            const unsigned at = (v_get ^ dt * 64) + c * T::PART + buf;
+            const pu2_t y0 = column_read(at), y1 = column_read(at + 8 * T::ROW);
+            return pu4_t{y0.x, y0.y, y1.x, y1.y};
+        };
+        if constexpr (MASKED)
+            if (sm.dirty[side][0] | sm.dirty[side][1] | sm.dirty[side][2] | sm.dirty[side][3]) {
+                // an element that is not finite makes that of the output NaN for the rows that see it, and is zero for the others
+#pragma unroll
+                for (int dt = 0; dt < ND; ++dt) {
+                    f32x16_t y;
+#pragma unroll
+                    for (int c = 0; c < 2 * NB; ++c) {
+                        pu4_t ones;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const unsigned two = (unsigned)(see >> (16 * c + 8 * (i / 2) + 2 * (i % 2))) & 3u;
+                            ones[i] = (two & 1) * 0x3f80u | (two >> 1) * 0x3f800000u;
+                        }
+                        const f32x16_t zero = {};
+                        y = mfma32(__builtin_bit_cast(bf16x8_t, not_finite_or_rest(v_read(dt, c), true)), __builtin_bit_cast(bf16x8_t, ones), c ? y : zero);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[dt][i] = y[i] > 0.f ? __uint_as_float(0x7fc00000u) : o[dt][i];
+                }
+                lds_tile_barrier();
+#pragma unroll 1
+                for (int j = 0; j < PL; ++j) {
+                    const unsigned at = lds + buf + V_OFF + wave * T::PART + j * 1024 + lane * 16;
+                    *(__attribute__((address_space(3))) pu4_t *)(size_t)at = not_finite_or_rest(__builtin_bit_cast(pu4_t, frag_read(at)), false);
+                }
+                lds_tile_barrier();
+            }
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+            for (int c = 0; c < 2 * NB; ++c) {
+                const bf16x8_t v = __builtin_bit_cast(bf16x8_t, v_read(dt, c));
+#pragma unroll
+                for (int k = 0; k < NT; ++k) o[dt] = mfma32(v, p[c][k], o[dt]);
+            }
+        now = next;
+        next = parts_of(min(t + 2, t_end - 1));
+    };
+    for (int t = ta; t < t_end; ++t) {
+        const bool masked = t * 64 + 64 > full || now.gone;
+        if (masked)
+            round(t, (t - ta) & 1 ? BUF : 0u, std::true_type{});
+        else if ((t - ta) & 1)
+            round(t, std::integral_constant<unsigned, BUF>{}, std::false_type{});
+        else
+            round(t, std::integral_constant<unsigned, 0>{}, std::false_type{});
+    }
+    sum += __shfl_xor(sum, 32);
+    if constexpr (KS == 2) {
+        // the keys' halves meet: the second's result to the same lane of the first's wavefront
+        static_assert(sizeof(PagedWideJoin<DH>) <= sizeof(sm.tile));
+        PagedWideJoin<DH> &jn = *(PagedWideJoin<DH> *)&sm;
+        __syncthreads();
+        if (key32) {
+#pragma unroll
+            for (int u = 0; u < ND * 4; ++u)
+                jn.o[rows32][u][lane] = pf4_t{o[u / 4][u % 4 * 4], o[u / 4][u % 4 * 4 + 1], o[u / 4][u % 4 * 4 + 2], o[u / 4][u % 4 * 4 + 3]};
+            jn.ml[rows32][lane] = make_float2(m, sum);
+        }
+        __syncthreads();
+        if (key32) return;
+        const float2 ml = jn.ml[rows32][lane];
+        const float mm = fmaxf(m, ml.x), mz = finite_or_zero(mm);
+        const float f0 = sum == 0.f ? 0.f : exp2f(m - mz), f1 = ml.y == 0.f ? 0.f : exp2f(ml.x - mz);    // 0: saw nothing
+        sum = f0 * sum + f1 * ml.y;
+        m = mm;
+#pragma unroll
+        for (int u = 0; u < ND * 4; ++u) {
+            const pf4_t y = jn.o[rows32][u][lane];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[u / 4][u % 4 * 4 + e] = f0 * o[u / 4][u % 4 * 4 + e] + f1 * y[e];
+        }
+    }
+    if (qr.token < 0) return;
+    // element i of o[dt]: dimension 32 dt + 8 (i / 4) + 4 half + i % 4 of row col
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const size_t at = slot >= 0 ? (size_t)(a.group() * 2 + slot) * RB + rows32 * 32 + col : (size_t)qr.row_of;
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            float y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = o[dt][i + e] * (slot >= 0 ? 1.f : inv);
+            const size_t to = at * DH + dt * 32 + 2 * i + 4 * half;
+            if (slot >= 0)
+                *(pf4_t *)(a.ws_o + to) = pf4_t{y[0], y[1], y[2], y[3]};
+            else
+                store_out<4>(a.out, a.bf16, to, y);
+        }
+    if (half == 0) {
+        if (slot >= 0)
+            a.ws_ml[at] = make_float2(m, sum);
+        else if (a.lse)
+            a.lse[at] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * P_LN2;
+    }
+}
+
+template <int DH, int NT, int KS>
+__global__ __launch_bounds__(P_THREADS, 2) void paged_wide_kernel(PagedAttend a)
+{
+    __shared__ PagedWideSmem<DH> sm;
+    run_parts(a, [&](const PartSeq &sq, int b, int hd, int rb, int ta, int tb, int slot) {
+        paged_wide_block<DH, NT, KS>(a, sm, sq, b, hd, rb, ta, tb, slot);
     });
 }
 
@@ -769,8 +1107,8 @@ PagedPlan paged_plan(const wnw_paged_config &c, int32_t n_layers, int32_t q_head
     const int64_t cap = (int64_t)c.table_width * c.page, heads = (int64_t)c.batch * n_layers * c.kv_heads, R = (int64_t)q_heads / c.kv_heads * n;
     const int64_t len = max_len ? std::min<int64_t>(max_len, cap) : cap;
     PagedPlan p;
-    p.RB = R > 16 ? 32 : 16;
-    p.tsh = c.head_dim == 64 ? 6 : 5;
+    p.RB = R > 64 ? WIDE_P : R > 32 ? WIDE_P / 2 : R > 16 ? 32 : 16;
+    p.tsh = c.head_dim == 64 || p.RB > 32 ? 6 : 5;
     const int64_t blocks = heads * ((R + p.RB - 1) / p.RB), per = (len + (1 << p.tsh) - 1) >> p.tsh, tiles = per * blocks;
     p.stream = R <= p.RB && heads * len * c.head_dim * 4 > (256ll << 20);
     p.whole = blocks >= 512;
@@ -788,6 +1126,13 @@ void launch_tokens(const PagedPlan &p, const PagedAttend &a, hipStream_t st)
     auto *k = p.eight ? (p.stream ? paged_token_kernel<DH, MT, true, 8> : paged_token_kernel<DH, MT, false, 8>)
                       : (p.stream ? paged_token_kernel<DH, MT, true, 4> : paged_token_kernel<DH, MT, false, 4>);
     hipLaunchKernelGGL(k, dim3(p.W), dim3(p.eight ? 512 : 256), 0, st, a);
+}
+
+template <int DH, int NT>
+void launch_wide(const PagedPlan &p, const PagedAttend &a, hipStream_t st)
+{
+    auto *k = p.RB == WIDE_P ? paged_wide_kernel<DH, NT, 1> : paged_wide_kernel<DH, NT, 2>;
+    hipLaunchKernelGGL(k, dim3(p.W), dim3(P_THREADS), 0, st, a);
 }
 
 wnw_status paged_heads(const wnw_paged_config &c, int32_t n_layers, int32_t q_heads, int32_t n, int32_t max_len)
@@ -929,7 +1274,9 @@ wnw_status wnw_paged_attend(const wnw_paged_config *cfg, const wnw_paged_cache *
                            P_LOG2E / sqrtf((float)cfg->head_dim)};
     paged_dispatch(*cfg, [&](auto d) {
         constexpr int DH = decltype(d)::value;
-        if (p.RB == 32)
+        if (p.RB > 32)
+            a.bf16 ? launch_wide<DH, 1>(p, a, (hipStream_t)hip_stream) : launch_wide<DH, 3>(p, a, (hipStream_t)hip_stream);
+        else if (p.RB == 32)
             launch_tokens<DH, 2>(p, a, (hipStream_t)hip_stream);
         else
             launch_tokens<DH, 1>(p, a, (hipStream_t)hip_stream);

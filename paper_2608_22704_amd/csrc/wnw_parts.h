@@ -4,7 +4,8 @@
 // A, the arguments of such a kernel, has: g with B sequences and nl * H KV-heads a sequence; len and count (device, see below; count
 // may be null); cap, the most rows of a sequence; tiles_of(rows); n tokens, G q-heads per KV-head, R = n G query rows of a KV-head (row
 // r is token r / G, q-head r % G), in blocks of RB = 2^rsh; W work-groups and inv_w = 1 / W; nrb > 0: a work-group for
-// every block of rows, nrb of them a head.
+// every block of rows, nrb of them a head.  group(): the work-group's number, 0 .. W - 1, in the order in which parts are dealt
+// out (and in which the workspace has them).
 #pragma once
 
 #include "wnw_lds.h"
@@ -293,15 +294,15 @@ __device__ inline void run_parts(const A &a, F f)
         hd = (int)uniform(hd + b * sh.heads), rb = (int)uniform(rb), ta = (int)uniform(ta), tb = (int)uniform(tb);
     };
     if (a.nrb > 0) {
-        hd = a.nrb == 1 ? (int)blockIdx.x : (int)blockIdx.x / a.nrb;
-        rb = (int)blockIdx.x - hd * a.nrb;
+        hd = a.nrb == 1 ? (int)a.group() : (int)a.group() / a.nrb;
+        rb = (int)a.group() - hd * a.nrb;
         if (a.g.B > 1) b = hd / (a.g.nl * a.g.H);
         sq = part_seq(a, b);
         if (rb >= sq.nrb) return;
         tb = sq.tiles;
     } else {
         sh.init(a, threadIdx.x & 63);
-        i = blockIdx.x * sh.per;
+        i = a.group() * sh.per;
         if (i >= sh.total) return;
         i1 = min(i + sh.per, sh.total);
         b = sh.find(a, i, start, sq);

@@ -561,6 +561,7 @@ struct QuantAttend {
     float *ws_m;               // masses: [rows][cap / 64] the maximum that a tile's masses are relative to
     float scale;               // log2(e) / sqrt(d)
     __device__ int cap() const { return g.cap; }
+    __device__ static unsigned group() { return blockIdx.x; }
     __device__ static int tiles_of(int rows) { return (rows + QT - 1) / QT; }
 };
 

@@ -9,8 +9,8 @@ the sum by 2^-24 each: together below 2^-21 (|x0| + |x1|) amplitude; and half a 
 Attention: products of bf16 are exact in fp32 and d of them are summed, so a base-2 logit is off by at most (d + 3) 2^-24
 sum|q k| / sqrt(d) log2(e) with its scaling and the subtraction of the maximum (at most twice that magnitude); a weight by ln 2 times
 that, its exponential by 2^-22, and the denominator alike.  T products are summed in fp32 (T 2^-24 at worst, taken with the joins).
-bf16 outputs add half a step, 2^-8 |y|; with more than 32 query rows of a KV-head weights are rounded to bf16 as well, 2^-8 each, and
-the denominator is off by no more: 2^-7 of sum p |v|.
+bf16 outputs add half a step, 2^-8 |y|; with more than 32 query rows of a KV-head the weights that multiply V are rounded to bf16
+as well, 2^-8 of sum p |v|.
 """
 import math
 
@@ -199,7 +199,7 @@ def check_outputs(out, lse, ref, D, bf16, rounded_weights):
     some = live & ~empty
     bound = (werr + seen * EPS + 4 * EPS).unsqueeze(-1) * absv
     if rounded_weights:
-        bound = bound + 2.0 ** -7 * absv
+        bound = bound + 2.0 ** -8 * absv
     if bf16:
         bound = bound * (1 + 2.0 ** -8) + 2.0 ** -8 * want.abs()
     err = (out.double() - want).abs()
