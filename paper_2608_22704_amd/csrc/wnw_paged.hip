@@ -241,6 +241,7 @@ struct PagedAttend {
     float *ws_o;               // [W][2][RB][d]: sums of weights times values of a block of rows over a piece of its cache
     float2 *ws_ml;             // [W][2][RB]: the piece's maximum (base 2) and sum of weights
     float scale;               // log2(e) / sqrt(d)
+    static constexpr int BLOCK_COST = 8;      // a block's start in tiles' times
     __device__ int cap() const { return g.cap(); }
     // Work-groups go to the eight dies in turn; those that follow each other here are on one die, whose cache then serves the blocks of
     // rows of one head.
@@ -708,7 +709,7 @@ constexpr float LAZY_P = 8.f;
 
 template <int DH>
 struct PagedWideSmem {
-    alignas(256) unsigned char tile[2][2][64 * DH * 2];   // [buffer][K, V]
+    alignas(256) unsigned char tile[2][2][64 * DH * 2];   // [K, V][buffer]
     unsigned dirty[2][4];      // a wavefront's part of V has a number that is not finite
 };
 // In the tiles' place at the end, where two wavefronts share 32 rows: sums, maximum and sum of weights of the second.
@@ -734,7 +735,7 @@ __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> 
 {
     using T = PagedTile<DH>;
     constexpr int NS = DH / 16, ND = DH / 32, RB = WIDE_P / KS, NB = 2 / KS, PL = 16 * T::ROW / 1024;   // PL: loads of a part
-    constexpr unsigned V_OFF = 64 * DH * 2, BUF = 2 * V_OFF;
+    constexpr unsigned BUF = 64 * DH * 2, V_OFF = 2 * BUF;
     const PagedGeo &g = a.g;
     const int len = sq.len, cnt = min(sq.cnt, len), base = len - cnt;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -769,18 +770,19 @@ __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> 
         for (int s = 0; s < 4; ++s) p.gone |= pages.has(id[s]) ? 0u : 1u << s;
         return p;
     };
-    auto load = [&](const Parts &p, unsigned buf) {
-        const unsigned to = lds + buf + wave * T::PART;
+    auto load = [&](const char *pool, const Parts &p, unsigned to) {
 #pragma unroll
-        for (int j = 0; j < PL; ++j) load_to_lds(pages.k + p.at + (j & ~1) * 1024, off[j & 1], to + j * 1024);
-#pragma unroll
-        for (int j = 0; j < PL; ++j) load_to_lds(pages.v + p.at + (j & ~1) * 1024, off[j & 1], to + V_OFF + j * 1024);
+        for (int j = 0; j < PL; ++j) load_to_lds(pool + p.at + (j & ~1) * 1024, off[j & 1], lds + to + wave * T::PART + j * 1024);
     };
-    Parts now, next;
+    // K of a tile is there a round before its V: buffers of K 0, 1, then of V
+    Parts now = {0, 0}, next = {0, 0}, after = {0, 0};
     if (ta < t_end) {
         now = parts_of(ta);
-        load(now, 0);
-        next = parts_of(min(ta + 1, t_end - 1));
+        next = parts_of(ta + 1);
+        after = parts_of(ta + 2);
+        load(pages.k, now, 0);
+        load(pages.k, next, BUF);
+        load(pages.v, now, V_OFF);
     }
 
     const PagedRow qr = paged_row(a, hd, rb * RB + rows32 * 32 + col, cnt);
@@ -806,7 +808,23 @@ __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> 
     const unsigned n16 = lane & 15, v_row = half * 4 + n16 / 4;
     const unsigned v_get = lds + V_OFF + (key32 * 32 + v_row) * T::ROW + ((2 * (lane >> 4 & 1)) ^ T::swz(v_row)) * 16 + (n16 & 3) * 8;
 
-    // one tile, from the buffer at `buf`; the next one goes to the other.  MASKED: some row may not see all of the tile.
+    auto logits = [&](f32x16_t (&x)[NB], unsigned buf) {
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+            for (int kb = 0; kb < NB; ++kb) {
+                const f32x16_t zero = {};
+                x[kb] = mfma32(frag_read((k_get ^ s * 32) + kb * 32 * T::ROW + buf), qf[s], s ? x[kb] : zero);
+            }
+    };
+    f32x16_t x[NB];      // products of the tile that is next
+    if (ta < t_end) {
+        lds_loads_wait<0>();
+        lds_tile_barrier();
+        logits(x, 0);
+    }
+    // one tile, whose K and V are in the buffers at `buf`: its softmax beside the next one's products with K, then its products with V.
+    // MASKED: some row may not see all of the tile.
     auto round = [&](int t, auto buf_c, auto masked_c) {
         const unsigned buf = buf_c, other = BUF - buf;
         constexpr bool MASKED = decltype(masked_c)::value;
@@ -834,57 +852,64 @@ __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> 
             if (lane == 0) sm.dirty[side][wave] = any;
         }
         lds_tile_barrier();
-        if (t + 1 < t_end) load(next, other);
-        f32x16_t x[NB];
-#pragma unroll
-        for (int s = 0; s < NS; ++s)
-#pragma unroll
-            for (int kb = 0; kb < NB; ++kb) {
-                const f32x16_t zero = {};
-                x[kb] = mfma32(frag_read((k_get ^ s * 32) + kb * 32 * T::ROW + buf), qf[s], s ? x[kb] : zero);
-            }
+        if (t + 2 < t_end) load(pages.k, after, buf);
+        if (t + 1 < t_end) load(pages.v, next, V_OFF + other);
         // element i of x[kb] is of the wavefront's key 32 kb + 8 (i / 4) + 4 half + i % 4; base-2 logits relative to m from here
         float mz = finite_or_zero(m);
+        f32x16_t y[NB];
+        __builtin_amdgcn_sched_barrier(0);
+        logits(y, other);
+        float w[2 * NB][8];        // of 16-row part c: elements 8 (c % 2) .. + 8 of x[c / 2]
 #pragma unroll
-        for (int kb = 0; kb < NB; ++kb)
+        for (int c = 0; c < 2 * NB; ++c)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[kb][i] = fmaf(x[kb][i], crow, -mz);
+            for (int i = 0; i < 8; ++i) w[c][i] = fmaf(x[c >> 1][8 * (c & 1) + i], crow, -mz);
         unsigned long long see = ~0ull;
         if constexpr (MASKED) {
             see = (sees(a, b, qr.token, t * 64, base, len) & here) >> (key32 * 32 + half * 4);
 #pragma unroll
-            for (int kb = 0; kb < NB; ++kb)
+            for (int c = 0; c < 2 * NB; ++c)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) x[kb][i] = seen_or_none((unsigned)(see >> 32 * kb), 8 * (i / 4) + i % 4, x[kb][i]);
+                for (int i = 0; i < 8; ++i) w[c][i] = seen_or_none((unsigned)(see >> (c & 2 ? 32 : 0)), 16 * (c & 1) + 8 * (i / 4) + i % 4, w[c][i]);
         }
-        float top = x[0][0];
+        float top = w[0][0];
 #pragma unroll
-        for (int kb = 0; kb < NB; ++kb)
+        for (int c = 0; c < 2 * NB; ++c)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, x[kb][i]);
+            for (int i = 0; i < 8; ++i) top = fmaxf(top, w[c][i]);
         {
             auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
             top = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+        }
+        if constexpr (!MASKED) {
+            // a read of K, a product and its share of the vector instructions in turn
+#pragma unroll
+            for (int i = 0; i < 3; ++i) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+#pragma unroll
+            for (int i = 0; i < NS * NB; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+            }
         }
         if (__any(top > (m == -INFINITY ? -INFINITY : LAZY_P))) {
             const float mn = fmaxf(m, mz + top), rise = finite_or_zero(mn) - mz, alpha = m == -INFINITY ? 0.f : exp2_hw(-rise);
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt) o[dt] *= alpha;
 #pragma unroll
-            for (int kb = 0; kb < NB; ++kb)
+            for (int c = 0; c < 2 * NB; ++c)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) x[kb][i] -= rise;
+                for (int i = 0; i < 8; ++i) w[c][i] -= rise;
             sum *= alpha;
             m = mn;
         }
         bf16x8_t p[2 * NB][NT];
 #pragma unroll
         for (int c = 0; c < 2 * NB; ++c) {
-            float w[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = exp2_hw(x[c >> 1][8 * (c & 1) + i]);
-            sum += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
-            weights_to_terms<NT>(w, p[c]);
+            for (int i = 0; i < 8; ++i) w[c][i] = exp2_hw(w[c][i]);
+            sum += ((w[c][0] + w[c][1]) + (w[c][2] + w[c][3])) + ((w[c][4] + w[c][5]) + (w[c][6] + w[c][7]));
+            weights_to_terms<NT>(w[c], p[c]);
         }
         auto v_read = [&](int dt, int c) {
             const unsigned at = (v_get ^ dt * 64) + c * T::PART + buf;
@@ -896,7 +921,7 @@ __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> 
                 // an element that is not finite makes that of the output NaN for the rows that see it, and is zero for the others
 #pragma unroll
                 for (int dt = 0; dt < ND; ++dt) {
-                    f32x16_t y;
+                    f32x16_t found;
 #pragma unroll
                     for (int c = 0; c < 2 * NB; ++c) {
                         pu4_t ones;
@@ -906,10 +931,11 @@ __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> 
                             ones[i] = (two & 1) * 0x3f80u | (two >> 1) * 0x3f800000u;
                         }
                         const f32x16_t zero = {};
-                        y = mfma32(__builtin_bit_cast(bf16x8_t, not_finite_or_rest(v_read(dt, c), true)), __builtin_bit_cast(bf16x8_t, ones), c ? y : zero);
+                        found = mfma32(__builtin_bit_cast(bf16x8_t, not_finite_or_rest(v_read(dt, c), true)), __builtin_bit_cast(bf16x8_t, ones),
+                                       c ? found : zero);
                     }
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) o[dt][i] = y[i] > 0.f ? __uint_as_float(0x7fc00000u) : o[dt][i];
+                    for (int i = 0; i < 16; ++i) o[dt][i] = found[i] > 0.f ? __uint_as_float(0x7fc00000u) : o[dt][i];
                 }
                 lds_tile_barrier();
 #pragma unroll 1
@@ -928,17 +954,19 @@ __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> 
                 for (int k = 0; k < NT; ++k) o[dt] = mfma32(v, p[c][k], o[dt]);
             }
         now = next;
-        next = parts_of(min(t + 2, t_end - 1));
+        next = after;
+        after = parts_of(t + 3);
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb) x[kb] = y[kb];
     };
-    for (int t = ta; t < t_end; ++t) {
-        const bool masked = t * 64 + 64 > full || now.gone;
-        if (masked)
-            round(t, (t - ta) & 1 ? BUF : 0u, std::true_type{});
-        else if ((t - ta) & 1)
-            round(t, std::integral_constant<unsigned, BUF>{}, std::false_type{});
-        else
-            round(t, std::integral_constant<unsigned, 0>{}, std::false_type{});
+    // tiles that every row sees, in pairs; then the others (all of them from the first page on that is not there)
+    int t = ta;
+    for (const int t_full = min(t_end, full / 64); t + 2 <= t_full && !(now.gone | next.gone); t += 2) {
+        round(t, std::integral_constant<unsigned, 0>{}, std::false_type{});
+        round(t + 1, std::integral_constant<unsigned, BUF>{}, std::false_type{});
     }
+#pragma unroll 1
+    for (; t < t_end; ++t) round(t, (t - ta) & 1 ? BUF : 0u, std::true_type{});
     sum += __shfl_xor(sum, 32);
     if constexpr (KS == 2) {
         // the keys' halves meet: the second's result to the same lane of the first's wavefront
@@ -999,12 +1027,14 @@ __global__ __launch_bounds__(P_THREADS, 2) void paged_wide_kernel(PagedAttend a)
     });
 }
 
-// Joins the pieces of a cache: a work-group per 16 rows of a head, sixteen threads a row.
-template <int DH>
+// Joins the pieces of a cache: sixteen threads have a row's pieces p, p + GP, ..., and a work-group 16 / GP rows of a head.
+template <int DH, int GP>
 __global__ __launch_bounds__(P_THREADS) void paged_join_kernel(PagedAttend a)
 {
-    constexpr int E = DH / 16;
-    const unsigned groups = (a.R + 15) / 16, hd = blockIdx.x / groups, r0 = (blockIdx.x - hd * groups) * 16;
+    constexpr int E = DH / 16, ROWS = 16 / GP;
+    __shared__ float so[GP > 1 ? GP : 1][ROWS][DH];
+    __shared__ float2 sml[GP > 1 ? GP : 1][ROWS];
+    const unsigned groups = (a.R + ROWS - 1) / ROWS, hd = blockIdx.x / groups, r0 = (blockIdx.x - hd * groups) * ROWS;
     const int b = hd / (a.g.nl * a.g.H);
     const PartSeq sq = part_seq(a, b);
     const int cnt = min(sq.cnt, sq.len);
@@ -1012,23 +1042,47 @@ __global__ __launch_bounds__(P_THREADS) void paged_join_kernel(PagedAttend a)
     PartShare<PagedAttend> sh;
     sh.init(a, threadIdx.x & 63);
     const PartPieces<PagedAttend> pc(a, sh, sq, b, hd, r0 >> a.rsh);
-    const unsigned r = r0 + (threadIdx.x >> 4), d0 = (threadIdx.x & 15) * E;
+    if (pc.n == 1) return;
+    const unsigned slot = threadIdx.x >> 4, rr = slot % ROWS, gp = slot / ROWS, r = r0 + rr, d0 = (threadIdx.x & 15) * E;
     const PagedRow row = paged_row(a, hd, r, cnt);
-    if (pc.n == 1 || row.token < 0) return;
     float m = -INFINITY, sum = 0.f, x[E] = {};
+    if (row.token >= 0) {
 #pragma unroll 4
-    for (unsigned p = 0; p < pc.n; ++p) m = fmaxf(m, a.ws_ml[pc.at(p, r)].x);
-    const float mz = finite_or_zero(m);
-#pragma unroll 2
-    for (unsigned p = 0; p < pc.n; ++p) {
-        const float2 ml = a.ws_ml[pc.at(p, r)];
-        const float f = ml.y == 0.f ? 0.f : exp2f(ml.x - mz);       // 0: the piece saw nothing
-        sum += f * ml.y;
-        float o[E];
-        __builtin_memcpy(o, __builtin_assume_aligned(a.ws_o + pc.at(p, r) * DH + d0, 16), sizeof(o));
+        for (unsigned p = gp; p < pc.n; p += GP) m = fmaxf(m, a.ws_ml[pc.at(p, r)].x);
+        const float mz = finite_or_zero(m);
+#pragma unroll 4
+        for (unsigned p = gp; p < pc.n; p += GP) {
+            const float2 ml = a.ws_ml[pc.at(p, r)];
+            const float f = ml.y == 0.f ? 0.f : exp2f(ml.x - mz);       // 0: the piece saw nothing
+            sum += f * ml.y;
+            float o[E];
+            __builtin_memcpy(o, __builtin_assume_aligned(a.ws_o + pc.at(p, r) * DH + d0, 16), sizeof(o));
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[e] += f * o[e];
+            for (int e = 0; e < E; ++e) x[e] += f * o[e];
+        }
     }
+    if constexpr (GP > 1) {
+        if (d0 == 0) sml[gp][rr] = make_float2(m, sum);
+#pragma unroll
+        for (int e = 0; e < E; ++e) so[gp][rr][d0 + e] = x[e];
+        __syncthreads();
+        if (gp) return;
+#pragma unroll
+        for (int k = 0; k < GP; ++k) m = fmaxf(m, sml[k][rr].x);
+        const float mz = finite_or_zero(m);
+        sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = 0.f;
+#pragma unroll
+        for (int k = 0; k < GP; ++k) {
+            const float2 ml = sml[k][rr];
+            const float f = ml.y == 0.f ? 0.f : exp2f(ml.x - mz);
+            sum += f * ml.y;
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] += f * so[k][rr][d0 + e];
+        }
+    }
+    if (row.token < 0) return;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] *= inv;
@@ -1098,7 +1152,7 @@ void paged_dispatch(const wnw_paged_config &c, F f)
 // How an attention call runs.
 struct PagedPlan {
     int RB, W, tsh;
-    bool whole, eight, stream;
+    bool whole, eight, stream, join_groups;
     int64_t rows, o_bytes, ml_bytes;
     int64_t total() const { return o_bytes + ml_bytes; }
 };
@@ -1115,6 +1169,7 @@ PagedPlan paged_plan(const wnw_paged_config &c, int32_t n_layers, int32_t q_head
     p.eight = false;
     p.W = (int)std::max<int64_t>(1, p.whole ? blocks : std::min<int64_t>(512, tiles / MIN_PIECE + blocks));
     p.rows = heads * R;
+    p.join_groups = p.rows <= 8192;
     p.o_bytes = p.whole ? 0 : (int64_t)p.W * 2 * p.RB * c.head_dim * 4;
     p.ml_bytes = p.whole ? 0 : (int64_t)p.W * 2 * p.RB * 8;
     return p;
@@ -1280,9 +1335,10 @@ wnw_status wnw_paged_attend(const wnw_paged_config *cfg, const wnw_paged_cache *
             launch_tokens<DH, 2>(p, a, (hipStream_t)hip_stream);
         else
             launch_tokens<DH, 1>(p, a, (hipStream_t)hip_stream);
-        if (!p.whole)
-            hipLaunchKernelGGL((paged_join_kernel<DH>), dim3((unsigned)(p.rows / R * ((R + 15) / 16))), dim3(P_THREADS), 0,
-                               (hipStream_t)hip_stream, a);
+        if (p.whole) return;
+        const int per = p.join_groups ? 1 : 16;
+        hipLaunchKernelGGL((p.join_groups ? paged_join_kernel<DH, 16> : paged_join_kernel<DH, 1>), dim3((unsigned)(p.rows / R * ((R + per - 1) / per))),
+                           dim3(P_THREADS), 0, (hipStream_t)hip_stream, a);
     });
     return paged_hip();
 }

@@ -5,7 +5,7 @@
 // may be null); cap, the most rows of a sequence; tiles_of(rows); n tokens, G q-heads per KV-head, R = n G query rows of a KV-head (row
 // r is token r / G, q-head r % G), in blocks of RB = 2^rsh; W work-groups and inv_w = 1 / W; nrb > 0: a work-group for
 // every block of rows, nrb of them a head.  group(): the work-group's number, 0 .. W - 1, in the order in which parts are dealt
-// out (and in which the workspace has them).
+// out (and in which the workspace has them).  BLOCK_COST: see below.
 #pragma once
 
 #include "wnw_lds.h"
@@ -113,7 +113,8 @@ __device__ inline float finite_or_zero(float m)
 // empty sequence's outputs are written).  W work-groups share them, whatever the lengths are, in one of two ways:
 //   pieces  a block's tiles are cut into pieces of at most `pp` tiles, a work-group each;
 //   line    all tiles in a line, in the order sequence, head, block of rows, tile, are cut into W equal parts (pp = 0), so that a
-//           work-group's part may end one block and begin another.
+//           work-group's part may end one block and begin another.  In front of its tiles a block has A::BLOCK_COST places
+//           that stand for its start, so that many short blocks do not count as little.
 // The line is even, but a second block costs a work-group about PIECE_COST tiles' time again (its queries, first tiles and
 // the join of its wavefronts).  A block that is not whole leaves its result in the workspace, in the work-group's slot 1
 // (its first tiles) or 0 (later ones), and a second kernel joins those.  With nrb > 0 there is none of this: every block has its
@@ -179,7 +180,7 @@ struct PartShare {
 
     __device__ PartSeq seq(const A &a, int b0) const { return b0 == 0 ? mine : part_seq(a, b0 + lane); }
     // items of a block of rows
-    __device__ unsigned span(const PartSeq &q) const { return pp ? (unsigned)div24(q.tiles + pp - 1, pp) : (unsigned)q.tiles; }
+    __device__ unsigned span(const PartSeq &q) const { return pp ? (unsigned)div24(q.tiles + pp - 1, pp) : (unsigned)(q.tiles + A::BLOCK_COST); }
     __device__ unsigned work(const PartSeq &q) const { return span(q) * (unsigned)(q.nrb * heads); }
 
     __device__ void init(const A &a, int lane_)
@@ -203,8 +204,8 @@ struct PartShare {
         per = max(at_least(t, a.inv_w), (unsigned)MIN_PIECE);
         if (units < (unsigned)a.W) {
             // pieces of at most p tiles are at most t / p + units
-            const unsigned p = min(max(at_least(t, __builtin_amdgcn_rcpf((float)(a.W - units))), (unsigned)MIN_PIECE), most);
-            if (p && piece_len((int)most, (int)p) <= (int)per + PIECE_COST) {
+            const unsigned p = min(max(at_least(t - units * A::BLOCK_COST, __builtin_amdgcn_rcpf((float)(a.W - units))), (unsigned)MIN_PIECE), most);
+            if (p && piece_len((int)most, (int)p) <= (int)per + (A::BLOCK_COST ? 0 : PIECE_COST)) {
                 pp = (int)p;
                 per = 1;
                 if (a.g.B == 1)
@@ -284,6 +285,7 @@ __device__ inline void run_parts(const A &a, F f)
         ta = (int)at;
         tb = (int)min(span, at + (i1 - i));
         i += tb - ta;
+        if (A::BLOCK_COST && !sh.pp) ta = max(0, ta - A::BLOCK_COST), tb = max(0, tb - A::BLOCK_COST);
         if (sh.pp) {
             const int len = PartShare<A>::piece_len(sq.tiles, sh.pp);
             ta = min(sq.tiles, (int)at * len);
@@ -309,7 +311,7 @@ __device__ inline void run_parts(const A &a, F f)
         item();
     }
     for (;;) {
-        f(sq, b, hd, rb, ta, tb, ta > 0 ? 0 : tb < sq.tiles ? 1 : -1);
+        if (!A::BLOCK_COST || tb > ta) f(sq, b, hd, rb, ta, tb, ta > 0 ? 0 : tb < sq.tiles ? 1 : -1);
         if (i >= i1) return;
         if (i - start >= sh.work(sq)) b = sh.find(a, i, start, sq);
         item();
@@ -325,7 +327,7 @@ struct PartPieces {
     __device__ PartPieces(const A &a, const PartShare<A> &sh, const PartSeq &sq, int b, unsigned hd, unsigned rb) : RB(a.RB)
     {
         const unsigned span = sh.span(sq), s0 = sh.before(a, b) + ((hd - b * sh.heads) * sq.nrb + rb) * span;
-        w0 = sh.per == 1 ? s0 : s0 / sh.per;
+        w0 = sh.per == 1 ? s0 : (s0 + A::BLOCK_COST) / sh.per;
         n = (sh.per == 1 ? s0 + span - 1 : (s0 + span - 1) / sh.per) - w0 + 1;
     }
     // row of piece p: slot 1 of its work-group for the first, 0 for the others

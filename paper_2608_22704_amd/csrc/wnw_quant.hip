@@ -560,6 +560,7 @@ struct QuantAttend {
     float2 *ws_row;            // masses: [rows] maximum and sum of rows whose cache is one piece
     float *ws_m;               // masses: [rows][cap / 64] the maximum that a tile's masses are relative to
     float scale;               // log2(e) / sqrt(d)
+    static constexpr int BLOCK_COST = 0;
     __device__ int cap() const { return g.cap; }
     __device__ static unsigned group() { return blockIdx.x; }
     __device__ static int tiles_of(int rows) { return (rows + QT - 1) / QT; }
