@@ -704,7 +704,6 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_token_kernel(PagedAttend a)
 // KS = 2, for 33 to 64 rows: two wavefronts share 32 rows, each with half of every tile's keys, and join at the end.
 // A row's maximum m is raised, and its output and sum scaled, only when a logit exceeds it by LAZY_P (base 2).
 // NT: operands of a weight: 1, rounded to bf16, for bf16 outputs; 3, all of its 24 bits, for fp32 ones.
-constexpr int WIDE_P = 128;
 constexpr float LAZY_P = 8.f;
 
 template <int DH>
@@ -729,12 +728,12 @@ __device__ inline void weights_to_terms(const float (&p)[8], bf16x8_t (&t)[NT])
         weights_to_bf16(p, t);
 }
 
-template <int DH, int NT, int KS>
+template <int DH, int NT, int KS, int NW>
 __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> &sm, const PartSeq &sq, int b, int hd, int rb, int ta,
                                         int tb, int slot)
 {
     using T = PagedTile<DH>;
-    constexpr int NS = DH / 16, ND = DH / 32, RB = WIDE_P / KS, NB = 2 / KS, PL = 16 * T::ROW / 1024;   // PL: loads of a part
+    constexpr int NS = DH / 16, ND = DH / 32, RB = 32 * NW / KS, NB = 2 / KS, PL = 16 * T::ROW / 1024;   // PL: loads of a part
     constexpr unsigned BUF = 64 * DH * 2, V_OFF = 2 * BUF;
     const PagedGeo &g = a.g;
     const int len = sq.len, cnt = min(sq.cnt, len), base = len - cnt;
@@ -765,14 +764,17 @@ __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> 
         int id[4];
 #pragma unroll
         for (int s = 0; s < 4; ++s) id[s] = pages.entry(t * 64 + s * 16);
-        Parts p = {pages.offset(wave & 2 ? (wave & 1 ? id[3] : id[2]) : (wave & 1 ? id[1] : id[0]), t * 64 + wave * 16), 0};
+        Parts p = {pages.offset(wave & 2 ? (wave & 1 ? id[3] : id[2]) : (wave & 1 ? id[1] : id[0]), t * 64 + (wave & 3) * 16), 0};
 #pragma unroll
         for (int s = 0; s < 4; ++s) p.gone |= pages.has(id[s]) ? 0u : 1u << s;
         return p;
     };
+    // of four wavefronts each loads a part of K and of V, of eight four do for K and four for V
+    const int part = wave & 3;
+    const bool has_k = NW == 4 || wave < 4, has_v = NW == 4 || wave >= 4;
     auto load = [&](const char *pool, const Parts &p, unsigned to) {
 #pragma unroll
-        for (int j = 0; j < PL; ++j) load_to_lds(pool + p.at + (j & ~1) * 1024, off[j & 1], lds + to + wave * T::PART + j * 1024);
+        for (int j = 0; j < PL; ++j) load_to_lds(pool + p.at + (j & ~1) * 1024, off[j & 1], lds + to + part * T::PART + j * 1024);
     };
     // K of a tile is there a round before its V: buffers of K 0, 1, then of V
     Parts now = {0, 0}, next = {0, 0}, after = {0, 0};
@@ -780,9 +782,11 @@ __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> 
         now = parts_of(ta);
         next = parts_of(ta + 1);
         after = parts_of(ta + 2);
-        load(pages.k, now, 0);
-        load(pages.k, next, BUF);
-        load(pages.v, now, V_OFF);
+        if (has_k) {
+            load(pages.k, now, 0);
+            load(pages.k, next, BUF);
+        }
+        if (has_v) load(pages.v, now, V_OFF);
     }
 
     const PagedRow qr = paged_row(a, hd, rb * RB + rows32 * 32 + col, cnt);
@@ -839,8 +843,8 @@ __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> 
             // Rows that are not there may hold anything: zeros instead.
             unsigned odd = 0;
 #pragma unroll 1
-            for (int j = 0; j < PL; ++j) {
-                const unsigned at = lds + buf + V_OFF + wave * T::PART + j * 1024 + lane * 16, r = wave * 16 + (unsigned)(j * 64 + lane) / T::UN;
+            for (int j = has_v ? 0 : PL; j < PL; ++j) {
+                const unsigned at = lds + buf + V_OFF + part * T::PART + j * 1024 + lane * 16, r = part * 16 + (unsigned)(j * 64 + lane) / T::UN;
                 pu4_t u = __builtin_bit_cast(pu4_t, frag_read(at));
                 if (!(here >> r & 1)) {
                     u = pu4_t{0, 0, 0, 0};
@@ -849,11 +853,11 @@ __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> 
                 odd |= not_finite(u);
             }
             const bool any = __any(odd & 0x80008000u);
-            if (lane == 0) sm.dirty[side][wave] = any;
+            if (has_v && lane == 0) sm.dirty[side][part] = any;
         }
         lds_tile_barrier();
-        if (t + 2 < t_end) load(pages.k, after, buf);
-        if (t + 1 < t_end) load(pages.v, next, V_OFF + other);
+        if (has_k && t + 2 < t_end) load(pages.k, after, buf);
+        if (has_v && t + 1 < t_end) load(pages.v, next, V_OFF + other);
         // element i of x[kb] is of the wavefront's key 32 kb + 8 (i / 4) + 4 half + i % 4; base-2 logits relative to m from here
         float mz = finite_or_zero(m);
         f32x16_t y[NB];
@@ -939,8 +943,8 @@ __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> 
                 }
                 lds_tile_barrier();
 #pragma unroll 1
-                for (int j = 0; j < PL; ++j) {
-                    const unsigned at = lds + buf + V_OFF + wave * T::PART + j * 1024 + lane * 16;
+                for (int j = has_v ? 0 : PL; j < PL; ++j) {
+                    const unsigned at = lds + buf + V_OFF + part * T::PART + j * 1024 + lane * 16;
                     *(__attribute__((address_space(3))) pu4_t *)(size_t)at = not_finite_or_rest(__builtin_bit_cast(pu4_t, frag_read(at)), false);
                 }
                 lds_tile_barrier();
@@ -1018,12 +1022,12 @@ __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> 
     }
 }
 
-template <int DH, int NT, int KS>
-__global__ __launch_bounds__(P_THREADS, 2) void paged_wide_kernel(PagedAttend a)
+template <int DH, int NT, int KS, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void paged_wide_kernel(PagedAttend a)
 {
     __shared__ PagedWideSmem<DH> sm;
     run_parts(a, [&](const PartSeq &sq, int b, int hd, int rb, int ta, int tb, int slot) {
-        paged_wide_block<DH, NT, KS>(a, sm, sq, b, hd, rb, ta, tb, slot);
+        paged_wide_block<DH, NT, KS, NW>(a, sm, sq, b, hd, rb, ta, tb, slot);
     });
 }
 
@@ -1149,9 +1153,43 @@ void paged_dispatch(const wnw_paged_config &c, F f)
     c.head_dim == 64 ? f(std::integral_constant<int, 64>{}) : f(std::integral_constant<int, 128>{});
 }
 
+// Times in us that decide how work is shared, measured on even batches: a whole block's start; a tile of a block that has a compute
+// unit to itself (`own`), and of one when the chip is full, as a compute unit's time (`full`); what shares cost a call beside their tiles
+// (the search, the parts' results, the join and its launch).
+struct PagedPrice {
+    double start, own, full, join;
+};
+PagedPrice paged_price(int RB, int head_dim, bool bf16, bool stream)
+{
+    const bool d64 = head_dim == 64;
+    if (RB >= 128) return bf16 ? (d64 ? PagedPrice{8, 0.89, 0.62, 17} : PagedPrice{13, 1.48, 1.03, 25})
+                                  : (d64 ? PagedPrice{8, 1.36, 1.05, 18} : PagedPrice{15, 2.8, 2.02, 28});
+    if (RB == 64) return bf16 ? (d64 ? PagedPrice{7, 0.54, 0.80, 13} : PagedPrice{11, stream ? 1.0 : 0.78, 1.45, 18})
+                                      : (d64 ? PagedPrice{7, 0.72, 0.85, 13} : PagedPrice{12, 1.1, 1.50, 18});
+    if (RB == 32) return d64 ? PagedPrice{6, stream ? 0.38 : 0.25, 0.66, 11} : PagedPrice{7, stream ? 0.35 : 0.25, 0.68, 14};
+    return d64 ? PagedPrice{5.5, stream ? 0.37 : 0.19, 0.62, 9} : PagedPrice{5, stream ? 0.34 : 0.165, 0.607, 11};
+}
+
+// Whether every block of rows gets a work-group of its own rather than the batch's tiles being cut into even parts that a second launch
+// joins.  Measured whole and cut, a block's rows of the cache and what they took: one token, d = 128: 8 blocks of 1064 11.5 and
+// 11.4, of 4000 25.5 and 13.2; 72 of 4000 29.2 and 30.6, of 15512 154 and 92; 128 of 1064 16 and 22, of 15512 174 and 157; 240 of 15512
+// 276 and 294; d = 64: 72 of 1064 9.3 and 12.8, of 15512 81 and 50; 240 of 15512 141 and 152; five tokens of four heads: 8 of 1064 16.8
+// and 15, 72 of 4000 44 and 38, 240 of 15512 299 and 341; blocks of 64 rows: 64 of 2000 38 and 34, 240 of 15512 339 and 372; of 128: 128 of 600 29
+// and 40, of 2000 61 and 49, 256 of 2000 65 and 72, of 15512 362 and 274, 512 of 15512 502 and 531; fp32: 256 of 15512 686 and 524.
+// Of a batch only the longest length is known here.  Whole blocks wait for the longest sequence's, which parts share out among all, so
+// parts of several sequences are priced as if half of the rows were there.
+bool paged_whole(const PagedPrice &c, int RB, int64_t blocks, int64_t tiles, int batch)
+{
+    const double b = blocks / 256.0, t = (double)tiles;
+    // (the wide kernels' work-groups are there in twos)
+    const double whole = c.start + t * std::max(c.own, RB > 32 && b > 1 ? c.full * 2 * (double)((blocks + 511) / 512) : c.full * b);
+    const double cut = c.join + std::max(c.own * MIN_PIECE, c.full * t * b * (batch > 1 ? 0.5 : 1.0));
+    return whole <= cut;
+}
+
 // How an attention call runs.
 struct PagedPlan {
-    int RB, W, tsh;
+    int RB, W, tsh;     // RB 16, 32, 64 or 128
     bool whole, eight, stream, join_groups;
     int64_t rows, o_bytes, ml_bytes;
     int64_t total() const { return o_bytes + ml_bytes; }
@@ -1161,14 +1199,18 @@ PagedPlan paged_plan(const wnw_paged_config &c, int32_t n_layers, int32_t q_head
     const int64_t cap = (int64_t)c.table_width * c.page, heads = (int64_t)c.batch * n_layers * c.kv_heads, R = (int64_t)q_heads / c.kv_heads * n;
     const int64_t len = max_len ? std::min<int64_t>(max_len, cap) : cap;
     PagedPlan p;
-    p.RB = R > 64 ? WIDE_P : R > 32 ? WIDE_P / 2 : R > 16 ? 32 : 16;
+    p.RB = R > 128 ? 256 : R > 64 ? 128 : R > 32 ? 64 : R > 16 ? 32 : 16;
     p.tsh = c.head_dim == 64 || p.RB > 32 ? 6 : 5;
     const int64_t blocks = heads * ((R + p.RB - 1) / p.RB), per = (len + (1 << p.tsh) - 1) >> p.tsh, tiles = per * blocks;
+    // bytes that one pass reads once and the 256 MB of the last-level cache cannot keep for the next one go past the caches
     p.stream = R <= p.RB && heads * len * c.head_dim * 4 > (256ll << 20);
-    p.whole = blocks >= 512;
-    p.eight = false;
-    p.W = (int)std::max<int64_t>(1, p.whole ? blocks : std::min<int64_t>(512, tiles / MIN_PIECE + blocks));
+    p.whole = paged_whole(paged_price(p.RB, c.head_dim, c.flags & WNW_F_OUT_BF16, p.stream), p.RB, blocks, per, c.batch);
+    // Eight wavefronts instead of four for whole blocks that have a compute unit each (one token, 72 blocks of 4000 rows 41 -> 29 us; two blocks
+    // of 16 rows take turns on the vector unit, so that 240 of 15512 rows take 299 with four and 316 with eight).
+    p.eight = p.whole && p.RB <= 32 && blocks <= (p.RB == 16 ? 256 : 128) && len > 256;
+    p.W = (int)std::max<int64_t>(1, p.whole ? blocks : std::min<int64_t>(p.RB == 256 ? 256 : 512, tiles / MIN_PIECE + blocks));
     p.rows = heads * R;
+    // sixteen threads for each of a few rows' pieces, a thread group a row where there are many
     p.join_groups = p.rows <= 8192;
     p.o_bytes = p.whole ? 0 : (int64_t)p.W * 2 * p.RB * c.head_dim * 4;
     p.ml_bytes = p.whole ? 0 : (int64_t)p.W * 2 * p.RB * 8;
@@ -1186,8 +1228,8 @@ void launch_tokens(const PagedPlan &p, const PagedAttend &a, hipStream_t st)
 template <int DH, int NT>
 void launch_wide(const PagedPlan &p, const PagedAttend &a, hipStream_t st)
 {
-    auto *k = p.RB == WIDE_P ? paged_wide_kernel<DH, NT, 1> : paged_wide_kernel<DH, NT, 2>;
-    hipLaunchKernelGGL(k, dim3(p.W), dim3(P_THREADS), 0, st, a);
+    auto *k = p.RB == 256 ? paged_wide_kernel<DH, NT, 1, 8> : p.RB == 128 ? paged_wide_kernel<DH, NT, 1, 4> : paged_wide_kernel<DH, NT, 2, 4>;
+    hipLaunchKernelGGL(k, dim3(p.W), dim3(p.RB == 256 ? 512 : 256), 0, st, a);
 }
 
 wnw_status paged_heads(const wnw_paged_config &c, int32_t n_layers, int32_t q_heads, int32_t n, int32_t max_len)
