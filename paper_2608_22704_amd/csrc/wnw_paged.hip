@@ -75,7 +75,7 @@ enum { TURN_NONE, TURN_PAIRS, TURN_HALVES, TURN_HALVES_ODD };
 template <int DH, int TURN>
 __global__ __launch_bounds__(P_THREADS) void paged_append_kernel(PagedAppend a, int TT)
 {
-    constexpr int UN = DH / 8, SLOTS = P_THREADS / UN;
+    constexpr int UN = DH / 8, SLOTS = P_THREADS / UN, UNROLL = TURN == TURN_HALVES_ODD ? 1 : 4;
     const PagedGeo &g = a.g;
     const int HH = SLOTS / TT, tid = threadIdx.x, u = tid % UN, slot = tid / UN, lane = tid & 63;
     int item = blockIdx.x;
@@ -117,64 +117,75 @@ __global__ __launch_bounds__(P_THREADS) void paged_append_kernel(PagedAppend a, 
             }
         }
     }
-    for (int v = part * HH + slot / TT; v < a.vectors; v += a.split * HH) {
-        const int kv = a.kn ? 2 * g.H : 0;
-        const bool is_v = v >= g.H && v < kv, is_q = v >= kv;
-        const int h = is_q ? v - kv : is_v ? v - g.H : v;
-        const uint16_t *src = is_q ? a.q : is_v ? a.vn : a.kn;
-        uint16_t *dst;
-        bool put = live;
-        if (is_q)
-            dst = a.q_out + ((((size_t)b * g.nl + l) * a.Hq + h) * a.n + i) * DH;
-        else {
-            put = place;
-            dst = (is_v ? g.v : g.k) + (g.page_row(place ? id : 0, l, h) + (row & ((1 << g.psh) - 1))) * DH;
+    // vectors of K, V and q in turn, UNROLL at a time, so that as many loads are under way
+    const int kv = a.kn ? 2 * g.H : 0, step = a.split * HH;
+    const size_t in_page = row & ((1 << g.psh) - 1), first = ((size_t)b * g.nl + l);
+    auto from = [&](int v) {
+        const bool is_q = v >= kv;
+        const int h = is_q ? v - kv : v >= g.H ? v - g.H : v;
+        return (is_q ? a.q : v >= g.H ? a.vn : a.kn) + ((first * (is_q ? a.Hq : g.H) + h) * a.n + i) * DH + u * 8;
+    };
+    auto to = [&](int v) {
+        if (v >= kv) return a.q_out + ((first * a.Hq + (v - kv)) * a.n + i) * DH + u * 8;
+        return (v >= g.H ? g.v : g.k) + (g.page_row(id, l, v >= g.H ? v - g.H : v) + in_page) * DH + u * 8;
+    };
+    for (int v0 = part * HH + slot / TT; v0 < a.vectors; v0 += UNROLL * step) {
+        pu4_t xs[UNROLL];
+#pragma unroll
+        for (int k = 0; k < UNROLL; ++k) {
+            const int v = v0 + k * step;
+            xs[k] = pu4_t{0, 0, 0, 0};
+            if (v < a.vectors && (v >= kv ? live : place)) xs[k] = __builtin_nontemporal_load((const pu4_t *)from(v));
         }
-        pu4_t x = {0, 0, 0, 0};
-        if (put) x = *(const pu4_t *)(src + ((((size_t)b * g.nl + l) * (is_q ? a.Hq : g.H) + h) * a.n + i) * DH + u * 8);
-        if constexpr (TURN != TURN_NONE) {
-            pu4_t o = x;     // partners
-            if constexpr (TURN == TURN_PAIRS) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = x[e] << 16 | x[e] >> 16;
-            } else if constexpr (TURN == TURN_HALVES) {
-                const int hu = half >> 3, other = u < hu ? u + hu : u < 2 * hu ? u - hu : u;
+        for (int k = 0; k < UNROLL; ++k) {
+            const int v = v0 + k * step;
+            pu4_t x = xs[k];
+            const bool is_v = v >= g.H && v < kv;
+            if constexpr (TURN != TURN_NONE) {
+                pu4_t o = x;     // partners
+                if constexpr (TURN == TURN_PAIRS) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = (unsigned)__shfl((int)x[e], lane - u + other);
-            } else {
-                const int up = half & 7, down = 8 - up;      // half = 8 hu + up
-                uint16_t y[8];
+                    for (int e = 0; e < 4; ++e) o[e] = x[e] << 16 | x[e] >> 16;
+                } else if constexpr (TURN == TURN_HALVES) {
+                    const int hu = half >> 3, other = u < hu ? u + hu : u < 2 * hu ? u - hu : u;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    // from u + hu (+ 1) or from u - hu (- 1); the words to send are the same for all lanes
-                    const int e0 = (e + up) & 7, e1 = (e + down) & 7, hu = half >> 3;
-                    unsigned w0 = x[0], w1 = x[0];
+                    for (int e = 0; e < 4; ++e) o[e] = (unsigned)__shfl((int)x[e], lane - u + other);
+                } else {
+                    const int up = half & 7, down = 8 - up, hu = half >> 3;      // half = 8 hu + up
+                    uint16_t y[8];
 #pragma unroll
-                    for (int k = 1; k < 4; ++k) {
-                        w0 = e0 >> 1 == k ? x[k] : w0;
-                        w1 = e1 >> 1 == k ? x[k] : w1;
+                    for (int e = 0; e < 8; ++e) {
+                        // from u + hu (+ 1) or from u - hu (- 1); the words to send are the same for all lanes
+                        const int e0 = (e + up) & 7, e1 = (e + down) & 7;
+                        unsigned w0 = x[0], w1 = x[0];
+#pragma unroll
+                        for (int j = 1; j < 4; ++j) {
+                            w0 = e0 >> 1 == j ? x[j] : w0;
+                            w1 = e1 >> 1 == j ? x[j] : w1;
+                        }
+                        const int l0 = u + hu + (e + up >= 8), l1 = u - hu - (e < up);
+                        const unsigned g0 = (unsigned)__shfl((int)w0, lane - u + min(max(l0, 0), UN - 1)),
+                                       g1 = (unsigned)__shfl((int)w1, lane - u + min(max(l1, 0), UN - 1));
+                        const bool low = u * 8 + e < half;
+                        const unsigned w = low ? g0 : g1;
+                        y[e] = (uint16_t)((low ? e0 : e1) & 1 ? w >> 16 : w);
                     }
-                    const int l0 = u + hu + (e + up >= 8), l1 = u - hu - (e < up);
-                    const unsigned g0 = (unsigned)__shfl((int)w0, lane - u + min(max(l0, 0), UN - 1)),
-                                   g1 = (unsigned)__shfl((int)w1, lane - u + min(max(l1, 0), UN - 1));
-                    const bool first = u * 8 + e < half;
-                    const unsigned w = first ? g0 : g1;
-                    y[e] = (uint16_t)((first ? e0 : e1) & 1 ? w >> 16 : w);
+                    __builtin_memcpy(&o, y, sizeof(o));
                 }
-                __builtin_memcpy(&o, y, sizeof(o));
-            }
-            if (!is_v) {
+                if (!is_v) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float y0 = fmaf(bf16_at(o, 2 * e), sn[2 * e], bf16_at(x, 2 * e) * cs[2 * e]),
-                                y1 = fmaf(bf16_at(o, 2 * e + 1), sn[2 * e + 1], bf16_at(x, 2 * e + 1) * cs[2 * e + 1]);
-                    const unsigned r0 = u * 8 + 2 * e < a.dim ? to_bf16(y0) : x[e] & 0xffffu,
-                                   r1 = u * 8 + 2 * e + 1 < a.dim ? to_bf16(y1) : x[e] >> 16;
-                    x[e] = r0 | r1 << 16;
+                    for (int e = 0; e < 4; ++e) {
+                        const float y0 = fmaf(bf16_at(o, 2 * e), sn[2 * e], bf16_at(x, 2 * e) * cs[2 * e]),
+                                    y1 = fmaf(bf16_at(o, 2 * e + 1), sn[2 * e + 1], bf16_at(x, 2 * e + 1) * cs[2 * e + 1]);
+                        const unsigned r0 = u * 8 + 2 * e < a.dim ? to_bf16(y0) : x[e] & 0xffffu,
+                                       r1 = u * 8 + 2 * e + 1 < a.dim ? to_bf16(y1) : x[e] >> 16;
+                        x[e] = r0 | r1 << 16;
+                    }
                 }
             }
+            if (v < a.vectors && (v >= kv ? live : place)) __builtin_nontemporal_store(x, (pu4_t *)to(v));
         }
-        if (put) *(pu4_t *)(dst + u * 8) = x;
     }
 }
 
