@@ -667,7 +667,7 @@ wnw_status wnw_draft_tree(int32_t batch, int32_t n, const int32_t *parent_dev, c
  *   path_dev      device int32 [B][n], written: the tokens that stand, ascending, then -1; may be NULL with n = 0
  *   accepted_dev  device int32 [B], written: how many stand
  *   next_dev      device int32 [B], written: the token after them
- *   workspace     as wnw_paged_attend's; wnw_draft_verify_workspace gives its size */
+ *   workspace     as wnw_paged_attend's; wnw_draft_verify_workspace gives its size (0 for small vocabularies) */
 wnw_status wnw_draft_verify(int32_t batch, int32_t n, int32_t vocab, const int32_t *token_dev, const int32_t *parent_dev,
                             const int32_t *count_dev, const float *target_dev, const float *draft_dev,
                             const float *uniform_dev, int32_t *path_dev, int32_t *accepted_dev, int32_t *next_dev,

@@ -1,6 +1,7 @@
 // Drafted decoding apart from its cache: the tree of a draft, and which of its tokens stand.  Definitions as in wnw.h.
 //
 //   draft_tree_kernel    ancestors' bits and positions by doubling paths
+//   draft_round_kernel   a sum over the vocabulary that the tokens' verification needs, by slices
 //   draft_verify_kernel  the tokens that stand and the one after them, a work-group per sequence
 #include "wnw.h"
 #include "wnw_parts.h"
@@ -59,17 +60,35 @@ __global__ __launch_bounds__(DRAFT_MAX) void draft_tree_kernel(int n, const int3
 // tokens is max(p - t_k q, 0) / s_k, since max(max(x, 0) - q, 0) = max(x - q, 0) for q >= 0.  So a refused token costs one sum over
 // the vocabulary, and only where another one is tried after it.
 //
-// A work-group has a sequence: the drafted tokens' probabilities come first, all at once; then all of its wavefronts take the same
-// steps along the path, and the sums by slices of the vocabulary; at the end the slices' sums name the slice that the last
-// uniform number falls into, and a scan of that one the token.
-constexpr int VERIFY_THREADS = 1024;
-constexpr int MAX_SLICES = 2048;
+// A sum over the vocabulary is one compute unit's work for 9 us (131072 tokens) where a work-group has a sequence, so for large
+// vocabularies and few sequences some launches go in front (draft_round_kernel) in which every sequence has a work-group for each
+// slice of the vocabulary: all of them walk to the next sum that is needed and leave their slice's part of it.  Rounds that a sequence
+// does not need end at once; sums that no round was there for are taken by its one work-group at the end (draft_verify_kernel), which also
+// finds the token after the path: the slices' sums name the slice that the last uniform number falls into, and a scan of that one the token.
+constexpr int ROUND_THREADS = 256, VERIFY_THREADS = 1024;
+constexpr int MAX_SLICES = 2048, ROUND_SLICES = 64;
+
+// How far a sequence is along its path.
+struct DraftState {
+    double t, s;       // of the row behind `at`; s is the sum for t if `known`
+    int at, stand;     // the last token that stands (-1: none), how many do
+    int i, known;      // tokens before i have been tried
+    int phase;         // what the sums that come next are for
+    int sums;          // the round that has them
+};
+enum { NEED_SUM, NEED_TOTAL, HAVE_TOTAL };
 
 struct Draft {
-    int n, V, slice;     // slice: tokens of a partial sum, a multiple of 1024
+    int n, V, slice, slices;     // slice: tokens of a partial sum, a multiple of 1024
+    int rounds;
     const int32_t *token, *parent, *count;
     const float *target, *draft, *uniform;
     int32_t *path, *accepted, *next;
+    DraftState *state;           // [2][B], by turns
+    double *sums;                // [B][rounds][slices]
+    float2 *pq;                  // [B][n] the tokens' probabilities, and what they follow and are, from the first round for later ones
+    int2 *link;
+    __device__ double *sums_of(int b, int round) const { return sums + ((size_t)b * rounds + round) * slices; }
 };
 
 __device__ inline double wave_sumd(double x)
@@ -87,16 +106,6 @@ __device__ inline double wave_scand(double x, int lane)
     }
     return x;
 }
-
-struct VerifySmem {
-    double sums[MAX_SLICES];
-    double part[VERIFY_THREADS / 64];
-    unsigned marked[MAX_SLICES / 32];       // slices with a refused token
-    float p[DRAFT_MAX], q[DRAFT_MAX], u[DRAFT_MAX];
-    int from[DRAFT_MAX], token[DRAFT_MAX];
-    int refused;                            // tokens refused at the last row, then in `token`
-    int got;
-};
 
 typedef float df4_t __attribute__((ext_vector_type(4)));
 
@@ -125,114 +134,228 @@ __device__ inline double left_sum(const float *p, const float *q, double t, int 
     return x;
 }
 
+// A sequence's drafted tokens, with their probabilities behind their parents.
+struct DraftTokens {
+    float p[DRAFT_MAX], q[DRAFT_MAX], u[DRAFT_MAX];
+    int from[DRAFT_MAX], token[DRAFT_MAX];
+    int refused;                            // tokens refused at the last row, then in `token`
+
+    // again: a round has been here
+    __device__ void load(const Draft &d, int b, int cnt, int threads, bool again, bool keep)
+    {
+        const int n = d.n, V = d.V;
+        if (again) {
+            for (int i = threadIdx.x; i < cnt; i += threads) {
+                const float2 x = d.pq[(size_t)b * n + i];
+                const int2 y = d.link[(size_t)b * n + i];
+                p[i] = x.x, q[i] = x.y, from[i] = y.x, token[i] = y.y, u[i] = d.uniform[(size_t)b * (n + 1) + i];
+            }
+            if (threadIdx.x == 0) refused = 0;
+            __syncthreads();
+            return;
+        }
+        const float *target = d.target + (size_t)b * (n + 1) * V, *draft = d.draft ? d.draft + (size_t)b * (n + 1) * V : nullptr;
+        for (int i = threadIdx.x; i < cnt; i += threads) {
+            const int x = d.token[(size_t)b * n + i];
+            int f = d.parent ? d.parent[(size_t)b * n + i] : i - 1;
+            if (f < 0 || f >= i) f = -1;
+            float pp = 0.f, qq = 0.f;
+            if (x >= 0 && x < V) {
+                const size_t at = (size_t)(f + 1) * V + x;
+                pp = target[at];
+                qq = draft ? draft[at] : 1.f;
+            }
+            p[i] = pp, q[i] = qq, u[i] = d.uniform[(size_t)b * (n + 1) + i], from[i] = f, token[i] = x;
+            if (keep) d.pq[(size_t)b * n + i] = make_float2(pp, qq), d.link[(size_t)b * n + i] = make_int2(f, x);
+        }
+        if (threadIdx.x == 0) refused = 0;
+        __syncthreads();
+    }
+    // On to the next sum that is needed; every wavefront takes the same steps.  path: where the tokens that stand go (one work-group's), or null.
+    __device__ void walk(const Draft &d, DraftState &st, int cnt, int32_t *path)
+    {
+        const int tid = threadIdx.x, lane = tid & 63;
+        for (int i0 = st.i & ~63; i0 < cnt; i0 += 64) {
+            unsigned long long later = st.i > i0 ? ~0ull << (st.i & 63) : ~0ull;
+            for (;;) {
+                // the next token that follows `at`
+                const unsigned long long follow = __ballot(i0 + lane < cnt && from[min(i0 + lane, cnt - 1)] == st.at) & later;
+                if (!follow) break;
+                const int j = __builtin_ctzll(follow), i = i0 + j;
+                later = j == 63 ? 0ull : ~0ull << (j + 1);
+                if (!st.known) {
+                    st.i = i, st.phase = NEED_SUM;
+                    return;
+                }
+                const double pp = (double)p[i], qq = (double)q[i], uu = (double)u[i];
+                if (d.draft ? uu * qq * st.s < fmax(st.t == 0.0 ? pp : pp - st.t * qq, 0.0) : uu * st.s < pp) {
+                    if (path && tid == 0) path[st.stand] = i;
+                    ++st.stand;
+                    st.at = i, st.t = 0.0, st.s = 1.0;
+                } else if (d.draft) {
+                    st.t += st.s;
+                    st.known = 0;
+                } else {
+                    // its token again, if another of the same follows, has nothing left
+                    st.s -= fmax(pp, 0.0);
+                    const int x = token[i];
+                    __syncthreads();
+                    for (int k = i + 1 + tid; k < cnt; k += blockDim.x)
+                        if (from[k] == st.at && token[k] == x) p[k] = 0.f;
+                    __syncthreads();
+                }
+            }
+        }
+        st.i = cnt, st.phase = NEED_TOTAL;
+    }
+    // The tokens refused at the last row that lie in v0 .. v1 - 1 to the front of `token` (in any order: they are only looked up).
+    __device__ void collect(int cnt, int at, int v0, int v1, int threads)
+    {
+        for (int i0 = 0; i0 < cnt; i0 += threads) {
+            const int i = i0 + threadIdx.x, x = i < cnt ? token[i] : -1;
+            const bool is = i < cnt && from[i] == at && x >= v0 && x < v1;
+            __syncthreads();
+            if (is) token[atomicAdd(&refused, 1)] = x;      // (entries below i0 + threads only, all of them read)
+        }
+        __syncthreads();
+    }
+    __device__ bool has_refused(int v) const
+    {
+        for (int k = 0; k < refused; ++k)
+            if (token[k] == v) return true;
+        return false;
+    }
+};
+
+// A round: the part that slice blockIdx.x of the vocabulary has in the next sum of sequence blockIdx.y.
+template <bool VEC>
+__global__ __launch_bounds__(ROUND_THREADS) void draft_round_kernel(Draft d, int round)
+{
+    __shared__ DraftTokens tokens;
+    __shared__ double part[ROUND_THREADS / 64];
+    const int g = blockIdx.x, b = blockIdx.y, B = gridDim.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int cnt = d.count ? clamp_to(d.count[b], d.n) : d.n;
+    DraftState st = {0.0, 1.0, -1, 0, 0, 1, NEED_SUM, 0};
+    if (round) {
+        st = d.state[(size_t)(round - 1 & 1) * B + b];
+        if (st.phase == NEED_TOTAL) st.phase = HAVE_TOTAL;
+        if (st.phase == HAVE_TOTAL) {
+            if (g == 0 && tid == 0) d.state[(size_t)(round & 1) * B + b] = st;
+            return;
+        }
+        st.s = wave_sumd(lane < d.slices ? d.sums_of(b, round - 1)[lane] : 0.0);
+        st.known = 1;
+    }
+    tokens.load(d, b, cnt, ROUND_THREADS, round > 0, round == 0 && g == 0);
+    int32_t *path = d.path + (size_t)b * d.n;
+    if (!round && g == 0) {
+        for (int i = tid; i < d.n; i += ROUND_THREADS) path[i] = -1;
+        __syncthreads();
+    }
+    tokens.walk(d, st, cnt, g == 0 ? path : nullptr);
+    st.sums = round;
+    if (g == 0 && tid == 0) d.state[(size_t)(round & 1) * B + b] = st;
+
+    const size_t row = ((size_t)b * (d.n + 1) + st.at + 1) * d.V;
+    const float *p = d.target + row, *q = d.draft && st.t > 0.0 ? d.draft + row : nullptr;
+    const int v0 = g * d.slice, v1 = min(d.V, v0 + d.slice);
+    double x = 0.0;
+    if (!d.draft) tokens.collect(cnt, st.at, v0, v1, ROUND_THREADS);
+    if (tokens.refused) {
+        for (int v = v0 + tid; v < v1; v += ROUND_THREADS) x += tokens.has_refused(v) ? 0.0 : fmax((double)p[v], 0.0);
+    } else if (q)
+        x = left_sum<true, VEC>(p, q, st.t, v0, v1, tid, ROUND_THREADS);
+    else
+        x = left_sum<false, VEC>(p, nullptr, 0.0, v0, v1, tid, ROUND_THREADS);
+    x = wave_sumd(x);
+    if (lane == 0) part[wave] = x;
+    __syncthreads();
+    if (tid == 0) d.sums_of(b, round)[g] = (part[0] + part[1]) + (part[2] + part[3]);
+}
+
+struct VerifySmem {
+    DraftTokens tokens;
+    double sums[MAX_SLICES];
+    double part[VERIFY_THREADS / 64];
+    unsigned marked[MAX_SLICES / 32];       // slices with a refused token
+    int first[VERIFY_THREADS / 64], last[VERIFY_THREADS / 64], got, found;
+};
+
 template <bool VEC>
 __global__ __launch_bounds__(VERIFY_THREADS) void draft_verify_kernel(Draft d)
 {
     __shared__ VerifySmem sm;
     constexpr int WAVES = VERIFY_THREADS / 64;
-    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = d.n, V = d.V;
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = d.n, V = d.V, slice = d.slice, slices = d.slices;
     const int cnt = d.count ? clamp_to(d.count[b], n) : n;
-    const float *target = d.target + (size_t)b * (n + 1) * V, *draft = d.draft ? d.draft + (size_t)b * (n + 1) * V : nullptr;
     const float *uniform = d.uniform + (size_t)b * (n + 1);
-    if (tid < n) {
-        float p = 0.f, q = 0.f;
-        int f = -2, x = -1;
-        if (tid < cnt) {
-            x = d.token[(size_t)b * n + tid];
-            f = d.parent ? d.parent[(size_t)b * n + tid] : tid - 1;
-            if (f < 0 || f >= tid) f = -1;
-            if (x >= 0 && x < V) {
-                const size_t at = (size_t)(f + 1) * V + x;
-                p = target[at];
-                q = draft ? draft[at] : 1.f;
-            }
-        }
-        sm.p[tid] = p, sm.q[tid] = q, sm.u[tid] = uniform[tid], sm.from[tid] = f, sm.token[tid] = x;
-        d.path[(size_t)b * n + tid] = -1;
+    int32_t *path = d.path + (size_t)b * n;
+    DraftState st = {0.0, 1.0, -1, 0, 0, 1, NEED_SUM, 0};
+    if (d.rounds) {
+        st = d.state[(size_t)(d.rounds - 1 & 1) * gridDim.x + b];
+        if (st.phase == NEED_TOTAL) st.phase = HAVE_TOTAL;
+        for (int k = tid; k < slices; k += VERIFY_THREADS) sm.sums[k] = d.sums_of(b, st.sums)[k];
     }
+    sm.tokens.load(d, b, cnt, VERIFY_THREADS, d.rounds > 0, false);
     if (tid < MAX_SLICES / 32) sm.marked[tid] = 0;
-    if (tid == 0) sm.refused = 0, sm.got = -1;
+    if (tid == 0) sm.got = -1, sm.found = 0;
+    if (!d.rounds && tid < n) path[tid] = -1;
     __syncthreads();
-
-    // the path
-    int at = -1, stand = 0;
-    double t = 0.0, s = 1.0;
-    bool known = true;      // s is the sum for t
-    for (int i0 = 0; i0 < cnt; i0 += 64) {
-        unsigned long long later = ~0ull;
+    if (st.phase == NEED_SUM) {
+        if (d.rounds) {
+            st.s = wave_sumd(lane < slices ? sm.sums[lane] : 0.0);
+            st.known = 1;
+            __syncthreads();
+        }
         for (;;) {
-            const unsigned long long follow = __ballot(i0 + lane < cnt && sm.from[min(i0 + lane, cnt - 1)] == at) & later;
-            if (!follow) break;
-            const int j = __builtin_ctzll(follow), i = i0 + j;
-            later = j == 63 ? 0ull : ~0ull << (j + 1);
-            if (!known) {
-                const double x = wave_sumd(left_sum<true, VEC>(target + (size_t)(at + 1) * V, draft + (size_t)(at + 1) * V, t, 0, V, tid, VERIFY_THREADS));
-                __syncthreads();
-                if (lane == 0) sm.part[wave] = x;
-                __syncthreads();
-                s = 0.0;
+            sm.tokens.walk(d, st, cnt, path);
+            if (st.phase == NEED_TOTAL) break;
+            const size_t row = ((size_t)b * (n + 1) + st.at + 1) * V;
+            const double x = wave_sumd(left_sum<true, VEC>(d.target + row, d.draft + row, st.t, 0, V, tid, VERIFY_THREADS));
+            if (lane == 0) sm.part[wave] = x;
+            __syncthreads();
+            st.s = 0.0;
 #pragma unroll
-                for (int w = 0; w < WAVES; ++w) s += sm.part[w];
-                known = true;
-            }
-            const double p = (double)sm.p[i], q = (double)sm.q[i], u = (double)sm.u[i];
-            if (draft ? u * q * s < fmax(t == 0.0 ? p : p - t * q, 0.0) : u * s < p) {
-                if (tid == 0) d.path[(size_t)b * n + stand] = i;
-                ++stand;
-                at = i, t = 0.0, s = 1.0;
-            } else if (draft) {
-                t += s;
-                known = false;
-            } else {
-                // its token again, if another of the same follows, has nothing left
-                s -= fmax(p, 0.0);
-                const int x = sm.token[i];
-                __syncthreads();
-                if (tid > i && tid < cnt && sm.from[tid] == at && sm.token[tid] == x) sm.p[tid] = 0.f;
-                __syncthreads();
-            }
+            for (int w = 0; w < WAVES; ++w) st.s += sm.part[w];
+            st.known = 1;
+            __syncthreads();
         }
     }
-    if (tid == 0) d.accepted[b] = stand;
+    if (tid == 0) d.accepted[b] = st.stand;
 
-    // the token after it
-    const float *p = target + (size_t)(at + 1) * V, *q = draft && t > 0.0 ? draft + (size_t)(at + 1) * V : nullptr;
-    const int slice = d.slice, slices = (V + slice - 1) / slice;
-    if (!draft) {
-        const int x = tid < cnt ? sm.token[tid] : -1;
-        const bool refused = tid < cnt && sm.from[tid] == at && x >= 0 && x < V;
-        __syncthreads();
-        if (refused) {
-            sm.token[atomicAdd(&sm.refused, 1)] = x;        // (in any order: they are only looked up)
-            atomicOr(&sm.marked[x / slice >> 5], 1u << (x / slice & 31));
-        }
+    // the token after them
+    const size_t row = ((size_t)b * (n + 1) + st.at + 1) * V;
+    const float *p = d.target + row, *q = d.draft && st.t > 0.0 ? d.draft + row : nullptr;
+    if (!d.draft) {
+        sm.tokens.collect(cnt, st.at, 0, V, VERIFY_THREADS);
+        for (int k = tid; k < sm.tokens.refused; k += VERIFY_THREADS)
+            atomicOr(&sm.marked[sm.tokens.token[k] / slice >> 5], 1u << (sm.tokens.token[k] / slice & 31));
         __syncthreads();
     }
     // of token v; whole: of the row as it is
     auto left = [&](int v, bool whole) {
         const double x = (double)p[v];
         if (whole) return fmax(x, 0.0);
-        if (q) return fmax(x - t * (double)q[v], 0.0);
-        for (int k = 0; k < sm.refused; ++k)
-            if (sm.token[k] == v) return 0.0;
-        return fmax(x, 0.0);
+        if (q) return fmax(x - st.t * (double)q[v], 0.0);
+        return sm.tokens.has_refused(v) ? 0.0 : fmax(x, 0.0);
     };
     bool whole = false;
     double total;
     for (;;) {
-        for (int k = wave; k < slices; k += WAVES) {
-            const int v0 = k * slice, v1 = min(V, v0 + slice);
-            double x;
-            if (!whole && sm.marked[k >> 5] >> (k & 31) & 1) {
-                x = 0.0;
-                for (int v = v0 + lane; v < v1; v += 64) x += left(v, false);
-            } else if (q && !whole)
-                x = left_sum<true, VEC>(p, q, t, v0, v1, lane, 64);
-            else
-                x = left_sum<false, VEC>(p, nullptr, 0.0, v0, v1, lane, 64);
-            x = wave_sumd(x);
-            if (lane == 0) sm.sums[k] = x;
-        }
+        if (st.phase != HAVE_TOTAL || whole)
+            for (int k = wave; k < slices; k += WAVES) {
+                const int v0 = k * slice, v1 = min(V, v0 + slice);
+                double x;
+                if (!whole && sm.marked[k >> 5] >> (k & 31) & 1) {
+                    x = 0.0;
+                    for (int v = v0 + lane; v < v1; v += 64) x += left(v, false);
+                } else if (q && !whole)
+                    x = left_sum<true, VEC>(p, q, st.t, v0, v1, lane, 64);
+                else
+                    x = left_sum<false, VEC>(p, nullptr, 0.0, v0, v1, lane, 64);
+                x = wave_sumd(x);
+                if (lane == 0) sm.sums[k] = x;
+            }
         __syncthreads();
         total = 0.0;
         for (int k = lane; k < slices; k += 64) total += sm.sums[k];
@@ -257,11 +380,10 @@ __global__ __launch_bounds__(VERIFY_THREADS) void draft_verify_kernel(Draft d)
         if (hit) break;
         run = __shfl(sum, 63);
     }
+    // in it, the first token at which it does, or the last one with anything left
     for (int v0 = in * slice; v0 < min(V, (in + 1) * slice); v0 += VERIFY_THREADS) {
         const int v = v0 + tid;
-        const double x = v < V ? left(v, whole) : 0.0;
-        const double sum = wave_scand(x, lane);
-        __syncthreads();
+        const double x = v < V ? left(v, whole) : 0.0, sum = wave_scand(x, lane);
         if (lane == 63) sm.part[wave] = sum;
         __syncthreads();
         double mine = before;
@@ -270,28 +392,22 @@ __global__ __launch_bounds__(VERIFY_THREADS) void draft_verify_kernel(Draft d)
             if (w == wave) mine = before + sum;
             before += sm.part[w];
         }
-        // the first that exceeds the goal, or the last one with anything left
         const unsigned long long some = __ballot(x > 0.0), hit = __ballot(x > 0.0 && mine > goal);
-        __syncthreads();
-        int *mark = (int *)sm.sums;
         if (lane == 0) {
-            mark[wave] = hit ? v0 + wave * 64 + __builtin_ctzll(hit) : -1;
-            mark[WAVES + wave] = some ? v0 + wave * 64 + 63 - __builtin_clzll(some) : -1;
+            sm.first[wave] = hit ? v0 + wave * 64 + __builtin_ctzll(hit) : -1;
+            sm.last[wave] = some ? v0 + wave * 64 + 63 - __builtin_clzll(some) : -1;
         }
         __syncthreads();
         if (tid == 0) {
-            int first = -1, last = -1;
+            int last = -1;
             for (int w = WAVES - 1; w >= 0; --w) {
-                if (mark[w] >= 0) first = mark[w];
-                if (last < 0) last = mark[WAVES + w];
+                if (sm.first[w] >= 0) sm.got = sm.first[w], sm.found = 1;
+                if (last < 0) last = sm.last[w];
             }
-            if (first >= 0)
-                sm.got = first, sm.refused = -1;
-            else if (last >= 0)
-                sm.got = last;
+            if (!sm.found && last >= 0) sm.got = last;
         }
         __syncthreads();
-        if (sm.refused < 0) break;
+        if (sm.found) break;
     }
     if (tid == 0) d.next[b] = sm.got;
 }
@@ -326,9 +442,30 @@ wnw_status verify_sizes(int32_t batch, int32_t n, int32_t vocab)
     if (vocab > (1 << 24)) return draft_fail(WNW_ERR_UNSUPPORTED, "more than 2^24 tokens in the vocabulary");
     return WNW_OK;
 }
-size_t verify_bytes(int32_t batch, int32_t vocab)
+// Launches in front of the last one.  With them a sum costs a launch instead of a compute unit's time for the vocabulary, which grows with
+// it: five tokens in a row, one sequence, TIMES_A; trees, eight sequences, TIMES_B.  A tree may need several sums for
+// its path; the path of a chain, and of tokens that were chosen, the last one only.
+int verify_rounds(int32_t batch, int32_t vocab, bool sums_on_the_way)
 {
-    return (size_t)batch * vocab * 0 + 16;
+    if (vocab < 49152 || batch > 32) return 0;
+    return sums_on_the_way ? 5 : 1;
+}
+struct VerifyPlan {
+    int slice, slices, rounds;
+    size_t state_bytes, sum_bytes, token_bytes, bytes;
+};
+VerifyPlan verify_plan(int32_t batch, int32_t n, int32_t vocab, bool sums_on_the_way)
+{
+    VerifyPlan p;
+    p.rounds = verify_rounds(batch, vocab, sums_on_the_way);
+    const int most = p.rounds ? ROUND_SLICES : MAX_SLICES;
+    p.slice = std::max(1024, (vocab + most * 1024 - 1) / (most * 1024) * 1024);
+    p.slices = (vocab + p.slice - 1) / p.slice;
+    p.state_bytes = p.rounds ? 2 * batch * sizeof(DraftState) : 0;
+    p.sum_bytes = (size_t)batch * p.rounds * p.slices * sizeof(double);
+    p.token_bytes = p.rounds ? (size_t)batch * n * sizeof(float2) : 0;
+    p.bytes = p.state_bytes + p.sum_bytes + 2 * p.token_bytes;
+    return p;
 }
 bool misaligned(const void *p, uintptr_t to)
 {
@@ -368,7 +505,7 @@ wnw_status wnw_draft_verify_workspace(int32_t batch, int32_t n, int32_t vocab, s
     const wnw_status st = verify_sizes(batch, n, vocab);
     if (st != WNW_OK) return st;
     if (!bytes) return draft_fail(WNW_ERR_INVALID, "NULL pointer");
-    *bytes = verify_bytes(batch, vocab);
+    *bytes = verify_plan(batch, n, vocab, true).bytes;
     return WNW_OK;
 }
 
@@ -384,11 +521,17 @@ wnw_status wnw_draft_verify(int32_t batch, int32_t n, int32_t vocab, const int32
     const void *all[] = {token_dev, parent_dev, count_dev, target_dev, draft_dev, uniform_dev, path_dev, accepted_dev, next_dev};
     for (const void *p : all)
         if (misaligned(p, 4)) return draft_fail(WNW_ERR_INVALID, "a pointer is not aligned to its elements");
-    if (!workspace || misaligned(workspace, 16) || workspace_bytes < verify_bytes(batch, vocab))
+    if (const size_t need = verify_plan(batch, n, vocab, true).bytes; need && (!workspace || misaligned(workspace, 16) || workspace_bytes < need))
         return draft_fail(WNW_ERR_INVALID, "workspace missing, too small or not aligned to 16 bytes");
-    const int slice = std::max(1024, (vocab + MAX_SLICES * 1024 - 1) / (MAX_SLICES * 1024) * 1024);
-    const Draft d = {n, vocab, slice, token_dev, parent_dev, count_dev, target_dev, draft_dev, uniform_dev, path_dev, accepted_dev, next_dev};
+    const VerifyPlan p = verify_plan(batch, n, vocab, parent_dev && draft_dev && n > 1);
+    char *ws = (char *)workspace;
+    const Draft d = {n, vocab, p.slice, p.slices, p.rounds, token_dev, parent_dev, count_dev, target_dev, draft_dev, uniform_dev, path_dev, accepted_dev,
+                     next_dev, (DraftState *)workspace, (double *)(ws + p.state_bytes), (float2 *)(ws + p.state_bytes + p.sum_bytes),
+                     (int2 *)(ws + p.state_bytes + p.sum_bytes + p.token_bytes)};
     const bool vec = vocab % 4 == 0 && !misaligned(target_dev, 16) && !misaligned(draft_dev, 16);
+    for (int r = 0; r < p.rounds; ++r)
+        hipLaunchKernelGGL(vec ? draft_round_kernel<true> : draft_round_kernel<false>, dim3((unsigned)p.slices, (unsigned)batch), dim3(ROUND_THREADS), 0,
+                           (hipStream_t)hip_stream, d, r);
     hipLaunchKernelGGL(vec ? draft_verify_kernel<true> : draft_verify_kernel<false>, dim3((unsigned)batch), dim3(VERIFY_THREADS), 0,
                        (hipStream_t)hip_stream, d);
     return draft_hip();

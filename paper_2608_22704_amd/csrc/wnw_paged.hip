@@ -1290,9 +1290,6 @@ wnw_status wnw_paged_append(const wnw_paged_config *cfg, const wnw_paged_cache *
     wnw_status st = paged_config(cfg, first_layer, n_layers, n);
     if (st == WNW_OK) st = paged_cache(cache);
     if (st != WNW_OK) return st;
-    if (!k_dev != !v_dev || !q_dev != !q_out) return paged_fail(WNW_ERR_INVALID, "keys and values, and queries and their place, come together");
-    if (!k_dev && !q_dev) return paged_fail(WNW_ERR_INVALID, "NULL pointer");
-    if (q_dev && (q_heads < 1 || q_heads > (1 << 20))) return paged_fail(WNW_ERR_INVALID, "q_heads must be at least 1");
     if (rotary) {
         if (rotary->dim < 0 || rotary->dim % 2 || rotary->dim > cfg->head_dim) return paged_fail(WNW_ERR_INVALID, "rotary: dim must be even, 0 .. head_dim");
         if (rotary->layout != WNW_ROTARY_HALVES && rotary->layout != WNW_ROTARY_PAIRS) return paged_fail(WNW_ERR_INVALID, "rotary: unknown layout");
@@ -1300,6 +1297,9 @@ wnw_status wnw_paged_append(const wnw_paged_config *cfg, const wnw_paged_cache *
         if (rotary->dim && (!rotary->freq || off4(rotary->freq))) return paged_fail(WNW_ERR_INVALID, "rotary: NULL or misaligned frequencies");
     }
     if (n == 0) return WNW_OK;
+    if (!k_dev != !v_dev || !q_dev != !q_out) return paged_fail(WNW_ERR_INVALID, "keys and values, and queries and their place, come together");
+    if (!k_dev && !q_dev) return paged_fail(WNW_ERR_INVALID, "NULL pointer");
+    if (q_dev && (q_heads < 1 || q_heads > (1 << 20))) return paged_fail(WNW_ERR_INVALID, "q_heads must be at least 1");
     if (!at_dev) return paged_fail(WNW_ERR_INVALID, "NULL pointer");
     if (off16(k_dev) || off16(v_dev) || off16(q_dev) || off16(q_out)) return paged_fail(WNW_ERR_INVALID, "rows must be aligned to 16 bytes");
     if (off4(at_dev) || off4(count_dev) || off4(position_dev)) return paged_fail(WNW_ERR_INVALID, "a pointer is not aligned to its elements");

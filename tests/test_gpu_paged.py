@@ -563,7 +563,7 @@ def probabilities(rng, *shape, sharp=1.3):
     return (x / x.sum(axis=-1, keepdims=True)).astype(np.float32)
 
 
-@pytest.mark.parametrize("V", [1, 2, 7, 100, 1023, 1024, 1025, 5000, 70001])
+@pytest.mark.parametrize("V", [1, 2, 7, 100, 1023, 1024, 1025, 5000, 65536, 70001])
 @pytest.mark.parametrize("n", [0, 1, 5, 40])
 @pytest.mark.parametrize("with_draft", [False, True])
 def test_verification(W, V, n, with_draft):
