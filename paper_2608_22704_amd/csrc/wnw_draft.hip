@@ -442,22 +442,29 @@ wnw_status verify_sizes(int32_t batch, int32_t n, int32_t vocab)
     if (vocab > (1 << 24)) return draft_fail(WNW_ERR_UNSUPPORTED, "more than 2^24 tokens in the vocabulary");
     return WNW_OK;
 }
-// Launches in front of the last one.  With them a sum costs a launch instead of a compute unit's time for the vocabulary, which grows with
-// it: five tokens in a row, one sequence, TIMES_A; trees, eight sequences, TIMES_B.  A tree may need several sums for
-// its path; the path of a chain, and of tokens that were chosen, the last one only.
-int verify_rounds(int32_t batch, int32_t vocab, bool sums_on_the_way)
+// What sums a verification takes: the last row's alone (tokens one after the other), some on the way (a tree whose tokens were drawn),
+// or the last row's without the tokens that were refused (tokens that were chosen).
+enum VerifyKind { VERIFY_CHAIN, VERIFY_TREE, VERIFY_CHOSEN };
+
+// Launches in front of the last one, 4 us each (2 us where a sequence has no more sums).  Measured without them and with: five tokens one
+// after the other, 32000 tokens in the vocabulary, one sequence 10.7 and 10.9 us, 50000 12.2 and 11.0, 131072 18.6 and 13.9, 65536
+// and 32 sequences 15.3 and 16.9; trees of 16, 50000, one sequence 16.6 and (three) 17.3, 131072 32.8 and 21.5, eight sequences 50.7
+// and (five) 32.1, 65536 and 32 sequences 33 and 35; chosen tokens, 16384, one sequence 15.4 and 13.3, 131072, eight 27.7 and 18.1.
+int verify_rounds(int32_t batch, int32_t vocab, VerifyKind kind)
 {
-    if (vocab < 49152 || batch > 32) return 0;
-    return sums_on_the_way ? 5 : 1;
+    if (kind == VERIFY_CHOSEN) return vocab >= 16384 && batch <= 32 ? 1 : 0;
+    if (batch > 16) return 0;
+    if (kind == VERIFY_CHAIN) return vocab >= 49152 ? 1 : 0;
+    return vocab >= 65536 ? (batch > 2 ? 5 : 3) : 0;
 }
 struct VerifyPlan {
     int slice, slices, rounds;
     size_t state_bytes, sum_bytes, token_bytes, bytes;
 };
-VerifyPlan verify_plan(int32_t batch, int32_t n, int32_t vocab, bool sums_on_the_way)
+VerifyPlan verify_plan(int32_t batch, int32_t n, int32_t vocab, VerifyKind kind)
 {
     VerifyPlan p;
-    p.rounds = verify_rounds(batch, vocab, sums_on_the_way);
+    p.rounds = verify_rounds(batch, vocab, kind);
     const int most = p.rounds ? ROUND_SLICES : MAX_SLICES;
     p.slice = std::max(1024, (vocab + most * 1024 - 1) / (most * 1024) * 1024);
     p.slices = (vocab + p.slice - 1) / p.slice;
@@ -466,6 +473,12 @@ VerifyPlan verify_plan(int32_t batch, int32_t n, int32_t vocab, bool sums_on_the
     p.token_bytes = p.rounds ? (size_t)batch * n * sizeof(float2) : 0;
     p.bytes = p.state_bytes + p.sum_bytes + 2 * p.token_bytes;
     return p;
+}
+size_t verify_bytes(int32_t batch, int32_t n, int32_t vocab)
+{
+    size_t most = 0;
+    for (const VerifyKind k : {VERIFY_CHAIN, VERIFY_TREE, VERIFY_CHOSEN}) most = std::max(most, verify_plan(batch, n, vocab, k).bytes);
+    return most;
 }
 bool misaligned(const void *p, uintptr_t to)
 {
@@ -505,7 +518,7 @@ wnw_status wnw_draft_verify_workspace(int32_t batch, int32_t n, int32_t vocab, s
     const wnw_status st = verify_sizes(batch, n, vocab);
     if (st != WNW_OK) return st;
     if (!bytes) return draft_fail(WNW_ERR_INVALID, "NULL pointer");
-    *bytes = verify_plan(batch, n, vocab, true).bytes;
+    *bytes = verify_bytes(batch, n, vocab);
     return WNW_OK;
 }
 
@@ -521,9 +534,9 @@ wnw_status wnw_draft_verify(int32_t batch, int32_t n, int32_t vocab, const int32
     const void *all[] = {token_dev, parent_dev, count_dev, target_dev, draft_dev, uniform_dev, path_dev, accepted_dev, next_dev};
     for (const void *p : all)
         if (misaligned(p, 4)) return draft_fail(WNW_ERR_INVALID, "a pointer is not aligned to its elements");
-    if (const size_t need = verify_plan(batch, n, vocab, true).bytes; need && (!workspace || misaligned(workspace, 16) || workspace_bytes < need))
+    if (const size_t need = verify_bytes(batch, n, vocab); need && (!workspace || misaligned(workspace, 16) || workspace_bytes < need))
         return draft_fail(WNW_ERR_INVALID, "workspace missing, too small or not aligned to 16 bytes");
-    const VerifyPlan p = verify_plan(batch, n, vocab, parent_dev && draft_dev && n > 1);
+    const VerifyPlan p = verify_plan(batch, n, vocab, n <= 1 || (draft_dev && !parent_dev) ? VERIFY_CHAIN : draft_dev ? VERIFY_TREE : VERIFY_CHOSEN);
     char *ws = (char *)workspace;
     const Draft d = {n, vocab, p.slice, p.slices, p.rounds, token_dev, parent_dev, count_dev, target_dev, draft_dev, uniform_dev, path_dev, accepted_dev,
                      next_dev, (DraftState *)workspace, (double *)(ws + p.state_bytes), (float2 *)(ws + p.state_bytes + p.sum_bytes),
