@@ -872,8 +872,10 @@ __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> 
         // element i of x[kb] is of the wavefront's key 32 kb + 8 (i / 4) + 4 half + i % 4; base-2 logits relative to m from here
         float mz = finite_or_zero(m);
         f32x16_t y[NB];
-        __builtin_amdgcn_sched_barrier(0);
-        logits(y, other);
+        if constexpr (!MASKED) {
+            __builtin_amdgcn_sched_barrier(0);
+            logits(y, other);
+        }
         float w[2 * NB][8];        // of 16-row part c: elements 8 (c % 2) .. + 8 of x[c / 2]
 #pragma unroll
         for (int c = 0; c < 2 * NB; ++c)
@@ -934,19 +936,21 @@ __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> 
         if constexpr (MASKED)
             if (sm.dirty[side][0] | sm.dirty[side][1] | sm.dirty[side][2] | sm.dirty[side][3]) {
                 // an element that is not finite makes that of the output NaN for the rows that see it, and is zero for the others
+                pu4_t ones[2 * NB];
+#pragma unroll
+                for (int c = 0; c < 2 * NB; ++c)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const unsigned two = (unsigned)(see >> (16 * c + 8 * (i / 2) + 2 * (i % 2))) & 3u;
+                        ones[c][i] = (two & 1) * 0x3f80u | (two >> 1) * 0x3f800000u;
+                    }
 #pragma unroll
                 for (int dt = 0; dt < ND; ++dt) {
                     f32x16_t found;
 #pragma unroll
                     for (int c = 0; c < 2 * NB; ++c) {
-                        pu4_t ones;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const unsigned two = (unsigned)(see >> (16 * c + 8 * (i / 2) + 2 * (i % 2))) & 3u;
-                            ones[i] = (two & 1) * 0x3f80u | (two >> 1) * 0x3f800000u;
-                        }
                         const f32x16_t zero = {};
-                        found = mfma32(__builtin_bit_cast(bf16x8_t, not_finite_or_rest(v_read(dt, c), true)), __builtin_bit_cast(bf16x8_t, ones),
+                        found = mfma32(__builtin_bit_cast(bf16x8_t, not_finite_or_rest(v_read(dt, c), true)), __builtin_bit_cast(bf16x8_t, ones[c]),
                                        c ? found : zero);
                     }
 #pragma unroll
@@ -971,8 +975,11 @@ __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> 
         now = next;
         next = after;
         after = parts_of(t + 3);
+        if constexpr (MASKED)
+            logits(x, other);       // (here, as registers are short before)
+        else
 #pragma unroll
-        for (int kb = 0; kb < NB; ++kb) x[kb] = y[kb];
+            for (int kb = 0; kb < NB; ++kb) x[kb] = y[kb];
     };
     // tiles that every row sees, in pairs; then the others (all of them from the first page on that is not there)
     int t = ta;
@@ -1008,23 +1015,32 @@ __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> 
             for (int e = 0; e < 4; ++e) o[u / 4][u % 4 * 4 + e] = f0 * o[u / 4][u % 4 * 4 + e] + f1 * y[e];
         }
     }
-    if (qr.token < 0) return;
+    const bool live = qr.token >= 0;
     // element i of o[dt]: dimension 32 dt + 8 (i / 4) + 4 half + i % 4 of row col
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const float inv = slot >= 0 ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
     const size_t at = slot >= 0 ? (size_t)(a.group() * 2 + slot) * RB + rows32 * 32 + col : (size_t)qr.row_of;
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-            float y[4];
+        for (int i = 0; i < 16; i += 8) {
+            float y[8];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = o[dt][i + e] * (slot >= 0 ? 1.f : inv);
-            const size_t to = at * DH + dt * 32 + 2 * i + 4 * half;
-            if (slot >= 0)
-                *(pf4_t *)(a.ws_o + to) = pf4_t{y[0], y[1], y[2], y[3]};
-            else
-                store_out<4>(a.out, a.bf16, to, y);
+            for (int e = 0; e < 8; ++e) y[e] = o[dt][i + e] * inv;
+            const size_t to = at * DH + dt * 32 + 2 * i;
+            if (slot < 0 && a.bf16) {
+                // the halves' four dimensions of eight meet, so that a lane has all of eight
+                unsigned u[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) u[e] = to_bf16(y[2 * e]) | (unsigned)to_bf16(y[2 * e + 1]) << 16;
+                const auto p = __builtin_amdgcn_permlane32_swap(u[0], u[2], false, false), q = __builtin_amdgcn_permlane32_swap(u[1], u[3], false, false);
+                if (live) *(pu4_t *)((uint16_t *)a.out + to + 8 * half) = pu4_t{p[0], q[0], p[1], q[1]};
+            } else if (live) {
+                float *f = (slot < 0 ? (float *)a.out : a.ws_o) + to + 4 * half;
+                *(pf4_t *)f = pf4_t{y[0], y[1], y[2], y[3]};
+                *(pf4_t *)(f + 8) = pf4_t{y[4], y[5], y[6], y[7]};
+            }
         }
+    if (!live) return;
     if (half == 0) {
         if (slot >= 0)
             a.ws_ml[at] = make_float2(m, sum);
@@ -1173,7 +1189,9 @@ struct PagedPrice {
 PagedPrice paged_price(int RB, int head_dim, bool bf16, bool stream)
 {
     const bool d64 = head_dim == 64;
-    if (RB >= 128) return bf16 ? (d64 ? PagedPrice{8, 0.89, 0.62, 17} : PagedPrice{13, 1.48, 1.03, 25})
+    if (RB == 256) return bf16 ? (d64 ? PagedPrice{8.5, 1.13, 1.21, 25} : PagedPrice{14, 1.63, 1.95, 31})
+                               : (d64 ? PagedPrice{9, 1.83, 2.03, 27} : PagedPrice{16, 2.83, 3.35, 42});
+    if (RB == 128) return bf16 ? (d64 ? PagedPrice{8, 0.89, 0.62, 17} : PagedPrice{13, 1.48, 1.03, 25})
                                   : (d64 ? PagedPrice{8, 1.36, 1.05, 18} : PagedPrice{15, 2.8, 2.02, 28});
     if (RB == 64) return bf16 ? (d64 ? PagedPrice{7, 0.54, 0.80, 13} : PagedPrice{11, stream ? 1.0 : 0.78, 1.45, 18})
                                       : (d64 ? PagedPrice{7, 0.72, 0.85, 13} : PagedPrice{12, 1.1, 1.50, 18});
@@ -1186,14 +1204,16 @@ PagedPrice paged_price(int RB, int head_dim, bool bf16, bool stream)
 // 11.4, of 4000 25.5 and 13.2; 72 of 4000 29.2 and 30.6, of 15512 154 and 92; 128 of 1064 16 and 22, of 15512 174 and 157; 240 of 15512
 // 276 and 294; d = 64: 72 of 1064 9.3 and 12.8, of 15512 81 and 50; 240 of 15512 141 and 152; five tokens of four heads: 8 of 1064 16.8
 // and 15, 72 of 4000 44 and 38, 240 of 15512 299 and 341; blocks of 64 rows: 64 of 2000 38 and 34, 240 of 15512 339 and 372; of 128: 128 of 600 29
-// and 40, of 2000 61 and 49, 256 of 2000 65 and 72, of 15512 362 and 274, 512 of 15512 502 and 531; fp32: 256 of 15512 686 and 524.
+// and 40, of 2000 61 and 49, 256 of 2000 65 and 72; of 256: 64 of 600 30 and 36, of 2000 66 and 48, 128 of 2000 69 and 69, of 8000 218 and 158,
+// 256 of 8000 256 and 283; fp32: 128 of 8000 372 and 252.
 // Of a batch only the longest length is known here.  Whole blocks wait for the longest sequence's, which parts share out among all, so
 // parts of several sequences are priced as if half of the rows were there.
 bool paged_whole(const PagedPrice &c, int RB, int64_t blocks, int64_t tiles, int batch)
 {
     const double b = blocks / 256.0, t = (double)tiles;
-    // (the wide kernels' work-groups are there in twos)
-    const double whole = c.start + t * std::max(c.own, RB > 32 && b > 1 ? c.full * 2 * (double)((blocks + 511) / 512) : c.full * b);
+    // (of the wide kernels' work-groups a compute unit holds one of 256 rows, two of others)
+    const int64_t held = RB == 256 ? 256 : 512;
+    const double whole = c.start + t * std::max(c.own, RB > 32 && b > 1 ? c.full * (held / 256) * (double)((blocks + held - 1) / held) : c.full * b);
     const double cut = c.join + std::max(c.own * MIN_PIECE, c.full * t * b * (batch > 1 ? 0.5 : 1.0));
     return whole <= cut;
 }
