@@ -393,13 +393,14 @@ __device__ inline pu4_t not_finite_or_rest(pu4_t u, bool ones)
     return y;
 }
 
-// Tiles of TR rows of d elements, 8 KB, in a wavefront's own shared memory.  16-byte unit u of row r stands at position u ^ swz(r)
-// of the row, so that eight lanes reading one unit of eight rows, and sixteen reading two units of four rows, meet distinct banks.
+// Tiles in shared memory (of the token kernel TR rows, 8 KB, a wavefront's own).  16-byte unit u of row r stands at position u ^ swz(r) of
+// the row: eight lanes that read one unit of eight rows meet distinct banks, and so do 32 that read two units of eight rows or four units
+// of four as columns (with 2 (r % 8) for d = 128 the latter met two by two: a third of the shared memory's time for 512 tokens).
 template <int DH>
 struct PagedTile {
     static constexpr int UN = DH / 8, TR = 4096 / DH, SUB = TR / 16;   // units of a row, rows, 16-row parts
     static constexpr int ROW = DH * 2, PART = 16 * ROW;                // bytes
-    static __device__ unsigned swz(unsigned r) { return DH == 128 ? (r & 7) * 2 : (r >> 1 & 3) * 2; }
+    static __device__ unsigned swz(unsigned r) { return (DH == 128 ? (r & 3) << 2 : (r & 2) << 1) | (r & 4) >> 1; }
 };
 template <int DH, int MT, int NW>
 struct PagedTokenSmem {
