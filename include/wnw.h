@@ -579,7 +579,7 @@ wnw_status wnw_rotary_frequencies(int32_t dim, double base, double factor, doubl
  *   count_dev     device int32 [B], 0 .. n; NULL = n for every sequence
  *   position_dev  device int32 [B][n], any values; NULL = at[b] + i
  *   rotary        NULL: nothing is rotated
- * Two calls whose work overlaps must not write the same rows. */
+ * At most 2^20 KV-heads and 2^20 q-heads.  Two calls whose work overlaps must not write the same rows. */
 wnw_status wnw_paged_append(const wnw_paged_config *cfg, const wnw_paged_cache *cache, const wnw_rotary *rotary,
                             int32_t first_layer, int32_t n_layers, int32_t q_heads, int32_t n, const void *k_dev,
                             const void *v_dev, const void *q_dev, void *q_out, const int32_t *at_dev,

@@ -508,6 +508,7 @@ wnw_status wnw_draft_tree(int32_t batch, int32_t n, const int32_t *parent_dev, c
     if (misaligned(parent_dev, 4) || misaligned(base_dev, 4) || misaligned(count_dev, 4) || misaligned(mask_dev, 8) || misaligned(position_dev, 4))
         return draft_fail(WNW_ERR_INVALID, "a pointer is not aligned to its elements");
     const int words = (n + 63) / 64;
+    if ((int64_t)batch * words * words * 64 > 0xffffffffll) return draft_fail(WNW_ERR_UNSUPPORTED, "too many tokens for one call");
     hipLaunchKernelGGL(draft_tree_kernel, dim3((unsigned)(batch * words)), dim3((unsigned)words * 64), 0, (hipStream_t)hip_stream, n,
                        parent_dev, base_dev, count_dev, mask_dev, position_dev);
     return draft_hip();

@@ -4,7 +4,7 @@
 //   paged_append_kernel  new rows of K and V to their pages and queries to their place, rotated on the way
 //   paged_keep_kernel    accepted rows to the end of their sequence, a wavefront per head's K or V
 //   paged_token_kernel   attention in blocks of 16 or 32 query rows of a KV-head, every wavefront with tiles of its own
-//   paged_wide_kernel    attention in blocks of 64 or 128 query rows, whose wavefronts share tiles
+//   paged_wide_kernel    attention in blocks of 64, 128 or 256 query rows, whose wavefronts share tiles
 //   paged_join_kernel    joins the parts of a cache that work-groups shared
 #include "wnw.h"
 #include "wnw_internal.h"
@@ -106,7 +106,7 @@ __global__ __launch_bounds__(P_THREADS) void paged_append_kernel(PagedAppend a, 
             cs[e] = 1.f, sn[e] = 0.f;
             if (x < a.dim) {
                 const int pair = TURN == TURN_PAIRS ? x >> 1 : x < half ? x : x - half;
-                // turns, and without the whole ones: the product of position and frequency is exact in a double
+                // turns, and without the whole ones: the product of position and frequency is exact in a double below 2^29
                 const double turns = pos * (double)a.freq[pair] * 0.15915494309189535;
                 const float rest = (float)(turns - rint(turns));
                 float s, c;
@@ -596,7 +596,7 @@ __device__ inline void paged_token_block(const PagedAttend &a, PagedTokenSmem<DH
                 odd |= not_finite(u);
             }
             __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            if (a.n > 1 && __any(odd & 0x80008000u)) {
+            if ((a.n > 1 || a.mask) && __any(odd & 0x80008000u)) {
 #pragma unroll
                 for (int r = 0; r < MT; ++r) {
                     bf16x8_t ones[T::SUB / 2];
@@ -910,8 +910,9 @@ __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> 
                 __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
             }
         }
-        if (__any(top > (m == -INFINITY ? -INFINITY : LAZY_P))) {
-            const float mn = fmaxf(m, mz + top), rise = finite_or_zero(mn) - mz, alpha = m == -INFINITY ? 0.f : exp2_hw(-rise);
+        const bool up = top > (m == -INFINITY ? -INFINITY : LAZY_P);
+        if (__any(up)) {      // (a row's own logits decide, so that its results do not depend on the rows beside it)
+            const float mn = up ? mz + top : m, rise = finite_or_zero(mn) - mz, alpha = m == -INFINITY ? 0.f : exp2_hw(-rise);
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt) o[dt] *= alpha;
 #pragma unroll
@@ -1221,7 +1222,7 @@ bool paged_whole(const PagedPrice &c, int RB, int64_t blocks, int64_t tiles, int
 
 // How an attention call runs.
 struct PagedPlan {
-    int RB, W, tsh;     // RB 16, 32, 64 or 128
+    int RB, W, tsh;     // RB 16, 32, 64, 128 or 256
     bool whole, eight, stream, join_groups;
     int64_t rows, o_bytes, ml_bytes;
     int64_t total() const { return o_bytes + ml_bytes; }
@@ -1319,8 +1320,9 @@ wnw_status wnw_paged_append(const wnw_paged_config *cfg, const wnw_paged_cache *
     }
     if (n == 0) return WNW_OK;
     if (!k_dev != !v_dev || !q_dev != !q_out) return paged_fail(WNW_ERR_INVALID, "keys and values, and queries and their place, come together");
+    if (cfg->kv_heads > (1 << 20)) return paged_fail(WNW_ERR_UNSUPPORTED, "more than 2^20 KV-heads");
     if (!k_dev && !q_dev) return paged_fail(WNW_ERR_INVALID, "NULL pointer");
-    if (q_dev && (q_heads < 1 || q_heads > (1 << 20))) return paged_fail(WNW_ERR_INVALID, "q_heads must be at least 1");
+    if (q_dev && (q_heads < 1 || q_heads > (1 << 20))) return paged_fail(WNW_ERR_INVALID, "q_heads must be 1 .. 2^20");
     if (!at_dev) return paged_fail(WNW_ERR_INVALID, "NULL pointer");
     if (off16(k_dev) || off16(v_dev) || off16(q_dev) || off16(q_out)) return paged_fail(WNW_ERR_INVALID, "rows must be aligned to 16 bytes");
     if (off4(at_dev) || off4(count_dev) || off4(position_dev)) return paged_fail(WNW_ERR_INVALID, "a pointer is not aligned to its elements");

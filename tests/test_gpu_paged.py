@@ -310,6 +310,9 @@ def test_pages_that_are_not_there(W):
     check_attend(W, 2, 2, 128, 16, 4, [100, 40, 200], None, True, holes=[(0, 0), (0, 3), (1, 2), (2, 12), (2, 5)])
     check_attend(W, 2, 2, 64, 16, 1, [100, 40, 30], None, False, holes=[(0, 6), (1, 0), (1, 1), (1, 2), (2, 0)])
     check_attend(W, 1, 20, 128, 32, 5, [100, 64], None, False, bf16=True, holes=[(0, 1), (1, 1), (1, 0)])
+    check_attend(W, 1, 12, 64, 16, 4, [150, 64], None, True, holes=[(0, 0), (0, 5), (1, 1)])
+    check_attend(W, 2, 16, 128, 16, 20, [400, 64, 90], None, True, bf16=True, holes=[(0, 2), (0, 24), (1, 1), (2, 0)])
+    check_attend(W, 1, 16, 64, 64, 20, [700, 64, 90], None, False, holes=[(0, 4), (1, 0), (2, 1)])
 
 
 def test_layers_lengths_and_counts(W):
@@ -332,7 +335,7 @@ def test_bf16_outputs_are_the_fp32_ones_rounded(W):
 
 
 @pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("G", [1, 12])
+@pytest.mark.parametrize("G", [1, 4, 8, 12, 24])
 def test_numbers_that_are_not_finite(W, D, G):
     """In rows that a token does not see they do nothing; in those that it sees they reach the outputs that they belong to."""
     log(f"[case] attend inf, NaN d={D} G={G}")
@@ -379,6 +382,42 @@ def test_numbers_that_are_not_finite(W, D, G):
         want[G - 1, 3] = True
         assert torch.equal(torch.isnan(out[0, 0]).all(dim=-1), want) and torch.equal(torch.isnan(lse[0, 0]), want)
         assert torch.equal(out[0, 0][~want], clean[0, 0][~want])
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("G", [1, 20, 40, 80, 200])
+def test_a_token_that_does_not_see_itself(W, D, G):
+    """A single token whose mask leaves out its own row, in which there is no number."""
+    log(f"[case] attend, own row unseen, d={D} G={G}")
+    g = torch.Generator().manual_seed(5)
+    T, page = 70, 16
+    cfg, c = new_cache(W, g, 1, 1, 1, D, page, 5)
+    to = R.place(c.table.cpu(), 0, T - 1, page, cfg.pages)
+    c.k[to[0], 0, 0, to[1]] = math.nan
+    c.v[to[0], 0, 0, to[1]] = math.inf
+    q = rows(g, 1, 1, G, 1, D)
+    see = [np.zeros((1, 1), dtype=bool)]
+    out, lse = run_attend(W, cfg, c, q.cuda(), [T], None, R.words(see[0])[None].cuda())
+    k, v = c.k.cpu(), c.v.cpu()
+    check_outputs(out.cpu(), lse.cpu(), R.attend(q, k, v, c.table.cpu(), page, [T], [1], see, 0), D, False, False)
+    assert torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("G", [12, 24])
+def test_rows_do_not_depend_on_the_rows_beside_them(W, G):
+    """Bit for bit: a token's logits that grow along the cache move its own maximum alone."""
+    log(f"[case] attend, rows beside each other, G={G}")
+    g = torch.Generator().manual_seed(6)
+    n, T, D, page = 6, 400, 128, 16
+    cfg, c = new_cache(W, g, 1, 1, 1, D, page, 25, bf16=True)
+    q = rows(g, 1, 1, G, n, D)
+    clean, clean_lse = (x.cpu() for x in run_attend(W, cfg, c, q.cuda(), [T], None))
+    q2 = q.clone()
+    q2[0, 0, :, 4] *= 64
+    out, lse = (x.cpu() for x in run_attend(W, cfg, c, q2.cuda(), [T], None))
+    others = [0, 1, 2, 3, 5]
+    assert torch.equal(out[0, 0][:, others], clean[0, 0][:, others]) and torch.equal(lse[0, 0][:, others], clean_lse[0, 0][:, others])
+    assert not torch.equal(lse[0, 0][:, 4], clean_lse[0, 0][:, 4])
 
 
 def test_offsets_past_32_bits(W):

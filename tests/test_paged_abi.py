@@ -107,6 +107,8 @@ def test_sizes_beyond_a_launch(W):
     got = calls(W, cfg, cache_of(W), n=1 << 24, q_heads=64)
     assert got["append"]() == W.WNW_ERR_UNSUPPORTED
     assert got["attend"]() == W.WNW_ERR_UNSUPPORTED
+    cfg = W.wnw_paged_config(**{**GOOD, "batch": 1, "layers": 1, "pages": 1, "kv_heads": (1 << 30) - 1})
+    assert calls(W, cfg, cache_of(W), nl=1)["append"]() == W.WNW_ERR_UNSUPPORTED
 
 
 def test_nothing_to_do(W):
@@ -140,7 +142,7 @@ def drafts(W, B=2, n=4, V=131072, ws=PTR, ws_bytes=1 << 40, **p):
 
 @pytest.mark.parametrize("kw,want,names", [
     (dict(B=0), "INVALID", "tree verify"), (dict(n=-1), "INVALID", "tree verify"), (dict(n=1025), "UNSUPPORTED", "tree verify"),
-    (dict(B=1 << 21), "UNSUPPORTED", "tree verify"), (dict(V=0), "INVALID", "verify"), (dict(V=(1 << 24) + 1), "UNSUPPORTED", "verify"),
+    (dict(B=1 << 21), "UNSUPPORTED", "tree verify"), (dict(B=1 << 20, n=1024), "UNSUPPORTED", "tree"), (dict(V=0), "INVALID", "verify"), (dict(V=(1 << 24) + 1), "UNSUPPORTED", "verify"),
     (dict(parent=None), "INVALID", "tree"), (dict(base=None), "INVALID", "tree"), (dict(parent=4098), "INVALID", "tree verify"),
     (dict(mask=4100), "INVALID", "tree"), (dict(position=4098), "INVALID", "tree"), (dict(count=4097), "INVALID", "tree verify"),
     (dict(token=None), "INVALID", "verify"), (dict(target=None), "INVALID", "verify"), (dict(uniform=None), "INVALID", "verify"),
