@@ -69,9 +69,13 @@ struct PagedAppend {
 enum { TURN_NONE, TURN_PAIRS, TURN_HALVES, TURN_HALVES_ODD };
 
 // A lane has 16 bytes (eight elements) of a vector: neighbours d / 8 lanes one vector, and the work-group TT tokens' vectors of
-// HH heads at a time, going through the layer's heads with the angles of its lanes in registers.  An element's partner is in
+// HH heads at a time, going through the layer's heads with the angles of its lanes in registers, which depend on token and element
+// alone (in a work-group per head the 64-bit angles, cosines and sines would be as much work as the bytes).  An element's partner is in
 // the lane itself (pairs) or comes from the lane that has it, halves of a multiple of eight elements by four moves, others by two
 // for each element.
+// Bound by memory, which it reads and writes once: 7756 rows of 36 layers with 16 q-heads and 2 KV-heads, 2.86 GB, take 511 us, 5.6 TB/s
+// (540 with one vector of a lane under way instead of UNROLL).  A single token is bound by the
+// launch and one chain of table, positions and rows: all of 30 layers with 32 and 8 heads 5.6 us on the GPU.
 template <int DH, int TURN>
 __global__ __launch_bounds__(P_THREADS) void paged_append_kernel(PagedAppend a, int TT)
 {
@@ -191,8 +195,10 @@ __global__ __launch_bounds__(P_THREADS) void paged_append_kernel(PagedAppend a, 
 
 // ---- keeping ---------------------------------------------------------------------------------
 
-// A wavefront has a head's K or V.  A path ascends, so that row base + i is no source of a later entry, and the rows of one step
-// are read before any of them is written.
+// A wavefront has a head's K or V, so that no other has the rows that it reads and writes.  A path ascends, so that row base + i is no
+// source of a later entry, and the rows of one step are read before any of them is written.  Bound by latency (path, table entry, row): a
+// path of 64 tokens of which three stand in one layer of 8 KV-heads takes 3.1 us on the GPU, eight sequences of 30 such layers with up to eight
+// 4.7; a launch with nothing to do takes 2.
 template <int DH>
 __global__ __launch_bounds__(P_THREADS) void paged_keep_kernel(PagedGeo g, int n, int items, const int32_t *__restrict__ base_dev,
                                                                const int32_t *__restrict__ path_dev,
@@ -414,6 +420,15 @@ struct PagedTokenSmem {
     static __device__ int unit(int row, int u) { return row * DH + (u ^ (row & (DH / 4 - 1) & 15)) * 4; }
 };
 
+// Up to 32 query rows of a KV-head, one pass over the rows with the running maximum and sum of every query row.
+//   S^T (16 keys x 16 rows) = K Q^T and O^T (16 dimensions x 16 rows) += V^T P^T by 16 x 16 x 32 products: a lane has four keys of ONE row
+//   in each 16-row part, so that maximum and sum meet over four lanes at the end of a tile, and the elements of two parts are P^T's operand as they
+//   stand; V^T's is read from the rows as columns, which the hardware does on the way out of shared memory.
+// Bound by the bytes of the cache.  So every wavefront has tiles of its own (K and V of 4096 elements each), which go straight from
+// global to shared memory and are asked for as soon as the products have read the tile before: no registers, no barrier between wavefronts, and
+// 64 to 128 KB of every compute unit under way or in use all the time.  Weights are three bf16 terms, exactly, which the matrix unit has time for (12 % busy).
+// One token, 30 layers of 8 KV-heads, 15512 rows: 1.907 GB in 278 us, 6.85 TB/s, what a loop of loads reaches (301 with tiles that
+// wavefronts share).  8 KV-heads of one layer, 1064 rows: 11.4 us, a chain of five tiles for each of eight wavefronts.
 // Tiles ta .. tb - 1 of block rb of head (b, hd)'s rows; slot: where a piece's result goes (-1: the block is whole).
 template <int DH, int MT, bool NTL, int NW>
 __device__ inline void paged_token_block(const PagedAttend &a, PagedTokenSmem<DH, MT, NW> &sm, const PartSeq &sq, int b, int hd, int rb,
@@ -707,15 +722,22 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_token_kernel(PagedAttend a)
     });
 }
 
-// Many query rows.  A work-group has blocks of RB = 128 rows, 32 for each of its four wavefronts, and all of them use the same
+// Many query rows.  A work-group of NW wavefronts has blocks of RB = 256 (NW 8), 128 or 64 (4) rows, and all of its wavefronts use the same
 // tiles of 64 cache rows, which go straight from global to one of two buffers in shared memory while the tile in the other is
-// in use; wavefront w loads part w of 16 rows.
+// in use; of four wavefronts each loads a part of 16 rows of K and of V, of eight four do for K and four for V.
 //   S^T (32 keys x 32 rows) = K Q^T and O^T (32 dimensions x 32 rows) += V^T P^T by 32 x 32 x 16 products (see wnw_lds.h for
 //   operands): a lane has 16 keys of ONE row, elements 0 .. 7 in the 16-row part 2 k and 8 .. 15 in 2 k + 1, so that S^T's elements are P^T's
 //   operand as they stand, and V^T's is read from the rows as columns.
 // KS = 2, for 33 to 64 rows: two wavefronts share 32 rows, each with half of every tile's keys, and join at the end.
 // A row's maximum m is raised, and its output and sum scaled, only when a logit exceeds it by LAZY_P (base 2).
 // NT: operands of a weight: 1, rounded to bf16, for bf16 outputs; 3, all of its 24 bits, for fp32 ones.
+// Bound by the matrix unit and, beside it, the vector unit and shared memory, in the card's power limit.  Hence 32 rows a wavefront, for each of which
+// K's and V's operands are read once from shared memory; K is a round ahead, so that the next tile's products with K run
+// between the vector instructions of this one's softmax; and 256 rows a work-group, which halve the bytes that are loaded per row.  512 tokens, 2 layers
+// of 32 heads over 8, 15512 rows: 256 GFLOP in 270 us, 950 TFLOP/s (283 with blocks of 128 rows, 551 by the token kernel); an 8192^3 product
+// reaches 1150-1230.  Four buffers for K and V each were 5 to 10 % slower (addresses that differ between rounds), units moved once more in odd
+// parts 2 % (no bank conflicts left, where they are a third of its cycles now, but registers in memory).
+// MASKED tiles are the causal edge, a draft's own rows, missing pages and the end of a sequence.
 constexpr float LAZY_P = 8.f;
 
 template <int DH>
@@ -1060,7 +1082,10 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_wide_kernel(PagedAttend a)
     });
 }
 
-// Joins the pieces of a cache: sixteen threads have a row's pieces p, p + GP, ..., and a work-group 16 / GP rows of a head.
+// Joins the pieces of a cache: sixteen threads have a row's pieces p, p + GP, ..., and a work-group 16 / GP rows of a head.  Every block's
+// pieces are found again from the lengths as the first kernel did, so that there is no list and no atomic operation, and the order of the
+// sum is fixed.  Bound by the pieces' bytes, which are still in the last-level cache: 65536 rows of about two pieces (4 sequences, 64 tokens, 8 layers
+// of 32 heads) 13-16 us, a few rows of many pieces 5.
 template <int DH, int GP>
 __global__ __launch_bounds__(P_THREADS) void paged_join_kernel(PagedAttend a)
 {
