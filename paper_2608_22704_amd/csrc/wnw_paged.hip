@@ -267,6 +267,26 @@ struct PagedAttend {
         const unsigned die = blockIdx.x & 7, each = (unsigned)W >> 3, more = (unsigned)W & 7;
         return die * each + min(die, more) + (blockIdx.x >> 3);
     }
+    // Which block a work-group has where blocks are whole.  Without a mask later tokens see more rows, so the last ones of a head begin, and
+    // the dies get as many of every length: whole heads each, one after the other, after those heads that are left over, whose blocks go to
+    // the dies in turn (a prompt of 7756 tokens, 32 heads over 8: 568 us in the order of heads and blocks, 490 so; 16 over 2: 401 and 255).
+    __device__ void whole_block(int &hd, int &rb) const
+    {
+        if (nrb == 1) {
+            hd = (int)group(), rb = 0;
+            return;
+        }
+        const int heads = g.B * g.nl * g.H, over = heads & 7, x = (int)blockIdx.x - over * nrb;
+        if (x < 0) {
+            rb = (int)blockIdx.x / over;
+            hd = heads - over + (int)blockIdx.x - rb * over;
+        } else {
+            hd = (x >> 3) / nrb;
+            rb = (x >> 3) - hd * nrb;
+            hd += (x & 7) * (heads >> 3);
+        }
+        rb = nrb - 1 - rb;
+    }
     __device__ int tiles_of(int rows) const { return (rows + (1 << tsh) - 1) >> tsh; }
 };
 
@@ -1235,13 +1255,17 @@ PagedPrice paged_price(int RB, int head_dim, bool bf16, bool stream)
 // 256 of 8000 256 and 283; fp32: 128 of 8000 372 and 252.
 // Of a batch only the longest length is known here.  Whole blocks wait for the longest sequence's, which parts share out among all, so
 // parts of several sequences are priced as if half of the rows were there.
-bool paged_whole(const PagedPrice &c, int RB, int64_t blocks, int64_t tiles, int batch)
+// skew: the tokens' part of the rows, of which the first tokens see none (a prompt's blocks of 256 rows whole and cut: 128 of 1024 40 and 50,
+// 32 of 2000 61 and 47, 122 of 7756 207 and 133, 250 of 4000 118 and 123, 486 of 7756 255 and 420, 976 of 7756 490 and 810).
+bool paged_whole(const PagedPrice &c, int RB, int64_t blocks, int64_t tiles, int batch, double skew)
 {
     const double b = blocks / 256.0, t = (double)tiles;
     // (of the wide kernels' work-groups a compute unit holds one of 256 rows, two of others)
     const int64_t held = RB == 256 ? 256 : 512;
-    const double whole = c.start + t * std::max(c.own, RB > 32 && b > 1 ? c.full * (held / 256) * (double)((blocks + held - 1) / held) : c.full * b);
-    const double cut = c.join + std::max(c.own * MIN_PIECE, c.full * t * b * (batch > 1 ? 0.5 : 1.0));
+    const double turns = (held / 256) * std::min((double)((blocks + held - 1) / held), (double)blocks / held * (1 - skew / 2) + (1 - skew) / 2);
+    const double later = RB == 256 ? c.start * std::max(0.0, b - 1) : 0.0;       // starts after the first
+    const double whole = c.start + later + t * std::max(c.own, RB > 32 && b > 1 ? c.full * turns : c.full * b);
+    const double cut = c.join + later + std::max(c.own * MIN_PIECE, c.full * t * b * (batch > 1 ? 0.5 : 1.0));
     return whole <= cut;
 }
 
@@ -1262,7 +1286,7 @@ PagedPlan paged_plan(const wnw_paged_config &c, int32_t n_layers, int32_t q_head
     const int64_t blocks = heads * ((R + p.RB - 1) / p.RB), per = (len + (1 << p.tsh) - 1) >> p.tsh, tiles = per * blocks;
     // bytes that one pass reads once and the 256 MB of the last-level cache cannot keep for the next one go past the caches
     p.stream = R <= p.RB && heads * len * c.head_dim * 4 > (256ll << 20);
-    p.whole = paged_whole(paged_price(p.RB, c.head_dim, c.flags & WNW_F_OUT_BF16, p.stream), p.RB, blocks, per, c.batch);
+    p.whole = paged_whole(paged_price(p.RB, c.head_dim, c.flags & WNW_F_OUT_BF16, p.stream), p.RB, blocks, per, c.batch, R > p.RB ? std::min(1.0, n / (double)len) : 0.0);
     // Eight wavefronts instead of four for whole blocks that have a compute unit each (one token, 72 blocks of 4000 rows 41 -> 29 us; two blocks
     // of 16 rows take turns on the vector unit, so that 240 of 15512 rows take 299 with four and 316 with eight).
     p.eight = p.whole && p.RB <= 32 && blocks <= (p.RB == 16 ? 256 : 128) && len > 256;

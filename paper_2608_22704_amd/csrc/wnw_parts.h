@@ -5,7 +5,7 @@
 // may be null); cap, the most rows of a sequence; tiles_of(rows); n tokens, G q-heads per KV-head, R = n G query rows of a KV-head (row
 // r is token r / G, q-head r % G), in blocks of RB = 2^rsh; W work-groups and inv_w = 1 / W; nrb > 0: a work-group for
 // every block of rows, nrb of them a head.  group(): the work-group's number, 0 .. W - 1, in the order in which parts are dealt
-// out (and in which the workspace has them).  BLOCK_COST: see below.
+// out (and in which the workspace has them).  whole_block(hd, rb): the block of a work-group where nrb > 0.  BLOCK_COST: see below.
 #pragma once
 
 #include "wnw_lds.h"
@@ -296,8 +296,7 @@ __device__ inline void run_parts(const A &a, F f)
         hd = (int)uniform(hd + b * sh.heads), rb = (int)uniform(rb), ta = (int)uniform(ta), tb = (int)uniform(tb);
     };
     if (a.nrb > 0) {
-        hd = a.nrb == 1 ? (int)a.group() : (int)a.group() / a.nrb;
-        rb = (int)a.group() - hd * a.nrb;
+        a.whole_block(hd, rb);
         if (a.g.B > 1) b = hd / (a.g.nl * a.g.H);
         sq = part_seq(a, b);
         if (rb >= sq.nrb) return;

@@ -563,6 +563,11 @@ struct QuantAttend {
     static constexpr int BLOCK_COST = 0;
     __device__ int cap() const { return g.cap; }
     __device__ static unsigned group() { return blockIdx.x; }
+    __device__ void whole_block(int &hd, int &rb) const
+    {
+        hd = nrb == 1 ? (int)group() : (int)group() / nrb;
+        rb = (int)group() - hd * nrb;
+    }
     __device__ static int tiles_of(int rows) { return (rows + QT - 1) / QT; }
 };
 

@@ -279,6 +279,13 @@ def test_a_prompt(W, D, bf16):
     check_attend(W, 1, 5, D, 16, 100, [413], None, False, bf16, L=1)
 
 
+@pytest.mark.parametrize("B,H,L,nl", [(1, 1, 1, 1), (1, 3, 1, 1), (2, 5, 1, 1), (1, 8, 1, 1), (3, 3, 2, 1), (2, 3, 3, 2), (2, 8, 1, 1)])
+def test_prompts_of_any_number_of_heads(W, B, H, L, nl):
+    """Several blocks of rows a head, which are dealt out to the dies."""
+    check_attend(W, H, 1, 64, 16, 600, [600, 37, 555][:B], [600, 37, 520][:B], False, L=L, first=L - nl, nl=nl)
+    check_attend(W, H, 3, 128, 32, 200, [300, 200, 170][:B], [200, 150, 0][:B], True, bf16=True, L=L, first=L - nl, nl=nl)
+
+
 @pytest.mark.parametrize("D", [64, 128])
 def test_long_sequences_that_are_shared(W, D):
     """Parts of a cache for many work-groups, the join, ragged batches."""
