@@ -10,6 +10,7 @@
 
 #include <algorithm>
 #include <cstring>
+#include <type_traits>
 
 namespace wnw {
 
@@ -67,7 +68,7 @@ __global__ __launch_bounds__(DRAFT_MAX) void draft_tree_kernel(int n, const int3
 // does not need end at once; sums that no round was there for are taken by its one work-group at the end (draft_verify_kernel), which also
 // finds the token after the path: the slices' sums name the slice that the last uniform number falls into, and a scan of that one the token.
 // Bound by latency, as one sum needs the one before it: five tokens one after the other, 32000 tokens in the vocabulary, 10.5 us; eight
-// trees of 64 tokens, 131072 in the vocabulary, 33 to 48 us by the number of sums that the random numbers ask for, 4 to 5.6 us each (357 with one
+// trees of 64 tokens, 131072 in the vocabulary, 30 to 42 us by the number of sums that the random numbers ask for, 4 to 5.2 us each (357 with one
 // work-group for a sequence and a sum for every token).
 constexpr int ROUND_THREADS = 256, VERIFY_THREADS = 1024;
 constexpr int MAX_SLICES = 2048, ROUND_SLICES = 64;
@@ -144,12 +145,12 @@ struct DraftTokens {
     int from[DRAFT_MAX], token[DRAFT_MAX];
     int refused;                            // tokens refused at the last row, then in `token`
 
-    // again: a round has been here
-    __device__ void load(const Draft &d, int b, int cnt, int threads, bool again, bool keep)
+    // again: a round has been here.  (All n tokens, so that nothing waits for the count.)
+    __device__ void load(const Draft &d, int b, int threads, bool again, bool keep)
     {
         const int n = d.n, V = d.V;
         if (again) {
-            for (int i = threadIdx.x; i < cnt; i += threads) {
+            for (int i = threadIdx.x; i < n; i += threads) {
                 const float2 x = d.pq[(size_t)b * n + i];
                 const int2 y = d.link[(size_t)b * n + i];
                 p[i] = x.x, q[i] = x.y, from[i] = y.x, token[i] = y.y, u[i] = d.uniform[(size_t)b * (n + 1) + i];
@@ -159,7 +160,7 @@ struct DraftTokens {
             return;
         }
         const float *target = d.target + (size_t)b * (n + 1) * V, *draft = d.draft ? d.draft + (size_t)b * (n + 1) * V : nullptr;
-        for (int i = threadIdx.x; i < cnt; i += threads) {
+        for (int i = threadIdx.x; i < n; i += threads) {
             const int x = d.token[(size_t)b * n + i];
             int f = d.parent ? d.parent[(size_t)b * n + i] : i - 1;
             if (f < 0 || f >= i) f = -1;
@@ -240,17 +241,22 @@ __global__ __launch_bounds__(ROUND_THREADS) void draft_round_kernel(Draft d, int
     const int g = blockIdx.x, b = blockIdx.y, B = gridDim.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int cnt = d.count ? clamp_to(d.count[b], d.n) : d.n;
     DraftState st = {0.0, 1.0, -1, 0, 0, 1, NEED_SUM, 0};
+    double sum = 0.0;
     if (round) {
+        // (before the state decides, so that all that was left is fetched at once)
         st = d.state[(size_t)(round - 1 & 1) * B + b];
+        if (lane < d.slices) sum = d.sums_of(b, round - 1)[lane];
+    }
+    tokens.load(d, b, ROUND_THREADS, round > 0, round == 0 && g == 0);
+    if (round) {
         if (st.phase == NEED_TOTAL) st.phase = HAVE_TOTAL;
         if (st.phase == HAVE_TOTAL) {
             if (g == 0 && tid == 0) d.state[(size_t)(round & 1) * B + b] = st;
             return;
         }
-        st.s = wave_sumd(lane < d.slices ? d.sums_of(b, round - 1)[lane] : 0.0);
+        st.s = wave_sumd(sum);
         st.known = 1;
     }
-    tokens.load(d, b, cnt, ROUND_THREADS, round > 0, round == 0 && g == 0);
     int32_t *path = d.path + (size_t)b * d.n;
     if (!round && g == 0) {
         for (int i = tid; i < d.n; i += ROUND_THREADS) path[i] = -1;
@@ -292,7 +298,7 @@ __global__ __launch_bounds__(VERIFY_THREADS) void draft_verify_kernel(Draft d)
     constexpr int WAVES = VERIFY_THREADS / 64;
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = d.n, V = d.V, slice = d.slice, slices = d.slices;
     const int cnt = d.count ? clamp_to(d.count[b], n) : n;
-    const float *uniform = d.uniform + (size_t)b * (n + 1);
+    const float chosen = d.uniform[(size_t)b * (n + 1) + n];
     int32_t *path = d.path + (size_t)b * n;
     DraftState st = {0.0, 1.0, -1, 0, 0, 1, NEED_SUM, 0};
     if (d.rounds) {
@@ -300,7 +306,7 @@ __global__ __launch_bounds__(VERIFY_THREADS) void draft_verify_kernel(Draft d)
         if (st.phase == NEED_TOTAL) st.phase = HAVE_TOTAL;
         for (int k = tid; k < slices; k += VERIFY_THREADS) sm.sums[k] = d.sums_of(b, st.sums)[k];
     }
-    sm.tokens.load(d, b, cnt, VERIFY_THREADS, d.rounds > 0, false);
+    sm.tokens.load(d, b, VERIFY_THREADS, d.rounds > 0, false);
     if (tid < MAX_SLICES / 32) sm.marked[tid] = 0;
     if (tid == 0) sm.got = -1, sm.found = 0;
     if (!d.rounds && tid < n) path[tid] = -1;
@@ -372,7 +378,7 @@ __global__ __launch_bounds__(VERIFY_THREADS) void draft_verify_kernel(Draft d)
         if (tid == 0) d.next[b] = -1;
         return;
     }
-    const double goal = (double)uniform[n] * total;
+    const double goal = (double)chosen * total;
     // the slice in which the running sum exceeds the goal, or the last one with anything left; every wavefront finds it
     int in = -1;
     double run = 0.0, before = 0.0;
@@ -384,35 +390,71 @@ __global__ __launch_bounds__(VERIFY_THREADS) void draft_verify_kernel(Draft d)
         if (hit) break;
         run = __shfl(sum, 63);
     }
-    // in it, the first token at which it does, or the last one with anything left
-    for (int v0 = in * slice; v0 < min(V, (in + 1) * slice); v0 += VERIFY_THREADS) {
-        const int v = v0 + tid;
-        const double x = v < V ? left(v, whole) : 0.0, sum = wave_scand(x, lane);
-        if (lane == 63) sm.part[wave] = sum;
-        __syncthreads();
-        double mine = before;
+    // in it, the first token at which it does, or the last one with anything left; E tokens a thread
+    const int end = min(V, (in + 1) * slice);
+    auto scan = [&](auto each) {
+        constexpr int E = decltype(each)::value;
+        for (int v0 = in * slice; v0 < end; v0 += E * VERIFY_THREADS) {
+            const int v = v0 + E * tid;
+            float ps[E] = {}, qs[E] = {};
+            if constexpr (VEC && E == 4) {
+                if (v < end) {
+                    __builtin_memcpy(ps, __builtin_assume_aligned(p + v, 16), sizeof(ps));
+                    if (q && !whole) __builtin_memcpy(qs, __builtin_assume_aligned(q + v, 16), sizeof(qs));
+                }
+            } else {
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            if (w == wave) mine = before + sum;
-            before += sm.part[w];
-        }
-        const unsigned long long some = __ballot(x > 0.0), hit = __ballot(x > 0.0 && mine > goal);
-        if (lane == 0) {
-            sm.first[wave] = hit ? v0 + wave * 64 + __builtin_ctzll(hit) : -1;
-            sm.last[wave] = some ? v0 + wave * 64 + 63 - __builtin_clzll(some) : -1;
-        }
-        __syncthreads();
-        if (tid == 0) {
-            int last = -1;
-            for (int w = WAVES - 1; w >= 0; --w) {
-                if (sm.first[w] >= 0) sm.got = sm.first[w], sm.found = 1;
-                if (last < 0) last = sm.last[w];
+                for (int e = 0; e < E; ++e)
+                    if (v + e < end) {
+                        ps[e] = p[v + e];
+                        if (q && !whole) qs[e] = q[v + e];
+                    }
             }
-            if (!sm.found && last >= 0) sm.got = last;
+            double x[E], sum = 0.0;      // what is left of each; of all of them
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                x[e] = fmax((double)ps[e] - st.t * (double)qs[e], 0.0);
+                if (!whole && sm.tokens.refused && sm.tokens.has_refused(v + e)) x[e] = 0.0;
+                sum += x[e];
+            }
+            const double upto = wave_scand(sum, lane);
+            if (lane == 63) sm.part[wave] = upto;
+            __syncthreads();
+            double mine = __shfl_up(upto, 1);
+            mine = before + (lane ? mine : 0.0);
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                if (w < wave) mine += sm.part[w];
+                before += sm.part[w];
+            }
+            int first = -1, last = -1;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                mine += x[e];
+                if (x[e] > 0.0) {
+                    last = v + e;
+                    if (first < 0 && mine > goal) first = v + e;
+                }
+            }
+            const unsigned long long some = __ballot(last >= 0), hit = __ballot(first >= 0);
+            first = hit ? __shfl(first, __builtin_ctzll(hit)) : -1;
+            last = some ? __shfl(last, 63 - __builtin_clzll(some)) : -1;
+            if (lane == 0) sm.first[wave] = first, sm.last[wave] = last;
+            __syncthreads();
+            if (tid == 0) {
+                last = -1;
+                for (int w = WAVES - 1; w >= 0; --w) {
+                    if (sm.first[w] >= 0) sm.got = sm.first[w], sm.found = 1;
+                    if (last < 0) last = sm.last[w];
+                }
+                if (!sm.found && last >= 0) sm.got = last;
+            }
+            __syncthreads();
+            if (sm.found) break;
         }
-        __syncthreads();
-        if (sm.found) break;
-    }
+    };
+    // (slices of 1024 are one step with a token each already)
+    slice > VERIFY_THREADS ? scan(std::integral_constant<int, 4>{}) : scan(std::integral_constant<int, 1>{});
     if (tid == 0) d.next[b] = sm.got;
 }
 
