@@ -782,7 +782,7 @@ __device__ inline void weights_to_terms(const float (&p)[8], bf16x8_t (&t)[NT])
         weights_to_bf16(p, t);
 }
 
-template <int DH, int NT, int KS, int NW>
+template <int DH, int NT, int KS, bool NTL, int NW>
 __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> &sm, const PartSeq &sq, int b, int hd, int rb, int ta,
                                         int tb, int slot)
 {
@@ -828,7 +828,11 @@ __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> 
     const bool has_k = NW == 4 || wave < 4, has_v = NW == 4 || wave >= 4;
     auto load = [&](const char *pool, const Parts &p, unsigned to) {
 #pragma unroll
-        for (int j = 0; j < PL; ++j) load_to_lds(pool + p.at + (j & ~1) * 1024, off[j & 1], lds + to + part * T::PART + j * 1024);
+        for (int j = 0; j < PL; ++j) {
+            const char *from = pool + p.at + (j & ~1) * 1024;
+            const unsigned at = lds + to + part * T::PART + j * 1024;
+            NTL ? stream_to_lds(from, off[j & 1], at) : load_to_lds(from, off[j & 1], at);
+        }
     };
     // K of a tile is there a round before its V: buffers of K 0, 1, then of V
     Parts now = {0, 0}, next = {0, 0}, after = {0, 0};
@@ -1093,12 +1097,12 @@ __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> 
     }
 }
 
-template <int DH, int NT, int KS, int NW>
+template <int DH, int NT, int KS, bool NTL, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void paged_wide_kernel(PagedAttend a)
 {
     __shared__ PagedWideSmem<DH> sm;
     run_parts(a, [&](const PartSeq &sq, int b, int hd, int rb, int ta, int tb, int slot) {
-        paged_wide_block<DH, NT, KS, NW>(a, sm, sq, b, hd, rb, ta, tb, slot);
+        paged_wide_block<DH, NT, KS, NTL, NW>(a, sm, sq, b, hd, rb, ta, tb, slot);
     });
 }
 
@@ -1284,7 +1288,9 @@ PagedPlan paged_plan(const wnw_paged_config &c, int32_t n_layers, int32_t q_head
     p.RB = R > 128 ? 256 : R > 64 ? 128 : R > 32 ? 64 : R > 16 ? 32 : 16;
     p.tsh = c.head_dim == 64 || p.RB > 32 ? 6 : 5;
     const int64_t blocks = heads * ((R + p.RB - 1) / p.RB), per = (len + (1 << p.tsh) - 1) >> p.tsh, tiles = per * blocks;
-    // bytes that one pass reads once and the 256 MB of the last-level cache cannot keep for the next one go past the caches
+    // bytes that one pass reads once and the 256 MB of the last-level cache cannot keep for the next one go past the caches (30 layers of 8
+    // KV-heads, 15512 rows: 64 query rows of a KV-head 334 -> 318 us, 128 402 -> 370; rows that several blocks read must not:
+    // 512 tokens 272 -> 290)
     p.stream = R <= p.RB && heads * len * c.head_dim * 4 > (256ll << 20);
     p.whole = paged_whole(paged_price(p.RB, c.head_dim, c.flags & WNW_F_OUT_BF16, p.stream), p.RB, blocks, per, c.batch, R > p.RB ? std::min(1.0, n / (double)len) : 0.0);
     // Eight wavefronts instead of four for whole blocks that have a compute unit each (one token, 72 blocks of 4000 rows 41 -> 29 us; two blocks
@@ -1307,11 +1313,17 @@ void launch_tokens(const PagedPlan &p, const PagedAttend &a, hipStream_t st)
     hipLaunchKernelGGL(k, dim3(p.W), dim3(p.eight ? 512 : 256), 0, st, a);
 }
 
+template <int DH, int NT, bool NTL>
+void launch_wide_as(const PagedPlan &p, const PagedAttend &a, hipStream_t st)
+{
+    auto *k = p.RB == 256 ? paged_wide_kernel<DH, NT, 1, NTL, 8> : p.RB == 128 ? paged_wide_kernel<DH, NT, 1, NTL, 4> : paged_wide_kernel<DH, NT, 2, NTL, 4>;
+    hipLaunchKernelGGL(k, dim3(p.W), dim3(p.RB == 256 ? 512 : 256), 0, st, a);
+}
+
 template <int DH, int NT>
 void launch_wide(const PagedPlan &p, const PagedAttend &a, hipStream_t st)
 {
-    auto *k = p.RB == 256 ? paged_wide_kernel<DH, NT, 1, 8> : p.RB == 128 ? paged_wide_kernel<DH, NT, 1, 4> : paged_wide_kernel<DH, NT, 2, 4>;
-    hipLaunchKernelGGL(k, dim3(p.W), dim3(p.RB == 256 ? 512 : 256), 0, st, a);
+    p.stream ? launch_wide_as<DH, NT, true>(p, a, st) : launch_wide_as<DH, NT, false>(p, a, st);
 }
 
 wnw_status paged_heads(const wnw_paged_config &c, int32_t n_layers, int32_t q_heads, int32_t n, int32_t max_len)

@@ -294,6 +294,24 @@ def test_long_sequences_that_are_shared(W, D):
     check_attend(W, 1, 8, D, 16, 12, [2500, 900], [12, 12], True, bf16=True, L=1)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n,bf16", [(1, False), (6, True), (16, True), (16, False), (32, True), (32, False), (64, True), (50, False)])
+def test_room_for_many_rows(W, n, bf16, D):
+    """A capacity that no cache of the device holds: tiles are loaded past the caches."""
+    log(f"[case] attend, large capacity, n={n} bf16={bf16} d={D}")
+    g = torch.Generator().manual_seed(n)
+    H, G, page, T = 8, 4, 16, 500
+    cfg = W.make_paged_config(1, 1, H, page, 40, 16384, head_dim=D, flags=W.WNW_F_OUT_BF16 if bf16 else 0)
+    c = W.make_paged_cache(cfg)
+    c.table[0, :32] = torch.randperm(40, generator=g)[:32].int().cuda()
+    for x in (c.k, c.v):
+        x.copy_(rows(g, *x.shape))
+    q = rows(g, 1, 1, H * G, n, D)
+    out, lse = run_attend(W, cfg, c, q.cuda(), [T], None)
+    ref = R.attend(q, c.k.cpu(), c.v.cpu(), c.table.cpu(), page, [T], [n], None, 0)
+    check_outputs(out.cpu(), lse.cpu(), ref, D, bf16, bf16 and G * n > 32)
+
+
 def test_many_sequences(W):
     """More sequences than a wavefront has lanes."""
     g = np.random.default_rng(7)
