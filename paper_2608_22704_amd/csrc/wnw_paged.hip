@@ -446,7 +446,7 @@ struct PagedTokenSmem {
 //   stand; V^T's is read from the rows as columns, which the hardware does on the way out of shared memory.
 // Bound by the bytes of the cache.  So every wavefront has tiles of its own (K and V of 4096 elements each), which go straight from
 // global to shared memory and are asked for as soon as the products have read the tile before: no registers, no barrier between wavefronts, and
-// 64 to 128 KB of every compute unit under way or in use all the time.  Weights are three bf16 terms, exactly, which the matrix unit has time for (12 % busy).
+// 64 to 128 KB of every compute unit under way or in use all the time.  Weights are three bf16 terms, exactly, which the matrix unit has time for (9 % busy).
 // One token, 30 layers of 8 KV-heads, 15512 rows: 1.907 GB in 278 us, 6.85 TB/s, what a loop of loads reaches (301 with tiles that
 // wavefronts share).  8 KV-heads of one layer, 1064 rows: 11.4 us, a chain of five tiles for each of eight wavefronts.
 // Tiles ta .. tb - 1 of block rb of head (b, hd)'s rows; slot: where a piece's result goes (-1: the block is whole).
@@ -754,7 +754,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_token_kernel(PagedAttend a)
 // Bound by the matrix unit and, beside it, the vector unit and shared memory, in the card's power limit.  Hence 32 rows a wavefront, for each of which
 // K's and V's operands are read once from shared memory; K is a round ahead, so that the next tile's products with K run
 // between the vector instructions of this one's softmax; and 256 rows a work-group, which halve the bytes that are loaded per row.  512 tokens, 2 layers
-// of 32 heads over 8, 15512 rows: 256 GFLOP in 270 us, 950 TFLOP/s (283 with blocks of 128 rows, 551 by the token kernel); an 8192^3 product
+// of 32 heads over 8, 15512 rows: 256 GFLOP in 269 to 282 us, 910-950 TFLOP/s (314 when K and V of a tile came together in blocks of 128 rows, 283 since K is a round ahead, 551 by the token kernel); an 8192^3 product
 // reaches 1150-1230.  Four buffers for K and V each were 5 to 10 % slower (addresses that differ between rounds), units moved once more in odd
 // parts 2 % (no bank conflicts left, where they are a third of its cycles now, but registers in memory).
 // MASKED tiles are the causal edge, a draft's own rows, missing pages and the end of a sequence.
