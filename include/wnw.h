@@ -536,7 +536,9 @@ typedef struct {
     int32_t page;         /* rows of a page: 16, 32, 64, 128 or 256                        */
     int32_t pages;        /* pages of the buffers, >= 1                                    */
     int32_t table_width;  /* pages of a sequence at most, >= 1; capacity <= 2^24           */
-    uint32_t flags;       /* WNW_F_OUT_BF16: wnw_paged_attend writes bf16 instead of fp32  */
+    uint32_t flags;       /* WNW_F_OUT_BF16: wnw_paged_attend writes bf16 (each fp32 result
+                             rounded to nearest, ties to even) instead of fp32; the
+                             arithmetic is unchanged                                       */
 } wnw_paged_config;
 
 typedef struct {          /* device pointers                                               */
@@ -588,8 +590,7 @@ wnw_status wnw_paged_append(const wnw_paged_config *cfg, const wnw_paged_cache *
 /* Attention of a sequence's last count[b] tokens over its rows, their own (already appended) among them: token i of count[b]
  * sees rows 0 .. len[b] - count[b] - 1, and of the tokens' own rows those that the mask says (row len[b] - count[b] + j is token
  * j's), without a mask those of tokens 0 .. i.  Logit scale 1 / sqrt(d); products of bf16 summed in fp32, softmax statistics
- * in fp32.  fp32 outputs: softmax weights to 24 bits.  bf16 outputs (WNW_F_OUT_BF16): up to 32 query rows n * H_q / H_kv the
- * fp32 results rounded (nearest, ties to even); with more, weights are rounded to bf16 before they multiply V.
+ * in fp32, softmax weights to 24 bits.  bf16 outputs (WNW_F_OUT_BF16) are the fp32 results rounded (nearest, ties to even).
  * What a token does not see has no part in its outputs, infinities and NaN
  * included.  A token that sees no row (or whose logits are all -inf) gets zeros and the log-sum-exp -inf; otherwise a query
  * row with a NaN or an infinity gets NaN in all of its outputs, and an element of out_dev for which a row seen has a V

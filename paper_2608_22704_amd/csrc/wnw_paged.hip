@@ -247,7 +247,7 @@ struct PagedAttend {
     int G, n, R;               // q-heads per KV-head, tokens, rows G * n of a KV-head: row r is token r / G, q-head r % G
     int W, RB, rsh;            // work-groups that share the batch's tiles, rows of a block and their log2
     int tsh;                   // log2 of the cache rows of a tile
-    int bf16;                  // outputs are bf16
+    int bf16;                  // outputs are bf16: the fp32 results, rounded as they are stored
     int nrb;                   // > 0: a work-group per block of rows, nrb blocks a head, nothing to join
     float inv_w;               // 1 / W
     const uint16_t *q;
@@ -750,12 +750,14 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_token_kernel(PagedAttend a)
 //   operand as they stand, and V^T's is read from the rows as columns.
 // KS = 2, for 33 to 64 rows: two wavefronts share 32 rows, each with half of every tile's keys, and join at the end.
 // A row's maximum m is raised, and its output and sum scaled, only when a logit exceeds it by LAZY_P (base 2).
-// NT: operands of a weight: 1, rounded to bf16, for bf16 outputs; 3, all of its 24 bits, for fp32 ones.
+// A weight is three bf16 terms, exactly, whatever the outputs' type.  As one term 13 to 31 % of bf16 outputs were not the fp32 ones rounded, which
+// is what the flag promises and what up to 32 rows get (512 tokens below would take 280 us and not 468); as two, rounded to 17 bits, still
+// 0.06 to 0.16 % were not nearest, where three leave the 0.02 to 0.06 % of fp32 sums (381 us).
 // Bound by the matrix unit and, beside it, the vector unit and shared memory, in the card's power limit.  Hence 32 rows a wavefront, for each of which
 // K's and V's operands are read once from shared memory; K is a round ahead, so that the next tile's products with K run
 // between the vector instructions of this one's softmax; and 256 rows a work-group, which halve the bytes that are loaded per row.  512 tokens, 2 layers
-// of 32 heads over 8, 15512 rows: 256 GFLOP in 269 to 282 us, 910-950 TFLOP/s (314 when K and V of a tile came together in blocks of 128 rows, 283 since K is a round ahead, 551 by the token kernel); an 8192^3 product
-// reaches 1150-1230.  Four buffers for K and V each were 5 to 10 % slower (addresses that differ between rounds), units moved once more in odd
+// of 32 heads over 8, 15512 rows: 256 GFLOP, of which V's half is done three times, in 467 us, so 1100 TFLOP/s of the matrix unit; an 8192^3
+// product reaches 1150-1230.  Four buffers for K and V each were 5 to 10 % slower (addresses that differ between rounds), units moved once more in odd
 // parts 2 % (no bank conflicts left, where they are a third of its cycles now, but registers in memory).
 // MASKED tiles are the causal edge, a draft's own rows, missing pages and the end of a sequence.
 constexpr float LAZY_P = 8.f;
@@ -772,17 +774,7 @@ struct PagedWideJoin {
     float2 ml[2][64];
 };
 
-template <int NT>
-__device__ inline void weights_to_terms(const float (&p)[8], bf16x8_t (&t)[NT])
-{
-    if constexpr (NT == 1) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) t[0][i] = (__bf16)p[i];
-    } else
-        weights_to_bf16(p, t);
-}
-
-template <int DH, int NT, int KS, bool NTL, int NW>
+template <int DH, int KS, bool NTL, int NW>
 __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> &sm, const PartSeq &sq, int b, int hd, int rb, int ta,
                                         int tb, int slot)
 {
@@ -968,13 +960,13 @@ __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> 
             sum *= alpha;
             m = mn;
         }
-        bf16x8_t p[2 * NB][NT];
+        bf16x8_t p[2 * NB][3];
 #pragma unroll
         for (int c = 0; c < 2 * NB; ++c) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[c][i] = exp2_hw(w[c][i]);
             sum += ((w[c][0] + w[c][1]) + (w[c][2] + w[c][3])) + ((w[c][4] + w[c][5]) + (w[c][6] + w[c][7]));
-            weights_to_terms<NT>(w[c], p[c]);
+            weights_to_bf16(w[c], p[c]);
         }
         auto v_read = [&](int dt, int c) {
             const unsigned at = (v_get ^ dt * 64) + c * T::PART + buf;
@@ -1018,7 +1010,7 @@ __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> 
             for (int c = 0; c < 2 * NB; ++c) {
                 const bf16x8_t v = __builtin_bit_cast(bf16x8_t, v_read(dt, c));
 #pragma unroll
-                for (int k = 0; k < NT; ++k) o[dt] = mfma32(v, p[c][k], o[dt]);
+                for (int k = 0; k < 3; ++k) o[dt] = mfma32(v, p[c][k], o[dt]);
             }
         now = next;
         next = after;
@@ -1097,12 +1089,12 @@ __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> 
     }
 }
 
-template <int DH, int NT, int KS, bool NTL, int NW>
+template <int DH, int KS, bool NTL, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void paged_wide_kernel(PagedAttend a)
 {
     __shared__ PagedWideSmem<DH> sm;
     run_parts(a, [&](const PartSeq &sq, int b, int hd, int rb, int ta, int tb, int slot) {
-        paged_wide_block<DH, NT, KS, NTL, NW>(a, sm, sq, b, hd, rb, ta, tb, slot);
+        paged_wide_block<DH, KS, NTL, NW>(a, sm, sq, b, hd, rb, ta, tb, slot);
     });
 }
 
@@ -1237,15 +1229,12 @@ void paged_dispatch(const wnw_paged_config &c, F f)
 struct PagedPrice {
     double start, own, full, join;
 };
-PagedPrice paged_price(int RB, int head_dim, bool bf16, bool stream)
+PagedPrice paged_price(int RB, int head_dim, bool stream)
 {
     const bool d64 = head_dim == 64;
-    if (RB == 256) return bf16 ? (d64 ? PagedPrice{8.5, 1.13, 1.21, 25} : PagedPrice{14, 1.63, 1.95, 31})
-                               : (d64 ? PagedPrice{9, 1.83, 2.03, 27} : PagedPrice{16, 2.83, 3.35, 42});
-    if (RB == 128) return bf16 ? (d64 ? PagedPrice{8, 0.89, 0.62, 17} : PagedPrice{13, 1.48, 1.03, 25})
-                                  : (d64 ? PagedPrice{8, 1.36, 1.05, 18} : PagedPrice{15, 2.8, 2.02, 28});
-    if (RB == 64) return bf16 ? (d64 ? PagedPrice{7, 0.54, 0.80, 13} : PagedPrice{11, stream ? 1.0 : 0.78, 1.45, 18})
-                                      : (d64 ? PagedPrice{7, 0.72, 0.85, 13} : PagedPrice{12, 1.1, 1.50, 18});
+    if (RB == 256) return d64 ? PagedPrice{9, 1.83, 2.03, 27} : PagedPrice{16, 2.83, 3.35, 42};
+    if (RB == 128) return d64 ? PagedPrice{8, 1.36, 1.05, 18} : PagedPrice{15, 2.8, 2.02, 28};
+    if (RB == 64) return d64 ? PagedPrice{7, 0.72, 0.85, 13} : PagedPrice{12, 1.1, 1.50, 18};
     if (RB == 32) return d64 ? PagedPrice{6, stream ? 0.38 : 0.25, 0.66, 11} : PagedPrice{7, stream ? 0.35 : 0.25, 0.68, 14};
     return d64 ? PagedPrice{5.5, stream ? 0.37 : 0.19, 0.62, 9} : PagedPrice{5, stream ? 0.34 : 0.165, 0.607, 11};
 }
@@ -1292,7 +1281,7 @@ PagedPlan paged_plan(const wnw_paged_config &c, int32_t n_layers, int32_t q_head
     // KV-heads, 15512 rows: 64 query rows of a KV-head 334 -> 318 us, 128 402 -> 370; rows that several blocks read must not:
     // 512 tokens 272 -> 290)
     p.stream = R <= p.RB && heads * len * c.head_dim * 4 > (256ll << 20);
-    p.whole = paged_whole(paged_price(p.RB, c.head_dim, c.flags & WNW_F_OUT_BF16, p.stream), p.RB, blocks, per, c.batch, R > p.RB ? std::min(1.0, n / (double)len) : 0.0);
+    p.whole = paged_whole(paged_price(p.RB, c.head_dim, p.stream), p.RB, blocks, per, c.batch, R > p.RB ? std::min(1.0, n / (double)len) : 0.0);
     // Eight wavefronts instead of four for whole blocks that have a compute unit each (one token, 72 blocks of 4000 rows 41 -> 29 us; two blocks
     // of 16 rows take turns on the vector unit, so that 240 of 15512 rows take 299 with four and 316 with eight).
     p.eight = p.whole && p.RB <= 32 && blocks <= (p.RB == 16 ? 256 : 128) && len > 256;
@@ -1313,17 +1302,17 @@ void launch_tokens(const PagedPlan &p, const PagedAttend &a, hipStream_t st)
     hipLaunchKernelGGL(k, dim3(p.W), dim3(p.eight ? 512 : 256), 0, st, a);
 }
 
-template <int DH, int NT, bool NTL>
+template <int DH, bool NTL>
 void launch_wide_as(const PagedPlan &p, const PagedAttend &a, hipStream_t st)
 {
-    auto *k = p.RB == 256 ? paged_wide_kernel<DH, NT, 1, NTL, 8> : p.RB == 128 ? paged_wide_kernel<DH, NT, 1, NTL, 4> : paged_wide_kernel<DH, NT, 2, NTL, 4>;
+    auto *k = p.RB == 256 ? paged_wide_kernel<DH, 1, NTL, 8> : p.RB == 128 ? paged_wide_kernel<DH, 1, NTL, 4> : paged_wide_kernel<DH, 2, NTL, 4>;
     hipLaunchKernelGGL(k, dim3(p.W), dim3(p.RB == 256 ? 512 : 256), 0, st, a);
 }
 
-template <int DH, int NT>
+template <int DH>
 void launch_wide(const PagedPlan &p, const PagedAttend &a, hipStream_t st)
 {
-    p.stream ? launch_wide_as<DH, NT, true>(p, a, st) : launch_wide_as<DH, NT, false>(p, a, st);
+    p.stream ? launch_wide_as<DH, true>(p, a, st) : launch_wide_as<DH, false>(p, a, st);
 }
 
 wnw_status paged_heads(const wnw_paged_config &c, int32_t n_layers, int32_t q_heads, int32_t n, int32_t max_len)
@@ -1467,7 +1456,7 @@ wnw_status wnw_paged_attend(const wnw_paged_config *cfg, const wnw_paged_cache *
     paged_dispatch(*cfg, [&](auto d) {
         constexpr int DH = decltype(d)::value;
         if (p.RB > 32)
-            a.bf16 ? launch_wide<DH, 1>(p, a, (hipStream_t)hip_stream) : launch_wide<DH, 3>(p, a, (hipStream_t)hip_stream);
+            launch_wide<DH>(p, a, (hipStream_t)hip_stream);
         else if (p.RB == 32)
             launch_tokens<DH, 2>(p, a, (hipStream_t)hip_stream);
         else
