@@ -724,9 +724,9 @@ __device__ inline void paged_token_block(const PagedAttend &a, PagedTokenSmem<DH
             __builtin_memcpy(__builtin_assume_aligned(z.ws_o + at * DH + d0, 16), x, sizeof(x));
             if (d0 == 0) z.ws_ml[at] = make_float2(mm, ll);
         } else {
-            const float inv = ll == 0.f ? 0.f : 1.f / ll;
+            const float inv = 1.f / ll;
 #pragma unroll
-            for (int e = 0; e < DH / 16; ++e) x[e] *= inv;
+            for (int e = 0; e < DH / 16; ++e) x[e] = ll == 0.f ? 0.f : x[e] * inv;     // (where no row has weight, x may be NaN)
             store_out<DH / 16>(z.out, z.bf16, (size_t)rr.row_of * DH + d0, x);
             if (d0 == 0 && z.lse) z.lse[rr.row_of] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * P_LN2;
         }
@@ -1057,7 +1057,8 @@ __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> 
     }
     const bool live = qr.token >= 0;
     // element i of o[dt]: dimension 32 dt + 8 (i / 4) + 4 half + i % 4 of row col
-    const float inv = slot >= 0 ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+    const bool none = slot < 0 && sum == 0.f;        // no row has weight, and o may be NaN
+    const float inv = slot >= 0 ? 1.f : 1.f / sum;
     const size_t at = slot >= 0 ? (size_t)(a.group() * 2 + slot) * RB + rows32 * 32 + col : (size_t)qr.row_of;
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt)
@@ -1065,7 +1066,7 @@ __device__ inline void paged_wide_block(const PagedAttend &a, PagedWideSmem<DH> 
         for (int i = 0; i < 16; i += 8) {
             float y[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = o[dt][i + e] * inv;
+            for (int e = 0; e < 8; ++e) y[e] = none ? 0.f : o[dt][i + e] * inv;
             const size_t to = at * DH + dt * 32 + 2 * i;
             if (slot < 0 && a.bf16) {
                 // the halves' four dimensions of eight meet, so that a lane has all of eight
@@ -1157,9 +1158,9 @@ __global__ __launch_bounds__(P_THREADS) void paged_join_kernel(PagedAttend a)
         }
     }
     if (row.token < 0) return;
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const float inv = 1.f / sum;
 #pragma unroll
-    for (int e = 0; e < E; ++e) x[e] *= inv;
+    for (int e = 0; e < E; ++e) x[e] = sum == 0.f ? 0.f : x[e] * inv;     // (where no row has weight, x may be NaN)
     store_out<E>(a.out, a.bf16, (size_t)row.row_of * DH + d0, x);
     if (a.lse && d0 == 0) a.lse[row.row_of] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * P_LN2;
 }

@@ -70,3 +70,31 @@ def test_bf16_outputs_are_the_fp32_ones_rounded(W, D, rb, way, tree):
     full, lse = run_attend(W, cfg, c, q, lens, counts, mask)
     short, short_lse = run_attend(W, half, c, q, lens, counts, mask)
     assert torch.equal(full.bfloat16(), short) and torch.equal(lse, short_lse)
+
+
+@pytest.mark.parametrize("T,way", [(70, "whole"), (5000, "pieces")])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("G", [1, 20, 40, 80, 200])
+def test_logits_that_are_all_minus_infinity(W, D, G, T, way):
+    """A token that gives no row any weight gets zeros and the log-sum-exp -inf, whatever is in the rows' V; one that gives some of them
+    weight gets what is in all that it sees."""
+    log(f"[case] attend, logits of -inf, d={D} G={G} T={T}")
+    for n in (1, 2):
+        cfg, c, g = filled(W, G, 1, 1, 1, D, 16, T, False)
+        assert S.share(W, cfg, 1, G * n, n, [T])[1] == way
+        q = torch.randn((1, 1, G, n, D), generator=g, device="cuda").bfloat16()
+        q[..., 0] = 1.0
+        c.k[..., 0] = -math.inf
+        c.v[..., 5] = math.nan
+        c.v[..., D - 1] = math.inf
+        out, lse = run_attend(W, cfg, c, q, [T], None)
+        assert bool((lse == -math.inf).all()) and bool((out == 0).all())
+        # the last row but one has a finite key, and every token sees it
+        page, row = R.place(c.table.cpu(), 0, T - 2, 16, cfg.pages)
+        c.k[page, 0, 0, row, 0] = 0.25
+        out, lse = run_attend(W, cfg, c, q, [T], None)
+        bad = torch.zeros(D, dtype=torch.bool, device="cuda")
+        bad[[5, D - 1]] = True
+        assert bool(torch.isfinite(lse).all()) and bool((torch.isfinite(out) == ~bad).all())
+        want = c.v[page, 0, 0, row].float()
+        assert bool(((out - want).abs() <= 2.0 ** -22 * want.abs())[..., ~bad].all())      # a weight of one over a sum of one
