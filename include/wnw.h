@@ -516,9 +516,15 @@ const char *wnw_quant_last_error(void);
 
 /* ---- a paged KV cache, and drafted decoding over it.  Rows of K and V are bf16 and live in pages of `page` rows, which
  * hold every layer and KV-head; a table gives the pages of every sequence, so that sequences grow, shrink and share
- * without copies.  One step of drafted decoding: wnw_draft_tree (which drafted tokens see each other, and their
- * positions), for every layer (or all at once) wnw_paged_append and wnw_paged_attend, then wnw_draft_verify, and
- * wnw_paged_keep.  A prompt is appended and attended to likewise (n its tokens, no mask), a single token with n = 1.
+ * without copies.
+ * One step of drafted decoding, of a sequence that has base rows: the token that came last (a prompt's last, or what
+ * wnw_draft_verify drew) has no row yet.  It is the first of the step's 1 + n tokens, and the n drafted ones follow it:
+ *   wnw_draft_tree with parents -1 for it and 1 + parent[i] for drafted token i (parent[i] in -1 .. i - 1, -1: follows it);
+ *   for every layer wnw_paged_append at base and wnw_paged_attend (length base + 1 + n): the target's 1 + n rows;
+ *   wnw_draft_verify of the n drafted tokens alone (the token that came last would have to pass twice, and what comes out
+ *   would not be distributed as the target says);
+ *   wnw_paged_keep with base + 1, and base becomes base + 1 + accepted.
+ * A prompt is appended and attended to likewise (n its tokens, no mask), a single token with n = 1.
  * The calls need no context; the caller owns every buffer, and all of them only enqueue work on hip_stream (NULL = null
  * stream), a stream of the current device, and allocate nothing, so they can be captured into a graph; tables, lengths and
  * positions are read on the device when the work runs.  A call handles n_layers layers from first_layer on.
@@ -604,7 +610,7 @@ wnw_status wnw_paged_append(const wnw_paged_config *cfg, const wnw_paged_cache *
  *   out_dev    device fp32 / bf16 [B][n_layers][H_q][n][d], 16-byte aligned
  *   lse_dev    device fp32 [B][n_layers][H_q][n], natural log of the sum of exp(logit); may be NULL
  *   max_len    upper bound of the lengths, 0 = capacity.  It only shapes the launch: a longer sequence is still attended to
- *              in full
+ *              in full.  Short sequences of a large table are cut into parts that a second launch joins if it is left out
  *   workspace  device memory, 16-byte aligned, of at least the bytes that wnw_paged_attend_workspace gives for the same cfg,
  *              n_layers, q_heads, n and max_len; may be NULL where that is 0.  It holds nothing between calls; calls whose work
  *              overlaps (two streams, two graphs replayed at once) need one each
@@ -621,7 +627,7 @@ wnw_status wnw_paged_attend_workspace(const wnw_paged_config *cfg, int32_t n_lay
 /* Keep the rows of the drafted tokens that stand: row base[b] + path[b][i] becomes row base[b] + i, for i < count[b], in the
  * layers from first_layer on; K rows keep the rotation of their positions.  A path ascends (as wnw_draft_verify gives it): it
  * ends in front of the first entry that is not larger than the one before it, is negative or lies past the capacity.
- *   base_dev   device int32 [B]: rows of the sequence without its draft
+ *   base_dev   device int32 [B]: rows of the sequence without its draft (with the token that came last, which the draft follows)
  *   n          entries of a path, 0 <= n <= 1024
  *   path_dev   device int32 [B][n]
  *   count_dev  device int32 [B], 0 .. n; NULL = n for every sequence */
@@ -660,14 +666,14 @@ wnw_status wnw_draft_tree(int32_t batch, int32_t n, const int32_t *parent_dev, c
  *   token_dev     device int32 [B][n]; may be NULL with n = 0
  *   parent_dev    device int32 [B][n], as above; NULL: each follows the one before it
  *   count_dev     device int32 [B], 0 .. n; NULL = n for every sequence
- *   target_dev    device fp32 [B][n + 1][vocab]: probabilities (they are taken to add up to 1) behind the sequence as it is
- *                 (row 0) and behind token i (row i + 1)
+ *   target_dev    device fp32 [B][n + 1][vocab]: probabilities (they are taken to add up to 1) behind the sequence as it is, that is
+ *                 its token that came last (row 0), and behind token i (row i + 1)
  *   draft_dev     device fp32 [B][n + 1][vocab]: the draft's, row i + 1 for the tokens that follow token i; rows that no token
  *                 follows are not read; may be NULL
  *   uniform_dev   device fp32 [B][n + 1], in [0, 1)
  *   path_dev      device int32 [B][n], written: the tokens that stand, ascending, then -1; may be NULL with n = 0
  *   accepted_dev  device int32 [B], written: how many stand
- *   next_dev      device int32 [B], written: the token after them
+ *   next_dev      device int32 [B], written: the token after them, which has no row in a cache yet
  *   workspace     as wnw_paged_attend's; wnw_draft_verify_workspace gives its size (0 for small vocabularies) */
 wnw_status wnw_draft_verify(int32_t batch, int32_t n, int32_t vocab, const int32_t *token_dev, const int32_t *parent_dev,
                             const int32_t *count_dev, const float *target_dev, const float *draft_dev,

@@ -8,7 +8,7 @@ import torch
 
 from tests import paged_reference as R
 from tests import paged_shares as S
-from tests.test_gpu_paged import check_outputs, i32, run_attend, some_tree
+from tests.test_gpu_paged import EPS, check_outputs, i32, logit_bound, run_attend, some_tree
 from tests.wnw_harness import log
 
 pytestmark = pytest.mark.gpu
@@ -98,3 +98,108 @@ def test_logits_that_are_all_minus_infinity(W, D, G, T, way):
         assert bool(torch.isfinite(lse).all()) and bool((torch.isfinite(out) == ~bad).all())
         want = c.v[page, 0, 0, row].float()
         assert bool(((out - want).abs() <= 2.0 ** -22 * want.abs())[..., ~bad].all())      # a weight of one over a sum of one
+
+
+# ---- together --------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("sampled", [False, True])
+def test_the_loop_of_a_program_that_drafts(W, sampled):
+    """Step after step: the token that came last is the first of the next call's, in front of its draft, and every row of the target that
+    verification takes is what the model says behind the text so far and the tokens on a path.  A model of two layers whose
+    vectors depend on tokens and positions and whose logits on both layers' outputs; drafts of any length, none among them."""
+    log(f"[case] the loop of drafted decoding, sampled={sampled}")
+    B, L, H, G, D, page, n, V, top = 2, 2, 2, 2, 64, 16, 7, 40, 128
+    g = torch.Generator().manual_seed(21)
+    rng = np.random.default_rng(21)
+    ek, ev, eq = ((torch.randn((V, L, h, D), generator=g)).bfloat16() for h in (H, H, H * G))
+    head = torch.randn((L * H * G * D, V), generator=g).double() * (0.5 if sampled else 1.0)
+    rot = W.make_rotary(torch.from_numpy(W.wnw_rotary_frequencies(D, 1e4)).cuda(), D)
+    cfg = W.make_paged_config(B, L, H, page, B * top // page, top // page, head_dim=D)
+    c = W.make_paged_cache(cfg)
+    c.k.fill_(math.nan)
+    c.v.fill_(math.nan)
+    c.table.copy_(torch.randperm(cfg.pages, generator=g).reshape(B, -1).int())
+
+    def turned(e):      # [V][L][heads][d] -> what appending makes of them at every position, [V][L][heads][top][d]
+        x = e.unsqueeze(3).expand(-1, -1, -1, top, -1).contiguous().cuda()
+        one = W.make_paged_config(V, L, H, page, 1, top // page, head_dim=D)
+        W.wnw_paged_append(one, W.PagedCache(c.k, c.v, torch.full((V, top // page), -1, dtype=torch.int32, device="cuda")), None, None,
+                           i32([0] * V), q_dev=x, q_out=x, rotary=rot)
+        return x.cpu()
+
+    tk, tq = turned(ek), turned(eq)
+
+    def model(text):
+        """Logits behind a text in 64 bits, and how far those of the calls may be off."""
+        T = len(text)
+        at = torch.arange(T)
+        k = tk[torch.tensor(text), :, :, at].permute(1, 2, 0, 3).double().repeat_interleave(G, dim=1)       # [L][Hq][T][d]
+        v = ev[torch.tensor(text)].permute(1, 2, 0, 3).double().repeat_interleave(G, dim=1)
+        q = tq[text[-1], :, :, T - 1].double()
+        x = (k @ q.unsqueeze(-1)).squeeze(-1) / math.sqrt(D)
+        p = torch.softmax(x, dim=-1).unsqueeze(-2)
+        absq = (k.abs() @ q.abs().unsqueeze(-1)).squeeze(-1).amax(dim=-1) / math.sqrt(D)
+        werr = logit_bound(D, absq, T)[1]
+        off = (werr + (T + 4) * EPS).unsqueeze(-1) * (p @ v.abs()).squeeze(-2)
+        return (p @ v).flatten() @ head, off.flatten() @ head.abs()
+
+    def append(tokens, position, count, q_out=None):
+        toks = torch.tensor(tokens)
+        k, v, q = (e[toks].permute(0, 2, 3, 1, 4).contiguous().cuda() for e in (ek, ev, eq))
+        W.wnw_paged_append(cfg, c, k, v, i32(base), i32(count), q_dev=None if q_out is None else q, q_out=q_out, rotary=rot, position_dev=position)
+
+    text = [[3, 1, 4, 1, 5], [9, 2, 6]]
+    base = [0, 0]
+    append([t[:-1] + [0] * (5 - len(t)) for t in text], None, [len(t) - 1 for t in text])
+    base, root = [len(t) - 1 for t in text], [t[-1] for t in text]
+    text = [t[:-1] for t in text]
+    ws2 = torch.zeros(W.wnw_draft_verify_workspace(B, n, V), dtype=torch.uint8, device="cuda")
+    stood = 0
+    for turn in range(9):
+        m = [n, n - 2] if turn % 3 == 0 else [1, n] if turn % 3 == 1 else [n, 0]        # drafted tokens
+        parent = [some_tree(rng, n) for _ in range(B)]
+        draft = rng.integers(0, V, (B, n)).tolist()
+        paths = []                                                   # the text up to and with every token
+        for b in range(B):
+            paths.append([])
+            for i, p in enumerate(parent[b]):
+                before = text[b] + [root[b]] if p < 0 else paths[b][p]
+                if rng.random() < 0.6:
+                    draft[b][i] = int(model(before)[0].argmax())
+                paths[b].append(before + [draft[b][i]])
+        # the call's tokens are the root and the draft behind it
+        calls = [[root[b]] + draft[b] for b in range(B)]
+        above = [[-1] + [p + 1 for p in parent[b]] for b in range(B)]
+        count = [x + 1 for x in m]
+        mask, position = torch.zeros((B, n + 1, 1), dtype=torch.int64, device="cuda"), torch.zeros((B, n + 1), dtype=torch.int32, device="cuda")
+        W.wnw_draft_tree(i32(above), i32(base), mask, position, i32(count))
+        q = torch.zeros((B, L, H * G, n + 1, D), dtype=torch.bfloat16, device="cuda")
+        append(calls, position, count, q)
+        out, _ = run_attend(W, cfg, c, q, [x + y for x, y in zip(base, count)], count, mask)
+        logits = out.permute(0, 3, 1, 2, 4).flatten(2).double().cpu() @ head
+        target = torch.softmax(logits, dim=-1) if sampled else torch.nn.functional.one_hot(logits.argmax(dim=-1), V)
+        target = target.float().numpy()
+        u = rng.random((B, n + 1)).astype(np.float32)
+        path, acc, nxt = (torch.zeros(s, dtype=torch.int32, device="cuda") for s in ((B, n), (B,), (B,)))
+        W.wnw_draft_verify(i32(draft), torch.from_numpy(target).cuda(), torch.from_numpy(u).cuda(), path, acc, nxt, parent_dev=i32(parent),
+                           count_dev=i32(m), workspace=ws2)
+        W.wnw_paged_keep(cfg, c, i32([x + 1 for x in base]), path, acc)
+        for b in range(B):
+            for i in range(-1, m[b]):
+                want, off = model(paths[b][i] if i >= 0 else text[b] + [root[b]])
+                assert bool(((logits[b, i + 1] - want).abs() <= off).all()), (turn, b, i)
+            want, after = R.verify(draft[b], parent[b], m[b], target[b], None, u[b])
+            got = acc.tolist()[b]
+            assert path[b].tolist() == want + [-1] * (n - len(want)) and got == len(want) and nxt.tolist()[b] == after, (turn, b)
+            text[b] = paths[b][want[-1]] if want else text[b] + [root[b]]
+            base[b] += 1 + got
+            assert base[b] == len(text[b])
+            root[b] = after
+            stood += got
+    assert stood >= 9
+    # the caches are those of the text
+    for b in range(B):
+        for r, t in enumerate(text[b]):
+            p, o = R.place(c.table.cpu(), b, r, page, cfg.pages)
+            assert torch.equal(c.k[p, :, :, o].cpu(), tk[t, :, :, r]) and torch.equal(c.v[p, :, :, o].cpu(), ev[t]), (b, r)
