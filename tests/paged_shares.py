@@ -51,13 +51,13 @@ def share(W, cfg, n_layers, q_heads, n, lens, counts=None, max_len=0):
 
 
 def exact(q, k, v, table, page, lens, counts, see=None):
-    """What paged_reference.attend gives (on the CPU), computed on the GPU: q [B][L][Hq][n][d], pools and table on the GPU, every
+    """What paged_reference.attend gives, computed and left where q is: q [B][L][Hq][n][d], pools and table there too, every
     entry of which that a sequence uses has a page; see: [B] of [n][n] bool, or None."""
     B, L, Hq, n, D = q.shape
     H = k.shape[2]
     G = Hq // H
-    out = torch.full(q.shape, math.nan, dtype=torch.float64)
-    lse = torch.full(q.shape[:-1], math.nan, dtype=torch.float64)
+    out = torch.full(q.shape, math.nan, dtype=torch.float64, device=q.device)
+    lse = torch.full(q.shape[:-1], math.nan, dtype=torch.float64, device=q.device)
     absv, absq, seen = torch.zeros_like(out), torch.zeros_like(lse), torch.zeros_like(lse)
     for b in range(B):
         T = clamp(lens[b], table.shape[1] * page)
@@ -76,9 +76,38 @@ def exact(q, k, v, table, page, lens, counts, see=None):
             x = (torch.matmul(rows, keys) / math.sqrt(D)).reshape(H, G, c, T).masked_fill(unseen, -math.inf)
             size = (torch.matmul(rows.abs(), keys.abs()) / math.sqrt(D)).reshape(H, G, c, T).masked_fill(unseen, 0.0)
             p = torch.softmax(x, dim=-1).reshape(H, G * c, T)
-            lse[b, l, :, :c] = torch.logsumexp(x, dim=-1).reshape(Hq, c).cpu()
-            absq[b, l, :, :c] = size.amax(dim=-1).reshape(Hq, c).cpu()
-            out[b, l, :, :c] = torch.matmul(p, vv[l]).reshape(Hq, c, D).cpu()
-            absv[b, l, :, :c] = torch.matmul(p, vv[l].abs()).reshape(Hq, c, D).cpu()
-        seen[b, :, :, :c] = sees.sum(dim=-1).double()
+            lse[b, l, :, :c] = torch.logsumexp(x, dim=-1).reshape(Hq, c)
+            absq[b, l, :, :c] = size.amax(dim=-1).reshape(Hq, c)
+            out[b, l, :, :c] = torch.matmul(p, vv[l]).reshape(Hq, c, D)
+            absv[b, l, :, :c] = torch.matmul(p, vv[l].abs()).reshape(Hq, c, D)
+        seen[b, :, :, :c] = sees.sum(dim=-1).double().to(q.device)
     return out, lse, absv, absq, seen
+
+
+# Softmax weights one by one.  Logits are k / sqrt(d) for one element k of a row of K, a multiple of 1 / 16 in -8 .. 8, and the largest, 8, is in
+# every tile; a dimension of the output is one row's weight over their sum.  Then nothing but the weights is rounded: in units of 2^-24,
+#   the scale (log2 e rounded, sqrt(d) rounded, their quotient) is off by 3, so that a weight is by 3 |x - 8| ln 2 <= 3 * 16 / sqrt(d) <= 6;
+#   k times the scale and less the maximum are two steps, of at most 1.45 and 2.89: ln 2 * 4.34 <= 3.01; the exponential 2^-22: 4; the
+#   product with 1 / sum: 1.  The sum itself is common to all of a query row's outputs.
+WEIGHT_SPREAD = (6 + 2 * (3.01 + 4 + 1)) * 2.0 ** -24
+
+
+def weight_keys(g, *shape):
+    """Rows of K [..., rows][d]."""
+    k = torch.randint(-128, 128, shape, generator=g, device=g.device).float() / 16
+    k[..., ::8, :] = 8.0
+    return k
+
+
+def weight_rows(g, rows, d):
+    """Which row every dimension of the output is the weight of, -1: none."""
+    at = torch.randperm(rows, generator=g, device=g.device)[:d]
+    return torch.cat([at, at.new_full((d - len(at),), -1)])
+
+
+def weight_spread(out, want):
+    """How far apart the ratios of weights and exact ones are, over every query row's outputs [..., d] that are not zero."""
+    some = want > 0
+    r = torch.where(some, out / torch.where(some, want, torch.ones_like(want)), torch.ones_like(want) * math.nan)
+    top, low = torch.where(some, r, -math.inf).amax(dim=-1), torch.where(some, r, math.inf).amin(dim=-1)
+    return top / low - 1

@@ -100,6 +100,76 @@ def test_logits_that_are_all_minus_infinity(W, D, G, T, way):
         assert bool(((out - want).abs() <= 2.0 ** -22 * want.abs())[..., ~bad].all())      # a weight of one over a sum of one
 
 
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("way", list(WAYS))
+@pytest.mark.parametrize("rb", list(BLOCKS))
+@pytest.mark.parametrize("D", [64, 128])
+def test_every_kernel_and_way_against_64_bits(W, D, rb, way, tree):
+    log(f"[case] attend against 64 bits, {rb} rows a block, {way}, d={D} tree={tree}")
+    cfg, c, q, lens, counts, see, mask = call(W, rb, way, D, tree, False)
+    out, lse = run_attend(W, cfg, c, q, lens, counts, mask)
+    check_outputs(out, lse, S.exact(q, c.k, c.v, c.table, cfg.page, lens, counts, see), D, False, False)
+
+
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("way", list(WAYS))
+@pytest.mark.parametrize("rb", list(BLOCKS))
+@pytest.mark.parametrize("D", [64, 128])
+def test_weights_have_24_bits(W, D, rb, way, tree):
+    """Outputs that are single weights, to the error of fp32 arithmetic on them (test_paged_weights.py: no shorter ones pass)."""
+    log(f"[case] attend, weights one by one, {rb} rows a block, {way}, d={D} tree={tree}")
+    cfg, c, q, lens, counts, see, mask = call(W, rb, way, D, tree, False)
+    g = torch.Generator(device="cuda").manual_seed(rb)
+    c.k.copy_(S.weight_keys(g, *c.k.shape))
+    c.v.zero_()
+    for b, T in enumerate(lens):
+        # (of the rows that all tokens see: the others' tiles may have a smaller maximum)
+        if T == 0:
+            continue
+        for l in range(cfg.layers):
+            for h in range(cfg.kv_heads):
+                at = S.weight_rows(g, T - counts[b], D)
+                dim = (at >= 0).nonzero().squeeze(1)
+                c.v[c.table[b][at[dim] // cfg.page].long(), l, h, at[dim] % cfg.page, dim] = 1.0
+    q.zero_().scatter_(-1, torch.randint(0, D, (*q.shape[:-1], 1), generator=g, device="cuda"), 1.0)
+    out, lse = run_attend(W, cfg, c, q, lens, counts, mask)
+    want, wlse, _, _, seen = S.exact(q, c.k, c.v, c.table, cfg.page, lens, counts, see)
+    live = ~torch.isnan(wlse)
+    assert bool((out[~live] == 7.0).all()) and bool((out[live][want[live] == 0] == 0).all())
+    out, want, lse, wlse, seen = out[live].double(), want[live], lse[live].double(), wlse[live], seen[live]
+    spread = S.weight_spread(out, want)
+    assert bool((spread <= S.WEIGHT_SPREAD).all()), float(spread.max())
+    # the sum of weights: a rounding for each of them at most
+    off = torch.where(want > 0, out / torch.where(want > 0, want, torch.ones_like(want)) - 1, torch.zeros_like(want)).abs().amax(dim=-1)
+    assert bool((off <= S.WEIGHT_SPREAD + (seen + 4) * EPS).all()), float(off.max())
+    # and of it log2 to 2^-23 of at most 12, times ln 2, and the maximum's product with the scale
+    assert bool(((lse - wlse).abs() <= S.WEIGHT_SPREAD + (seen + 4) * EPS + 8 * EPS * (1 + wlse.abs())).all())
+
+
+@pytest.mark.parametrize("B,L,H,G,n,D,rb,way", [
+    (70, 1, 2, 2, 1, 64, 16, "pieces"), (70, 1, 2, 4, 1, 128, 16, "pieces"), (70, 1, 1, 9, 3, 64, 32, "pieces"), (70, 1, 1, 20, 3, 128, 64, "pieces"),
+    (70, 1, 1, 30, 4, 64, 128, "pieces"), (70, 1, 1, 40, 4, 128, 256, "pieces"), (150, 2, 2, 2, 1, 64, 16, "line"), (150, 1, 4, 4, 1, 128, 16, "line"),
+    (150, 2, 2, 5, 5, 64, 32, "line"), (150, 1, 4, 12, 4, 128, 64, "line"), (90, 2, 4, 20, 6, 128, 128, "line"), (90, 2, 4, 12, 20, 64, 256, "line")])
+def test_more_sequences_than_lanes_that_are_shared(W, B, L, H, G, n, D, rb, way):
+    """Long sequences, empty ones and ones without a token on both sides of the sixty-fourth."""
+    log(f"[case] attend, {B} sequences, {rb} rows a block, {way}, d={D} layers={L} H={H} G={G} n={n}")
+    top = 3000
+    lens = [n + 7 * i % 90 for i in range(B)]
+    lens[5], lens[66], lens[B - 1], lens[10], lens[63], lens[64] = top, 2200, 1500, 0, 0, 700
+    cfg, c, g = filled(W, B + rb, B, L, H, D, 32, top, False)
+    rng = np.random.default_rng(B + rb)
+    counts = [int(x) for x in rng.integers(n // 2, n + 1, B)] if n > 1 else [1] * B
+    for b in (5, 64, 66, B - 1):
+        counts[b] = n
+    counts[65] = counts[7] = 0
+    assert S.share(W, cfg, L, H * G, n, lens, counts)[:2] == (rb, way)
+    q = torch.randn((B, L, H * G, n, D), generator=g, device="cuda").bfloat16()
+    see = [R.ancestors(some_tree(rng, n)) for _ in range(B)]
+    for masks in (None, see):
+        out, lse = run_attend(W, cfg, c, q, lens, counts, None if masks is None else torch.stack([R.words(s) for s in masks]).cuda())
+        check_outputs(out, lse, S.exact(q, c.k, c.v, c.table, cfg.page, lens, counts, masks), D, False, False)
+
+
 # ---- together --------------------------------------------------------------------------------
 
 
