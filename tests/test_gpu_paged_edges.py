@@ -8,7 +8,7 @@ import torch
 
 from tests import paged_reference as R
 from tests import paged_shares as S
-from tests.test_gpu_paged import EPS, check_outputs, i32, logit_bound, run_attend, some_tree
+from tests.test_gpu_paged import EPS, check_outputs, check_verify, i32, logit_bound, probabilities, run_attend, some_tree
 from tests.wnw_harness import log
 
 pytestmark = pytest.mark.gpu
@@ -168,6 +168,58 @@ def test_more_sequences_than_lanes_that_are_shared(W, B, L, H, G, n, D, rb, way)
     for masks in (None, see):
         out, lse = run_attend(W, cfg, c, q, lens, counts, None if masks is None else torch.stack([R.words(s) for s in masks]).cuda())
         check_outputs(out, lse, S.exact(q, c.k, c.v, c.table, cfg.page, lens, counts, masks), D, False, False)
+
+
+# ---- verification ----------------------------------------------------------------------------
+
+
+def drawn(rng, B, n, V, kind):
+    """(tokens, parents or None, target, draft or None): kind "chain", "tree" (tokens that were drawn) or "chosen"."""
+    target = probabilities(rng, B, n + 1, V)
+    draft = None if kind == "chosen" else (0.5 * target + 0.5 * probabilities(rng, B, n + 1, V, sharp=0.7)).astype(np.float32)
+    parent = [list(range(-1, n - 1)) if kind == "chain" else some_tree(rng, n) for _ in range(B)]
+    src = target if draft is None else draft
+    token = np.zeros((B, n), dtype=np.int32)
+    for b in range(B):
+        for i in range(n):
+            total = src[b, parent[b][i] + 1].astype(np.float64).cumsum()
+            token[b, i] = min(int(np.searchsorted(total, rng.random() * total[-1], side="right")), V - 1)
+    return token, None if kind == "chain" else np.array(parent, dtype=np.int32).reshape(B, n), target, draft
+
+
+# rows at 16 bytes and others; launches in front of the last: of chains one, of trees three (up to two sequences) and five (up to 16); of
+# chosen tokens one (up to 32).  Beyond those the one work-group has more than 64 slices.
+@pytest.mark.parametrize("V,B,kind", [(V, B, kind) for V in (131072, 70004, 70001) for B in (1, 2, 8) for kind in ("chain", "tree", "chosen")]
+                         + [(70004, 17, "chain"), (70001, 17, "tree"), (70004, 17, "tree"), (70001, 33, "chosen"), (70004, 33, "chosen"),
+                            (131072, 17, "tree"), (131072, 33, "chosen")])
+def test_verification_of_large_vocabularies(W, V, B, kind):
+    """The last uniform number in the first, middle and last slices of the vocabulary, rows whose last slices hold nothing, refused tokens
+    in the first and the last slices."""
+    log(f"[case] verify V={V} B={B} {kind}")
+    n = 5
+    rng = np.random.default_rng(V + B)
+    token, parent, target, draft = drawn(rng, B, n, V, kind)
+    ends = np.nextafter(np.float32(1), np.float32(0))
+    at = [0.0, ends, 0.97, 0.5, 0.999, 0.02]
+    for turn, scale in enumerate((0.3, 1.0, 1.7)):        # of the tokens' numbers: most of them stand, some, few
+        uniform = np.minimum(rng.random((B, n + 1)) * scale, ends).astype(np.float32)
+        for b in range(B):
+            uniform[b, n] = at[(b + turn) % len(at)]
+        check_verify(W, token, parent, None, target, draft, uniform)
+    uniform[:, :n] = ends
+    check_verify(W, token, parent, None, target, draft, uniform)
+    target[:, :, V - 3000:] = 0
+    target /= target.sum(axis=-1, keepdims=True)
+    token[:, : n // 2] = V - 1 - token[:, : n // 2] % 2000
+    token[:, n // 2: n - 1] %= 900
+    uniform[:, n] = ends
+    check_verify(W, token, parent, np.array([n - b % 2 for b in range(B)], dtype=np.int32), target, draft, uniform)
+    # the slices in front hold nothing
+    target[:, :, : V - 5000] = 0
+    target[:, :, V - 3000: V - 10] = 1e-4
+    target /= target.sum(axis=-1, keepdims=True)
+    uniform[:, n] = rng.random(B)
+    check_verify(W, token, parent, None, target, draft, uniform)
 
 
 # ---- together --------------------------------------------------------------------------------
