@@ -269,7 +269,7 @@ struct PagedAttend {
     }
     // Which block a work-group has where blocks are whole.  Without a mask later tokens see more rows, so the last ones of a head begin, and
     // the dies get as many of every length: whole heads each, one after the other, after those heads that are left over, whose blocks go to
-    // the dies in turn (a prompt of 7756 tokens, 32 heads over 8: 568 us in the order of heads and blocks, 490 so; 16 over 2: 401 and 255).
+    // the dies in turn (a prompt of 7756 tokens, 32 heads over 8: 976 us in the order of heads and blocks, 850 so; 16 over 2: 674 and 436).
     __device__ void whole_block(int &hd, int &rb) const
     {
         if (nrb == 1) {
@@ -751,14 +751,14 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_token_kernel(PagedAttend a)
 // KS = 2, for 33 to 64 rows: two wavefronts share 32 rows, each with half of every tile's keys, and join at the end.
 // A row's maximum m is raised, and its output and sum scaled, only when a logit exceeds it by LAZY_P (base 2).
 // A weight is three bf16 terms, exactly, whatever the outputs' type.  As one term 13 to 31 % of bf16 outputs were not the fp32 ones rounded, which
-// is what the flag promises and what up to 32 rows get (512 tokens below would take 280 us and not 468); as two, rounded to 17 bits, still
+// is what the flag promises and what up to 32 rows get (512 tokens below would take 280 us and not 446 to 468); as two, rounded to 17 bits, still
 // 0.06 to 0.16 % were not nearest, where three leave the 0.02 to 0.06 % of fp32 sums (381 us).
 // Bound by the matrix unit and, beside it, the vector unit and shared memory, in the card's power limit.  Hence 32 rows a wavefront, for each of which
 // K's and V's operands are read once from shared memory; K is a round ahead, so that the next tile's products with K run
 // between the vector instructions of this one's softmax; and 256 rows a work-group, which halve the bytes that are loaded per row.  512 tokens, 2 layers
-// of 32 heads over 8, 15512 rows: 256 GFLOP, of which V's half is done three times, in 467 us, so 1100 TFLOP/s of the matrix unit; an 8192^3
-// product reaches 1150-1230.  Four buffers for K and V each were 5 to 10 % slower (addresses that differ between rounds), units moved once more in odd
-// parts 2 % (no bank conflicts left, where they are a third of its cycles now, but registers in memory).
+// of 32 heads over 8, 15512 rows: 256 GFLOP, of which V's half is done three times, in 446 to 468 us, so 1100-1150 TFLOP/s of the matrix unit; an
+// 8192^3 product reaches 1150-1230.  Measured with one term a weight: four buffers for K and V each were 5 to 10 % slower (addresses that differ
+// between rounds), units moved once more in odd parts 2 % (no bank conflicts left, but registers in memory).
 // MASKED tiles are the causal edge, a draft's own rows, missing pages and the end of a sequence.
 constexpr float LAZY_P = 8.f;
 
@@ -1234,7 +1234,7 @@ PagedPrice paged_price(int RB, int head_dim, bool stream)
 {
     const bool d64 = head_dim == 64;
     if (RB == 256) return d64 ? PagedPrice{9, 1.83, 2.03, 27} : PagedPrice{16, 2.83, 3.35, 42};
-    if (RB == 128) return d64 ? PagedPrice{8, 1.36, 1.05, 18} : PagedPrice{15, 2.8, 2.02, 28};
+    if (RB == 128) return d64 ? PagedPrice{8, 1.36, 1.05, 18} : PagedPrice{14, 2.5, 2.05, 36};
     if (RB == 64) return d64 ? PagedPrice{7, 0.72, 0.85, 13} : PagedPrice{12, 1.1, 1.50, 18};
     if (RB == 32) return d64 ? PagedPrice{6, stream ? 0.38 : 0.25, 0.66, 11} : PagedPrice{7, stream ? 0.35 : 0.25, 0.68, 14};
     return d64 ? PagedPrice{5.5, stream ? 0.37 : 0.19, 0.62, 9} : PagedPrice{5, stream ? 0.34 : 0.165, 0.607, 11};
@@ -1244,13 +1244,14 @@ PagedPrice paged_price(int RB, int head_dim, bool stream)
 // joins.  Measured whole and cut, a block's rows of the cache and what they took: one token, d = 128: 8 blocks of 1064 11.5 and
 // 11.4, of 4000 25.5 and 13.2; 72 of 4000 29.2 and 30.6, of 15512 154 and 92; 128 of 1064 16 and 22, of 15512 174 and 157; 240 of 15512
 // 276 and 294; d = 64: 72 of 1064 9.3 and 12.8, of 15512 81 and 50; 240 of 15512 141 and 152; five tokens of four heads: 8 of 1064 16.8
-// and 15, 72 of 4000 44 and 38, 240 of 15512 299 and 341; blocks of 64 rows: 64 of 2000 38 and 34, 240 of 15512 339 and 372; of 128: 128 of 600 29
-// and 40, of 2000 61 and 49, 256 of 2000 65 and 72; of 256: 64 of 600 30 and 36, of 2000 66 and 48, 128 of 2000 69 and 69, of 8000 218 and 158,
-// 256 of 8000 256 and 283; fp32: 128 of 8000 372 and 252.
+// and 15, 72 of 4000 44 and 38, 240 of 15512 299 and 341; blocks of 64 rows: 64 of 2000 48 and 40, 240 of 15512 358 and 354; of 128: 128 of 600 38
+// and 47, of 2000 94 and 70, 256 of 2000 109 and 116, 240 of 15512 725 and 553; of 256: 64 of 600 44 and 46, of 2000 105 and 65, 128 of 2000 108 and
+// 99, of 8000 366 and 274, 256 of 8000 491 and 518; d = 64: blocks of 128 rows, 128 of 600 21 and 28, of 2000 50 and 41, of 256 rows, 128 of
+// 2000 69 and 61, 256 of 8000 288 and 307.
 // Of a batch only the longest length is known here.  Whole blocks wait for the longest sequence's, which parts share out among all, so
 // parts of several sequences are priced as if half of the rows were there.
-// skew: the tokens' part of the rows, of which the first tokens see none (a prompt's blocks of 256 rows whole and cut: 128 of 1024 40 and 50,
-// 32 of 2000 61 and 47, 122 of 7756 207 and 133, 250 of 4000 118 and 123, 486 of 7756 255 and 420, 976 of 7756 490 and 810).
+// skew: the tokens' part of the rows, of which the first tokens see none (a prompt's blocks of 256 rows whole and cut: 128 of 1024 58 and 66,
+// 126 of 2000 102 and 83, 122 of 7756 353 and 207, 256 of 2000 107 and 134, 504 of 4000 245 and 395, 486 of 7756 436 and 708, 976 of 7756 850 and 1373).
 bool paged_whole(const PagedPrice &c, int RB, int64_t blocks, int64_t tiles, int batch, double skew)
 {
     const double b = blocks / 256.0, t = (double)tiles;
@@ -1279,8 +1280,8 @@ PagedPlan paged_plan(const wnw_paged_config &c, int32_t n_layers, int32_t q_head
     p.tsh = c.head_dim == 64 || p.RB > 32 ? 6 : 5;
     const int64_t blocks = heads * ((R + p.RB - 1) / p.RB), per = (len + (1 << p.tsh) - 1) >> p.tsh, tiles = per * blocks;
     // bytes that one pass reads once and the 256 MB of the last-level cache cannot keep for the next one go past the caches (30 layers of 8
-    // KV-heads, 15512 rows: 64 query rows of a KV-head 334 -> 318 us, 128 402 -> 370; rows that several blocks read must not:
-    // 512 tokens 272 -> 290)
+    // KV-heads, 15512 rows: 64 query rows of a KV-head 366 -> 348 us, 128 568 -> 554; rows that several blocks read must not:
+    // 512 tokens 445 -> 474)
     p.stream = R <= p.RB && heads * len * c.head_dim * 4 > (256ll << 20);
     p.whole = paged_whole(paged_price(p.RB, c.head_dim, p.stream), p.RB, blocks, per, c.batch, R > p.RB ? std::min(1.0, n / (double)len) : 0.0);
     // Eight wavefronts instead of four for whole blocks that have a compute unit each (one token, 72 blocks of 4000 rows 41 -> 29 us; two blocks
